@@ -44,7 +44,8 @@ typedef enum actq_status {
 
 typedef enum actq_dtype {
     ACTQ_F32 = 0, /* IEEE binary32 */
-    ACTQ_F16 = 1  /* IEEE binary16; widened exactly to binary32 before any arithmetic */
+    ACTQ_F16 = 1, /* IEEE binary16; widened exactly to binary32 before any arithmetic */
+    ACTQ_BF16 = 2 /* bfloat16: the calls for attention heads at the end of this file only */
 } actq_dtype;
 
 /* Per-group header kept beside the codes. */
@@ -377,6 +378,152 @@ int actq_maxpool2d_backward(const uint8_t* argmax, const void* grad_y, actq_dtyp
 int actq_linear_backward(const void* grad_y, const void* weight, const void* x, actq_dtype dt,
                          int64_t rows, int64_t inputs, int64_t outputs, void* grad_x,
                          void* grad_w, void* grad_b, void* stream);
+
+/*
+ * Attention heads: the norm and rotation of queries and keys, a paged cache of keys
+ * and values quantised as it is written, and the attention that reads it.
+ *
+ * A tensor of heads is [tokens, heads, dim] with dim = 64, 128 or 256 contiguous
+ * elements per head and any other strides, so the queries and keys that lie side by
+ * side in the output of one projection are passed as they are.  It is aligned to its
+ * element size.  The descriptors live in HOST memory, the pointers inside are device
+ * pointers.  tokens is at least 0 with tokens * heads < 2^26; no token is no work.
+ * Every type of actq_dtype is taken; arithmetic is binary32, a result is rounded once.
+ */
+typedef struct actq_heads {
+    void* data;           /* element (0, 0, 0); may be NULL where tokens is 0 */
+    int64_t token_stride; /* in elements */
+    int64_t head_stride;
+    int32_t heads;        /* in [1, 65535] */
+} actq_heads;
+
+/*
+ * Rotation by position.  Pair p of a head is its elements (p, p + rotated / 2), or
+ * (2p, 2p + 1) with `interleaved`, and is turned by the angle whose cosine and sine
+ * are entry (positions[token], p) of the tables.  Elements from `rotated` on keep
+ * their place.  A token whose position is not in [0, rows) is padding: its outputs
+ * are zeros and it has no part in any gradient.
+ */
+typedef struct actq_rotation {
+    const int32_t* positions; /* device [tokens]                              */
+    const float* cos;         /* device [rows, rotated / 2]                   */
+    const float* sin;
+    int64_t rows;             /* in [1, 2^31)                                 */
+    int32_t rotated;          /* a multiple of 16, at most dim                */
+    int32_t interleaved;      /* 0 or 1                                       */
+} actq_rotation;
+
+/*
+ * RMS norm of every query and key head, with the rotation in the same pass:
+ *   n = x * r * weight,  r = (mean(x^2) + eps)^(-1/2) over the head,  y = rotated n.
+ *
+ * q, k              in : heads of the queries and the keys; k (and k_out) may be NULL
+ * q_weight, k_weight in: device [dim] of type weight_dt, which is dt or ACTQ_F32; NULL means ones
+ * q_out, k_out      out: may be the memory of q and k with the same strides
+ * Errors: ACTQ_EINVAL on a null or misaligned pointer, an unknown type, sizes out of
+ * range, eps not finite or not above zero; ACTQ_EHIP if the launch fails.
+ */
+int actq_head_norm_rotate(const actq_heads* q, const actq_heads* k, actq_dtype dt, int64_t tokens, int32_t dim,
+                          const void* q_weight, const void* k_weight, actq_dtype weight_dt,
+                          const actq_rotation* rotation, float eps, const actq_heads* q_out,
+                          const actq_heads* k_out, void* stream);
+
+/*
+ * Its gradients: with g the gradient of the output rotated back,
+ *   grad_x = r * (g * weight - x * r^2 * mean(g * weight * x)),
+ *   grad_weight = sum over tokens and heads of g * x * r,
+ * in a fixed order (the same call gives the same bits).
+ *
+ * grad_q, grad_k            in : gradients of q_out and k_out
+ * q, k, weights, rotation, eps : as in the forward call
+ * grad_q_in, grad_k_in      out: gradients of q and k; may be the memory of grad_q and grad_k with the same strides
+ * grad_q_weight, grad_k_weight : device [dim] of type weight_dt, out; NULL where none is wanted
+ * workspace                    : device, actq_head_norm_workspace bytes, 16-byte aligned; may be
+ *                                NULL where no gradient of a weight is wanted
+ */
+int actq_head_norm_workspace(int64_t tokens, int32_t dim, uint64_t* bytes_host);
+int actq_head_norm_rotate_backward(const actq_heads* grad_q, const actq_heads* grad_k, const actq_heads* q,
+                                   const actq_heads* k, actq_dtype dt, int64_t tokens, int32_t dim,
+                                   const void* q_weight, const void* k_weight, actq_dtype weight_dt,
+                                   const actq_rotation* rotation, float eps, const actq_heads* grad_q_in,
+                                   const actq_heads* grad_k_in, void* grad_q_weight, void* grad_k_weight,
+                                   void* workspace, uint64_t workspace_bytes, void* stream);
+
+/*
+ * A paged cache of keys and values.  A group is one token's head of `dim` elements:
+ * Z = min, R = max - min, B = 2^bits - 1, step = R / B, and
+ *   code = nearest(min((x - Z) * (B / R), B)), ties to even,
+ * every operation rounded to binary32 (a group whose R is zero, or whose B / R
+ * overflows, has step 0 and codes 0): the quantizer of actq_quantize_pack with rounding
+ * to nearest, since a cache feeds no gradient.  A code stands for Z + code * step.
+ *
+ * Token slot s of the cache is offset s mod page_size of page s div page_size.
+ *   key_codes   device [pages, heads, page_size, dim * key_bits / 8] bytes, LSB-first as above
+ *   key_header  device [pages, heads, page_size, 2] floats, (Z, step)
+ *   value_codes, value_header: likewise
+ * Codes are aligned to 16 bytes, headers to 8.
+ */
+typedef struct actq_cache {
+    uint8_t* key_codes;
+    float* key_header;
+    uint8_t* value_codes;
+    float* value_header;
+    int64_t pages;      /* in [1, 2^31) */
+    int32_t page_size;  /* a power of two from 16 to 1024 */
+    int32_t heads;      /* in [1, 65535] */
+    int32_t dim;        /* 64, 128 or 256 */
+    int32_t key_bits;   /* 4 or 8 */
+    int32_t value_bits; /* 4 or 8 */
+} actq_cache;
+
+/*
+ * Writes the keys and values of `tokens` tokens into their slots / reads those slots back
+ * (code * step + Z, one fused multiply-add, rounded to dt).
+ *
+ * k, v   : heads equal to the cache's
+ * slots  device [tokens]: a slot outside [0, pages * page_size) is skipped by the write and
+ *          reads as zeros.  A write must not name a slot twice.
+ */
+int actq_cache_write(const actq_cache* cache, const actq_heads* k, const actq_heads* v, actq_dtype dt,
+                     int64_t tokens, const int64_t* slots, void* stream);
+int actq_cache_read(const actq_cache* cache, const int64_t* slots, int64_t tokens, const actq_heads* k,
+                    const actq_heads* v, actq_dtype dt, void* stream);
+
+/*
+ * Attention of new tokens over the cached ones, their own among them:
+ *   out = sum_j p_j v_j,  p = softmax_j(s_j),  s_j = cap(scale * q . k_j),
+ * cap(s) = softcap * tanh(s / softcap) where softcap > 0, else s.
+ *
+ * Sequence n holds lengths[n] tokens, of which token j lies in page table[n][j div page_size]
+ * at offset j mod page_size.  Its new tokens are rows query_start[n] .. query_start[n + 1] - 1
+ * of q, the last ones of the sequence: the last row is position lengths[n] - 1.  A row at
+ * position i sees the positions j <= i, and with window > 0 only those with j > i - window.
+ * A row that sees nothing (a position below zero) gives zeros.  Head h of q reads head
+ * h div (heads / cache heads) of the cache.
+ *
+ * The device arrays cannot be checked by the host: a length is cut to what the table
+ * holds, a page to the cache's last, rows to [0, tokens); what such entries give is
+ * unspecified, and nothing outside the buffers is read or written.  So is the output of a row of q
+ * that belongs to no sequence.
+ *
+ * q, out       [tokens, heads, dim] of type dt, heads a multiple of the cache's, dim the cache's
+ * table        device [sequences, table_width] int32
+ * lengths      device [sequences] int32
+ * query_start  device [sequences + 1] int32, ascending
+ * max_query, max_length: the most new tokens and the most tokens of a sequence, or more.  They
+ *              shape the launch; a sequence beyond them is served all the same, more slowly
+ * workspace    device, actq_cache_attention_workspace bytes (may be 0: then NULL), 16-byte aligned
+ * Errors: ACTQ_EINVAL on a null or misaligned pointer, sizes out of range (sequences * cache
+ * heads > 2^20, table_width * page_size > 2^30, max_query or max_length above that), heads that are no
+ * multiple, scale or softcap not finite, softcap or window negative, a workspace too small.
+ */
+int actq_cache_attention_workspace(const actq_cache* cache, int32_t heads, int64_t tokens, int64_t sequences,
+                                   int64_t max_query, int64_t max_length, int32_t window, uint64_t* bytes_host);
+int actq_cache_attention(const actq_cache* cache, const actq_heads* q, actq_dtype dt, int64_t tokens,
+                         int64_t sequences, const int32_t* table, int32_t table_width, const int32_t* lengths,
+                         const int32_t* query_start, int64_t max_query, int64_t max_length, float scale,
+                         float softcap, int32_t window, const actq_heads* out, void* workspace,
+                         uint64_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

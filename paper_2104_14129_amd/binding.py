@@ -19,7 +19,7 @@ LIB_PATH = os.path.join(_HERE, "libactq.so")
 HOST_PATH = os.path.join(_HERE, "actq_torch.so")
 
 ACTQ_OK, ACTQ_EINVAL, ACTQ_EINFEASIBLE, ACTQ_EHIP = 0, -1, -2, -3
-ACTQ_F32, ACTQ_F16 = 0, 1
+ACTQ_F32, ACTQ_F16, ACTQ_BF16 = 0, 1, 2
 G_DEFAULT = 256
 
 ACTQ_HDR_F32, ACTQ_HDR_BF16, ACTQ_HDR_TENSOR = 0, 1, 2
@@ -29,13 +29,33 @@ EXPORTS = ("actq_version", "actq_source_hash", "actq_last_error", "actq_packed_b
            "actq_quantize_pack", "actq_unpack_dequantize", "actq_sample_sensitivity", "actq_allocate_bits",
            "actq_allocate_bits_device", "actq_relu_mask_bytes", "actq_relu_forward", "actq_relu_backward",
            "actq_pool2d_output_size", "actq_maxpool2d_forward", "actq_maxpool2d_backward", "actq_tensor_stats",
-           "actq_group_stats_multi", "actq_quantize_pack_multi", "actq_unpack_dequantize_multi", "actq_linear_backward")
+           "actq_group_stats_multi", "actq_quantize_pack_multi", "actq_unpack_dequantize_multi", "actq_linear_backward",
+           "actq_head_norm_rotate", "actq_head_norm_workspace", "actq_head_norm_rotate_backward", "actq_cache_write", "actq_cache_read",
+           "actq_cache_attention_workspace", "actq_cache_attention")
 
 
 class ActqError(RuntimeError):
     def __init__(self, code: int, message: str):
         super().__init__(f"libactq error {code}: {message}")
         self.code = code
+
+
+class Heads(ctypes.Structure):
+    """Mirror of `actq_heads` (include/actq.h)."""
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("heads", ctypes.c_int32)]
+
+
+class RotationDesc(ctypes.Structure):
+    """Mirror of `actq_rotation`."""
+    _fields_ = [("positions", ctypes.c_void_p), ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("rotated", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+class CacheDesc(ctypes.Structure):
+    """Mirror of `actq_cache`."""
+    _fields_ = [("key_codes", ctypes.c_void_p), ("key_header", ctypes.c_void_p), ("value_codes", ctypes.c_void_p), ("value_header", ctypes.c_void_p),
+                ("pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("heads", ctypes.c_int32), ("dim", ctypes.c_int32),
+                ("key_bits", ctypes.c_int32), ("value_bits", ctypes.c_int32)]
 
 
 _lib = None
@@ -133,6 +153,21 @@ def lib() -> ctypes.CDLL:
     L.actq_maxpool2d_backward.argtypes = [vp, vp, c.c_int, i64] + [i32] * 10 + [vp, vp]
     L.actq_linear_backward.restype = c.c_int
     L.actq_linear_backward.argtypes = [vp, vp, vp, c.c_int, i64, i64, i64, vp, vp, vp, vp]
+    c_float, heads, rotation, cache = c.c_float, c.POINTER(Heads), c.POINTER(RotationDesc), c.POINTER(CacheDesc)
+    L.actq_head_norm_rotate.restype = c.c_int
+    L.actq_head_norm_rotate.argtypes = [heads, heads, c.c_int, i64, i32, vp, vp, c.c_int, rotation, c_float, heads, heads, vp]
+    L.actq_head_norm_workspace.restype = c.c_int
+    L.actq_head_norm_workspace.argtypes = [i64, i32, vp]
+    L.actq_head_norm_rotate_backward.restype = c.c_int
+    L.actq_head_norm_rotate_backward.argtypes = [heads] * 4 + [c.c_int, i64, i32, vp, vp, c.c_int, rotation, c_float, heads, heads, vp, vp, vp, u64, vp]
+    L.actq_cache_write.restype = c.c_int
+    L.actq_cache_write.argtypes = [cache, heads, heads, c.c_int, i64, vp, vp]
+    L.actq_cache_read.restype = c.c_int
+    L.actq_cache_read.argtypes = [cache, vp, i64, heads, heads, c.c_int, vp]
+    L.actq_cache_attention_workspace.restype = c.c_int
+    L.actq_cache_attention_workspace.argtypes = [cache, i32, i64, i64, i64, i64, i32, vp]
+    L.actq_cache_attention.restype = c.c_int
+    L.actq_cache_attention.argtypes = [cache, heads, c.c_int, i64, i64, vp, i32, vp, vp, i64, i64, c_float, c_float, i32, heads, vp, u64, vp]
     L.actq_allocate_bits_device.restype = c.c_int
     L.actq_allocate_bits_device.argtypes = [vp, vp, i64, i64, i32, i64, c.c_uint32, vp, vp, vp, vp]
     _lib = L
@@ -143,7 +178,8 @@ _host = None
 # the library's entry points that the native module calls, in the order in which it takes their addresses
 _ATTACHED = ("actq_last_error", "actq_group_stats", "actq_sample_sensitivity", "actq_allocate_bits_device", "actq_quantize_pack",
              "actq_unpack_dequantize", "actq_relu_mask_bytes", "actq_relu_forward", "actq_relu_backward", "actq_pool2d_output_size",
-             "actq_maxpool2d_forward", "actq_maxpool2d_backward", "actq_linear_backward")
+             "actq_maxpool2d_forward", "actq_maxpool2d_backward", "actq_linear_backward", "actq_head_norm_rotate", "actq_head_norm_workspace",
+             "actq_head_norm_rotate_backward", "actq_cache_write", "actq_cache_read", "actq_cache_attention_workspace", "actq_cache_attention")
 
 
 def host():
@@ -351,6 +387,48 @@ def tensor_stats(x, zr=None, stream=None):
     _check(lib().actq_tensor_stats(_dev(x, None, "x"), _dtype_code(x), int(x.numel()), _dev(zr, torch.float32, "zr"),
                                    _stream(stream)))
     return zr
+
+
+# ----------------------------------------------------------------------------- attention heads
+#
+# Tensors of heads are [tokens, heads, dim] (float32, float16 or bfloat16) with contiguous heads and any other strides.  These
+# calls run on the current stream, where what they allocate belongs.
+
+def head_norm_rotate(q, k, q_weight, k_weight, positions, cos, sin, eps: float = 1e-6, interleaved: bool = False, q_out=None, k_out=None):
+    """Device: RMS norm of every head of q and k (k may be None), times its weight (None: ones), and rotation by position, in one
+    launch.  `positions` int32 [tokens] are rows of the float32 tables cos and sin [rows, rotated / 2]; a position that is none of them
+    is padding and gives zeros.  Returns (q_out, k_out); q_out = q and k_out = k work in place."""
+    return (_host or host()).head_norm_rotate(q, k, q_weight, k_weight, positions, cos, sin, float(eps), bool(interleaved), q_out, k_out)
+
+
+def head_norm_rotate_backward(grad_q, grad_k, q, k, q_weight, k_weight, positions, cos, sin, eps: float = 1e-6, interleaved: bool = False,
+                              need_weights: bool = True):
+    """Device: gradients of head_norm_rotate's q, k, q_weight and k_weight from those of its outputs (None for what is None, and for
+    the weights unless need_weights)."""
+    return (_host or host()).head_norm_rotate_backward(grad_q, grad_k, q, k, q_weight, k_weight, positions, cos, sin, float(eps), bool(interleaved),
+                                                       bool(need_weights))
+
+
+def cache_write(k, v, slots, key_codes, key_header, value_codes, value_header) -> None:
+    """Device: quantises k and v [tokens, heads, dim] to nearest into the slots (int64 [tokens], page * page_size + offset) of a paged
+    cache: codes uint8 [pages, heads, page_size, dim * bits / 8] of 8 or 4 bits, headers float32 [pages, heads, page_size, 2].  A slot outside
+    the cache is skipped; none may be named twice."""
+    (_host or host()).cache_write(k, v, slots, key_codes, key_header, value_codes, value_header)
+
+
+def cache_read(slots, key_codes, key_header, value_codes, value_header, dim: int, dtype, k=None, v=None):
+    """Device: the keys and values that those slots hold, [tokens, heads, dim] of type dtype (zeros for a slot outside the cache)."""
+    return (_host or host()).cache_read(slots, key_codes, key_header, value_codes, value_header, int(dim), dtype, k, v)
+
+
+def cache_attention(q, key_codes, key_header, value_codes, value_header, table, lengths, query_start, max_query: int, max_length: int, scale=None,
+                    softcap: float = 0.0, window: int = 0, out=None):
+    """Device: attention of the new tokens q [tokens, heads, dim] over a paged cache that holds them too.  Sequence n has lengths[n]
+    tokens in pages table[n], the last of which are rows query_start[n] .. query_start[n + 1] - 1 of q (all int32).  Causal; with
+    window > 0 a token sees that many positions up to its own; softcap > 0 caps the scores.  max_query and max_length are the most new
+    tokens and the most tokens of a sequence, or more; scale defaults to dim ** -0.5."""
+    return (_host or host()).cache_attention(q, key_codes, key_header, value_codes, value_header, table, lengths, query_start, int(max_query),
+                                             int(max_length), scale, float(softcap), int(window), out)
 
 
 # ----------------------------------------------------------------------------- several tensors per launch

@@ -6,12 +6,13 @@ import os
 import shutil
 import subprocess
 import sys
+import tempfile
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(_HERE)
 CSRC = os.path.join(_HERE, "csrc")
 LIB = os.path.join(_HERE, "libactq.so")
-SOURCES = ["actq_api.cpp", "actq_kernels.hip", "actq_context.hip", "actq_linear.hip"]
+SOURCES = ["actq_api.cpp", "actq_kernels.hip", "actq_context.hip", "actq_linear.hip", "actq_head_norm.hip", "actq_cache.hip", "actq_attention.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -76,20 +77,28 @@ def hipcc() -> str:
 
 def build(verbose: bool = False) -> str:
     """Compile every source of the library; always recompiles."""
+    from concurrent.futures import ThreadPoolExecutor
     tmp = LIB + f".{os.getpid()}.tmp"
-    cmd = [hipcc(), *HIPCC_FLAGS, f'-DACTQ_SOURCE_HASH="{source_hash()}"',
-           "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-x", "hip"]
-    cmd += [os.path.join(CSRC, s) for s in SOURCES]
-    cmd += ["-o", tmp]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    r = subprocess.run(cmd, capture_output=True, text=True)
+    flags = [f for f in HIPCC_FLAGS if f != "-shared"]
     noise = "'-packed-fp32-ops' is not a recognized feature"
-    err = "\n".join(l for l in r.stderr.splitlines() if noise not in l)
-    if r.returncode != 0:
-        raise RuntimeError(f"hipcc failed:\n{err}")
-    if verbose and err.strip():
-        print(err, file=sys.stderr)
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        r = subprocess.run(cmd, capture_output=True, text=True)
+        err = "\n".join(l for l in r.stderr.splitlines() if noise not in l)
+        if r.returncode != 0:
+            raise RuntimeError(f"hipcc failed:\n{err}")
+        if verbose and err.strip():
+            print(err, file=sys.stderr)
+
+    # one object per source, side by side: the largest takes as long as the others together
+    with tempfile.TemporaryDirectory() as objects, ThreadPoolExecutor(min(len(SOURCES), os.cpu_count() or 1)) as pool:
+        common = [hipcc(), *flags, f'-DACTQ_SOURCE_HASH="{source_hash()}"', "-I", os.path.join(ROOT, "include"), "-I", CSRC]
+        made = [os.path.join(objects, s + ".o") for s in SOURCES]
+        for done in [pool.submit(run, [*common, "-x", "hip", "-c", os.path.join(CSRC, s), "-o", o]) for s, o in zip(SOURCES, made)]:
+            done.result()
+        run([hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", *made, "-o", tmp])
     os.replace(tmp, LIB)
     return LIB
 

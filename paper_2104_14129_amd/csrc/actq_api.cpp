@@ -440,4 +440,201 @@ int actq_linear_backward(const void* grad_y, const void* weight, const void* x, 
     return launch_linear_backward(grad_y, weight, x, dt, rows, inputs, outputs, grad_x, grad_w, grad_b, stream);
 }
 
+// ----------------------------------------------------------------------------- attention heads
+
+static int check_heads_dtype(const char* who, int dt)
+{
+    if (dt != ACTQ_F32 && dt != ACTQ_F16 && dt != ACTQ_BF16) return fail(ACTQ_EINVAL, "%s: unknown dtype %d", who, dt);
+    return ACTQ_OK;
+}
+
+static uintptr_t size_of(int dt) { return dt == ACTQ_F32 ? 4 : 2; }
+
+static int check_dim(const char* who, int32_t dim)
+{
+    if (dim != 64 && dim != 128 && dim != 256) return fail(ACTQ_EINVAL, "%s: unsupported head size %d (64, 128 or 256)", who, dim);
+    return ACTQ_OK;
+}
+
+// Threads of a launch are counted in 32 bits, and a head takes up to 64 of them.
+static constexpr int64_t kMostHeads = int64_t(1) << 26;
+static constexpr int64_t kMostStride = int64_t(1) << 36;
+
+static int check_tokens(const char* who, int64_t tokens, int64_t heads)
+{
+    if (heads < 1 || heads > 65535) return fail(ACTQ_EINVAL, "%s: the number of heads must be in [1, 65535]", who);
+    if (tokens < 0 || tokens >= kMostHeads || tokens * heads >= kMostHeads) return fail(ACTQ_EINVAL, "%s: tokens must be at least 0 and tokens * heads below 2^26", who);
+    return ACTQ_OK;
+}
+
+static int check_heads(const char* who, const char* name, const actq_heads* h, int dt, int64_t tokens, int32_t heads)
+{
+    if (!h) return fail(ACTQ_EINVAL, "%s: null %s", who, name);
+    if (h->heads != heads) return fail(ACTQ_EINVAL, "%s: %s has %d heads, expected %d", who, name, h->heads, heads);
+    if (int rc = check_tokens(who, tokens, heads)) return rc;
+    if (tokens == 0) return ACTQ_OK;
+    if (!h->data || !aligned(h->data, size_of(dt))) return fail(ACTQ_EINVAL, "%s: %s is null or not aligned to its element size", who, name);
+    // (tokens - 1) * |stride| stays below 2^62
+    if (h->token_stride <= -kMostStride || h->token_stride >= kMostStride || h->head_stride <= -kMostStride || h->head_stride >= kMostStride)
+        return fail(ACTQ_EINVAL, "%s: strides of %s out of range", who, name);
+    return ACTQ_OK;
+}
+
+static int check_rotation(const char* who, const actq_rotation* r, int64_t tokens, int32_t dim)
+{
+    if (!r) return fail(ACTQ_EINVAL, "%s: null rotation", who);
+    if (r->rotated < 16 || r->rotated > dim || r->rotated % 16 != 0) return fail(ACTQ_EINVAL, "%s: rotated must be a multiple of 16 from 16 to the head size, got %d", who, r->rotated);
+    if (r->interleaved != 0 && r->interleaved != 1) return fail(ACTQ_EINVAL, "%s: interleaved must be 0 or 1", who);
+    if (r->rows < 1 || r->rows >= (int64_t(1) << 31)) return fail(ACTQ_EINVAL, "%s: rows of the rotation's tables out of range", who);
+    if (tokens == 0) return ACTQ_OK;
+    if (!r->positions || !r->cos || !r->sin || !aligned(r->positions, 4) || !aligned(r->cos, 4) || !aligned(r->sin, 4))
+        return fail(ACTQ_EINVAL, "%s: positions, cos or sin is null or misaligned", who);
+    return ACTQ_OK;
+}
+
+// What the forward and the backward call of the head norm have in common.
+static int check_norm(const char* who, const actq_heads* q, const actq_heads* k, int dt, int64_t tokens, int32_t dim, const void* q_weight, const void* k_weight,
+                      int weight_dt, const actq_rotation* rotation, float eps)
+{
+    if (int rc = check_heads_dtype(who, dt)) return rc;
+    if (int rc = check_dim(who, dim)) return rc;
+    if (!q) return fail(ACTQ_EINVAL, "%s: null q", who);
+    if (int rc = check_heads(who, "q", q, dt, tokens, q->heads)) return rc;
+    if (k) {
+        if (int rc = check_heads(who, "k", k, dt, tokens, k->heads)) return rc;
+        if (int rc = check_tokens(who, tokens, static_cast<int64_t>(q->heads) + k->heads)) return rc;
+    }
+    if (weight_dt != dt && weight_dt != ACTQ_F32) return fail(ACTQ_EINVAL, "%s: weights must have the heads' type or ACTQ_F32", who);
+    if (!aligned(q_weight, size_of(weight_dt)) || !aligned(k_weight, size_of(weight_dt))) return fail(ACTQ_EINVAL, "%s: a weight is not aligned to its element size", who);
+    if (int rc = check_rotation(who, rotation, tokens, dim)) return rc;
+    if (!(eps > 0.0f) || std::isinf(eps)) return fail(ACTQ_EINVAL, "%s: eps must be finite and above zero", who);
+    return ACTQ_OK;
+}
+
+int actq_head_norm_rotate(const actq_heads* q, const actq_heads* k, actq_dtype dt, int64_t tokens, int32_t dim, const void* q_weight, const void* k_weight,
+                          actq_dtype weight_dt, const actq_rotation* rotation, float eps, const actq_heads* q_out, const actq_heads* k_out, void* stream)
+{
+    const char* who = "actq_head_norm_rotate";
+    if (int rc = check_norm(who, q, k, dt, tokens, dim, q_weight, k_weight, weight_dt, rotation, eps)) return rc;
+    if (int rc = check_heads(who, "q_out", q_out, dt, tokens, q->heads)) return rc;
+    if (k)
+        if (int rc = check_heads(who, "k_out", k_out, dt, tokens, k->heads)) return rc;
+    if (tokens == 0) return ACTQ_OK;
+    return launch_head_norm(q, k, dt, tokens, dim, q_weight, k_weight, weight_dt, rotation, eps, q_out, k ? k_out : nullptr, stream);
+}
+
+int actq_head_norm_workspace(int64_t tokens, int32_t dim, uint64_t* bytes_host)
+{
+    const char* who = "actq_head_norm_workspace";
+    if (int rc = check_dim(who, dim)) return rc;
+    if (int rc = check_tokens(who, tokens, 1)) return rc;
+    if (!bytes_host) return fail(ACTQ_EINVAL, "%s: null output", who);
+    *bytes_host = head_norm_workspace(tokens, dim);
+    return ACTQ_OK;
+}
+
+int actq_head_norm_rotate_backward(const actq_heads* grad_q, const actq_heads* grad_k, const actq_heads* q, const actq_heads* k, actq_dtype dt, int64_t tokens,
+                                   int32_t dim, const void* q_weight, const void* k_weight, actq_dtype weight_dt, const actq_rotation* rotation, float eps,
+                                   const actq_heads* grad_q_in, const actq_heads* grad_k_in, void* grad_q_weight, void* grad_k_weight, void* workspace,
+                                   uint64_t workspace_bytes, void* stream)
+{
+    const char* who = "actq_head_norm_rotate_backward";
+    if (int rc = check_norm(who, q, k, dt, tokens, dim, q_weight, k_weight, weight_dt, rotation, eps)) return rc;
+    if (int rc = check_heads(who, "grad_q", grad_q, dt, tokens, q->heads)) return rc;
+    if (int rc = check_heads(who, "grad_q_in", grad_q_in, dt, tokens, q->heads)) return rc;
+    if (k) {
+        if (int rc = check_heads(who, "grad_k", grad_k, dt, tokens, k->heads)) return rc;
+        if (int rc = check_heads(who, "grad_k_in", grad_k_in, dt, tokens, k->heads)) return rc;
+    }
+    if (!aligned(grad_q_weight, size_of(weight_dt)) || !aligned(grad_k_weight, size_of(weight_dt)))
+        return fail(ACTQ_EINVAL, "%s: a weight's gradient is not aligned to its element size", who);
+    if (grad_k_weight && !k) return fail(ACTQ_EINVAL, "%s: grad_k_weight without k", who);
+    if ((grad_q_weight || grad_k_weight) && tokens > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < head_norm_workspace(tokens, dim)))
+        return fail(ACTQ_EINVAL, "%s: the workspace is null, misaligned or smaller than actq_head_norm_workspace says", who);
+    return launch_head_norm_backward(grad_q, grad_k, q, k, dt, tokens, dim, q_weight, k_weight, weight_dt, rotation, eps, grad_q_in, k ? grad_k_in : nullptr,
+                                     grad_q_weight, grad_k_weight, workspace, stream);
+}
+
+static int check_cache(const char* who, const actq_cache* c)
+{
+    if (!c) return fail(ACTQ_EINVAL, "%s: null cache", who);
+    if (int rc = check_dim(who, c->dim)) return rc;
+    if (c->pages < 1 || c->pages >= (int64_t(1) << 31)) return fail(ACTQ_EINVAL, "%s: the number of pages must be in [1, 2^31)", who);
+    if (c->page_size < 16 || c->page_size > 1024 || (c->page_size & (c->page_size - 1)) != 0)
+        return fail(ACTQ_EINVAL, "%s: page_size must be a power of two from 16 to 1024, got %d", who, c->page_size);
+    if (c->heads < 1 || c->heads > 65535) return fail(ACTQ_EINVAL, "%s: the number of heads must be in [1, 65535]", who);
+    if ((c->key_bits != 4 && c->key_bits != 8) || (c->value_bits != 4 && c->value_bits != 8)) return fail(ACTQ_EINVAL, "%s: key_bits and value_bits must be 4 or 8", who);
+    if (!c->key_codes || !c->key_header || !c->value_codes || !c->value_header) return fail(ACTQ_EINVAL, "%s: null pointer in the cache", who);
+    if (!aligned(c->key_codes, 16) || !aligned(c->value_codes, 16) || !aligned(c->key_header, 8) || !aligned(c->value_header, 8))
+        return fail(ACTQ_EINVAL, "%s: codes must be aligned to 16 bytes, headers to 8", who);
+    return ACTQ_OK;
+}
+
+static int check_cached(const char* who, const actq_cache* c, const actq_heads* k, const actq_heads* v, int dt, int64_t tokens, const int64_t* slots)
+{
+    if (int rc = check_cache(who, c)) return rc;
+    if (int rc = check_heads_dtype(who, dt)) return rc;
+    if (int rc = check_heads(who, "k", k, dt, tokens, c->heads)) return rc;
+    if (int rc = check_heads(who, "v", v, dt, tokens, c->heads)) return rc;
+    if (tokens > 0 && (!slots || !aligned(slots, 8))) return fail(ACTQ_EINVAL, "%s: slots is null or misaligned", who);
+    return ACTQ_OK;
+}
+
+int actq_cache_write(const actq_cache* cache, const actq_heads* k, const actq_heads* v, actq_dtype dt, int64_t tokens, const int64_t* slots, void* stream)
+{
+    if (int rc = check_cached("actq_cache_write", cache, k, v, dt, tokens, slots)) return rc;
+    return tokens == 0 ? ACTQ_OK : launch_cache_write(cache, k, v, dt, tokens, slots, stream);
+}
+
+int actq_cache_read(const actq_cache* cache, const int64_t* slots, int64_t tokens, const actq_heads* k, const actq_heads* v, actq_dtype dt, void* stream)
+{
+    if (int rc = check_cached("actq_cache_read", cache, k, v, dt, tokens, slots)) return rc;
+    return tokens == 0 ? ACTQ_OK : launch_cache_read(cache, k, v, dt, tokens, slots, stream);
+}
+
+// Sizes that shape the launch of the attention.
+static int check_attention(const char* who, const actq_cache* c, int32_t heads, int64_t tokens, int64_t sequences, int64_t max_query, int64_t max_length, int32_t window)
+{
+    if (int rc = check_cache(who, c)) return rc;
+    if (int rc = check_tokens(who, tokens, heads)) return rc;
+    if (heads % c->heads != 0) return fail(ACTQ_EINVAL, "%s: %d heads are no multiple of the cache's %d", who, heads, c->heads);
+    if (sequences < 0 || sequences * c->heads > (int64_t(1) << 20) || sequences > (int64_t(1) << 20)) return fail(ACTQ_EINVAL, "%s: sequences * cache heads must be at most 2^20", who);
+    if (max_query < 0 || max_length < 0 || max_query > (int64_t(1) << 30) || max_length > (int64_t(1) << 30))
+        return fail(ACTQ_EINVAL, "%s: max_query and max_length must be in [0, 2^30]", who);
+    if (window < 0 || window > (1 << 30)) return fail(ACTQ_EINVAL, "%s: window must be in [0, 2^30]", who);
+    return ACTQ_OK;
+}
+
+int actq_cache_attention_workspace(const actq_cache* cache, int32_t heads, int64_t tokens, int64_t sequences, int64_t max_query, int64_t max_length,
+                                   int32_t window, uint64_t* bytes_host)
+{
+    const char* who = "actq_cache_attention_workspace";
+    if (int rc = check_attention(who, cache, heads, tokens, sequences, max_query, max_length, window)) return rc;
+    if (!bytes_host) return fail(ACTQ_EINVAL, "%s: null output", who);
+    *bytes_host = cache_attention_workspace(cache, heads, tokens, sequences, max_query, max_length, window);
+    return ACTQ_OK;
+}
+
+int actq_cache_attention(const actq_cache* cache, const actq_heads* q, actq_dtype dt, int64_t tokens, int64_t sequences, const int32_t* table,
+                         int32_t table_width, const int32_t* lengths, const int32_t* query_start, int64_t max_query, int64_t max_length, float scale,
+                         float softcap, int32_t window, const actq_heads* out, void* workspace, uint64_t workspace_bytes, void* stream)
+{
+    const char* who = "actq_cache_attention";
+    if (!q) return fail(ACTQ_EINVAL, "%s: null q", who);
+    if (int rc = check_attention(who, cache, q->heads, tokens, sequences, max_query, max_length, window)) return rc;
+    if (int rc = check_heads_dtype(who, dt)) return rc;
+    if (int rc = check_heads(who, "q", q, dt, tokens, q->heads)) return rc;
+    if (int rc = check_heads(who, "out", out, dt, tokens, q->heads)) return rc;
+    if (!(std::fabs(scale) < INFINITY) || !(softcap >= 0.0f && softcap < INFINITY)) return fail(ACTQ_EINVAL, "%s: scale must be finite, softcap finite and not negative", who);
+    if (tokens == 0 || sequences == 0) return ACTQ_OK;
+    if (!table || !lengths || !query_start || !aligned(table, 4) || !aligned(lengths, 4) || !aligned(query_start, 4))
+        return fail(ACTQ_EINVAL, "%s: table, lengths or query_start is null or misaligned", who);
+    if (table_width < 1 || static_cast<int64_t>(table_width) * cache->page_size > (int64_t(1) << 30)) return fail(ACTQ_EINVAL, "%s: table_width * page_size must be in [1, 2^30]", who);
+    const uint64_t need = cache_attention_workspace(cache, q->heads, tokens, sequences, max_query, max_length, window);
+    if (need > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < need))
+        return fail(ACTQ_EINVAL, "%s: the workspace is null, misaligned or smaller than actq_cache_attention_workspace says", who);
+    return launch_cache_attention(cache, q, dt, tokens, sequences, table, table_width, lengths, query_start, max_query, max_length, scale, softcap, window, out,
+                                  need > 0 ? workspace : nullptr, stream);
+}
+
 }  // extern "C"

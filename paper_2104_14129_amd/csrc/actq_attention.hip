@@ -1,0 +1,676 @@
+// Attention of new tokens over a paged, quantised cache.
+//
+//   out = sum_j p_j v_j / sum_j p_j,  p_j = 2^(x_j - m),  x_j = log2(e) cap(scale q . k_j)
+//
+// with k_j = Zk_j + step_j code_j and v_j likewise.  The codes stay whole numbers: as they are, a byte or a nibble under zeros, they
+// are subnormal binary16 numbers code * 2^-24, which the matrix instructions multiply exactly, so that
+//   q . k_j = step_j 2^24 (q . code_j 2^-24) + Zk_j sum(q)
+// has no rounding but that of its binary32 sum.  q is scaled by a power of two so that its largest element fills binary16's range
+// (exact for 16-bit types; binary32 takes two binary16 numbers, 22 bits).  The values' codes are centred, u_j = code_j - c, and
+//   sum_j p_j v_j = sum_j (p_j step_j) u_j + sum_j p_j (Zv_j + c step_j),
+// the second sum in binary32, one number per row.  p_j step_j is rounded to binary16 (to two of them for binary32 outputs) at a scale
+// 2^E of the largest step so far; centred codes keep that error at what rounding the values themselves would cost.
+//
+// Scores are computed transposed, keys by rows: a lane holds keys of one row, so that maximum and sum are per lane, and the
+// probabilities are already laid out as the right operand of the second product, whose keys come in the same order.  A group's
+// constants lie in the lanes of the 16-lane row that needs them and are broadcast by the instruction that uses them (DPP).
+// The running maximum m moves only when a score passes it by 8 (p <= 2^8 then), so that sums are rarely rescaled.
+#include "actq_heads.h"
+
+namespace actq {
+namespace {
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+constexpr float kNothing = -3.0e38f;   // running maximum of a row that has seen no key
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kSlack = 8.0f;         // by how much a score may pass the running maximum
+constexpr int kStepBits = 6;           // p * step is scaled to stay below 2^(kSlack + kStepBits + 1), inside binary16's range
+constexpr int kUnitBits = 9;           // centred codes are held as code * 2^-9
+
+struct AttendArgs {
+    const uint8_t* key_codes;
+    const float* key_header;
+    const uint8_t* value_codes;
+    const float* value_header;
+    int64_t pages;
+    int32_t page_shift, kv_heads;
+    int32_t key_bits, value_bits;
+    HeadsOf<const void> q;      // strides in elements of dtype
+    HeadsOf<void> out;
+    int32_t dtype;
+    int32_t tokens, sequences, q_heads, group;
+    FastDiv by_group;
+    const int32_t* table;
+    int32_t table_width;
+    const int32_t* lengths;
+    const int32_t* query_start;
+    float factor;               // scale * log2(e); with a cap scale / cap
+    float cap;                  // softcap * log2(e); 0: none
+    int32_t window;             // 0: none
+    uint32_t tiles, parts;      // row tiles of the grid, parts of the keys
+    FastDiv by_tiles, by_parts, by_heads;
+    int32_t per_part;           // keys of a part, a multiple of the kernels' block of keys
+    float* partial;             // [parts][tokens * q_heads][dim], null: one part
+    float* partial_lse;         // [parts][tokens * q_heads]
+};
+
+__device__ __forceinline__ uint32_t divide(uint32_t n, FastDiv by) { return (__umulhi(n, by.m) + n) >> by.s; }
+
+// What a workgroup is for.
+struct Work {
+    int32_t sequence, head, part, tile;
+    int32_t start, rows, length, first;   // first row of q; rows (new tokens * group); tokens in the cache; position of the first new token
+};
+
+__device__ __forceinline__ Work work_of(const AttendArgs& a, uint32_t id)
+{
+    Work w;
+    const uint32_t by_tile = divide(id, a.by_tiles), by_part = divide(by_tile, a.by_parts);
+    w.tile = static_cast<int32_t>(id - by_tile * a.tiles);
+    w.part = static_cast<int32_t>(by_tile - by_part * a.parts);
+    w.sequence = static_cast<int32_t>(divide(by_part, a.by_heads));
+    w.head = static_cast<int32_t>(by_part - w.sequence * a.kv_heads);
+    const int32_t start = a.query_start[w.sequence], end = a.query_start[w.sequence + 1];
+    w.start = min(max(start, 0), a.tokens);
+    const int32_t count = max(min(end, a.tokens) - w.start, 0);
+    w.rows = count * a.group;
+    w.length = static_cast<int32_t>(min(static_cast<int64_t>(max(a.lengths[w.sequence], 0)), static_cast<int64_t>(a.table_width) << a.page_shift));
+    w.first = w.length - count;
+    return w;
+}
+
+// Keys that the rows [row, row + count) of a sequence see, cut to a part: [begin, end), begin a multiple of `block`.
+struct Span {
+    int32_t begin, end;
+    int32_t low, high;   // positions of the first and the last row
+    int32_t from;        // first key that any row sees
+
+    // Whether some row does not see some of the keys [base, base + block).
+    __device__ __forceinline__ bool edge(int32_t base, int32_t block, int32_t window) const
+    {
+        return base + block - 1 > low || base + block > end || (window > 0 && base <= high - window);
+    }
+};
+
+__device__ __forceinline__ Span span_of(const AttendArgs& a, const Work& w, int32_t row, int32_t count, int32_t block)
+{
+    Span s;
+    s.low = w.first + static_cast<int32_t>(divide(row, a.by_group));
+    s.high = w.first + static_cast<int32_t>(divide(min(row + count, w.rows) - 1, a.by_group));
+    s.from = a.window > 0 ? max(s.low - a.window + 1, 0) : 0;
+    const int32_t to = s.high + 1;
+    // 64 bits: parts beyond a short sequence's end
+    const int64_t begin = s.from / block * block + static_cast<int64_t>(w.part) * a.per_part;
+    s.begin = static_cast<int32_t>(min(begin, static_cast<int64_t>(max(to, 0))));
+    s.end = w.part == static_cast<int32_t>(a.parts) - 1 ? to : static_cast<int32_t>(min(begin + a.per_part, static_cast<int64_t>(to)));
+    return s;
+}
+
+__device__ __forceinline__ int64_t page_of(const AttendArgs& a, const int32_t* table, int32_t key)
+{
+    const int32_t at = min(key >> a.page_shift, a.table_width - 1);
+    const int32_t page = table[at];
+    return min(max(static_cast<int64_t>(page), static_cast<int64_t>(0)), a.pages - 1);
+}
+
+// Row of the pages where the 16 keys from `key` on lie; key is a multiple of 16, and so is a page.
+__device__ __forceinline__ int64_t row_of(const AttendArgs& a, int32_t head, int64_t page, int32_t key)
+{
+    return ((page * a.kv_heads + head) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
+}
+
+__device__ __forceinline__ void load_eight(const void* p, int dtype, int64_t at, float (&f)[8])
+{
+    if (dtype == ACTQ_F32) {
+        Eight<float> e;
+        e.load(static_cast<const float*>(p) + at);
+        e.widen(f);
+    } else if (dtype == ACTQ_F16) {
+        Eight<_Float16> e;
+        e.load(static_cast<const _Float16*>(p) + at);
+        e.widen(f);
+    } else {
+        Eight<__bf16> e;
+        e.load(static_cast<const __bf16*>(p) + at);
+        e.widen(f);
+    }
+}
+
+__device__ __forceinline__ void store_element(void* p, int dtype, int64_t at, float v)
+{
+    if (dtype == ACTQ_F32) static_cast<float*>(p)[at] = v;
+    else if (dtype == ACTQ_F16) static_cast<_Float16*>(p)[at] = static_cast<_Float16>(v);
+    else static_cast<__bf16*>(p)[at] = static_cast<__bf16>(v);
+}
+
+template <int N>
+__device__ __forceinline__ void store_some(void* p, int dtype, int64_t at, const float (&f)[N])
+{
+    static_assert(N % 4 == 0, "whole vectors");
+    const auto put = [&](auto type) {
+        typedef decltype(type) T;
+        typedef T vector __attribute__((ext_vector_type(4)));
+        typedef vector unaligned __attribute__((aligned(sizeof(T))));
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            vector v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = static_cast<T>(f[i + j]);
+            *reinterpret_cast<unaligned*>(static_cast<T*>(p) + at + i) = v;
+        }
+    };
+    if (dtype == ACTQ_F32) put(float{});
+    else if (dtype == ACTQ_F16) put(_Float16{});
+    else put(__bf16{});
+}
+
+__device__ __forceinline__ int exponent(float v) { return static_cast<int>(__builtin_bit_cast(uint32_t, v) >> 23 & 255u) - 127; }
+
+// Whether v is exactly that constant.  Of the bits: the compiler takes it that floating-point data holds no NaN, and may ask the
+// opposite question, to which a NaN gives the same answer.
+__device__ __forceinline__ bool is(float v, float constant) { return __builtin_bit_cast(uint32_t, v) == __builtin_bit_cast(uint32_t, constant); }
+
+__device__ __forceinline__ float wave_max(float v)
+{
+    return over_lanes<64>(v, [](float a, float b) { return fmaxf(a, b); });
+}
+
+// tanh(x): for 16-bit outputs from one exponential, off by some 2^-23 of the cap; for binary32 the function's own.
+template <bool FINE>
+__device__ __forceinline__ float tanh_of(float x)
+{
+    if (FINE) return tanhf(x);
+    const float e = __builtin_amdgcn_exp2f(x * (2.0f * kLog2e));
+    return 1.0f - 2.0f * __builtin_amdgcn_rcpf(e + 1.0f);
+}
+
+// f16 pair under zeros: byte B of `low` and of `high`.
+template <int B>
+__device__ __forceinline__ uint32_t byte_pair(uint32_t low, uint32_t high)
+{
+    return __builtin_amdgcn_perm(high, low, B | 0x0c00 | (4 + B) << 16 | 0x0c000000);
+}
+
+// The lane's order of a word's eight nibbles as pairs of nibble and nibble four further up: 0 4 1 5 2 6 3 7.
+__device__ __forceinline__ int code_order(int bits, int j) { return bits == 8 ? j : (j >> 1) + 4 * (j & 1); }
+
+// Eight codes as subnormal binary16 numbers: two words of bytes, or one of nibbles in code_order.
+template <int BITS>
+__device__ __forceinline__ f16x8 key_codes_of(const uint32_t* w)
+{
+    u32x4 r;
+    if (BITS == 8) {
+        r[0] = __builtin_amdgcn_perm(0, w[0], 0x0c010c00);
+        r[1] = __builtin_amdgcn_perm(0, w[0], 0x0c030c02);
+        r[2] = __builtin_amdgcn_perm(0, w[1], 0x0c010c00);
+        r[3] = __builtin_amdgcn_perm(0, w[1], 0x0c030c02);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = w[0] >> 4 * i & 0x000f000fu;
+    }
+    return __builtin_bit_cast(f16x8, r);
+}
+
+// Centred code pair (code - c) * 2^-9 of element I (of the words of two keys): exact in binary16.
+template <int BITS, int I>
+__device__ __forceinline__ f16x2 value_pair(const uint32_t* low, const uint32_t* high)
+{
+    if (BITS == 8) {
+        const f16x2 raw = __builtin_bit_cast(f16x2, byte_pair<I % 4>(low[I / 4], high[I / 4]));
+        return __builtin_elementwise_fma(raw, f16x2{32768.0f, 32768.0f}, f16x2{-0.25f, -0.25f});
+    }
+    const uint32_t both = byte_pair<I / 2 % 4>(low[I / 8], high[I / 8]);
+    // the upper nibble of a byte stands for 16 times as much
+    const f16x2 raw = __builtin_bit_cast(f16x2, both & (I % 2 ? 0x00f000f0u : 0x000f000fu));
+    const _Float16 unit = I % 2 ? 2048.0f : 32768.0f;
+    return __builtin_elementwise_fma(raw, f16x2{unit, unit}, f16x2{-0.015625f, -0.015625f});
+}
+
+// f(integral_constant 0), .., f(N - 1): a loop whose counter is a constant.
+template <int N, typename F, int I = 0>
+__device__ __forceinline__ void each(F f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>{});
+        each<N, F, I + 1>(f);
+    }
+}
+
+__device__ __forceinline__ f32x4 multiply(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// A group's constants, lane by lane: scores are key * (q . codes) + key_zero * sum(q); step and middle of the values.
+struct Constants {
+    float key, key_zero, step, middle;
+};
+
+// ----------------------------------------------------------------------------- few rows
+
+// Sixteen rows, whose keys four wavefronts share out in turn, blocks of 16 * TILES keys each.  Codes go from memory to the matrix
+// instructions without the LDS: of a 16-key tile a lane loads its own pieces of one key, and for the values its own columns of eight
+// keys, which it transposes itself as it widens them.  The next block's codes are loaded while one is computed.
+constexpr int kFewWaves = 4;
+
+template <int DIM, int SPLIT, int KEY_BITS, int VALUE_BITS>
+struct Few {
+    static constexpr int kTiles = DIM == 256 ? 2 : 4, kBlock = 16 * kTiles;
+    static constexpr int kSteps = DIM / 32;                              // of the first product
+    static constexpr int kKeyBytes = DIM * KEY_BITS / 8;
+    static constexpr int kPiece = kKeyBytes < 64 ? kKeyBytes / 4 : 16;   // bytes that a lane loads at once
+    static constexpr int kPieces = kKeyBytes / 4 / kPiece;
+    static constexpr int kPieceSteps = kPiece * 8 / KEY_BITS / 8;        // steps of the first product in a piece
+    static constexpr int kColumns = DIM / 16;                            // of the values, per lane
+    static constexpr int kValueBytes = kColumns * VALUE_BITS / 8;        // 2 to 16
+    static constexpr int kValueWords = (kValueBytes + 3) / 4;
+
+    struct Block {
+        uint32_t key[kTiles][kPieces][kPiece / 4];
+        uint32_t value[kTiles][4][kValueWords];   // [tile][key][word]
+        f32x2 key_header, value_header;           // of the lane's own key
+    };
+};
+
+template <int BYTES>
+__device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w)
+{
+    if constexpr (BYTES == 16) {
+        const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = v[i];
+    } else if constexpr (BYTES == 8) {
+        const u32x2 v = *reinterpret_cast<const u32x2*>(p);
+        w[0] = v[0];
+        w[1] = v[1];
+    } else if constexpr (BYTES == 4) {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else {
+        w[0] = *reinterpret_cast<const uint16_t*>(p);
+    }
+}
+
+template <int DIM, int SPLIT, int KEY_BITS, int VALUE_BITS>
+__global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArgs a)
+{
+    typedef Few<DIM, SPLIT, KEY_BITS, VALUE_BITS> K;
+    __shared__ float joined_out[2][K::kColumns][4][64];
+    __shared__ float joined_max[kFewWaves][16], joined_sum[kFewWaves][16];
+    const Work w = work_of(a, blockIdx.x);
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int n = lane % 16, g = lane / 16;
+    const int32_t* const table = a.table + static_cast<int64_t>(w.sequence) * a.table_width;
+    for (int32_t tile = w.tile; 16 * static_cast<int64_t>(tile) < w.rows; tile += a.tiles) {
+        const int32_t row = 16 * tile + n;
+        const bool there = row < w.rows;
+        const int32_t token = static_cast<int32_t>(divide(there ? row : w.rows - 1, a.by_group));
+        const int32_t head = w.head * a.group + (there ? row : w.rows - 1) - token * a.group;
+        const int32_t position = w.first + token;
+        const Span span = span_of(a, w, 16 * tile, 16, K::kBlock);
+
+        // q, a lane's 8 elements of its row for every step
+        f16x8 q[SPLIT][K::kSteps];
+        float q_sum = 0.0f;
+        int q_exponent;
+        {
+            const int64_t at = (static_cast<int64_t>(w.start) + token) * a.q.token + head * a.q.head;
+            float f[K::kSteps][8], top = 0.0f;
+#pragma unroll
+            for (int s = 0; s < K::kSteps; ++s) {
+                const int piece = s / K::kPieceSteps, in_piece = s % K::kPieceSteps;
+                load_eight(a.q.p, a.dtype, at + (4 * piece + g) * (8 * K::kPieceSteps) + 8 * in_piece, f[s]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    top = fmaxf(top, fabsf(f[s][j]));
+                    q_sum += f[s][j];
+                }
+            }
+            q_sum += __shfl_xor(q_sum, 16);
+            q_sum += __shfl_xor(q_sum, 32);
+            q_exponent = max(__builtin_amdgcn_readfirstlane(exponent(wave_max(top))), -100);
+#pragma unroll
+            for (int s = 0; s < K::kSteps; ++s)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float v = ldexpf(f[s][code_order(KEY_BITS, j)], 14 - q_exponent);
+                    q[0][s][j] = static_cast<_Float16>(v);
+                    if (SPLIT == 2) q[SPLIT - 1][s][j] = static_cast<_Float16>(v - static_cast<float>(q[0][s][j]));
+                }
+        }
+
+        float m = kNothing, sum = 0.0f, middle = 0.0f;
+        int E = -126;
+        f32x4 acc[K::kColumns];
+#pragma unroll
+        for (int i = 0; i < K::kColumns; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+        const auto load = [&](typename K::Block& b, int32_t base) {
+            int64_t rows[K::kTiles];
+#pragma unroll
+            for (int t = 0; t < K::kTiles; ++t) rows[t] = row_of(a, w.head, page_of(a, table, base + 16 * t), base + 16 * t);
+#pragma unroll
+            for (int t = 0; t < K::kTiles; ++t)
+#pragma unroll
+                for (int p = 0; p < K::kPieces; ++p)
+                    load_words<K::kPiece>(a.key_codes + rows[t] * K::kKeyBytes + n * K::kKeyBytes + (4 * p + g) * K::kPiece, b.key[t][p]);
+            // the lane's own key: number n % 4 of group g's four of tile n / 4
+            int64_t own = rows[0];
+#pragma unroll
+            for (int t = 1; t < K::kTiles; ++t) own = n / 4 % K::kTiles == t ? rows[t] : own;
+            own += 4 * g + n % 4;
+            b.key_header = *reinterpret_cast<const f32x2*>(a.key_header + 2 * own);
+            b.value_header = *reinterpret_cast<const f32x2*>(a.value_header + 2 * own);
+#pragma unroll
+            for (int t = 0; t < K::kTiles; ++t)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    load_words<K::kValueBytes>(a.value_codes + (rows[t] + 4 * g + k) * (DIM * VALUE_BITS / 8) + n * K::kValueBytes, b.value[t][k]);
+        };
+
+        // EDGE: some row does not see some key of the block.  What a row does not see has no part in it, infinities and NaN among it.
+        const auto use = [&](const typename K::Block& b, int32_t base, auto edge) {
+            constexpr bool EDGE = decltype(edge)::value;
+            Constants c;
+            {
+                const int32_t own = base + 16 * (n / 4 % K::kTiles) + 4 * g + n % 4;
+                const bool seen = !EDGE || (own >= span.from && own < span.end);   // by any row
+                const float step = seen ? b.value_header[1] : 0.0f;
+                c.key = ldexpf(b.key_header[1] * a.factor, 24 - 14 + q_exponent);
+                c.key_zero = b.key_header[0] * a.factor;
+                const int top = max(__builtin_amdgcn_readfirstlane(exponent(wave_max(exponent(step) == 128 ? 0.0f : step))), -126);
+                if (top > E) {
+#pragma unroll
+                    for (int i = 0; i < K::kColumns; ++i)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[i][r] = ldexpf(acc[i][r], E - top);
+                    E = top;
+                }
+                c.step = ldexpf(step, kStepBits - E);
+                c.middle = fmaf(VALUE_BITS == 8 ? 128.0f : 8.0f, step, b.value_header[0]);
+            }
+            f32x4 x[K::kTiles];
+#pragma unroll
+            for (int t = 0; t < K::kTiles; ++t) {
+                x[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                for (int s = 0; s < K::kSteps; ++s) {
+                    const f16x8 codes = key_codes_of<KEY_BITS>(&b.key[t][s / K::kPieceSteps][s % K::kPieceSteps * (KEY_BITS / 4)]);
+#pragma unroll
+                    for (int h = 0; h < SPLIT; ++h) x[t] = multiply(codes, q[h][s], x[t]);
+                }
+            }
+            float top = kNothing;
+            each<K::kTiles>([&](auto t) {
+                each<4>([&](auto e) {
+                    constexpr int i = e, kAt = kDppBroadcast + 4 * t + i;
+                    x[t][i] = fmaf(dpp<kAt>(c.key), x[t][i], dpp<kAt>(c.key_zero) * q_sum);
+                });
+            });
+            if (a.cap > 0.0f) {
+#pragma unroll
+                for (int t = 0; t < K::kTiles; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[t][i] = a.cap * tanh_of<SPLIT == 2>(x[t][i]);
+            }
+            uint32_t hidden = 0;
+            if (EDGE) {
+#pragma unroll
+                for (int t = 0; t < K::kTiles; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int32_t key = base + 16 * t + 4 * g + i;
+                        if (key >= span.end || key > position || (a.window > 0 && key <= position - a.window)) {
+                            x[t][i] = -INFINITY;
+                            hidden |= 1u << (4 * t + i);
+                        }
+                    }
+            }
+#pragma unroll
+            for (int t = 0; t < K::kTiles; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, x[t][i]);
+            if (__any(top > m + kSlack)) {
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float now = fmaxf(m, top), less = __builtin_amdgcn_exp2f(m - now);
+                m = now;
+                sum *= less;
+                middle *= less;
+#pragma unroll
+                for (int i = 0; i < K::kColumns; ++i) acc[i] *= less;
+            }
+            f16x8 p[SPLIT][K::kTiles / 2];
+            each<K::kTiles>([&](auto t) {
+                each<4>([&](auto e) {
+                    constexpr int i = e, kAt = kDppBroadcast + 4 * t + i;
+                    const float v = __builtin_amdgcn_exp2f(x[t][i] - m);
+                    const bool off = EDGE && (hidden >> (4 * t + i) & 1u) != 0;
+                    sum += v;
+                    const float part = dpp<kAt>(c.middle) * v, product = dpp<kAt>(c.step) * v;
+                    middle += off ? 0.0f : part;
+                    const float weight = off ? 0.0f : product;
+                    const _Float16 high = static_cast<_Float16>(weight);
+                    p[0][t / 2][4 * (t % 2) + i] = high;
+                    if (SPLIT == 2) p[SPLIT - 1][t / 2][4 * (t % 2) + i] = static_cast<_Float16>(weight - static_cast<float>(high));
+                });
+            });
+#pragma unroll
+            for (int s = 0; s < K::kTiles / 2; ++s)
+                each<K::kColumns>([&](auto i) {
+                    f16x8 values;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const f16x2 pair = value_pair<VALUE_BITS, i>(b.value[2 * s + k / 2][2 * (k % 2)], b.value[2 * s + k / 2][2 * (k % 2) + 1]);
+                        values[2 * k] = pair[0];
+                        values[2 * k + 1] = pair[1];
+                    }
+#pragma unroll
+                    for (int h = 0; h < SPLIT; ++h) acc[i] = multiply(values, p[h][s], acc[i]);
+                });
+        };
+
+        int32_t base = span.begin + wave * K::kBlock;
+        if (base < span.end) {
+            typename K::Block now, next;
+            load(now, base);
+            while (true) {
+                const int32_t after = base + kFewWaves * K::kBlock;
+                if (after < span.end) load(next, after);
+                if (span.edge(base, K::kBlock, a.window)) use(now, base, std::true_type{});
+                else use(now, base, std::false_type{});
+                if (after >= span.end) break;
+                now = next;
+                base = after;
+            }
+        }
+
+        // the wavefronts' shares: a row's maximum and sum first, then the outputs in two steps through the LDS
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+        middle += __shfl_xor(middle, 16);
+        middle += __shfl_xor(middle, 32);
+        if (g == 0) {
+            joined_max[wave][n] = m;
+            joined_sum[wave][n] = sum;
+        }
+        __syncthreads();
+        float top = joined_max[0][n];
+#pragma unroll
+        for (int k = 1; k < kFewWaves; ++k) top = fmaxf(top, joined_max[k][n]);
+        float total = 0.0f;
+#pragma unroll
+        for (int k = 0; k < kFewWaves; ++k) total = fmaf(joined_sum[k][n], __builtin_amdgcn_exp2f(joined_max[k][n] - top), total);
+        const float share = __builtin_amdgcn_exp2f(m - top);
+#pragma unroll
+        for (int i = 0; i < K::kColumns; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[i][r] = (ldexpf(acc[i][r], E + kUnitBits - kStepBits) + middle) * share;
+#pragma unroll
+        for (int step = kFewWaves / 2; step >= 1; step /= 2) {
+            if (wave >= step && wave < 2 * step) {
+#pragma unroll
+                for (int i = 0; i < K::kColumns; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) joined_out[wave - step][i][r][lane] = acc[i][r];
+            }
+            __syncthreads();
+            if (wave < step) {
+#pragma unroll
+                for (int i = 0; i < K::kColumns; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[i][r] += joined_out[wave][i][r][lane];
+            }
+        }
+        if (wave == 0 && there) {
+            const float scale = is(total, 0.0f) ? 0.0f : 1.0f / total;   // nothing in sight: zeros
+            const int64_t out_row = (static_cast<int64_t>(w.start) + token) * a.q_heads + head;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                float f[K::kColumns];
+#pragma unroll
+                for (int i = 0; i < K::kColumns; ++i) f[i] = acc[i][r] * scale;
+                const int at = K::kColumns * (4 * g + r);
+                if (a.partial) store_some(a.partial, ACTQ_F32, (static_cast<int64_t>(w.part) * a.tokens * a.q_heads + out_row) * DIM + at, f);
+                else store_some(a.out.p, a.dtype, (static_cast<int64_t>(w.start) + token) * a.out.token + head * a.out.head + at, f);
+            }
+            if (a.partial && g == 0) a.partial_lse[static_cast<int64_t>(w.part) * a.tokens * a.q_heads + out_row] = is(total, 0.0f) ? kNothing : top + __builtin_amdgcn_logf(total);
+        }
+        __syncthreads();   // the next tile writes the LDS again
+    }
+}
+
+// ----------------------------------------------------------------------------- joining parts
+
+// A wavefront per row: the parts' outputs weighted by 2^(lse - largest).
+constexpr int kJoinWaves = 4;
+
+template <int DIM>
+__global__ __launch_bounds__(kJoinWaves * 64) void attend_join_kernel(AttendArgs a)
+{
+    constexpr int kEach = DIM / 64;
+    const int lane = threadIdx.x % 64;
+    const int64_t rows = static_cast<int64_t>(a.tokens) * a.q_heads;
+    const int64_t row = static_cast<int64_t>(blockIdx.x) * kJoinWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    if (row >= rows) return;
+    float top = kNothing;
+    for (uint32_t p = 0; p < a.parts; ++p) top = fmaxf(top, a.partial_lse[p * rows + row]);
+    float total = 0.0f, sum[kEach] = {};
+    for (uint32_t p = 0; p < a.parts; ++p) {
+        const float lse = a.partial_lse[p * rows + row];
+        if (is(lse, kNothing)) continue;
+        const float weight = __builtin_amdgcn_exp2f(lse - top);
+        total += weight;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) sum[i] = fmaf(weight, a.partial[(p * rows + row) * DIM + kEach * lane + i], sum[i]);
+    }
+    const int64_t token = row / a.q_heads, head = row - token * a.q_heads;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i)
+        store_element(a.out.p, a.dtype, token * a.out.token + head * a.out.head + kEach * lane + i, is(total, 0.0f) ? 0.0f : sum[i] / total);
+}
+
+// ----------------------------------------------------------------------------- launches
+
+constexpr int64_t kMostBlocks = int64_t(1) << 22;
+// Workgroups that the keys are cut for where there are few rows: two per compute unit are resident.
+constexpr int64_t kWantedBlocks = 1024;
+constexpr int64_t kMostParts = 128;
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+struct Shape {
+    int64_t tiles, parts, per_part;
+};
+
+Shape shape_of(const actq_cache* c, int32_t heads, int64_t sequences, int64_t max_query, int64_t max_length, int32_t window)
+{
+    const int64_t group = heads / c->heads, groups = sequences * c->heads;
+    Shape s;
+    s.tiles = ceil_div(max_query < 1 ? 1 : max_query * group, 16);
+    if (s.tiles > kMostBlocks / groups) s.tiles = kMostBlocks / groups;
+    const int64_t block = c->dim == 256 ? 32 : 64, least = kFewWaves * block;
+    int64_t span = max_length < 1 ? 1 : max_length;
+    if (window > 0 && span > window + ceil_div(16, group) + block) span = window + ceil_div(16, group) + block;
+    s.parts = ceil_div(kWantedBlocks, groups * s.tiles);
+    if (s.parts > ceil_div(span, least)) s.parts = ceil_div(span, least);
+    if (s.parts > kMostParts) s.parts = kMostParts;
+    s.per_part = ceil_div(ceil_div(span, s.parts), block) * block;
+    s.parts = ceil_div(span, s.per_part);
+    return s;
+}
+
+template <typename F>
+int by_bits(int bits, F f)
+{
+    return bits == 8 ? f(std::integral_constant<int, 8>{}) : f(std::integral_constant<int, 4>{});
+}
+
+}  // namespace
+
+uint64_t cache_attention_workspace(const actq_cache* c, int32_t heads, int64_t tokens, int64_t sequences, int64_t max_query, int64_t max_length, int32_t window)
+{
+    if (tokens == 0 || sequences == 0) return 0;
+    const Shape s = shape_of(c, heads, sequences, max_query, max_length, window);
+    return s.parts == 1 ? 0 : static_cast<uint64_t>(s.parts) * tokens * heads * (c->dim + 1) * sizeof(float);
+}
+
+int launch_cache_attention(const actq_cache* c, const actq_heads* q, int dtype, int64_t tokens, int64_t sequences, const int32_t* table, int32_t table_width,
+                           const int32_t* lengths, const int32_t* query_start, int64_t max_query, int64_t max_length, float scale, float softcap, int32_t window,
+                           const actq_heads* out, void* workspace, void* stream)
+{
+    const char* who = "actq_cache_attention";
+    const Shape shape = shape_of(c, q->heads, sequences, max_query, max_length, window);
+    AttendArgs a = {};
+    a.key_codes = c->key_codes;
+    a.key_header = c->key_header;
+    a.value_codes = c->value_codes;
+    a.value_header = c->value_header;
+    a.pages = c->pages;
+    a.page_shift = __builtin_ctz(static_cast<unsigned>(c->page_size));
+    a.kv_heads = c->heads;
+    a.key_bits = c->key_bits;
+    a.value_bits = c->value_bits;
+    a.q = {q->data, q->token_stride, q->head_stride};
+    a.out = {out->data, out->token_stride, out->head_stride};
+    a.dtype = dtype;
+    a.tokens = static_cast<int32_t>(tokens);
+    a.sequences = static_cast<int32_t>(sequences);
+    a.q_heads = q->heads;
+    a.group = q->heads / c->heads;
+    a.by_group = make_fastdiv(static_cast<uint32_t>(a.group));
+    a.table = table;
+    a.table_width = table_width;
+    a.lengths = lengths;
+    a.query_start = query_start;
+    a.factor = softcap > 0.0f ? scale / softcap : scale * kLog2e;
+    a.cap = softcap * kLog2e;
+    a.window = window;
+    a.tiles = static_cast<uint32_t>(shape.tiles);
+    a.parts = static_cast<uint32_t>(shape.parts);
+    a.by_tiles = make_fastdiv(a.tiles);
+    a.by_parts = make_fastdiv(a.parts);
+    a.by_heads = make_fastdiv(static_cast<uint32_t>(c->heads));
+    a.per_part = static_cast<int32_t>(shape.per_part);
+    if (shape.parts > 1) {
+        a.partial = static_cast<float*>(workspace);
+        a.partial_lse = a.partial + shape.parts * tokens * q->heads * c->dim;
+    }
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const unsigned blocks = static_cast<unsigned>(sequences * c->heads * shape.parts * shape.tiles);
+    const int rc = by_dim(c->dim, [&](auto d) {
+        return by_bits(c->key_bits, [&](auto kb) {
+            return by_bits(c->value_bits, [&](auto vb) {
+                constexpr int kDim = decltype(d)::value, kKey = decltype(kb)::value, kValue = decltype(vb)::value;
+                if (dtype == ACTQ_F32) launch(attend_few_kernel<kDim, 2, kKey, kValue>, blocks, kFewWaves * 64, s, a);
+                else launch(attend_few_kernel<kDim, 1, kKey, kValue>, blocks, kFewWaves * 64, s, a);
+                return launched(who);
+            });
+        });
+    });
+    if (rc != ACTQ_OK || shape.parts == 1) return rc;
+    return by_dim(c->dim, [&](auto d) {
+        launch(attend_join_kernel<decltype(d)::value>, static_cast<unsigned>(ceil_div(tokens * q->heads, kJoinWaves)), kJoinWaves * 64, s, a);
+        return launched(who);
+    });
+}
+
+}  // namespace actq

@@ -104,6 +104,20 @@ int launch_maxpool2d_backward(const uint8_t* argmax, const void* grad_y, int dty
 int launch_linear_backward(const void* grad_y, const void* weight, const void* x, int dtype, int64_t rows, int64_t inputs, int64_t outputs,
                            void* grad_x, void* grad_w, void* grad_b, void* stream);
 
+// Attention heads (head norm, cache and attention kernels files).
+uint64_t head_norm_workspace(int64_t tokens, int32_t dim);
+int launch_head_norm(const actq_heads* q, const actq_heads* k, int dtype, int64_t tokens, int32_t dim, const void* q_weight, const void* k_weight, int weight_dtype,
+                     const actq_rotation* rotation, float eps, const actq_heads* q_out, const actq_heads* k_out, void* stream);
+int launch_head_norm_backward(const actq_heads* grad_q, const actq_heads* grad_k, const actq_heads* q, const actq_heads* k, int dtype, int64_t tokens, int32_t dim,
+                              const void* q_weight, const void* k_weight, int weight_dtype, const actq_rotation* rotation, float eps, const actq_heads* q_out,
+                              const actq_heads* k_out, void* grad_q_weight, void* grad_k_weight, void* workspace, void* stream);
+int launch_cache_write(const actq_cache* c, const actq_heads* k, const actq_heads* v, int dtype, int64_t tokens, const int64_t* slots, void* stream);
+int launch_cache_read(const actq_cache* c, const actq_heads* k, const actq_heads* v, int dtype, int64_t tokens, const int64_t* slots, void* stream);
+uint64_t cache_attention_workspace(const actq_cache* c, int32_t heads, int64_t tokens, int64_t sequences, int64_t max_query, int64_t max_length, int32_t window);
+int launch_cache_attention(const actq_cache* c, const actq_heads* q, int dtype, int64_t tokens, int64_t sequences, const int32_t* table, int32_t table_width,
+                           const int32_t* lengths, const int32_t* query_start, int64_t max_query, int64_t max_length, float scale, float softcap, int32_t window,
+                           const actq_heads* out, void* workspace, void* stream);
+
 }  // namespace actq
 
 #endif

@@ -11,6 +11,7 @@
 // the library are built and replaced independently.
 #include <Python.h>
 
+#include <cmath>
 #include <cstdint>
 #include <cstring>
 #include <initializer_list>
@@ -25,6 +26,7 @@
 #include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -50,6 +52,13 @@ struct Api {
     decltype(&actq_maxpool2d_forward) maxpool2d_forward;
     decltype(&actq_maxpool2d_backward) maxpool2d_backward;
     decltype(&actq_linear_backward) linear_backward;
+    decltype(&actq_head_norm_rotate) head_norm_rotate;
+    decltype(&actq_head_norm_workspace) head_norm_workspace;
+    decltype(&actq_head_norm_rotate_backward) head_norm_rotate_backward;
+    decltype(&actq_cache_write) cache_write;
+    decltype(&actq_cache_read) cache_read;
+    decltype(&actq_cache_attention_workspace) cache_attention_workspace;
+    decltype(&actq_cache_attention) cache_attention;
 };
 Api api = {};
 PyObject* actq_error = nullptr;   // the binding's exception class, called with (code, message)
@@ -617,6 +626,283 @@ PyObject* maxpool2d_backward_impl(PyObject* const* a)
 }
 ACTQ_ENTRY(maxpool2d_backward, 10)
 
+// ----------------------------------------------------------------------------- attention heads
+
+actq_dtype heads_dtype(const Tensor& t, const char* name)
+{
+    if (t.scalar_type() == at::kFloat) return ACTQ_F32;
+    if (t.scalar_type() == at::kHalf) return ACTQ_F16;
+    TORCH_CHECK_TYPE(t.scalar_type() == at::kBFloat16, name, " must be torch.float32, torch.float16 or torch.bfloat16, got ", dtype_name(t.scalar_type()));
+    return ACTQ_BF16;
+}
+
+// These calls go to the current device's current stream.
+void on_current_device(const Tensor& t, const char* name)
+{
+    TORCH_CHECK_VALUE(t.is_cuda(), name, " must live on the GPU");
+    TORCH_CHECK_VALUE(t.get_device() == c10::hip::current_device(), name, " must live on the current device");
+    TORCH_CHECK_VALUE(t.layout() == at::kStrided && !t.is_neg(), name, " must be an ordinary tensor in memory");
+}
+
+Memory contiguous_on_device(const Tensor& t, at::ScalarType type, const char* name)
+{
+    on_current_device(t, name);
+    return on_gpu(t, type, name);
+}
+
+// [tokens, heads, dim] as the library takes it.
+actq_heads heads_of(const Tensor& t, const char* name)
+{
+    on_current_device(t, name);
+    TORCH_CHECK_VALUE(t.dim() == 3, name, " must be [tokens, heads, dim]");
+    TORCH_CHECK_VALUE(t.stride(2) == 1 || t.numel() == 0, name, " must have contiguous heads");
+    TORCH_CHECK_VALUE(t.size(1) <= INT32_MAX && t.size(2) <= INT32_MAX, name, " is too large");
+    return {t.data_ptr(), t.stride(0), t.stride(1), static_cast<int32_t>(t.size(1))};
+}
+
+// One that is written: elements do not share memory.
+actq_heads heads_to(const Tensor& t, const char* name)
+{
+    for (int64_t i = 0; i < t.dim(); ++i) TORCH_CHECK_VALUE(t.size(i) <= 1 || t.stride(i) != 0, name, " must not be expanded");
+    return heads_of(t, name);
+}
+
+void same_heads(const Tensor& t, const Tensor& like, const char* name)
+{
+    TORCH_CHECK_VALUE(t.sizes() == like.sizes(), name, " has another shape than expected");
+    TORCH_CHECK_TYPE(t.scalar_type() == like.scalar_type(), name, " must be ", dtype_name(like.scalar_type()), ", got ", dtype_name(t.scalar_type()));
+}
+
+struct Norm {
+    Tensor q, positions, cos, sin;
+    std::optional<Tensor> k, q_weight, k_weight;
+    actq_heads hq, hk;
+    const actq_heads* k_heads;   // null without k
+    actq_dtype dt, weight_dt;
+    at::ScalarType weight_type;
+    int64_t tokens;
+    int32_t dim;
+    Memory wq, wk;
+    actq_rotation rotation;
+    float eps;
+};
+
+// (q, k or None, q_weight or None, k_weight or None, positions, cos, sin, eps, interleaved)
+void norm_of(PyObject* const* a, Norm& n)
+{
+    n.q = tensor_of(a[0], "q");
+    n.k = optional_tensor(a[1], "k");
+    n.q_weight = optional_tensor(a[2], "q_weight");
+    n.k_weight = optional_tensor(a[3], "k_weight");
+    n.positions = tensor_of(a[4], "positions");
+    n.cos = tensor_of(a[5], "cos");
+    n.sin = tensor_of(a[6], "sin");
+    n.dt = heads_dtype(n.q, "q");
+    n.hq = heads_of(n.q, "q");
+    n.tokens = n.q.size(0);
+    n.dim = static_cast<int32_t>(n.q.size(2));
+    n.k_heads = nullptr;
+    if (n.k) {
+        n.hk = heads_of(*n.k, "k");
+        TORCH_CHECK_VALUE(n.k->size(0) == n.tokens && n.k->size(2) == n.dim, "q and k must have the same tokens and head size");
+        TORCH_CHECK_TYPE(n.k->scalar_type() == n.q.scalar_type(), "q and k must have the same dtype");
+        n.k_heads = &n.hk;
+    }
+    TORCH_CHECK_VALUE(n.k || !n.k_weight, "k_weight without k");
+    n.weight_type = n.q_weight ? n.q_weight->scalar_type() : n.k_weight ? n.k_weight->scalar_type() : at::kFloat;
+    n.weight_dt = n.weight_type == at::kFloat ? ACTQ_F32 : n.dt;
+    TORCH_CHECK_TYPE(n.weight_type == at::kFloat || n.weight_type == n.q.scalar_type(), "weights must have the heads' dtype or torch.float32");
+    n.wq = n.wk = {nullptr};
+    if (n.q_weight) {
+        TORCH_CHECK_VALUE(n.q_weight->numel() == n.dim, "q_weight must have dim entries");
+        n.wq = contiguous_on_device(*n.q_weight, n.weight_type, "q_weight");
+    }
+    if (n.k_weight) {
+        TORCH_CHECK_VALUE(n.k_weight->numel() == n.dim, "k_weight must have dim entries");
+        n.wk = contiguous_on_device(*n.k_weight, n.weight_type, "k_weight");
+    }
+    TORCH_CHECK_VALUE(n.positions.dim() == 1 && n.positions.size(0) == n.tokens, "positions must have an entry per token");
+    TORCH_CHECK_VALUE(n.cos.dim() == 2 && n.cos.sizes() == n.sin.sizes(), "cos and sin must be [rows, rotated / 2]");
+    TORCH_CHECK_VALUE(n.cos.size(1) <= 128, "cos and sin have more columns than a head has pairs");
+    const Memory positions = contiguous_on_device(n.positions, at::kInt, "positions"), cos = contiguous_on_device(n.cos, at::kFloat, "cos");
+    const Memory sin = contiguous_on_device(n.sin, at::kFloat, "sin");
+    n.rotation = {positions, cos, sin, n.cos.size(0), static_cast<int32_t>(2 * n.cos.size(1)), a[8] == Py_True};
+    n.eps = static_cast<float>(PyFloat_AsDouble(a[7]));
+    if (PyErr_Occurred()) throw python_error();
+}
+
+// What an output is unless one is passed: contiguous.
+Tensor heads_output(PyObject* passed, const Tensor& like, const char* name)
+{
+    if (passed == Py_None) return empty_on(like, like.sizes(), like.scalar_type());
+    const Tensor& t = tensor_of(passed, name);
+    same_heads(t, like, name);
+    return t;
+}
+
+PyObject* wrap_or_none(const Tensor& t)
+{
+    if (t.defined()) return THPVariable_Wrap(t);
+    Py_INCREF(Py_None);
+    return Py_None;
+}
+
+// norm_of's nine, (q_out or None, k_out or None) -> (q_out, k_out or None)
+PyObject* head_norm_rotate_impl(PyObject* const* a)
+{
+    Norm n;
+    norm_of(a, n);
+    const Tensor q_out = heads_output(a[9], n.q, "q_out");
+    const actq_heads hq = heads_to(q_out, "q_out");
+    Tensor k_out;
+    actq_heads hk = {};
+    if (n.k) {
+        k_out = heads_output(a[10], *n.k, "k_out");
+        hk = heads_to(k_out, "k_out");
+    }
+    TORCH_CHECK_VALUE(n.k || a[10] == Py_None, "k_out without k");
+    const actq_heads* const k_to = n.k ? &hk : nullptr;
+    call(api.head_norm_rotate, &n.hq, n.k_heads, n.dt, n.tokens, n.dim, n.wq, n.wk, n.weight_dt, &n.rotation, n.eps, &hq, k_to, current_stream());
+    return tuple_of({wrap_or_none(q_out), wrap_or_none(k_out)});
+}
+ACTQ_ENTRY(head_norm_rotate, 11)
+
+// (grad_q, grad_k or None), norm_of's nine, whether the weights need theirs -> gradients of q, k, q_weight, k_weight (None for what is None)
+PyObject* head_norm_rotate_backward_impl(PyObject* const* a)
+{
+    Norm n;
+    norm_of(a + 2, n);
+    const Tensor& grad_q = tensor_of(a[0], "grad_q");
+    const std::optional<Tensor> grad_k = optional_tensor(a[1], "grad_k");
+    TORCH_CHECK_VALUE(grad_k.has_value() == n.k.has_value(), "grad_k goes with k");
+    same_heads(grad_q, n.q, "grad_q");
+    const actq_heads gq = heads_of(grad_q, "grad_q");
+    const Tensor q_in = empty_on(n.q, n.q.sizes(), n.q.scalar_type());
+    const actq_heads to_q = heads_of(q_in, "grad_q");
+    Tensor k_in, q_weight, k_weight, workspace;
+    actq_heads gk = {}, to_k = {};
+    if (n.k) {
+        same_heads(*grad_k, *n.k, "grad_k");
+        gk = heads_of(*grad_k, "grad_k");
+        k_in = empty_on(*n.k, n.k->sizes(), n.k->scalar_type());
+        to_k = heads_of(k_in, "grad_k");
+    }
+    uint64_t bytes = 0;
+    if (a[11] == Py_True) {
+        if (n.q_weight) q_weight = empty_on(n.q, n.q_weight->sizes(), n.weight_type);
+        if (n.k_weight) k_weight = empty_on(n.q, n.k_weight->sizes(), n.weight_type);
+        if (n.q_weight || n.k_weight) {
+            call(api.head_norm_workspace, n.tokens, n.dim, &bytes);
+            workspace = empty_on(n.q, {static_cast<int64_t>(bytes)}, at::kByte);
+        }
+    }
+    const auto pointer = [](const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; };
+    const actq_heads *const from_k = n.k ? &gk : nullptr, *const into_k = n.k ? &to_k : nullptr;
+    call(api.head_norm_rotate_backward, &gq, from_k, &n.hq, n.k_heads, n.dt, n.tokens, n.dim, n.wq, n.wk, n.weight_dt, &n.rotation, n.eps, &to_q, into_k,
+         pointer(q_weight), pointer(k_weight), pointer(workspace), bytes, current_stream());
+    return tuple_of({wrap_or_none(q_in), wrap_or_none(k_in), wrap_or_none(q_weight), wrap_or_none(k_weight)});
+}
+ACTQ_ENTRY(head_norm_rotate_backward, 12)
+
+// (key_codes, key_header, value_codes, value_header) of a cache whose heads have `dim` elements
+actq_cache cache_of(PyObject* const* a, int64_t dim)
+{
+    const Tensor &kc = tensor_of(a[0], "key_codes"), &kh = tensor_of(a[1], "key_header"), &vc = tensor_of(a[2], "value_codes"), &vh = tensor_of(a[3], "value_header");
+    TORCH_CHECK_VALUE(kc.dim() == 4 && vc.dim() == 4, "codes must be [pages, heads, page_size, dim * bits / 8]");
+    TORCH_CHECK_VALUE(kc.sizes().slice(0, 3) == vc.sizes().slice(0, 3), "key_codes and value_codes must have the same pages, heads and page_size");
+    TORCH_CHECK_VALUE(kh.dim() == 4 && kh.size(3) == 2 && kh.sizes().slice(0, 3) == kc.sizes().slice(0, 3) && vh.sizes() == kh.sizes(),
+                      "headers must be [pages, heads, page_size, 2]");
+    TORCH_CHECK_VALUE(dim > 0 && dim <= 256 && kc.size(1) <= INT32_MAX && kc.size(2) <= INT32_MAX, "head size, heads or page_size out of range");
+    const auto bits = [&](const Tensor& t, const char* name) {
+        TORCH_CHECK_VALUE(t.size(3) == dim || 2 * t.size(3) == dim, name, " must hold 8 or 4 bits for each of ", dim, " elements");
+        return t.size(3) == dim ? 8 : 4;
+    };
+    actq_cache c;
+    c.key_codes = contiguous_on_device(kc, at::kByte, "key_codes");
+    c.key_header = contiguous_on_device(kh, at::kFloat, "key_header");
+    c.value_codes = contiguous_on_device(vc, at::kByte, "value_codes");
+    c.value_header = contiguous_on_device(vh, at::kFloat, "value_header");
+    c.pages = kc.size(0);
+    c.page_size = static_cast<int32_t>(kc.size(2));
+    c.heads = static_cast<int32_t>(kc.size(1));
+    c.dim = static_cast<int32_t>(dim);
+    c.key_bits = bits(kc, "key_codes");
+    c.value_bits = bits(vc, "value_codes");
+    return c;
+}
+
+// (k, v, slots, the cache's four)
+PyObject* cache_write_impl(PyObject* const* a)
+{
+    const Tensor &k = tensor_of(a[0], "k"), &v = tensor_of(a[1], "v"), &slots = tensor_of(a[2], "slots");
+    const actq_dtype dt = heads_dtype(k, "k");
+    const actq_heads hk = heads_of(k, "k");
+    same_heads(v, k, "v");
+    const actq_heads hv = heads_of(v, "v");
+    TORCH_CHECK_VALUE(slots.dim() == 1 && slots.size(0) == k.size(0), "slots must have an entry per token");
+    const Memory sp = contiguous_on_device(slots, at::kLong, "slots");
+    const actq_cache c = cache_of(a + 3, k.size(2));
+    call(api.cache_write, &c, &hk, &hv, dt, k.size(0), sp, current_stream());
+    Py_RETURN_NONE;
+}
+ACTQ_ENTRY(cache_write, 7)
+
+// (slots, the cache's four, dim, dtype, k or None, v or None) -> (k, v)
+PyObject* cache_read_impl(PyObject* const* a)
+{
+    const Tensor& slots = tensor_of(a[0], "slots");
+    TORCH_CHECK_VALUE(slots.dim() == 1, "slots must have one dimension");
+    const Memory sp = contiguous_on_device(slots, at::kLong, "slots");
+    const actq_cache c = cache_of(a + 1, integer(a[5]));
+    TORCH_CHECK_TYPE(THPDtype_Check(a[6]), "dtype must be a torch dtype");
+    const at::ScalarType type = reinterpret_cast<THPDtype*>(a[6])->scalar_type;
+    const std::vector<int64_t> shape = {slots.size(0), c.heads, c.dim};
+    const auto output = [&](PyObject* passed, const char* name) {
+        if (passed == Py_None) return empty_on(slots, shape, type);
+        const Tensor& t = tensor_of(passed, name);
+        TORCH_CHECK_VALUE(t.sizes() == at::IntArrayRef(shape), name, " must be [tokens, heads, dim]");
+        TORCH_CHECK_TYPE(t.scalar_type() == type, name, " must be ", dtype_name(type), ", got ", dtype_name(t.scalar_type()));
+        return t;
+    };
+    const Tensor k = output(a[7], "k"), v = output(a[8], "v");
+    const actq_dtype dt = heads_dtype(k, "k");
+    const actq_heads hk = heads_to(k, "k"), hv = heads_to(v, "v");
+    call(api.cache_read, &c, sp, slots.size(0), &hk, &hv, dt, current_stream());
+    return tuple_of({give(a[7], k), give(a[8], v)});
+}
+ACTQ_ENTRY(cache_read, 9)
+
+// (q, the cache's four, table, lengths, query_start, max_query, max_length, scale or None, softcap, window, out or None) -> out
+PyObject* cache_attention_impl(PyObject* const* a)
+{
+    const Tensor &q = tensor_of(a[0], "q"), &table = tensor_of(a[5], "table"), &lengths = tensor_of(a[6], "lengths"), &start = tensor_of(a[7], "query_start");
+    const actq_dtype dt = heads_dtype(q, "q");
+    const actq_heads hq = heads_of(q, "q");
+    const actq_cache c = cache_of(a + 1, q.size(2));
+    const int64_t tokens = q.size(0), sequences = lengths.numel();
+    TORCH_CHECK_VALUE(table.dim() == 2 && table.size(0) == sequences && table.size(1) <= INT32_MAX, "table must be [sequences, pages of a sequence]");
+    TORCH_CHECK_VALUE(lengths.dim() == 1 && start.dim() == 1 && start.size(0) == sequences + 1, "lengths must be [sequences], query_start [sequences + 1]");
+    const Memory tp = contiguous_on_device(table, at::kInt, "table"), lp = contiguous_on_device(lengths, at::kInt, "lengths");
+    const Memory sp = contiguous_on_device(start, at::kInt, "query_start");
+    const int64_t most = integer(a[8]), longest = integer(a[9]), window = integer(a[12]);
+    TORCH_CHECK_VALUE(window >= 0 && window <= INT32_MAX, "window must not be negative and fit 32 bits, got ", window);
+    const double scale = a[10] == Py_None ? 1.0 / std::sqrt(static_cast<double>(c.dim)) : PyFloat_AsDouble(a[10]);
+    if (PyErr_Occurred()) throw python_error();
+    const double softcap = PyFloat_AsDouble(a[11]);
+    if (PyErr_Occurred()) throw python_error();
+    const Tensor out = heads_output(a[13], q, "out");
+    const actq_heads ho = heads_to(out, "out");
+    uint64_t bytes = 0;
+    call(api.cache_attention_workspace, &c, hq.heads, tokens, sequences, most, longest, static_cast<int32_t>(window), &bytes);
+    Tensor workspace;
+    if (bytes > 0) workspace = empty_on(q, {static_cast<int64_t>(bytes)}, at::kByte);
+    void* const wp = bytes > 0 ? workspace.data_ptr() : nullptr;
+    call(api.cache_attention, &c, &hq, dt, tokens, sequences, tp, static_cast<int32_t>(table.size(1)), lp, sp, most, longest, static_cast<float>(scale),
+         static_cast<float>(softcap), static_cast<int32_t>(window), &ho, wp, bytes, current_stream());
+    return give(a[13], out);
+}
+ACTQ_ENTRY(cache_attention, 14)
+
 // ----------------------------------------------------------------------------- autograd
 
 using torch::autograd::AutogradContext;
@@ -888,6 +1174,7 @@ PyMethodDef methods[] = {
     ACTQ_METHOD(attach), ACTQ_METHOD(plain), ACTQ_METHOD(group_stats), ACTQ_METHOD(sample_sensitivity), ACTQ_METHOD(allocate_bits_device),
     ACTQ_METHOD(quantize_pack), ACTQ_METHOD(unpack_dequantize), ACTQ_METHOD(compress_mixed), ACTQ_METHOD(relu_forward), ACTQ_METHOD(relu_backward),
     ACTQ_METHOD(maxpool2d_forward), ACTQ_METHOD(maxpool2d_backward), ACTQ_METHOD(linear_one_launch), ACTQ_METHOD(linear_gradients), ACTQ_METHOD(linear), ACTQ_METHOD(relu), ACTQ_METHOD(maxpool2d),
+    ACTQ_METHOD(head_norm_rotate), ACTQ_METHOD(head_norm_rotate_backward), ACTQ_METHOD(cache_write), ACTQ_METHOD(cache_read), ACTQ_METHOD(cache_attention),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "actq_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
