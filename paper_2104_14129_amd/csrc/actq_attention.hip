@@ -431,7 +431,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
             if (__any(top > m + kSlack)) {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
-                const float now = fmaxf(m, top), less = __builtin_amdgcn_exp2f(m - now);
+                const float now = top > m + kSlack ? top : m, less = __builtin_amdgcn_exp2f(m - now);   // a row's doing alone
                 m = now;
                 sum *= less;
                 middle *= less;
@@ -445,8 +445,9 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
                     const float v = __builtin_amdgcn_exp2f(x[t][i] - m);
                     const bool off = EDGE && (hidden >> (4 * t + i) & 1u) != 0;
                     sum += v;
-                    const float part = dpp<kAt>(c.middle) * v, product = dpp<kAt>(c.step) * v;
-                    middle += off ? 0.0f : part;
+                    // outside the conditions: a broadcast needs every lane
+                    const float part = fmaf(dpp<kAt>(c.middle), v, middle), product = dpp<kAt>(c.step) * v;
+                    middle = off ? middle : part;
                     const float weight = off ? 0.0f : product;
                     const _Float16 high = static_cast<_Float16>(weight);
                     p[0][t / 2][4 * (t % 2) + i] = high;
@@ -538,6 +539,345 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
     }
 }
 
+// ----------------------------------------------------------------------------- many rows
+
+// 32 rows per wavefront, WAVES of them over the same keys.  Tiles of keys are widened once per workgroup into the LDS (keys as
+// they lie, values transposed), twice buffered: while one is computed the next one's codes are on their way to registers.  Half of the wavefronts
+// widen keys and half values; the last one prepares the groups' constants.
+//
+// The 32 x 32 product gives a lane the scores of its row (lane % 32) for the keys 8 (i / 4) + 4 (lane / 32) + i % 4, i = 0..15; two
+// steps of the second product take eight of them each, and the transposed values hold a step's sixteen keys in that order.
+// Rows of the LDS are 16-byte chunks; a chunk's place is its number XOR some bits of the row, so that neither the rows that eight lanes read
+// together nor those that they write share a bank.
+template <int DIM, int WAVES>
+struct Many {
+    static constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES;
+    static constexpr int kTile = 8192 / DIM;           // keys of a tile
+    static constexpr int kSteps = DIM / 16;            // of the first product
+    static constexpr int kBlocks = DIM / 32;           // of the outputs
+    static constexpr int kHalf = kThreads / 2;         // threads that widen keys, and values
+    static constexpr int kKeyUnits = 512 / kHalf;      // a unit: 16 codes of a key
+    static constexpr int kValueUnits = 256 / kHalf;    // a unit: 8 columns of 4 keys
+    static constexpr int kOwn = kTile > 64 ? 2 : 1;    // groups of a lane whose constants it prepares
+    static constexpr int kChunks = kTile / 8;          // of a row of values
+
+    __device__ static __forceinline__ int key_place(int key, int chunk) { return key * (DIM * 2) + ((chunk ^ (key & 7)) << 4); }
+    __device__ static __forceinline__ int value_place(int column, int chunk)
+    {
+        const int x = kChunks >= 8 ? (column ^ (column >> 3 & 3)) & 7 : (column >> 1 ^ column >> 3) & 3;
+        return column * (kTile * 2) + ((chunk ^ x) << 4);
+    }
+};
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <int DIM, int SPLIT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_kernel(AttendArgs a)
+{
+    typedef Many<DIM, WAVES> K;
+    __shared__ __attribute__((aligned(16))) uint8_t keys[2][16384];
+    __shared__ __attribute__((aligned(16))) uint8_t values[2][16384];
+    __shared__ f32x4 constants[2][K::kTile];   // as in Constants
+    __shared__ int exponents[2];
+    __shared__ float tops[WAVES];
+
+    const Work w = work_of(a, blockIdx.x);
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int n = lane % 32, h = lane / 32;
+    const int32_t* const table = a.table + static_cast<int64_t>(w.sequence) * a.table_width;
+    const bool of_values = wave < WAVES / 2, of_constants = wave == WAVES - 1;
+    const int unit = threadIdx.x % K::kHalf;
+    const int key_bytes = DIM / 8 * a.key_bits, value_bytes = DIM / 8 * a.value_bits;
+
+    // the thread's units: keys 16 codes (chunk, key), values 8 columns of 4 keys
+    const auto key_of = [&](int u) { return (unit + u * K::kHalf) / (DIM / 16); };
+    const auto chunk_of = [&](int u) { return (unit + u * K::kHalf) % (DIM / 16); };
+    const auto quad_of = [&](int u) { return (unit + u * K::kHalf) >> 4 & 1 | (unit + u * K::kHalf) >> 2 & 2; };   // of the four keys of a step
+    const auto columns_of = [&](int u) { return (unit & 7) + 8 * ((unit + u * K::kHalf) >> 5 & (DIM / 64 - 1)); };
+    // where the lane reads: of the first step, the others' chunks by XOR, blocks of 32 columns by their distance
+    const int key_at = K::key_place(n, h), value_at = K::value_place(n, h);
+    const auto step_of = [&](int u) { return ((unit + u * K::kHalf) >> 5) / (DIM / 64); };
+
+    for (int32_t tile = static_cast<int32_t>(a.tiles) - 1 - w.tile; K::kRows * static_cast<int64_t>(tile) < w.rows; tile += a.tiles) {
+        const int32_t first_row = K::kRows * tile + 32 * wave;
+        const int32_t row = first_row + n;
+        const bool there = row < w.rows, any = first_row < w.rows;
+        const int32_t token = static_cast<int32_t>(divide(there ? row : w.rows - 1, a.by_group));
+        const int32_t head = w.head * a.group + (there ? row : w.rows - 1) - token * a.group;
+        const int32_t position = w.first + token;
+        const Span span = span_of(a, w, K::kRows * tile, K::kRows, K::kTile);
+        Span mine = span;   // of the wavefront's rows
+        if (any) {
+            mine.low = w.first + static_cast<int32_t>(divide(first_row, a.by_group));
+            mine.high = w.first + static_cast<int32_t>(divide(min(first_row + 32, w.rows) - 1, a.by_group));
+            mine.from = a.window > 0 ? max(mine.low - a.window + 1, 0) : 0;
+        }
+
+        // q, a lane's 8 elements of its row for every step
+        f16x8 q[SPLIT][K::kSteps];
+        float q_sum = 0.0f;
+        int q_exponent;
+        {
+            const int64_t at = (static_cast<int64_t>(w.start) + token) * a.q.token + head * a.q.head;
+            float f[K::kSteps][8], top = 0.0f;
+#pragma unroll
+            for (int s = 0; s < K::kSteps; ++s) {
+                load_eight(a.q.p, a.dtype, at + 16 * s + 8 * h, f[s]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    top = fmaxf(top, fabsf(f[s][j]));
+                    q_sum += f[s][j];
+                }
+            }
+            q_sum += __shfl_xor(q_sum, 32);
+            top = wave_max(top);
+            if (lane == 0) tops[wave] = top;
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < WAVES; ++k) top = fmaxf(top, tops[k]);
+            q_exponent = max(__builtin_amdgcn_readfirstlane(exponent(top)), -100);
+#pragma unroll
+            for (int s = 0; s < K::kSteps; ++s)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const float v = ldexpf(a.key_bits == 8 ? f[s][j] : f[s][code_order(4, j)], 14 - q_exponent);
+                    q[0][s][j] = static_cast<_Float16>(v);
+                    if (SPLIT == 2) q[SPLIT - 1][s][j] = static_cast<_Float16>(v - static_cast<float>(q[0][s][j]));
+                }
+        }
+
+        float m = kNothing, sum = 0.0f, middle = 0.0f;
+        int E = -126, running = -126;   // of the sums; of the tiles prepared so far
+        f32x16 acc[K::kBlocks];
+#pragma unroll
+        for (int b = 0; b < K::kBlocks; ++b) acc[b] = f32x16{};
+
+        int32_t pages[K::kKeyUnits], own_pages[K::kOwn];
+        uint32_t codes[8 * K::kValueUnits];
+        f32x2 key_header[K::kOwn], value_header[K::kOwn];
+
+        // pages of a tile, then its codes, then the LDS
+        const auto find = [&](int32_t base) {
+            if (of_values) {
+#pragma unroll
+                for (int u = 0; u < K::kValueUnits; ++u) pages[u] = static_cast<int32_t>(page_of(a, table, base + 16 * step_of(u)));
+            } else {
+#pragma unroll
+                for (int u = 0; u < K::kKeyUnits; ++u) pages[u] = static_cast<int32_t>(page_of(a, table, base + key_of(u)));
+            }
+            if (of_constants) {
+#pragma unroll
+                for (int o = 0; o < K::kOwn; ++o) own_pages[o] = static_cast<int32_t>(page_of(a, table, base + (lane + 64 * o) % K::kTile));
+            }
+        };
+        const auto load = [&](int32_t base) {
+            if (of_values) {
+#pragma unroll
+                for (int u = 0; u < K::kValueUnits; ++u) {
+                    const uint8_t* const p = a.value_codes + (row_of(a, w.head, pages[u], base + 16 * step_of(u)) + 4 * quad_of(u)) * value_bytes + columns_of(u) * a.value_bits;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (a.value_bits == 8) load_words<8>(p + k * value_bytes, codes + 8 * u + 2 * k);
+                        else load_words<4>(p + k * value_bytes, codes + 8 * u + 2 * k);
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int u = 0; u < K::kKeyUnits; ++u) {
+                    const uint8_t* const p = a.key_codes + row_of(a, w.head, pages[u], base + key_of(u)) * key_bytes + chunk_of(u) * 2 * a.key_bits;
+                    if (a.key_bits == 8) load_words<16>(p, codes + 4 * u);
+                    else load_words<8>(p, codes + 4 * u);
+                }
+            }
+            if (of_constants) {
+#pragma unroll
+                for (int o = 0; o < K::kOwn; ++o) {
+                    const int64_t own = row_of(a, w.head, own_pages[o], base + (lane + 64 * o) % K::kTile);
+                    key_header[o] = *reinterpret_cast<const f32x2*>(a.key_header + 2 * own);
+                    value_header[o] = *reinterpret_cast<const f32x2*>(a.value_header + 2 * own);
+                }
+            }
+        };
+        const auto store = [&](int32_t base, int to) {
+            if (of_values) {
+#pragma unroll
+                for (int u = 0; u < K::kValueUnits; ++u) {
+                    const int chunk = 2 * step_of(u) + (quad_of(u) & 1), half = 8 * (quad_of(u) >> 1);
+                    const uint32_t* const c = codes + 8 * u;
+                    each<8>([&](auto i) {
+                        f16x2 pair[2];
+                        if (a.value_bits == 8) {
+                            pair[0] = value_pair<8, i>(c, c + 2);
+                            pair[1] = value_pair<8, i>(c + 4, c + 6);
+                        } else {
+                            pair[0] = value_pair<4, i>(c, c + 2);
+                            pair[1] = value_pair<4, i>(c + 4, c + 6);
+                        }
+                        const u32x2 both = {__builtin_bit_cast(uint32_t, pair[0]), __builtin_bit_cast(uint32_t, pair[1])};
+                        *reinterpret_cast<u32x2*>(&values[to][K::value_place(8 * columns_of(u) + i, chunk) + half]) = both;
+                    });
+                }
+            } else {
+#pragma unroll
+                for (int u = 0; u < K::kKeyUnits; ++u) {
+                    const uint32_t* const c = codes + 4 * u;
+                    const int key = key_of(u), chunk = 2 * chunk_of(u);
+                    f16x8 first, second;
+                    if (a.key_bits == 8) {
+                        first = key_codes_of<8>(c);
+                        second = key_codes_of<8>(c + 2);
+                    } else {
+                        first = key_codes_of<4>(c);
+                        second = key_codes_of<4>(c + 1);
+                    }
+                    *reinterpret_cast<f16x8*>(&keys[to][K::key_place(key, chunk)]) = first;
+                    *reinterpret_cast<f16x8*>(&keys[to][K::key_place(key, chunk + 1)]) = second;
+                }
+            }
+            if (of_constants) {
+                float step[K::kOwn], top = 0.0f;
+#pragma unroll
+                for (int o = 0; o < K::kOwn; ++o) {
+                    const int32_t own = base + (lane + 64 * o) % K::kTile;
+                    step[o] = own >= span.from && own < span.end ? value_header[o][1] : 0.0f;   // by any row
+                    top = fmaxf(top, exponent(step[o]) == 128 ? 0.0f : step[o]);
+                }
+                running = max(running, __builtin_amdgcn_readfirstlane(exponent(wave_max(top))));
+#pragma unroll
+                for (int o = 0; o < K::kOwn; ++o) {
+                    f32x4 c;
+                    c[0] = ldexpf(key_header[o][1] * a.factor, 24 - 14 + q_exponent);
+                    c[1] = key_header[o][0] * a.factor;
+                    c[2] = ldexpf(step[o], kStepBits - running);
+                    c[3] = fmaf(a.value_bits == 8 ? 128.0f : 8.0f, step[o], value_header[o][0]);
+                    if (lane + 64 * o < K::kTile) constants[to][lane + 64 * o] = c;
+                }
+                if (lane == 0) exponents[to] = running;
+            }
+        };
+
+        const auto use = [&](int32_t base, int from, int s, auto edge) {
+            constexpr bool EDGE = decltype(edge)::value;
+            f32x16 x = {};
+#pragma unroll
+            for (int k = 0; k < K::kSteps; ++k) {
+                const f16x8 c = *reinterpret_cast<const f16x8*>(&keys[from][0] + (key_at + s * (64 * DIM) ^ k << 5));
+#pragma unroll
+                for (int i = 0; i < SPLIT; ++i) x = __builtin_amdgcn_mfma_f32_32x32x16_f16(c, q[i][k], x, 0, 0, 0);
+            }
+            const f32x4 v = constants[from][32 * s + 8 * (lane % 16 / 4) + 4 * h + lane % 4];
+            const Constants c = {v[0], v[1], v[2], v[3]};
+            each<16>([&](auto e) {
+                constexpr int i = e, kAt = kDppBroadcast + i;
+                x[i] = fmaf(dpp<kAt>(c.key), x[i], dpp<kAt>(c.key_zero) * q_sum);
+            });
+            if (a.cap > 0.0f) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i] = a.cap * tanh_of<SPLIT == 2>(x[i]);
+            }
+            uint32_t hidden = 0;
+            if (EDGE) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int32_t key = base + 8 * (i / 4) + 4 * h + i % 4;
+                    if (key >= span.end || key > position || (a.window > 0 && key <= position - a.window)) {
+                        x[i] = -INFINITY;
+                        hidden |= 1u << i;
+                    }
+                }
+            }
+            float top = kNothing;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, x[i]);
+            if (__any(top > m + kSlack)) {
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float now = top > m + kSlack ? top : m, less = __builtin_amdgcn_exp2f(m - now);   // a row's doing alone
+                m = now;
+                sum *= less;
+                middle *= less;
+#pragma unroll
+                for (int b = 0; b < K::kBlocks; ++b) acc[b] *= less;
+            }
+            f16x8 p[SPLIT][2];
+            each<16>([&](auto e) {
+                constexpr int i = e, kAt = kDppBroadcast + i;
+                const float v = __builtin_amdgcn_exp2f(x[i] - m);
+                const bool off = EDGE && (hidden >> i & 1u) != 0;
+                sum += v;
+                // outside the conditions: a broadcast needs every lane
+                const float part = fmaf(dpp<kAt>(c.middle), v, middle), product = dpp<kAt>(c.step) * v;
+                middle = off ? middle : part;
+                const float weight = off ? 0.0f : product;
+                const _Float16 high = static_cast<_Float16>(weight);
+                p[0][i / 8][i % 8] = high;
+                if (SPLIT == 2) p[SPLIT - 1][i / 8][i % 8] = static_cast<_Float16>(weight - static_cast<float>(high));
+            });
+#pragma unroll
+            for (int b = 0; b < K::kBlocks; ++b)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const f16x8 u = *reinterpret_cast<const f16x8*>(&values[from][0] + (value_at ^ (2 * s + k) << 5) + b * (64 * K::kTile));
+#pragma unroll
+                    for (int i = 0; i < SPLIT; ++i) acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(u, p[i][k], acc[b], 0, 0, 0);
+                }
+        };
+
+        if (span.begin < span.end) {
+            find(span.begin);
+            load(span.begin);
+            find(min(span.begin + K::kTile, span.end - 1));
+            store(span.begin, 0);
+            __syncthreads();
+            int at = 0;
+            for (int32_t base = span.begin; base < span.end; base += K::kTile, at ^= 1) {
+                const int32_t after = base + K::kTile;
+                if (after < span.end) {
+                    load(after);
+                    find(min(after + K::kTile, span.end - 1));
+                }
+                if (any && base <= mine.high && base + K::kTile > mine.from) {
+                    const int now = __builtin_amdgcn_readfirstlane(exponents[at]);
+                    if (now != E) {
+#pragma unroll
+                        for (int b = 0; b < K::kBlocks; ++b)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) acc[b][i] = ldexpf(acc[b][i], E - now);
+                        E = now;
+                    }
+                    for (int s = 0; s < K::kTile / 32; ++s) {
+                        const int32_t from = base + 32 * s;
+                        if (from > mine.high || from >= span.end || from + 32 <= mine.from) continue;
+                        if (mine.edge(from, 32, a.window)) use(from, at, s, std::true_type{});
+                        else use(from, at, s, std::false_type{});
+                    }
+                }
+                if (after < span.end) store(after, at ^ 1);
+                __syncthreads();
+            }
+        }
+
+        sum += __shfl_xor(sum, 32);
+        middle += __shfl_xor(middle, 32);
+        if (there) {
+            const float scale = is(sum, 0.0f) ? 0.0f : 1.0f / sum;   // nothing in sight: zeros
+            const int64_t out_row = (static_cast<int64_t>(w.start) + token) * a.q_heads + head;
+            const int64_t part_row = static_cast<int64_t>(w.part) * a.tokens * a.q_heads + out_row;
+#pragma unroll
+            for (int b = 0; b < K::kBlocks; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    float f[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) f[j] = (ldexpf(acc[b][i + j], E + kUnitBits - kStepBits) + middle) * scale;
+                    const int column = 32 * b + 2 * i + 4 * h;
+                    if (a.partial) store_some(a.partial, ACTQ_F32, part_row * DIM + column, f);
+                    else store_some(a.out.p, a.dtype, (static_cast<int64_t>(w.start) + token) * a.out.token + head * a.out.head + column, f);
+                }
+            if (a.partial && h == 0) a.partial_lse[part_row] = is(sum, 0.0f) ? kNothing : m + __builtin_amdgcn_logf(sum);
+        }
+    }
+}
+
 // ----------------------------------------------------------------------------- joining parts
 
 // A wavefront per row: the parts' outputs weighted by 2^(lse - largest).
@@ -571,26 +911,32 @@ __global__ __launch_bounds__(kJoinWaves * 64) void attend_join_kernel(AttendArgs
 // ----------------------------------------------------------------------------- launches
 
 constexpr int64_t kMostBlocks = int64_t(1) << 22;
-// Workgroups that the keys are cut for where there are few rows: two per compute unit are resident.
-constexpr int64_t kWantedBlocks = 1024;
 constexpr int64_t kMostParts = 128;
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 struct Shape {
+    int rows;      // of a tile: 16, or 32 per wavefront of the kernel for many rows
     int64_t tiles, parts, per_part;
 };
 
+// Rows of a sequence and head of the cache from which on the kernel for many rows serves.
+constexpr int64_t kManyRows = 64;
+
 Shape shape_of(const actq_cache* c, int32_t heads, int64_t sequences, int64_t max_query, int64_t max_length, int32_t window)
 {
-    const int64_t group = heads / c->heads, groups = sequences * c->heads;
+    const int64_t group = heads / c->heads, groups = sequences * c->heads, rows = max_query < 1 ? group : max_query * group;
     Shape s;
-    s.tiles = ceil_div(max_query < 1 ? 1 : max_query * group, 16);
+    s.rows = rows < kManyRows ? 16 : rows <= 128 || c->dim == 256 ? 128 : 256;
+    s.tiles = ceil_div(rows, s.rows);
     if (s.tiles > kMostBlocks / groups) s.tiles = kMostBlocks / groups;
-    const int64_t block = c->dim == 256 ? 32 : 64, least = kFewWaves * block;
+    // keys of a step; the fewest that are worth a workgroup; workgroups that are wanted: what is resident twice over, and once
+    const int64_t block = s.rows == 16 ? (c->dim == 256 ? 32 : 64) : 8192 / c->dim;
+    const int64_t least = s.rows == 16 ? kFewWaves * block : 256, wanted = s.rows == 16 ? 1024 : s.rows == 128 ? 512 : 256;
     int64_t span = max_length < 1 ? 1 : max_length;
-    if (window > 0 && span > window + ceil_div(16, group) + block) span = window + ceil_div(16, group) + block;
-    s.parts = ceil_div(kWantedBlocks, groups * s.tiles);
+    if (window > 0 && span > window + ceil_div(s.rows, group) + block) span = window + ceil_div(s.rows, group) + block;
+    s.parts = wanted / (groups * s.tiles);
+    if (s.parts < 1) s.parts = 1;
     if (s.parts > ceil_div(span, least)) s.parts = ceil_div(span, least);
     if (s.parts > kMostParts) s.parts = kMostParts;
     s.per_part = ceil_div(ceil_div(span, s.parts), block) * block;
@@ -657,9 +1003,24 @@ int launch_cache_attention(const actq_cache* c, const actq_heads* q, int dtype, 
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const unsigned blocks = static_cast<unsigned>(sequences * c->heads * shape.parts * shape.tiles);
     const int rc = by_dim(c->dim, [&](auto d) {
+        constexpr int kDim = decltype(d)::value;
+        if (shape.rows != 16) {
+            const auto start = [&](auto waves) {
+                constexpr int kWaves = decltype(waves)::value;
+                if (dtype == ACTQ_F32) launch(attend_many_kernel<kDim, 2, kWaves>, blocks, 64 * kWaves, s, a);
+                else launch(attend_many_kernel<kDim, 1, kWaves>, blocks, 64 * kWaves, s, a);
+            };
+            if constexpr (kDim != 256) {
+                if (shape.rows == 256) start(std::integral_constant<int, 8>{});
+                else start(std::integral_constant<int, 4>{});
+            } else {
+                start(std::integral_constant<int, 4>{});
+            }
+            return launched(who);
+        }
         return by_bits(c->key_bits, [&](auto kb) {
             return by_bits(c->value_bits, [&](auto vb) {
-                constexpr int kDim = decltype(d)::value, kKey = decltype(kb)::value, kValue = decltype(vb)::value;
+                constexpr int kKey = decltype(kb)::value, kValue = decltype(vb)::value;
                 if (dtype == ACTQ_F32) launch(attend_few_kernel<kDim, 2, kKey, kValue>, blocks, kFewWaves * 64, s, a);
                 else launch(attend_few_kernel<kDim, 1, kKey, kValue>, blocks, kFewWaves * 64, s, a);
                 return launched(who);
