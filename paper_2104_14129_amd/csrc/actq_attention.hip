@@ -108,17 +108,14 @@ __device__ __forceinline__ Span span_of(const AttendArgs& a, const Work& w, int3
     return s;
 }
 
-__device__ __forceinline__ int64_t page_of(const AttendArgs& a, const int32_t* table, int32_t key)
-{
-    const int32_t at = min(key >> a.page_shift, a.table_width - 1);
-    const int32_t page = table[at];
-    return min(max(static_cast<int64_t>(page), static_cast<int64_t>(0)), a.pages - 1);
-}
+// The page of a key as the table has it: what waits for the load is row_of.
+__device__ __forceinline__ int32_t page_of(const AttendArgs& a, const int32_t* table, int32_t key) { return table[min(key >> a.page_shift, a.table_width - 1)]; }
 
 // Row of the pages where the 16 keys from `key` on lie; key is a multiple of 16, and so is a page.
-__device__ __forceinline__ int64_t row_of(const AttendArgs& a, int32_t head, int64_t page, int32_t key)
+__device__ __forceinline__ int64_t row_of(const AttendArgs& a, int32_t head, int32_t page, int32_t key)
 {
-    return ((page * a.kv_heads + head) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
+    const uint32_t inside = min(static_cast<uint32_t>(max(page, 0)), static_cast<uint32_t>(a.pages - 1));
+    return ((static_cast<int64_t>(inside) * a.kv_heads + head) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
 }
 
 __device__ __forceinline__ void load_eight(const void* p, int dtype, int64_t at, float (&f)[8])
@@ -166,11 +163,27 @@ __device__ __forceinline__ void store_some(void* p, int dtype, int64_t at, const
     else put(__bf16{});
 }
 
-__device__ __forceinline__ int exponent(float v) { return static_cast<int>(__builtin_bit_cast(uint32_t, v) >> 23 & 255u) - 127; }
+// The bits of a value that may be no number.  The compiler takes it that floating-point data holds no NaN, and would fold a
+// question about the bits that it recognises as one about the number.
+__device__ __forceinline__ uint32_t bits_of(float v)
+{
+    uint32_t b = __builtin_bit_cast(uint32_t, v);
+    asm("" : "+v"(b));
+    return b;
+}
 
-// Whether v is exactly that constant.  Of the bits: the compiler takes it that floating-point data holds no NaN, and may ask the
-// opposite question, to which a NaN gives the same answer.
-__device__ __forceinline__ bool is(float v, float constant) { return __builtin_bit_cast(uint32_t, v) == __builtin_bit_cast(uint32_t, constant); }
+__device__ __forceinline__ float nan_where(bool bad)
+{
+    uint32_t b = bad ? 0x7fc00000u : 0u;
+    asm("" : "+v"(b));
+    return __builtin_bit_cast(float, b);
+}
+
+__device__ __forceinline__ int exponent(float v) { return static_cast<int>(bits_of(v) >> 23 & 255u) - 127; }
+
+__device__ __forceinline__ bool finite(float v) { return exponent(v) != 128; }
+
+__device__ __forceinline__ bool is(float v, float constant) { return bits_of(v) == __builtin_bit_cast(uint32_t, constant); }
 
 __device__ __forceinline__ float wave_max(float v)
 {
@@ -244,6 +257,15 @@ __device__ __forceinline__ f32x4 multiply(f16x8 a, f16x8 b, f32x4 c) { return __
 struct Constants {
     float key, key_zero, step, middle;
 };
+
+// Constants of a key that some row sees, or (value header zero) of one that none does.  Where a value is no number, step is zero and
+// middle is none: nothing times an infinity is no number either, so rows that see the key are made none on their own.
+__device__ __forceinline__ f32x4 constants_of(f32x2 key_header, f32x2 value_header, const AttendArgs& a, int q_exponent, int E, int value_bits)
+{
+    const float middle = fmaf(value_bits == 8 ? 128.0f : 8.0f, value_header[1], value_header[0]);
+    return f32x4{ldexpf(key_header[1] * a.factor, 24 - 14 + q_exponent), key_header[0] * a.factor,
+                 finite(middle) ? ldexpf(value_header[1], kStepBits - E) : 0.0f, middle};
+}
 
 // ----------------------------------------------------------------------------- few rows
 
@@ -366,27 +388,22 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
                     load_words<K::kValueBytes>(a.value_codes + (rows[t] + 4 * g + k) * (DIM * VALUE_BITS / 8) + n * K::kValueBytes, b.value[t][k]);
         };
 
-        // EDGE: some row does not see some key of the block.  What a row does not see has no part in it, infinities and NaN among it.
-        const auto use = [&](const typename K::Block& b, int32_t base, auto edge) {
-            constexpr bool EDGE = decltype(edge)::value;
-            Constants c;
-            {
-                const int32_t own = base + 16 * (n / 4 % K::kTiles) + 4 * g + n % 4;
-                const bool seen = !EDGE || (own >= span.from && own < span.end);   // by any row
-                const float step = seen ? b.value_header[1] : 0.0f;
-                c.key = ldexpf(b.key_header[1] * a.factor, 24 - 14 + q_exponent);
-                c.key_zero = b.key_header[0] * a.factor;
-                const int top = max(__builtin_amdgcn_readfirstlane(exponent(wave_max(exponent(step) == 128 ? 0.0f : step))), -126);
-                if (top > E) {
+        const auto use = [&](const typename K::Block& b, int32_t base) {
+            const int32_t own = base + 16 * (n / 4 % K::kTiles) + 4 * g + n % 4;
+            const bool seen = own >= span.from && own < span.end;   // by any row
+            const f32x2 value_header = {seen ? b.value_header[0] : 0.0f, seen ? b.value_header[1] : 0.0f};
+            const float proper = finite(value_header[1]) ? value_header[1] : 0.0f;
+            if (__any(exponent(proper) > E)) {
+                const int top = __builtin_amdgcn_readfirstlane(exponent(wave_max(proper)));
 #pragma unroll
-                    for (int i = 0; i < K::kColumns; ++i)
+                for (int i = 0; i < K::kColumns; ++i)
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) acc[i][r] = ldexpf(acc[i][r], E - top);
-                    E = top;
-                }
-                c.step = ldexpf(step, kStepBits - E);
-                c.middle = fmaf(VALUE_BITS == 8 ? 128.0f : 8.0f, step, b.value_header[0]);
+                    for (int r = 0; r < 4; ++r) acc[i][r] = ldexpf(acc[i][r], E - top);
+                E = top;
             }
+            const f32x4 four = constants_of(b.key_header, value_header, a, q_exponent, E, VALUE_BITS);
+            Constants c = {four[0], four[1], four[2], four[3]};
+            settled(c.key_zero);
             f32x4 x[K::kTiles];
 #pragma unroll
             for (int t = 0; t < K::kTiles; ++t) {
@@ -402,7 +419,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
             each<K::kTiles>([&](auto t) {
                 each<4>([&](auto e) {
                     constexpr int i = e, kAt = kDppBroadcast + 4 * t + i;
-                    x[t][i] = fmaf(dpp<kAt>(c.key), x[t][i], dpp<kAt>(c.key_zero) * q_sum);
+                    x[t][i] = add_broadcast<4 * t + i>(dpp<kAt>(c.key) * x[t][i], c.key_zero, q_sum, q_sum);
                 });
             });
             if (a.cap > 0.0f) {
@@ -411,18 +428,16 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
 #pragma unroll
                     for (int i = 0; i < 4; ++i) x[t][i] = a.cap * tanh_of<SPLIT == 2>(x[t][i]);
             }
-            uint32_t hidden = 0;
-            if (EDGE) {
-#pragma unroll
-                for (int t = 0; t < K::kTiles; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int32_t key = base + 16 * t + 4 * g + i;
-                        if (key >= span.end || key > position || (a.window > 0 && key <= position - a.window)) {
-                            x[t][i] = -INFINITY;
-                            hidden |= 1u << (4 * t + i);
-                        }
-                    }
+            // f(tile, i, whether the row sees key i of it): key = base + 4 g + a constant, between the window's begin and the last one in sight
+            const auto each_key = [&](auto f) {
+                const int32_t last = min(position, span.end - 1) - base - 4 * g, before = a.window > 0 ? position - a.window - base - 4 * g : -1;
+                each<K::kTiles>([&](auto t) { each<4>([&](auto e) { f(t, e, 16 * t + e <= last && 16 * t + e > before); }); });
+            };
+            if (span.edge(base, K::kBlock, a.window)) {
+                each_key([&](auto t, auto e, bool sees) {
+                    constexpr int i = e;
+                    x[t][i] = sees ? x[t][i] : -INFINITY;
+                });
             }
 #pragma unroll
             for (int t = 0; t < K::kTiles; ++t)
@@ -438,17 +453,23 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
 #pragma unroll
                 for (int i = 0; i < K::kColumns; ++i) acc[i] *= less;
             }
+            const bool bad = !finite(c.middle);
+            if (__any(bad)) {
+                each_key([&](auto t, auto e, bool sees) {
+                    const float none = dpp<kDppBroadcast + 4 * t + e>(nan_where(bad));
+                    sum += sees ? none : 0.0f;
+                });
+                c.middle = bad ? 0.0f : c.middle;
+            }
+            settled(c.middle);
             f16x8 p[SPLIT][K::kTiles / 2];
             each<K::kTiles>([&](auto t) {
                 each<4>([&](auto e) {
                     constexpr int i = e, kAt = kDppBroadcast + 4 * t + i;
                     const float v = __builtin_amdgcn_exp2f(x[t][i] - m);
-                    const bool off = EDGE && (hidden >> (4 * t + i) & 1u) != 0;
                     sum += v;
-                    // outside the conditions: a broadcast needs every lane
-                    const float part = fmaf(dpp<kAt>(c.middle), v, middle), product = dpp<kAt>(c.step) * v;
-                    middle = off ? middle : part;
-                    const float weight = off ? 0.0f : product;
+                    const float weight = dpp<kAt>(c.step) * v;
+                    middle = add_broadcast<4 * t + i>(middle, c.middle, v, weight);
                     const _Float16 high = static_cast<_Float16>(weight);
                     p[0][t / 2][4 * (t % 2) + i] = high;
                     if (SPLIT == 2) p[SPLIT - 1][t / 2][4 * (t % 2) + i] = static_cast<_Float16>(weight - static_cast<float>(high));
@@ -476,8 +497,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
             while (true) {
                 const int32_t after = base + kFewWaves * K::kBlock;
                 if (after < span.end) load(next, after);
-                if (span.edge(base, K::kBlock, a.window)) use(now, base, std::true_type{});
-                else use(now, base, std::false_type{});
+                use(now, base);
                 if (after >= span.end) break;
                 now = next;
                 base = after;
@@ -541,18 +561,19 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
 
 // ----------------------------------------------------------------------------- many rows
 
-// 32 rows per wavefront, WAVES of them over the same keys.  Tiles of keys are widened once per workgroup into the LDS (keys as
+// SETS times 32 rows per wavefront, WAVES of them over the same keys.  Tiles of keys are widened once per workgroup into the LDS (keys as
 // they lie, values transposed), twice buffered: while one is computed the next one's codes are on their way to registers.  Half of the wavefronts
 // widen keys and half values; the last one prepares the groups' constants.
 //
 // The 32 x 32 product gives a lane the scores of its row (lane % 32) for the keys 8 (i / 4) + 4 (lane / 32) + i % 4, i = 0..15; two
 // steps of the second product take eight of them each, and the transposed values hold a step's sixteen keys in that order.
 // Rows of the LDS are 16-byte chunks; a chunk's place is its number XOR some bits of the row, so that neither the rows that eight lanes read
-// together nor those that they write share a bank.
-template <int DIM, int WAVES>
+// together nor those that they write share a bank.  Of sixteen neighbouring codes of a key the first eight go to the row's first half.
+template <int DIM, int SPLIT, int WAVES, int SETS>
 struct Many {
-    static constexpr int kThreads = 64 * WAVES, kRows = 32 * WAVES;
+    static constexpr int kThreads = 64 * WAVES, kOwnRows = 32 * SETS, kRows = kOwnRows * WAVES;
     static constexpr int kTile = 8192 / DIM;           // keys of a tile
+    static constexpr int kParts = kTile / 32;          // of 32 keys
     static constexpr int kSteps = DIM / 16;            // of the first product
     static constexpr int kBlocks = DIM / 32;           // of the outputs
     static constexpr int kHalf = kThreads / 2;         // threads that widen keys, and values
@@ -571,10 +592,10 @@ struct Many {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-template <int DIM, int SPLIT, int WAVES>
+template <int DIM, int SPLIT, int WAVES, int SETS>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_kernel(AttendArgs a)
 {
-    typedef Many<DIM, WAVES> K;
+    typedef Many<DIM, SPLIT, WAVES, SETS> K;
     __shared__ __attribute__((aligned(16))) uint8_t keys[2][16384];
     __shared__ __attribute__((aligned(16))) uint8_t values[2][16384];
     __shared__ f32x4 constants[2][K::kTile];   // as in Constants
@@ -587,70 +608,98 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
     const int32_t* const table = a.table + static_cast<int64_t>(w.sequence) * a.table_width;
     const bool of_values = wave < WAVES / 2, of_constants = wave == WAVES - 1;
     const int unit = threadIdx.x % K::kHalf;
-    const int key_bytes = DIM / 8 * a.key_bits, value_bytes = DIM / 8 * a.value_bits;
+    constexpr std::integral_constant<int, 8> eight;
+    constexpr std::integral_constant<int, 4> four;
+    // two wavefronts share a SIMD: one goes ahead, so that one's products meet the other's softmax
+    if (WAVES == 8 && wave >= WAVES / 2) __builtin_amdgcn_s_setprio(1);
 
     // the thread's units: keys 16 codes (chunk, key), values 8 columns of 4 keys
     const auto key_of = [&](int u) { return (unit + u * K::kHalf) / (DIM / 16); };
     const auto chunk_of = [&](int u) { return (unit + u * K::kHalf) % (DIM / 16); };
-    const auto quad_of = [&](int u) { return (unit + u * K::kHalf) >> 4 & 1 | (unit + u * K::kHalf) >> 2 & 2; };   // of the four keys of a step
-    const auto columns_of = [&](int u) { return (unit & 7) + 8 * ((unit + u * K::kHalf) >> 5 & (DIM / 64 - 1)); };
+    // a unit's bits, low ones first, so that sixteen lanes write all banks: half of a chunk, two bits of the columns, the upper bit of the step ..
+    const auto bit = [&](int u, int i) { return (unit + u * K::kHalf) >> i & 1; };
+    const auto half_of = [&](int u) { return bit(u, 0); };   // the four keys are quad 2 half + odd of a step's
+    const auto odd_of = [&](int u) { return bit(u, DIM == 256 ? 3 : 5); };
+    const auto columns_of = [&](int u) {
+        return bit(u, 1) + 2 * bit(u, 2) + 4 * bit(u, 4) + (DIM == 64 ? 0 : DIM == 128 ? 8 * bit(u, 7) : 8 * bit(u, 6) + 16 * bit(u, 7));
+    };
+    const auto step_of = [&](int u) { return DIM == 256 ? bit(u, 5) : bit(u, 6) + 2 * bit(u, 3) + (DIM == 64 ? 4 * bit(u, 7) : 0); };
     // where the lane reads: of the first step, the others' chunks by XOR, blocks of 32 columns by their distance
     const int key_at = K::key_place(n, h), value_at = K::value_place(n, h);
-    const auto step_of = [&](int u) { return ((unit + u * K::kHalf) >> 5) / (DIM / 64); };
 
     for (int32_t tile = static_cast<int32_t>(a.tiles) - 1 - w.tile; K::kRows * static_cast<int64_t>(tile) < w.rows; tile += a.tiles) {
-        const int32_t first_row = K::kRows * tile + 32 * wave;
-        const int32_t row = first_row + n;
-        const bool there = row < w.rows, any = first_row < w.rows;
-        const int32_t token = static_cast<int32_t>(divide(there ? row : w.rows - 1, a.by_group));
-        const int32_t head = w.head * a.group + (there ? row : w.rows - 1) - token * a.group;
-        const int32_t position = w.first + token;
+        const int32_t first_row = K::kRows * tile + K::kOwnRows * wave;
+        const bool any = first_row < w.rows;
         const Span span = span_of(a, w, K::kRows * tile, K::kRows, K::kTile);
         Span mine = span;   // of the wavefront's rows
         if (any) {
             mine.low = w.first + static_cast<int32_t>(divide(first_row, a.by_group));
-            mine.high = w.first + static_cast<int32_t>(divide(min(first_row + 32, w.rows) - 1, a.by_group));
+            mine.high = w.first + static_cast<int32_t>(divide(min(first_row + K::kOwnRows, w.rows) - 1, a.by_group));
             mine.from = a.window > 0 ? max(mine.low - a.window + 1, 0) : 0;
         }
+        // the lane's rows, one of each set; beyond the last one the last one again
+        const auto row_at = [&](int r) { return first_row + 32 * r + n; };
+        const auto token_at = [&](int r) { return static_cast<int32_t>(divide(min(row_at(r), w.rows - 1), a.by_group)); };
+        const auto head_at = [&](int r) { return w.head * a.group + min(row_at(r), w.rows - 1) - token_at(r) * a.group; };
 
-        // q, a lane's 8 elements of its row for every step
-        f16x8 q[SPLIT][K::kSteps];
-        float q_sum = 0.0f;
+        // q, a lane's 8 elements of its rows for every step
+        f16x8 q[SETS][SPLIT][K::kSteps];
+        float q_sum[SETS];
         int q_exponent;
         {
-            const int64_t at = (static_cast<int64_t>(w.start) + token) * a.q.token + head * a.q.head;
-            float f[K::kSteps][8], top = 0.0f;
+            // element of q in slot 0 of a step: the order of the chunks in the LDS
+            const auto at = [&](int r, int s) {
+                const int chunk = 2 * s + h;
+                return (static_cast<int64_t>(w.start) + token_at(r)) * a.q.token + head_at(r) * a.q.head + (chunk < DIM / 16 ? 16 * chunk : 16 * chunk - DIM + 8);
+            };
+            float top = 0.0f;
 #pragma unroll
-            for (int s = 0; s < K::kSteps; ++s) {
-                load_eight(a.q.p, a.dtype, at + 16 * s + 8 * h, f[s]);
+            for (int r = 0; r < SETS; ++r) {
+                q_sum[r] = 0.0f;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    top = fmaxf(top, fabsf(f[s][j]));
-                    q_sum += f[s][j];
+                for (int s = 0; s < K::kSteps; ++s) {
+                    float f[8];
+                    load_eight(a.q.p, a.dtype, at(r, s), f);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        top = fmaxf(top, fabsf(f[j]));
+                        q_sum[r] += f[j];
+                    }
                 }
+                q_sum[r] += __shfl_xor(q_sum[r], 32);
             }
-            q_sum += __shfl_xor(q_sum, 32);
             top = wave_max(top);
             if (lane == 0) tops[wave] = top;
             __syncthreads();
 #pragma unroll
             for (int k = 0; k < WAVES; ++k) top = fmaxf(top, tops[k]);
             q_exponent = max(__builtin_amdgcn_readfirstlane(exponent(top)), -100);
+            // once more, from the cache: held until here they would be twice the registers of everything else
 #pragma unroll
-            for (int s = 0; s < K::kSteps; ++s)
+            for (int r = 0; r < SETS; ++r)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const float v = ldexpf(a.key_bits == 8 ? f[s][j] : f[s][code_order(4, j)], 14 - q_exponent);
-                    q[0][s][j] = static_cast<_Float16>(v);
-                    if (SPLIT == 2) q[SPLIT - 1][s][j] = static_cast<_Float16>(v - static_cast<float>(q[0][s][j]));
+                for (int s = 0; s < K::kSteps; ++s) {
+                    float f[8];
+                    load_eight(a.q.p, a.dtype, at(r, s), f);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float v = ldexpf(a.key_bits == 8 ? f[j] : f[code_order(4, j)], 14 - q_exponent);
+                        q[r][0][s][j] = static_cast<_Float16>(v);
+                        if (SPLIT == 2) q[r][SPLIT - 1][s][j] = static_cast<_Float16>(v - static_cast<float>(q[r][0][s][j]));
+                    }
                 }
         }
 
-        float m = kNothing, sum = 0.0f, middle = 0.0f;
+        float m[SETS], sum[SETS], middle[SETS];
         int E = -126, running = -126;   // of the sums; of the tiles prepared so far
-        f32x16 acc[K::kBlocks];
+        f32x16 acc[SETS][K::kBlocks];
 #pragma unroll
-        for (int b = 0; b < K::kBlocks; ++b) acc[b] = f32x16{};
+        for (int r = 0; r < SETS; ++r) {
+            m[r] = kNothing;
+            sum[r] = middle[r] = 0.0f;
+#pragma unroll
+            for (int b = 0; b < K::kBlocks; ++b) acc[r][b] = f32x16{};
+        }
 
         int32_t pages[K::kKeyUnits], own_pages[K::kOwn];
         uint32_t codes[8 * K::kValueUnits];
@@ -660,35 +709,34 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
         const auto find = [&](int32_t base) {
             if (of_values) {
 #pragma unroll
-                for (int u = 0; u < K::kValueUnits; ++u) pages[u] = static_cast<int32_t>(page_of(a, table, base + 16 * step_of(u)));
+                for (int u = 0; u < K::kValueUnits; ++u) pages[u] = page_of(a, table, base + 16 * step_of(u));
             } else {
 #pragma unroll
-                for (int u = 0; u < K::kKeyUnits; ++u) pages[u] = static_cast<int32_t>(page_of(a, table, base + key_of(u)));
+                for (int u = 0; u < K::kKeyUnits; ++u) pages[u] = page_of(a, table, base + key_of(u));
             }
             if (of_constants) {
 #pragma unroll
-                for (int o = 0; o < K::kOwn; ++o) own_pages[o] = static_cast<int32_t>(page_of(a, table, base + (lane + 64 * o) % K::kTile));
+                for (int o = 0; o < K::kOwn; ++o) own_pages[o] = page_of(a, table, base + (lane + 64 * o) % K::kTile);
             }
         };
         const auto load = [&](int32_t base) {
-            if (of_values) {
+            const auto load_values = [&](auto bits) {
+                constexpr int kBits = decltype(bits)::value, kBytes = DIM / 8 * kBits;
 #pragma unroll
                 for (int u = 0; u < K::kValueUnits; ++u) {
-                    const uint8_t* const p = a.value_codes + (row_of(a, w.head, pages[u], base + 16 * step_of(u)) + 4 * quad_of(u)) * value_bytes + columns_of(u) * a.value_bits;
+                    const uint8_t* const p = a.value_codes + (row_of(a, w.head, pages[u], base + 16 * step_of(u)) + 8 * half_of(u) + 4 * odd_of(u)) * kBytes + columns_of(u) * kBits;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if (a.value_bits == 8) load_words<8>(p + k * value_bytes, codes + 8 * u + 2 * k);
-                        else load_words<4>(p + k * value_bytes, codes + 8 * u + 2 * k);
-                    }
+                    for (int k = 0; k < 4; ++k) load_words<kBits>(p + k * kBytes, codes + 8 * u + 2 * k);
                 }
-            } else {
+            };
+            const auto load_keys = [&](auto bits) {
+                constexpr int kBits = decltype(bits)::value, kBytes = DIM / 8 * kBits;
 #pragma unroll
-                for (int u = 0; u < K::kKeyUnits; ++u) {
-                    const uint8_t* const p = a.key_codes + row_of(a, w.head, pages[u], base + key_of(u)) * key_bytes + chunk_of(u) * 2 * a.key_bits;
-                    if (a.key_bits == 8) load_words<16>(p, codes + 4 * u);
-                    else load_words<8>(p, codes + 4 * u);
-                }
-            }
+                for (int u = 0; u < K::kKeyUnits; ++u)
+                    load_words<2 * kBits>(a.key_codes + row_of(a, w.head, pages[u], base + key_of(u)) * kBytes + chunk_of(u) * 2 * kBits, codes + 4 * u);
+            };
+            if (of_values) a.value_bits == 8 ? load_values(eight) : load_values(four);
+            else a.key_bits == 8 ? load_keys(eight) : load_keys(four);
             if (of_constants) {
 #pragma unroll
                 for (int o = 0; o < K::kOwn; ++o) {
@@ -699,181 +747,218 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
             }
         };
         const auto store = [&](int32_t base, int to) {
-            if (of_values) {
+            const auto store_values = [&](auto bits) {
+                constexpr int kBits = decltype(bits)::value;
 #pragma unroll
                 for (int u = 0; u < K::kValueUnits; ++u) {
-                    const int chunk = 2 * step_of(u) + (quad_of(u) & 1), half = 8 * (quad_of(u) >> 1);
+                    const int chunk = 2 * step_of(u) + odd_of(u), half = 8 * half_of(u);
                     const uint32_t* const c = codes + 8 * u;
                     each<8>([&](auto i) {
-                        f16x2 pair[2];
-                        if (a.value_bits == 8) {
-                            pair[0] = value_pair<8, i>(c, c + 2);
-                            pair[1] = value_pair<8, i>(c + 4, c + 6);
-                        } else {
-                            pair[0] = value_pair<4, i>(c, c + 2);
-                            pair[1] = value_pair<4, i>(c + 4, c + 6);
-                        }
-                        const u32x2 both = {__builtin_bit_cast(uint32_t, pair[0]), __builtin_bit_cast(uint32_t, pair[1])};
+                        const u32x2 both = {__builtin_bit_cast(uint32_t, value_pair<kBits, i>(c, c + 2)), __builtin_bit_cast(uint32_t, value_pair<kBits, i>(c + 4, c + 6))};
                         *reinterpret_cast<u32x2*>(&values[to][K::value_place(8 * columns_of(u) + i, chunk) + half]) = both;
                     });
                 }
-            } else {
+            };
+            const auto store_keys = [&](auto bits) {
+                constexpr int kBits = decltype(bits)::value;
 #pragma unroll
                 for (int u = 0; u < K::kKeyUnits; ++u) {
-                    const uint32_t* const c = codes + 4 * u;
-                    const int key = key_of(u), chunk = 2 * chunk_of(u);
-                    f16x8 first, second;
-                    if (a.key_bits == 8) {
-                        first = key_codes_of<8>(c);
-                        second = key_codes_of<8>(c + 2);
-                    } else {
-                        first = key_codes_of<4>(c);
-                        second = key_codes_of<4>(c + 1);
-                    }
-                    *reinterpret_cast<f16x8*>(&keys[to][K::key_place(key, chunk)]) = first;
-                    *reinterpret_cast<f16x8*>(&keys[to][K::key_place(key, chunk + 1)]) = second;
+                    *reinterpret_cast<f16x8*>(&keys[to][K::key_place(key_of(u), chunk_of(u))]) = key_codes_of<kBits>(codes + 4 * u);
+                    *reinterpret_cast<f16x8*>(&keys[to][K::key_place(key_of(u), chunk_of(u) + DIM / 16)]) = key_codes_of<kBits>(codes + 4 * u + kBits / 4);
                 }
-            }
+            };
+            if (of_values) a.value_bits == 8 ? store_values(eight) : store_values(four);
+            else a.key_bits == 8 ? store_keys(eight) : store_keys(four);
             if (of_constants) {
                 float step[K::kOwn], top = 0.0f;
 #pragma unroll
                 for (int o = 0; o < K::kOwn; ++o) {
                     const int32_t own = base + (lane + 64 * o) % K::kTile;
-                    step[o] = own >= span.from && own < span.end ? value_header[o][1] : 0.0f;   // by any row
-                    top = fmaxf(top, exponent(step[o]) == 128 ? 0.0f : step[o]);
+                    const bool seen = own >= span.from && own < span.end;   // by any row
+                    step[o] = seen ? value_header[o][1] : 0.0f;
+                    value_header[o][0] = seen ? value_header[o][0] : 0.0f;
+                    top = fmaxf(top, finite(step[o]) ? step[o] : 0.0f);
                 }
-                running = max(running, __builtin_amdgcn_readfirstlane(exponent(wave_max(top))));
+                if (__any(exponent(top) > running)) running = __builtin_amdgcn_readfirstlane(exponent(wave_max(top)));
 #pragma unroll
-                for (int o = 0; o < K::kOwn; ++o) {
-                    f32x4 c;
-                    c[0] = ldexpf(key_header[o][1] * a.factor, 24 - 14 + q_exponent);
-                    c[1] = key_header[o][0] * a.factor;
-                    c[2] = ldexpf(step[o], kStepBits - running);
-                    c[3] = fmaf(a.value_bits == 8 ? 128.0f : 8.0f, step[o], value_header[o][0]);
-                    if (lane + 64 * o < K::kTile) constants[to][lane + 64 * o] = c;
-                }
+                for (int o = 0; o < K::kOwn; ++o)
+                    if (lane + 64 * o < K::kTile)
+                        constants[to][lane + 64 * o] = constants_of(key_header[o], f32x2{value_header[o][0], step[o]}, a, q_exponent, running, a.value_bits);
                 if (lane == 0) exponents[to] = running;
             }
         };
 
-        const auto use = [&](int32_t base, int from, int s, auto edge) {
-            constexpr bool EDGE = decltype(edge)::value;
-            f32x16 x = {};
+        // keys of part s of the tile in buffer `from`, all on their way before the first product: left to itself the compiler waits for each
+        f16x8 c_keys[K::kSteps];
+        const auto load_part = [&](int from, int s) {
 #pragma unroll
-            for (int k = 0; k < K::kSteps; ++k) {
-                const f16x8 c = *reinterpret_cast<const f16x8*>(&keys[from][0] + (key_at + s * (64 * DIM) ^ k << 5));
-#pragma unroll
-                for (int i = 0; i < SPLIT; ++i) x = __builtin_amdgcn_mfma_f32_32x32x16_f16(c, q[i][k], x, 0, 0, 0);
-            }
+            for (int k = 0; k < K::kSteps; ++k) c_keys[k] = *reinterpret_cast<const f16x8*>(&keys[from][0] + (key_at + s * (64 * DIM) ^ k << 5));
+        };
+
+        // Scores and sums of the keys [base, base + 32), that part; the next part's keys are loaded behind the products that need these.
+        const auto use = [&](int32_t base, int from, int s, bool more) {
             const f32x4 v = constants[from][32 * s + 8 * (lane % 16 / 4) + 4 * h + lane % 4];
-            const Constants c = {v[0], v[1], v[2], v[3]};
-            each<16>([&](auto e) {
-                constexpr int i = e, kAt = kDppBroadcast + i;
-                x[i] = fmaf(dpp<kAt>(c.key), x[i], dpp<kAt>(c.key_zero) * q_sum);
-            });
-            if (a.cap > 0.0f) {
+            const int now_read = exponents[from];
+            __builtin_amdgcn_sched_barrier(0);
+            f32x16 x[SETS] = {};
 #pragma unroll
-                for (int i = 0; i < 16; ++i) x[i] = a.cap * tanh_of<SPLIT == 2>(x[i]);
-            }
-            uint32_t hidden = 0;
-            if (EDGE) {
+            for (int r = 0; r < SETS; ++r)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int32_t key = base + 8 * (i / 4) + 4 * h + i % 4;
-                    if (key >= span.end || key > position || (a.window > 0 && key <= position - a.window)) {
-                        x[i] = -INFINITY;
-                        hidden |= 1u << i;
-                    }
-                }
-            }
-            float top = kNothing;
+                for (int k = 0; k < K::kSteps; ++k)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) top = fmaxf(top, x[i]);
-            if (__any(top > m + kSlack)) {
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float now = top > m + kSlack ? top : m, less = __builtin_amdgcn_exp2f(m - now);   // a row's doing alone
-                m = now;
-                sum *= less;
-                middle *= less;
-#pragma unroll
-                for (int b = 0; b < K::kBlocks; ++b) acc[b] *= less;
-            }
-            f16x8 p[SPLIT][2];
-            each<16>([&](auto e) {
-                constexpr int i = e, kAt = kDppBroadcast + i;
-                const float v = __builtin_amdgcn_exp2f(x[i] - m);
-                const bool off = EDGE && (hidden >> i & 1u) != 0;
-                sum += v;
-                // outside the conditions: a broadcast needs every lane
-                const float part = fmaf(dpp<kAt>(c.middle), v, middle), product = dpp<kAt>(c.step) * v;
-                middle = off ? middle : part;
-                const float weight = off ? 0.0f : product;
-                const _Float16 high = static_cast<_Float16>(weight);
-                p[0][i / 8][i % 8] = high;
-                if (SPLIT == 2) p[SPLIT - 1][i / 8][i % 8] = static_cast<_Float16>(weight - static_cast<float>(high));
-            });
+                    for (int i = 0; i < SPLIT; ++i) x[r] = __builtin_amdgcn_mfma_f32_32x32x16_f16(c_keys[k], q[r][i][k], x[r], 0, 0, 0);
+            f16x8 u[K::kBlocks][2];
 #pragma unroll
             for (int b = 0; b < K::kBlocks; ++b)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const f16x8 u = *reinterpret_cast<const f16x8*>(&values[from][0] + (value_at ^ (2 * s + k) << 5) + b * (64 * K::kTile));
+                for (int k = 0; k < 2; ++k) u[b][k] = *reinterpret_cast<const f16x8*>(&values[from][0] + (value_at ^ (2 * s + k) << 5) + b * (64 * K::kTile));
+            const int now = __builtin_amdgcn_readfirstlane(now_read);
+            if (now != E) {
 #pragma unroll
-                    for (int i = 0; i < SPLIT; ++i) acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(u, p[i][k], acc[b], 0, 0, 0);
+                for (int r = 0; r < SETS; ++r)
+#pragma unroll
+                    for (int b = 0; b < K::kBlocks; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[r][b][i] = ldexpf(acc[r][b][i], E - now);
+                E = now;
+            }
+            Constants c = {v[0], v[1], v[2], v[3]};
+            settled(c.key_zero);
+#pragma unroll
+            for (int r = 0; r < SETS; ++r)
+                each<16>([&](auto e) {
+                    constexpr int i = e, kAt = kDppBroadcast + i;
+                    x[r][i] = add_broadcast<i>(dpp<kAt>(c.key) * x[r][i], c.key_zero, q_sum[r], q_sum[r]);
+                });
+            if (a.cap > 0.0f) {
+#pragma unroll
+                for (int r = 0; r < SETS; ++r)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[r][i] = a.cap * tanh_of<SPLIT == 2>(x[r][i]);
+            }
+            // f(i, whether the row sees key i): key = base + 4 h + a constant, between the window's begin and the last one in sight
+            const auto each_key = [&](int r, auto f) {
+                const int32_t position = w.first + token_at(r);
+                const int32_t last = min(position, span.end - 1) - base - 4 * h, before = a.window > 0 ? position - a.window - base - 4 * h : -1;
+                each<16>([&](auto e) {
+                    constexpr int kKey = 8 * (e / 4) + e % 4;
+                    f(e, kKey <= last && kKey > before);
+                });
+            };
+            if (mine.edge(base, 32, a.window)) {
+#pragma unroll
+                for (int r = 0; r < SETS; ++r)
+                    each_key(r, [&](auto e, bool sees) {
+                        constexpr int i = e;
+                        x[r][i] = sees ? x[r][i] : -INFINITY;
+                    });
+            }
+            float top[SETS];
+            bool over = false;
+#pragma unroll
+            for (int r = 0; r < SETS; ++r) {
+                top[r] = kNothing;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) top[r] = fmaxf(top[r], x[r][i]);
+                over |= top[r] > m[r] + kSlack;
+            }
+            if (__any(over)) {
+#pragma unroll
+                for (int r = 0; r < SETS; ++r) {
+                    top[r] = fmaxf(top[r], __shfl_xor(top[r], 32));
+                    const float now = top[r] > m[r] + kSlack ? top[r] : m[r], less = __builtin_amdgcn_exp2f(m[r] - now);   // a row's doing alone
+                    m[r] = now;
+                    sum[r] *= less;
+                    middle[r] *= less;
+#pragma unroll
+                    for (int b = 0; b < K::kBlocks; ++b) acc[r][b] *= less;
                 }
+            }
+            const bool bad = !finite(c.middle);
+            if (__any(bad)) {
+#pragma unroll
+                for (int r = 0; r < SETS; ++r)
+                    each_key(r, [&](auto e, bool sees) {
+                        const float none = dpp<kDppBroadcast + e>(nan_where(bad));
+                        sum[r] += sees ? none : 0.0f;
+                    });
+                c.middle = bad ? 0.0f : c.middle;
+            }
+            settled(c.middle);
+            if (more) load_part(from, s + 1);
+#pragma unroll
+            for (int r = 0; r < SETS; ++r) {
+                f16x8 p[SPLIT][2];
+                each<16>([&](auto e) {
+                    constexpr int i = e, kAt = kDppBroadcast + i;
+                    const float v = __builtin_amdgcn_exp2f(x[r][i] - m[r]);
+                    sum[r] += v;
+                    const float weight = dpp<kAt>(c.step) * v;
+                    middle[r] = add_broadcast<i>(middle[r], c.middle, v, weight);
+                    const _Float16 high = static_cast<_Float16>(weight);
+                    p[0][i / 8][i % 8] = high;
+                    if (SPLIT == 2) p[SPLIT - 1][i / 8][i % 8] = static_cast<_Float16>(weight - static_cast<float>(high));
+                });
+#pragma unroll
+                for (int b = 0; b < K::kBlocks; ++b)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int i = 0; i < SPLIT; ++i) acc[r][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(u[b][k], p[i][k], acc[r][b], 0, 0, 0);
+            }
         };
 
         if (span.begin < span.end) {
+            const int32_t last = span.end - 1;
             find(span.begin);
             load(span.begin);
-            find(min(span.begin + K::kTile, span.end - 1));
+            find(min(span.begin + K::kTile, last));
             store(span.begin, 0);
+            if (span.begin + K::kTile < span.end) load(span.begin + K::kTile);
+            find(min(span.begin + 2 * K::kTile, last));
             __syncthreads();
             int at = 0;
             for (int32_t base = span.begin; base < span.end; base += K::kTile, at ^= 1) {
-                const int32_t after = base + K::kTile;
-                if (after < span.end) {
-                    load(after);
-                    find(min(after + K::kTile, span.end - 1));
-                }
+                // the next tile from the registers to the LDS, the one after it on its way to them
+                const auto stage = [&] {
+                    if (base + K::kTile < span.end) store(base + K::kTile, at ^ 1);
+                    if (base + 2 * K::kTile < span.end) {
+                        load(base + 2 * K::kTile);
+                        find(min(base + 3 * K::kTile, last));
+                    }
+                };
+                if (of_values) stage();
                 if (any && base <= mine.high && base + K::kTile > mine.from) {
-                    const int now = __builtin_amdgcn_readfirstlane(exponents[at]);
-                    if (now != E) {
-#pragma unroll
-                        for (int b = 0; b < K::kBlocks; ++b)
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) acc[b][i] = ldexpf(acc[b][i], E - now);
-                        E = now;
-                    }
-                    for (int s = 0; s < K::kTile / 32; ++s) {
-                        const int32_t from = base + 32 * s;
-                        if (from > mine.high || from >= span.end || from + 32 <= mine.from) continue;
-                        if (mine.edge(from, 32, a.window)) use(from, at, s, std::true_type{});
-                        else use(from, at, s, std::false_type{});
-                    }
+                    // the parts that some row sees
+                    const int s_begin = max(mine.from - base, 0) / 32, s_end = min((min(mine.high + 1, span.end) - base + 31) / 32, K::kParts);
+                    if (s_begin < s_end) load_part(at, s_begin);
+                    for (int s = s_begin; s < s_end; ++s) use(base + 32 * s, at, s, s + 1 < s_end);
                 }
-                if (after < span.end) store(after, at ^ 1);
+                if (!of_values) stage();   // behind the products where the others stage ahead of them
                 __syncthreads();
             }
         }
 
-        sum += __shfl_xor(sum, 32);
-        middle += __shfl_xor(middle, 32);
-        if (there) {
-            const float scale = is(sum, 0.0f) ? 0.0f : 1.0f / sum;   // nothing in sight: zeros
-            const int64_t out_row = (static_cast<int64_t>(w.start) + token) * a.q_heads + head;
-            const int64_t part_row = static_cast<int64_t>(w.part) * a.tokens * a.q_heads + out_row;
+#pragma unroll
+        for (int r = 0; r < SETS; ++r) {
+            sum[r] += __shfl_xor(sum[r], 32);
+            middle[r] += __shfl_xor(middle[r], 32);
+            if (row_at(r) >= w.rows) continue;
+            const float scale = is(sum[r], 0.0f) ? 0.0f : 1.0f / sum[r];   // nothing in sight: zeros
+            const int32_t token = token_at(r), head = head_at(r);
+            const int64_t part_row = static_cast<int64_t>(w.part) * a.tokens * a.q_heads + (static_cast<int64_t>(w.start) + token) * a.q_heads + head;
 #pragma unroll
             for (int b = 0; b < K::kBlocks; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4) {
                     float f[4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) f[j] = (ldexpf(acc[b][i + j], E + kUnitBits - kStepBits) + middle) * scale;
+                    for (int j = 0; j < 4; ++j) f[j] = (ldexpf(acc[r][b][i + j], E + kUnitBits - kStepBits) + middle[r]) * scale;
                     const int column = 32 * b + 2 * i + 4 * h;
                     if (a.partial) store_some(a.partial, ACTQ_F32, part_row * DIM + column, f);
                     else store_some(a.out.p, a.dtype, (static_cast<int64_t>(w.start) + token) * a.out.token + head * a.out.head + column, f);
                 }
-            if (a.partial && h == 0) a.partial_lse[part_row] = is(sum, 0.0f) ? kNothing : m + __builtin_amdgcn_logf(sum);
+            if (a.partial && h == 0) a.partial_lse[part_row] = is(sum[r], 0.0f) ? kNothing : m[r] + __builtin_amdgcn_logf(sum[r]);
         }
     }
 }
@@ -1005,16 +1090,12 @@ int launch_cache_attention(const actq_cache* c, const actq_heads* q, int dtype, 
     const int rc = by_dim(c->dim, [&](auto d) {
         constexpr int kDim = decltype(d)::value;
         if (shape.rows != 16) {
-            const auto start = [&](auto waves) {
-                constexpr int kWaves = decltype(waves)::value;
-                if (dtype == ACTQ_F32) launch(attend_many_kernel<kDim, 2, kWaves>, blocks, 64 * kWaves, s, a);
-                else launch(attend_many_kernel<kDim, 1, kWaves>, blocks, 64 * kWaves, s, a);
-            };
-            if constexpr (kDim != 256) {
-                if (shape.rows == 256) start(std::integral_constant<int, 8>{});
-                else start(std::integral_constant<int, 4>{});
-            } else {
-                start(std::integral_constant<int, 4>{});
+            if (shape.rows == 128) {
+                if (dtype == ACTQ_F32) launch(attend_many_kernel<kDim, 2, 4, 1>, blocks, 256, s, a);
+                else launch(attend_many_kernel<kDim, 1, 4, 1>, blocks, 256, s, a);
+            } else if constexpr (kDim != 256) {
+                if (dtype == ACTQ_F32) launch(attend_many_kernel<kDim, 2, 8, 1>, blocks, 512, s, a);
+                else launch(attend_many_kernel<kDim, 1, 8, 1>, blocks, 512, s, a);
             }
             return launched(who);
         }

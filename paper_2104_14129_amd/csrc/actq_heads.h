@@ -63,6 +63,18 @@ __device__ __forceinline__ float dpp(float v)
 
 constexpr int kDppXor1 = 0xB1, kDppXor2 = 0x4E, kDppHalfMirror = 0x141, kDppMirror = 0x140, kDppBroadcast = 0x150;
 
+// sum + v of lane AT of the 16-lane row * factor, in one instruction; the compiler makes two of it.  Of an instruction of ours it does
+// not know what it has to wait for: a value that has just been written takes two cycles to be seen by other lanes, so
+// `settled` goes first; and the result of an exponential one cycle to be seen at all, so `after` is something that was computed from it.
+__device__ __forceinline__ void settled(float& v) { asm volatile("s_nop 1" : "+v"(v)); }
+
+template <int AT>
+__device__ __forceinline__ float add_broadcast(float sum, float v, float factor, float after)
+{
+    asm("v_fmac_f32_dpp %0, %1, %2 row_newbcast:%3 row_mask:0xf bank_mask:0xf" : "+v"(sum) : "v"(v), "v"(factor), "n"(AT), "v"(after));
+    return sum;
+}
+
 // op over the LANES lanes of a head, in all of them: neighbours, pairs, then mirrored halves, whose lanes are alike by then.
 template <int LANES, typename Op>
 __device__ __forceinline__ float over_lanes(float v, Op op)
