@@ -81,6 +81,12 @@ __device__ __forceinline__ Work work_of(const AttendArgs& a, uint32_t id)
     return w;
 }
 
+// Row of the parts' outputs of a new token's head.
+__device__ __forceinline__ int64_t part_row_of(const AttendArgs& a, const Work& w, int32_t token, int32_t head)
+{
+    return (static_cast<int64_t>(w.part) * a.tokens + w.start + token) * a.q_heads + head;
+}
+
 // Keys that the rows [row, row + count) of a sequence see, cut to a part: [begin, end), begin a multiple of `block`.
 struct Span {
     int32_t begin, end;
@@ -110,6 +116,13 @@ __device__ __forceinline__ Span span_of(const AttendArgs& a, const Work& w, int3
 
 // The page of a key as the table has it: what waits for the load is row_of.
 __device__ __forceinline__ int32_t page_of(const AttendArgs& a, const int32_t* table, int32_t key) { return table[min(key >> a.page_shift, a.table_width - 1)]; }
+
+// The same for a key that is the whole wavefront's, by a scalar load: it neither waits for the vector loads in flight nor they for it.
+__device__ __forceinline__ int32_t shared_page_of(const AttendArgs& a, const int32_t* table, int32_t key)
+{
+    typedef const int32_t __attribute__((address_space(4))) * constant;
+    return reinterpret_cast<constant>(reinterpret_cast<uintptr_t>(table))[__builtin_amdgcn_readfirstlane(min(key >> a.page_shift, a.table_width - 1))];
+}
 
 // Row of the pages where the 16 keys from `key` on lie; key is a multiple of 16, and so is a page.
 __device__ __forceinline__ int64_t row_of(const AttendArgs& a, int32_t head, int32_t page, int32_t key)
@@ -172,6 +185,14 @@ __device__ __forceinline__ uint32_t bits_of(float v)
     return b;
 }
 
+// A number whose uses are computed where it is asked for: what is computed from a lane's number alone would otherwise be held in
+// registers from the kernel's begin on, through the loop over the keys.
+__device__ __forceinline__ int here(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 __device__ __forceinline__ float nan_where(bool bad)
 {
     uint32_t b = bad ? 0x7fc00000u : 0u;
@@ -206,10 +227,11 @@ __device__ __forceinline__ uint32_t byte_pair(uint32_t low, uint32_t high)
     return __builtin_amdgcn_perm(high, low, B | 0x0c00 | (4 + B) << 16 | 0x0c000000);
 }
 
-// The lane's order of a word's eight nibbles as pairs of nibble and nibble four further up: 0 4 1 5 2 6 3 7.
+// Eight codes as subnormal binary16 numbers: two words of bytes, or one of nibbles, as pairs of nibble and nibble four further up
+// (0 4 1 5 2 6 3 7).  Odd nibbles stay where they are, sixteen times as large; q has a sixteenth in their places.
 __device__ __forceinline__ int code_order(int bits, int j) { return bits == 8 ? j : (j >> 1) + 4 * (j & 1); }
+__device__ __forceinline__ int code_bits(int bits, int j) { return bits == 8 ? 0 : (j & 2) * 2; }   // to the left of where they belong
 
-// Eight codes as subnormal binary16 numbers: two words of bytes, or one of nibbles in code_order.
 template <int BITS>
 __device__ __forceinline__ f16x8 key_codes_of(const uint32_t* w)
 {
@@ -220,25 +242,29 @@ __device__ __forceinline__ f16x8 key_codes_of(const uint32_t* w)
         r[2] = __builtin_amdgcn_perm(0, w[1], 0x0c010c00);
         r[3] = __builtin_amdgcn_perm(0, w[1], 0x0c030c02);
     } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = w[0] >> 4 * i & 0x000f000fu;
+        const uint32_t up = w[0] >> 8;
+        r[0] = w[0] & 0x000f000fu;
+        r[1] = w[0] & 0x00f000f0u;
+        r[2] = up & 0x000f000fu;
+        r[3] = up & 0x00f000f0u;
     }
     return __builtin_bit_cast(f16x8, r);
 }
 
-// Centred code pair (code - c) * 2^-9 of element I (of the words of two keys): exact in binary16.
+// Code pair of element I (of the words of two keys) as it lies: code * 2^-24, of odd nibbles code * 2^-20.
+template <int BITS, int I>
+__device__ __forceinline__ uint32_t raw_pair(const uint32_t* low, const uint32_t* high)
+{
+    if (BITS == 8) return byte_pair<I % 4>(low[I / 4], high[I / 4]);
+    return byte_pair<I / 2 % 4>(low[I / 8], high[I / 8]) & (I % 2 ? 0x00f000f0u : 0x000f000fu);
+}
+
+// The same centred and scaled, (code - c) * 2^-9: exact in binary16.
 template <int BITS, int I>
 __device__ __forceinline__ f16x2 value_pair(const uint32_t* low, const uint32_t* high)
 {
-    if (BITS == 8) {
-        const f16x2 raw = __builtin_bit_cast(f16x2, byte_pair<I % 4>(low[I / 4], high[I / 4]));
-        return __builtin_elementwise_fma(raw, f16x2{32768.0f, 32768.0f}, f16x2{-0.25f, -0.25f});
-    }
-    const uint32_t both = byte_pair<I / 2 % 4>(low[I / 8], high[I / 8]);
-    // the upper nibble of a byte stands for 16 times as much
-    const f16x2 raw = __builtin_bit_cast(f16x2, both & (I % 2 ? 0x00f000f0u : 0x000f000fu));
-    const _Float16 unit = I % 2 ? 2048.0f : 32768.0f;
-    return __builtin_elementwise_fma(raw, f16x2{unit, unit}, f16x2{-0.015625f, -0.015625f});
+    const _Float16 unit = BITS == 4 && I % 2 ? 2048.0f : 32768.0f, center = BITS == 8 ? -0.25f : -0.015625f;
+    return __builtin_elementwise_fma(__builtin_bit_cast(f16x2, raw_pair<BITS, I>(low, high)), f16x2{unit, unit}, f16x2{center, center});
 }
 
 // f(integral_constant 0), .., f(N - 1): a loop whose counter is a constant.
@@ -328,6 +354,10 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
         const int32_t head = w.head * a.group + (there ? row : w.rows - 1) - token * a.group;
         const int32_t position = w.first + token;
         const Span span = span_of(a, w, 16 * tile, 16, K::kBlock);
+        if (a.partial && span.begin >= span.end) {   // a part beyond a short sequence's end
+            if (threadIdx.x < 16 && there) a.partial_lse[part_row_of(a, w, token, head)] = kNothing;
+            continue;
+        }
 
         // q, a lane's 8 elements of its row for every step
         f16x8 q[SPLIT][K::kSteps];
@@ -353,7 +383,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
             for (int s = 0; s < K::kSteps; ++s)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float v = ldexpf(f[s][code_order(KEY_BITS, j)], 14 - q_exponent);
+                    const float v = ldexpf(f[s][code_order(KEY_BITS, j)], 14 - q_exponent - code_bits(KEY_BITS, j));
                     q[0][s][j] = static_cast<_Float16>(v);
                     if (SPLIT == 2) q[SPLIT - 1][s][j] = static_cast<_Float16>(v - static_cast<float>(q[0][s][j]));
                 }
@@ -364,16 +394,23 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
         f32x4 acc[K::kColumns];
 #pragma unroll
         for (int i = 0; i < K::kColumns; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        // Codes are multiplied as they lie and centred at the end, by the sum of the very weights that they were multiplied with: one product
+        // more for one instruction less per pair of codes.
+        f32x4 weights = {0.0f, 0.0f, 0.0f, 0.0f};
+        const _Float16 one = 1.0f;
+        const f16x8 ones = {one, one, one, one, one, one, one, one};
 
+        // pages of a block, whose look-up is not waited for; then its codes: rows of the pages are the wavefront's, places in them the lane's
+        int32_t pages[K::kTiles];
+        const auto find = [&](int32_t base) {
+#pragma unroll
+            for (int t = 0; t < K::kTiles; ++t) pages[t] = shared_page_of(a, table, base + 16 * t);
+        };
+        const uint32_t key_place = n * K::kKeyBytes + g * K::kPiece, value_place = 4 * g * (DIM / 8 * VALUE_BITS) + n * K::kValueBytes;
         const auto load = [&](typename K::Block& b, int32_t base) {
             int64_t rows[K::kTiles];
 #pragma unroll
-            for (int t = 0; t < K::kTiles; ++t) rows[t] = row_of(a, w.head, page_of(a, table, base + 16 * t), base + 16 * t);
-#pragma unroll
-            for (int t = 0; t < K::kTiles; ++t)
-#pragma unroll
-                for (int p = 0; p < K::kPieces; ++p)
-                    load_words<K::kPiece>(a.key_codes + rows[t] * K::kKeyBytes + n * K::kKeyBytes + (4 * p + g) * K::kPiece, b.key[t][p]);
+            for (int t = 0; t < K::kTiles; ++t) rows[t] = row_of(a, w.head, pages[t], base + 16 * t);
             // the lane's own key: number n % 4 of group g's four of tile n / 4
             int64_t own = rows[0];
 #pragma unroll
@@ -382,10 +419,17 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
             b.key_header = *reinterpret_cast<const f32x2*>(a.key_header + 2 * own);
             b.value_header = *reinterpret_cast<const f32x2*>(a.value_header + 2 * own);
 #pragma unroll
-            for (int t = 0; t < K::kTiles; ++t)
+            for (int t = 0; t < K::kTiles; ++t) {
+                const uint8_t* const p = a.key_codes + rows[t] * K::kKeyBytes;
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    load_words<K::kValueBytes>(a.value_codes + (rows[t] + 4 * g + k) * (DIM * VALUE_BITS / 8) + n * K::kValueBytes, b.value[t][k]);
+                for (int i = 0; i < K::kPieces; ++i) load_words<K::kPiece>(p + key_place + 4 * i * K::kPiece, b.key[t][i]);
+            }
+#pragma unroll
+            for (int t = 0; t < K::kTiles; ++t) {
+                const uint8_t* const p = a.value_codes + rows[t] * (DIM / 8 * VALUE_BITS);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) load_words<K::kValueBytes>(p + value_place + k * (DIM / 8 * VALUE_BITS), b.value[t][k]);
+            }
         };
 
         const auto use = [&](const typename K::Block& b, int32_t base) {
@@ -399,6 +443,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
                 for (int i = 0; i < K::kColumns; ++i)
 #pragma unroll
                     for (int r = 0; r < 4; ++r) acc[i][r] = ldexpf(acc[i][r], E - top);
+                weights[0] = ldexpf(weights[0], E - top);
                 E = top;
             }
             const f32x4 four = constants_of(b.key_header, value_header, a, q_exponent, E, VALUE_BITS);
@@ -452,6 +497,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
                 middle *= less;
 #pragma unroll
                 for (int i = 0; i < K::kColumns; ++i) acc[i] *= less;
+                weights[0] *= less;
             }
             const bool bad = !finite(c.middle);
             if (__any(bad)) {
@@ -477,11 +523,16 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
             });
 #pragma unroll
             for (int s = 0; s < K::kTiles / 2; ++s)
+#pragma unroll
+                for (int h = 0; h < SPLIT; ++h) weights = multiply(ones, p[h][s], weights);
+#pragma unroll
+            for (int s = 0; s < K::kTiles / 2; ++s)
                 each<K::kColumns>([&](auto i) {
                     f16x8 values;
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const f16x2 pair = value_pair<VALUE_BITS, i>(b.value[2 * s + k / 2][2 * (k % 2)], b.value[2 * s + k / 2][2 * (k % 2) + 1]);
+                        const uint32_t (&key)[4][K::kValueWords] = b.value[2 * s + k / 2];
+                        const f16x2 pair = __builtin_bit_cast(f16x2, raw_pair<VALUE_BITS, i>(key[2 * (k % 2)], key[2 * (k % 2) + 1]));
                         values[2 * k] = pair[0];
                         values[2 * k + 1] = pair[1];
                     }
@@ -492,11 +543,18 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
 
         int32_t base = span.begin + wave * K::kBlock;
         if (base < span.end) {
+            constexpr int32_t kStride = kFewWaves * K::kBlock;
+            const int32_t last = span.end - 1;
             typename K::Block now, next;
+            find(base);
             load(now, base);
+            find(min(base + kStride, last));
             while (true) {
-                const int32_t after = base + kFewWaves * K::kBlock;
-                if (after < span.end) load(next, after);
+                const int32_t after = base + kStride;
+                if (after < span.end) {
+                    load(next, after);
+                    find(min(after + kStride, last));
+                }
                 use(now, base);
                 if (after >= span.end) break;
                 now = next;
@@ -505,6 +563,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
         }
 
         // the wavefronts' shares: a row's maximum and sum first, then the outputs in two steps through the LDS
+        const int place = here(lane);
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         middle += __shfl_xor(middle, 16);
@@ -524,36 +583,39 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
 #pragma unroll
         for (int i = 0; i < K::kColumns; ++i)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) acc[i][r] = (ldexpf(acc[i][r], E + kUnitBits - kStepBits) + middle) * share;
+            for (int r = 0; r < 4; ++r) {
+                const int unit = VALUE_BITS == 4 && i % 2 ? 20 : 24;
+                const float centered = fmaf(weights[0], VALUE_BITS == 8 ? -128.0f / (1 << 24) : -8.0f / (1 << unit), acc[i][r]);
+                acc[i][r] = (ldexpf(centered, E + unit - kStepBits) + middle) * share;
+            }
 #pragma unroll
         for (int step = kFewWaves / 2; step >= 1; step /= 2) {
             if (wave >= step && wave < 2 * step) {
 #pragma unroll
                 for (int i = 0; i < K::kColumns; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) joined_out[wave - step][i][r][lane] = acc[i][r];
+                    for (int r = 0; r < 4; ++r) joined_out[wave - step][i][r][place] = acc[i][r];
             }
             __syncthreads();
             if (wave < step) {
 #pragma unroll
                 for (int i = 0; i < K::kColumns; ++i)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[i][r] += joined_out[wave][i][r][lane];
+                    for (int r = 0; r < 4; ++r) acc[i][r] += joined_out[wave][i][r][place];
             }
         }
         if (wave == 0 && there) {
             const float scale = is(total, 0.0f) ? 0.0f : 1.0f / total;   // nothing in sight: zeros
-            const int64_t out_row = (static_cast<int64_t>(w.start) + token) * a.q_heads + head;
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 float f[K::kColumns];
 #pragma unroll
                 for (int i = 0; i < K::kColumns; ++i) f[i] = acc[i][r] * scale;
-                const int at = K::kColumns * (4 * g + r);
-                if (a.partial) store_some(a.partial, ACTQ_F32, (static_cast<int64_t>(w.part) * a.tokens * a.q_heads + out_row) * DIM + at, f);
+                const int at = K::kColumns * (4 * (place / 16) + r);
+                if (a.partial) store_some(a.partial, ACTQ_F32, part_row_of(a, w, token, head) * DIM + at, f);
                 else store_some(a.out.p, a.dtype, (static_cast<int64_t>(w.start) + token) * a.out.token + head * a.out.head + at, f);
             }
-            if (a.partial && g == 0) a.partial_lse[static_cast<int64_t>(w.part) * a.tokens * a.q_heads + out_row] = is(total, 0.0f) ? kNothing : top + __builtin_amdgcn_logf(total);
+            if (a.partial && g == 0) a.partial_lse[part_row_of(a, w, token, head)] = is(total, 0.0f) ? kNothing : top + __builtin_amdgcn_logf(total);
         }
         __syncthreads();   // the next tile writes the LDS again
     }
@@ -631,6 +693,13 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
         const int32_t first_row = K::kRows * tile + K::kOwnRows * wave;
         const bool any = first_row < w.rows;
         const Span span = span_of(a, w, K::kRows * tile, K::kRows, K::kTile);
+        if (a.partial && span.begin >= span.end) {   // a part beyond a short sequence's end
+            for (int r = threadIdx.x; r < K::kRows && K::kRows * tile + r < w.rows; r += K::kThreads) {
+                const int32_t token = static_cast<int32_t>(divide(K::kRows * tile + r, a.by_group));
+                a.partial_lse[part_row_of(a, w, token, w.head * a.group + K::kRows * tile + r - token * a.group)] = kNothing;
+            }
+            continue;
+        }
         Span mine = span;   // of the wavefront's rows
         if (any) {
             mine.low = w.first + static_cast<int32_t>(divide(first_row, a.by_group));
@@ -683,7 +752,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
                     load_eight(a.q.p, a.dtype, at(r, s), f);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const float v = ldexpf(a.key_bits == 8 ? f[j] : f[code_order(4, j)], 14 - q_exponent);
+                        const float v = ldexpf(a.key_bits == 8 ? f[j] : f[code_order(4, j)], 14 - q_exponent - (a.key_bits == 8 ? 0 : code_bits(4, j)));
                         q[r][0][s][j] = static_cast<_Float16>(v);
                         if (SPLIT == 2) q[r][SPLIT - 1][s][j] = static_cast<_Float16>(v - static_cast<float>(q[r][0][s][j]));
                     }
@@ -946,7 +1015,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
             if (row_at(r) >= w.rows) continue;
             const float scale = is(sum[r], 0.0f) ? 0.0f : 1.0f / sum[r];   // nothing in sight: zeros
             const int32_t token = token_at(r), head = head_at(r);
-            const int64_t part_row = static_cast<int64_t>(w.part) * a.tokens * a.q_heads + (static_cast<int64_t>(w.start) + token) * a.q_heads + head;
+            const int64_t part_row = part_row_of(a, w, token, head);
 #pragma unroll
             for (int b = 0; b < K::kBlocks; ++b)
 #pragma unroll
@@ -954,7 +1023,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
                     float f[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) f[j] = (ldexpf(acc[r][b][i + j], E + kUnitBits - kStepBits) + middle[r]) * scale;
-                    const int column = 32 * b + 2 * i + 4 * h;
+                    const int column = 32 * b + 2 * i + 4 * (here(lane) / 32);
                     if (a.partial) store_some(a.partial, ACTQ_F32, part_row * DIM + column, f);
                     else store_some(a.out.p, a.dtype, (static_cast<int64_t>(w.start) + token) * a.out.token + head * a.out.head + column, f);
                 }
@@ -965,39 +1034,65 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
 
 // ----------------------------------------------------------------------------- joining parts
 
-// A wavefront per row: the parts' outputs weighted by 2^(lse - largest).
-constexpr int kJoinWaves = 4;
+// A workgroup per row: the parts' outputs weighted by 2^(lse - largest).  DIM / 4 threads take a part, four columns each, the others the
+// next ones, with four parts' loads in flight; their sums meet in the LDS.  In a loop of one wavefront a part costs a trip to memory, 1.2 us.
+constexpr int kJoinThreads = 256;
+constexpr int kMostParts = 128;
 
 template <int DIM>
-__global__ __launch_bounds__(kJoinWaves * 64) void attend_join_kernel(AttendArgs a)
+__global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a)
 {
-    constexpr int kEach = DIM / 64;
-    const int lane = threadIdx.x % 64;
-    const int64_t rows = static_cast<int64_t>(a.tokens) * a.q_heads;
-    const int64_t row = static_cast<int64_t>(blockIdx.x) * kJoinWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    if (row >= rows) return;
-    float top = kNothing;
-    for (uint32_t p = 0; p < a.parts; ++p) top = fmaxf(top, a.partial_lse[p * rows + row]);
-    float total = 0.0f, sum[kEach] = {};
-    for (uint32_t p = 0; p < a.parts; ++p) {
-        const float lse = a.partial_lse[p * rows + row];
-        if (is(lse, kNothing)) continue;
-        const float weight = __builtin_amdgcn_exp2f(lse - top);
-        total += weight;
+    constexpr int kColumns = DIM / 4, kTeams = kJoinThreads / kColumns, kAhead = 4;
+    __shared__ float weights[kMostParts];
+    __shared__ float tops[kJoinThreads / 64];
+    __shared__ f32x4 sums[kTeams][kColumns];
+    const int64_t rows = static_cast<int64_t>(a.tokens) * a.q_heads, row = blockIdx.x;
+    const int parts = static_cast<int>(a.parts);
+    const float lse = static_cast<int>(threadIdx.x) < parts ? a.partial_lse[threadIdx.x * rows + row] : kNothing;
+    const float most = wave_max(lse);
+    if (threadIdx.x % 64 == 0) tops[threadIdx.x / 64] = most;
+    __syncthreads();
+    float top = tops[0];
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) sum[i] = fmaf(weight, a.partial[(p * rows + row) * DIM + kEach * lane + i], sum[i]);
+    for (int k = 1; k < kJoinThreads / 64; ++k) top = fmaxf(top, tops[k]);
+    if (static_cast<int>(threadIdx.x) < parts) weights[threadIdx.x] = is(lse, kNothing) ? 0.0f : __builtin_amdgcn_exp2f(lse - top);
+    __syncthreads();
+    const int column = threadIdx.x % kColumns, team = threadIdx.x / kColumns;
+    f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int p = team; p < parts; p += kTeams * kAhead) {
+        f32x4 v[kAhead];
+        float weight[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int at = p + k * kTeams;
+            weight[k] = at < parts ? weights[at] : 0.0f;
+            v[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            // a part that saw nothing has written no outputs
+            if (!is(weight[k], 0.0f)) v[k] = *reinterpret_cast<const f32x4*>(a.partial + (at * rows + row) * DIM + 4 * column);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] = fmaf(weight[k], v[k][i], sum[i]);
+        }
     }
-    const int64_t token = row / a.q_heads, head = row - token * a.q_heads;
+    sums[team][column] = sum;
+    __syncthreads();
+    if (team != 0) return;
+    float total = 0.0f;
+    for (int p = 0; p < parts; ++p) total += weights[p];
 #pragma unroll
-    for (int i = 0; i < kEach; ++i)
-        store_element(a.out.p, a.dtype, token * a.out.token + head * a.out.head + kEach * lane + i, is(total, 0.0f) ? 0.0f : sum[i] / total);
+    for (int k = 1; k < kTeams; ++k) sum += sums[k][column];
+    const int64_t token = row / a.q_heads, head = row - token * a.q_heads;
+    float f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = is(total, 0.0f) ? 0.0f : sum[i] / total;
+    store_some(a.out.p, a.dtype, token * a.out.token + head * a.out.head + 4 * column, f);
 }
 
 // ----------------------------------------------------------------------------- launches
 
 constexpr int64_t kMostBlocks = int64_t(1) << 22;
-constexpr int64_t kMostParts = 128;
-
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 struct Shape {
@@ -1015,9 +1110,11 @@ Shape shape_of(const actq_cache* c, int32_t heads, int64_t sequences, int64_t ma
     s.rows = rows < kManyRows ? 16 : rows <= 128 || c->dim == 256 ? 128 : 256;
     s.tiles = ceil_div(rows, s.rows);
     if (s.tiles > kMostBlocks / groups) s.tiles = kMostBlocks / groups;
-    // keys of a step; the fewest that are worth a workgroup; workgroups that are wanted: what is resident twice over, and once
+    // keys of a step; the fewest that are worth a workgroup; workgroups that are wanted, as many as are resident: two per compute unit, one of 256
+    // rows.  More of them cost more than they balance (16 rows, 1024 and 2048 instead of 512: 32 sequences of different lengths 85 -> 91, 103 us,
+    // one of 32768 23 -> 27, 27)
     const int64_t block = s.rows == 16 ? (c->dim == 256 ? 32 : 64) : 8192 / c->dim;
-    const int64_t least = s.rows == 16 ? kFewWaves * block : 256, wanted = s.rows == 16 ? 1024 : s.rows == 128 ? 512 : 256;
+    const int64_t least = s.rows == 16 ? kFewWaves * block : 256, wanted = s.rows == 256 ? 256 : 512;
     int64_t span = max_length < 1 ? 1 : max_length;
     if (window > 0 && span > window + ceil_div(s.rows, group) + block) span = window + ceil_div(s.rows, group) + block;
     s.parts = wanted / (groups * s.tiles);
@@ -1110,7 +1207,7 @@ int launch_cache_attention(const actq_cache* c, const actq_heads* q, int dtype, 
     });
     if (rc != ACTQ_OK || shape.parts == 1) return rc;
     return by_dim(c->dim, [&](auto d) {
-        launch(attend_join_kernel<decltype(d)::value>, static_cast<unsigned>(ceil_div(tokens * q->heads, kJoinWaves)), kJoinWaves * 64, s, a);
+        launch(attend_join_kernel<decltype(d)::value>, static_cast<unsigned>(tokens * q->heads), kJoinThreads, s, a);
         return launched(who);
     });
 }
