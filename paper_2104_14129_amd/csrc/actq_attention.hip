@@ -341,7 +341,7 @@ template <int DIM, int SPLIT, int KEY_BITS, int VALUE_BITS>
 __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArgs a)
 {
     typedef Few<DIM, SPLIT, KEY_BITS, VALUE_BITS> K;
-    __shared__ float joined_out[2][K::kColumns][4][64];
+    __shared__ float joined_out[kFewWaves / 2][K::kColumns][4][64];
     __shared__ float joined_max[kFewWaves][16], joined_sum[kFewWaves][16];
     const Work w = work_of(a, blockIdx.x);
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -357,6 +357,48 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
         if (a.partial && span.begin >= span.end) {   // a part beyond a short sequence's end
             if (threadIdx.x < 16 && there) a.partial_lse[part_row_of(a, w, token, head)] = kNothing;
             continue;
+        }
+
+        // pages of a block, whose look-up is not waited for; then its codes: rows of the pages are the wavefront's, places in them the lane's
+        int32_t pages[K::kTiles];
+        const auto find = [&](int32_t base) {
+#pragma unroll
+            for (int t = 0; t < K::kTiles; ++t) pages[t] = shared_page_of(a, table, base + 16 * t);
+        };
+        const uint32_t key_place = n * K::kKeyBytes + g * K::kPiece, value_place = 4 * g * (DIM / 8 * VALUE_BITS) + n * K::kValueBytes;
+        const auto load = [&](typename K::Block& b, int32_t base) {
+            int64_t rows[K::kTiles];
+#pragma unroll
+            for (int t = 0; t < K::kTiles; ++t) rows[t] = row_of(a, w.head, pages[t], base + 16 * t);
+            // the lane's own key: number n % 4 of group g's four of tile n / 4
+            int64_t own = rows[0];
+#pragma unroll
+            for (int t = 1; t < K::kTiles; ++t) own = n / 4 % K::kTiles == t ? rows[t] : own;
+            own += 4 * g + n % 4;
+            b.key_header = *reinterpret_cast<const f32x2*>(a.key_header + 2 * own);
+            b.value_header = *reinterpret_cast<const f32x2*>(a.value_header + 2 * own);
+#pragma unroll
+            for (int t = 0; t < K::kTiles; ++t) {
+                const uint8_t* const p = a.key_codes + rows[t] * K::kKeyBytes;
+#pragma unroll
+                for (int i = 0; i < K::kPieces; ++i) load_words<K::kPiece>(p + key_place + 4 * i * K::kPiece, b.key[t][i]);
+            }
+#pragma unroll
+            for (int t = 0; t < K::kTiles; ++t) {
+                const uint8_t* const p = a.value_codes + rows[t] * (DIM / 8 * VALUE_BITS);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) load_words<K::kValueBytes>(p + value_place + k * (DIM / 8 * VALUE_BITS), b.value[t][k]);
+            }
+        };
+
+        // the first block is on its way before q is asked for: a workgroup's begin is a chain of trips to memory
+        int32_t base = span.begin + wave * K::kBlock;
+        constexpr int32_t kStride = kFewWaves * K::kBlock;
+        typename K::Block now;
+        if (base < span.end) {
+            find(base);
+            load(now, base);
+            find(min(base + kStride, span.end - 1));
         }
 
         // q, a lane's 8 elements of its row for every step
@@ -399,38 +441,6 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
         f32x4 weights = {0.0f, 0.0f, 0.0f, 0.0f};
         const _Float16 one = 1.0f;
         const f16x8 ones = {one, one, one, one, one, one, one, one};
-
-        // pages of a block, whose look-up is not waited for; then its codes: rows of the pages are the wavefront's, places in them the lane's
-        int32_t pages[K::kTiles];
-        const auto find = [&](int32_t base) {
-#pragma unroll
-            for (int t = 0; t < K::kTiles; ++t) pages[t] = shared_page_of(a, table, base + 16 * t);
-        };
-        const uint32_t key_place = n * K::kKeyBytes + g * K::kPiece, value_place = 4 * g * (DIM / 8 * VALUE_BITS) + n * K::kValueBytes;
-        const auto load = [&](typename K::Block& b, int32_t base) {
-            int64_t rows[K::kTiles];
-#pragma unroll
-            for (int t = 0; t < K::kTiles; ++t) rows[t] = row_of(a, w.head, pages[t], base + 16 * t);
-            // the lane's own key: number n % 4 of group g's four of tile n / 4
-            int64_t own = rows[0];
-#pragma unroll
-            for (int t = 1; t < K::kTiles; ++t) own = n / 4 % K::kTiles == t ? rows[t] : own;
-            own += 4 * g + n % 4;
-            b.key_header = *reinterpret_cast<const f32x2*>(a.key_header + 2 * own);
-            b.value_header = *reinterpret_cast<const f32x2*>(a.value_header + 2 * own);
-#pragma unroll
-            for (int t = 0; t < K::kTiles; ++t) {
-                const uint8_t* const p = a.key_codes + rows[t] * K::kKeyBytes;
-#pragma unroll
-                for (int i = 0; i < K::kPieces; ++i) load_words<K::kPiece>(p + key_place + 4 * i * K::kPiece, b.key[t][i]);
-            }
-#pragma unroll
-            for (int t = 0; t < K::kTiles; ++t) {
-                const uint8_t* const p = a.value_codes + rows[t] * (DIM / 8 * VALUE_BITS);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) load_words<K::kValueBytes>(p + value_place + k * (DIM / 8 * VALUE_BITS), b.value[t][k]);
-            }
-        };
 
         const auto use = [&](const typename K::Block& b, int32_t base) {
             const int32_t own = base + 16 * (n / 4 % K::kTiles) + 4 * g + n % 4;
@@ -541,19 +551,13 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
                 });
         };
 
-        int32_t base = span.begin + wave * K::kBlock;
         if (base < span.end) {
-            constexpr int32_t kStride = kFewWaves * K::kBlock;
-            const int32_t last = span.end - 1;
-            typename K::Block now, next;
-            find(base);
-            load(now, base);
-            find(min(base + kStride, last));
+            typename K::Block next;
             while (true) {
                 const int32_t after = base + kStride;
                 if (after < span.end) {
                     load(next, after);
-                    find(min(after + kStride, last));
+                    find(min(after + kStride, span.end - 1));
                 }
                 use(now, base);
                 if (after >= span.end) break;
@@ -711,6 +715,59 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
         const auto token_at = [&](int r) { return static_cast<int32_t>(divide(min(row_at(r), w.rows - 1), a.by_group)); };
         const auto head_at = [&](int r) { return w.head * a.group + min(row_at(r), w.rows - 1) - token_at(r) * a.group; };
 
+        int32_t pages[K::kKeyUnits], own_pages[K::kOwn];
+        uint32_t codes[8 * K::kValueUnits];
+        f32x2 key_header[K::kOwn], value_header[K::kOwn];
+
+        // pages of a tile, then its codes, then the LDS
+        const auto find = [&](int32_t base) {
+            if (of_values) {
+#pragma unroll
+                for (int u = 0; u < K::kValueUnits; ++u) pages[u] = page_of(a, table, base + 16 * step_of(u));
+            } else {
+#pragma unroll
+                for (int u = 0; u < K::kKeyUnits; ++u) pages[u] = page_of(a, table, base + key_of(u));
+            }
+            if (of_constants) {
+#pragma unroll
+                for (int o = 0; o < K::kOwn; ++o) own_pages[o] = page_of(a, table, base + (lane + 64 * o) % K::kTile);
+            }
+        };
+        const auto load = [&](int32_t base) {
+            const auto load_values = [&](auto bits) {
+                constexpr int kBits = decltype(bits)::value, kBytes = DIM / 8 * kBits;
+#pragma unroll
+                for (int u = 0; u < K::kValueUnits; ++u) {
+                    const uint8_t* const p = a.value_codes + (row_of(a, w.head, pages[u], base + 16 * step_of(u)) + 8 * half_of(u) + 4 * odd_of(u)) * kBytes + columns_of(u) * kBits;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) load_words<kBits>(p + k * kBytes, codes + 8 * u + 2 * k);
+                }
+            };
+            const auto load_keys = [&](auto bits) {
+                constexpr int kBits = decltype(bits)::value, kBytes = DIM / 8 * kBits;
+#pragma unroll
+                for (int u = 0; u < K::kKeyUnits; ++u)
+                    load_words<2 * kBits>(a.key_codes + row_of(a, w.head, pages[u], base + key_of(u)) * kBytes + chunk_of(u) * 2 * kBits, codes + 4 * u);
+            };
+            if (of_values) a.value_bits == 8 ? load_values(eight) : load_values(four);
+            else a.key_bits == 8 ? load_keys(eight) : load_keys(four);
+            if (of_constants) {
+#pragma unroll
+                for (int o = 0; o < K::kOwn; ++o) {
+                    const int64_t own = row_of(a, w.head, own_pages[o], base + (lane + 64 * o) % K::kTile);
+                    key_header[o] = *reinterpret_cast<const f32x2*>(a.key_header + 2 * own);
+                    value_header[o] = *reinterpret_cast<const f32x2*>(a.value_header + 2 * own);
+                }
+            }
+        };
+        // the first tile is on its way before q is asked for: a workgroup's begin is a chain of trips to memory
+        const int32_t last = span.end - 1;
+        if (span.begin < span.end) {
+            find(span.begin);
+            load(span.begin);
+            find(min(span.begin + K::kTile, last));
+        }
+
         // q, a lane's 8 elements of its rows for every step
         f16x8 q[SETS][SPLIT][K::kSteps];
         float q_sum[SETS];
@@ -770,51 +827,6 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
             for (int b = 0; b < K::kBlocks; ++b) acc[r][b] = f32x16{};
         }
 
-        int32_t pages[K::kKeyUnits], own_pages[K::kOwn];
-        uint32_t codes[8 * K::kValueUnits];
-        f32x2 key_header[K::kOwn], value_header[K::kOwn];
-
-        // pages of a tile, then its codes, then the LDS
-        const auto find = [&](int32_t base) {
-            if (of_values) {
-#pragma unroll
-                for (int u = 0; u < K::kValueUnits; ++u) pages[u] = page_of(a, table, base + 16 * step_of(u));
-            } else {
-#pragma unroll
-                for (int u = 0; u < K::kKeyUnits; ++u) pages[u] = page_of(a, table, base + key_of(u));
-            }
-            if (of_constants) {
-#pragma unroll
-                for (int o = 0; o < K::kOwn; ++o) own_pages[o] = page_of(a, table, base + (lane + 64 * o) % K::kTile);
-            }
-        };
-        const auto load = [&](int32_t base) {
-            const auto load_values = [&](auto bits) {
-                constexpr int kBits = decltype(bits)::value, kBytes = DIM / 8 * kBits;
-#pragma unroll
-                for (int u = 0; u < K::kValueUnits; ++u) {
-                    const uint8_t* const p = a.value_codes + (row_of(a, w.head, pages[u], base + 16 * step_of(u)) + 8 * half_of(u) + 4 * odd_of(u)) * kBytes + columns_of(u) * kBits;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) load_words<kBits>(p + k * kBytes, codes + 8 * u + 2 * k);
-                }
-            };
-            const auto load_keys = [&](auto bits) {
-                constexpr int kBits = decltype(bits)::value, kBytes = DIM / 8 * kBits;
-#pragma unroll
-                for (int u = 0; u < K::kKeyUnits; ++u)
-                    load_words<2 * kBits>(a.key_codes + row_of(a, w.head, pages[u], base + key_of(u)) * kBytes + chunk_of(u) * 2 * kBits, codes + 4 * u);
-            };
-            if (of_values) a.value_bits == 8 ? load_values(eight) : load_values(four);
-            else a.key_bits == 8 ? load_keys(eight) : load_keys(four);
-            if (of_constants) {
-#pragma unroll
-                for (int o = 0; o < K::kOwn; ++o) {
-                    const int64_t own = row_of(a, w.head, own_pages[o], base + (lane + 64 * o) % K::kTile);
-                    key_header[o] = *reinterpret_cast<const f32x2*>(a.key_header + 2 * own);
-                    value_header[o] = *reinterpret_cast<const f32x2*>(a.value_header + 2 * own);
-                }
-            }
-        };
         const auto store = [&](int32_t base, int to) {
             const auto store_values = [&](auto bits) {
                 constexpr int kBits = decltype(bits)::value;
@@ -978,10 +990,6 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
         };
 
         if (span.begin < span.end) {
-            const int32_t last = span.end - 1;
-            find(span.begin);
-            load(span.begin);
-            find(min(span.begin + K::kTile, last));
             store(span.begin, 0);
             if (span.begin + K::kTile < span.end) load(span.begin + K::kTile);
             find(min(span.begin + 2 * K::kTile, last));
@@ -1039,50 +1047,60 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
 constexpr int kJoinThreads = 256;
 constexpr int kMostParts = 128;
 
-template <int DIM>
+// SHARED: all teams share a row; else each has its own, which is faster below kSharedParts parts.
+constexpr int kSharedParts = 16;
+
+template <int DIM, bool SHARED>
 __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a)
 {
-    constexpr int kColumns = DIM / 4, kTeams = kJoinThreads / kColumns, kAhead = 4;
-    __shared__ float weights[kMostParts];
+    constexpr int kColumns = DIM / 4, kTeams = kJoinThreads / kColumns, kAhead = 4, kStride = SHARED ? kTeams : 1;
+    __shared__ float weights[SHARED ? 1 : kTeams][SHARED ? kMostParts : kSharedParts];
+    __shared__ f32x4 sums[SHARED ? kTeams : 1][kColumns];
     __shared__ float tops[kJoinThreads / 64];
-    __shared__ f32x4 sums[kTeams][kColumns];
-    const int64_t rows = static_cast<int64_t>(a.tokens) * a.q_heads, row = blockIdx.x;
-    const int parts = static_cast<int>(a.parts);
-    const float lse = static_cast<int>(threadIdx.x) < parts ? a.partial_lse[threadIdx.x * rows + row] : kNothing;
-    const float most = wave_max(lse);
-    if (threadIdx.x % 64 == 0) tops[threadIdx.x / 64] = most;
-    __syncthreads();
-    float top = tops[0];
+    const int64_t rows = static_cast<int64_t>(a.tokens) * a.q_heads;
+    const int column = threadIdx.x % kColumns, team = threadIdx.x / kColumns, parts = static_cast<int>(a.parts);
+    const int64_t row = SHARED ? static_cast<int64_t>(blockIdx.x) : static_cast<int64_t>(blockIdx.x) * kTeams + team;
+    const bool there = row < rows;
+    const int own = SHARED ? static_cast<int>(threadIdx.x) : column;   // the part whose weight the thread works out
+    const float lse = there && own < parts ? a.partial_lse[own * rows + row] : kNothing;
+    float top = SHARED ? wave_max(lse) : over_lanes<16>(lse, [](float x, float y) { return fmaxf(x, y); });   // the first 16 threads of a team
+    if (SHARED) {
+        if (threadIdx.x % 64 == 0) tops[threadIdx.x / 64] = top;
+        __syncthreads();
+        top = tops[0];
 #pragma unroll
-    for (int k = 1; k < kJoinThreads / 64; ++k) top = fmaxf(top, tops[k]);
-    if (static_cast<int>(threadIdx.x) < parts) weights[threadIdx.x] = is(lse, kNothing) ? 0.0f : __builtin_amdgcn_exp2f(lse - top);
+        for (int k = 1; k < kJoinThreads / 64; ++k) top = fmaxf(top, tops[k]);
+    }
+    float* const mine = weights[SHARED ? 0 : team];
+    if (own < parts) mine[own] = is(lse, kNothing) ? 0.0f : __builtin_amdgcn_exp2f(lse - top);
     __syncthreads();
-    const int column = threadIdx.x % kColumns, team = threadIdx.x / kColumns;
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int p = team; p < parts; p += kTeams * kAhead) {
+    for (int p = SHARED ? team : 0; there && p < parts; p += kStride * kAhead) {
         f32x4 v[kAhead];
         float weight[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-            const int at = p + k * kTeams;
-            weight[k] = at < parts ? weights[at] : 0.0f;
+            const int at = p + k * kStride;
+            weight[k] = at < parts ? mine[at] : 0.0f;
             v[k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
             // a part that saw nothing has written no outputs
             if (!is(weight[k], 0.0f)) v[k] = *reinterpret_cast<const f32x4*>(a.partial + (at * rows + row) * DIM + 4 * column);
         }
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
+        for (int k = 0; k < kAhead; ++k)
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum[i] = fmaf(weight[k], v[k][i], sum[i]);
-        }
     }
-    sums[team][column] = sum;
-    __syncthreads();
-    if (team != 0) return;
-    float total = 0.0f;
-    for (int p = 0; p < parts; ++p) total += weights[p];
+    if (SHARED) {
+        sums[team][column] = sum;
+        __syncthreads();
+        if (team != 0) return;
 #pragma unroll
-    for (int k = 1; k < kTeams; ++k) sum += sums[k][column];
+        for (int k = 1; k < kTeams; ++k) sum += sums[k][column];
+    }
+    if (!there) return;
+    float total = 0.0f;
+    for (int p = 0; p < parts; ++p) total += mine[p];
     const int64_t token = row / a.q_heads, head = row - token * a.q_heads;
     float f[4];
 #pragma unroll
@@ -1207,7 +1225,10 @@ int launch_cache_attention(const actq_cache* c, const actq_heads* q, int dtype, 
     });
     if (rc != ACTQ_OK || shape.parts == 1) return rc;
     return by_dim(c->dim, [&](auto d) {
-        launch(attend_join_kernel<decltype(d)::value>, static_cast<unsigned>(tokens * q->heads), kJoinThreads, s, a);
+        constexpr int kDim = decltype(d)::value;
+        const int64_t rows = tokens * q->heads;
+        if (shape.parts >= kSharedParts) launch(attend_join_kernel<kDim, true>, static_cast<unsigned>(rows), kJoinThreads, s, a);
+        else launch(attend_join_kernel<kDim, false>, static_cast<unsigned>(ceil_div(rows, kJoinThreads / (kDim / 4))), kJoinThreads, s, a);
         return launched(who);
     });
 }

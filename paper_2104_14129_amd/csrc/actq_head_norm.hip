@@ -265,7 +265,7 @@ __global__ __launch_bounds__(kNormBlock) void head_norm_backward_kernel(NormGrad
 }
 
 // grad_w [dim] of the queries and of the keys: the workgroups' shares in binary64, each of 16 threads a sixteenth of them.
-constexpr int kSumColumns = 16, kSumRows = 16;
+constexpr int kSumColumns = 16, kSumRows = 16, kSumAhead = 8;
 
 template <typename W>
 __global__ __launch_bounds__(kSumColumns* kSumRows) void head_norm_weights_kernel(const float* partial, int32_t blocks, int32_t dim, W* grad_q, W* grad_k)
@@ -273,7 +273,17 @@ __global__ __launch_bounds__(kSumColumns* kSumRows) void head_norm_weights_kerne
     __shared__ double sums[kSumRows][kSumColumns];
     const int column = threadIdx.x % kSumColumns, row = threadIdx.x / kSumColumns, at = blockIdx.x * kSumColumns + column;
     double sum = 0.0;
-    for (int b = row; b < blocks; b += kSumRows) sum += static_cast<double>(partial[static_cast<int64_t>(b) * 2 * dim + at]);
+    // eight loads in flight: one after the other each of up to 32 costs a trip to memory
+    for (int b = row; b < blocks; b += kSumRows * kSumAhead) {
+        float v[kSumAhead];
+#pragma unroll
+        for (int k = 0; k < kSumAhead; ++k) {
+            const int from = b + k * kSumRows;
+            v[k] = from < blocks ? partial[static_cast<int64_t>(from) * 2 * dim + at] : 0.0f;
+        }
+#pragma unroll
+        for (int k = 0; k < kSumAhead; ++k) sum += static_cast<double>(v[k]);
+    }
     sums[row][column] = sum;
     __syncthreads();
     if (row != 0) return;
