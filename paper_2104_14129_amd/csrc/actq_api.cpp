@@ -448,6 +448,15 @@ static int check_heads_dtype(const char* who, int dt)
     return ACTQ_OK;
 }
 
+// Of the bits: the compiler takes it that floating-point data holds no NaN.
+static bool finite(float v, bool above_zero = false, bool below_zero = true)
+{
+    uint32_t b;
+    memcpy(&b, &v, sizeof(b));
+    if (b << 1 >= 0xff000000u) return false;
+    return b << 1 == 0 ? !above_zero : below_zero || b >> 31 == 0;
+}
+
 static uintptr_t size_of(int dt) { return dt == ACTQ_F32 ? 4 : 2; }
 
 static int check_dim(const char* who, int32_t dim)
@@ -507,7 +516,7 @@ static int check_norm(const char* who, const actq_heads* q, const actq_heads* k,
     if (weight_dt != dt && weight_dt != ACTQ_F32) return fail(ACTQ_EINVAL, "%s: weights must have the heads' type or ACTQ_F32", who);
     if (!aligned(q_weight, size_of(weight_dt)) || !aligned(k_weight, size_of(weight_dt))) return fail(ACTQ_EINVAL, "%s: a weight is not aligned to its element size", who);
     if (int rc = check_rotation(who, rotation, tokens, dim)) return rc;
-    if (!(eps > 0.0f) || std::isinf(eps)) return fail(ACTQ_EINVAL, "%s: eps must be finite and above zero", who);
+    if (!finite(eps, true, false)) return fail(ACTQ_EINVAL, "%s: eps must be finite and above zero", who);
     return ACTQ_OK;
 }
 
@@ -625,7 +634,7 @@ int actq_cache_attention(const actq_cache* cache, const actq_heads* q, actq_dtyp
     if (int rc = check_heads_dtype(who, dt)) return rc;
     if (int rc = check_heads(who, "q", q, dt, tokens, q->heads)) return rc;
     if (int rc = check_heads(who, "out", out, dt, tokens, q->heads)) return rc;
-    if (!(std::fabs(scale) < INFINITY) || !(softcap >= 0.0f && softcap < INFINITY)) return fail(ACTQ_EINVAL, "%s: scale must be finite, softcap finite and not negative", who);
+    if (!finite(scale) || !finite(softcap, false, false)) return fail(ACTQ_EINVAL, "%s: scale must be finite, softcap finite and not negative", who);
     if (tokens == 0 || sequences == 0) return ACTQ_OK;
     if (!table || !lengths || !query_start || !aligned(table, 4) || !aligned(lengths, 4) || !aligned(query_start, 4))
         return fail(ACTQ_EINVAL, "%s: table, lengths or query_start is null or misaligned", who);

@@ -264,8 +264,8 @@ __global__ __launch_bounds__(kNormBlock) void head_norm_backward_kernel(NormGrad
     }
 }
 
-// grad_w [dim] of the queries and of the keys: the workgroups' shares in binary64, each of 16 threads a sixteenth of them.
-constexpr int kSumColumns = 16, kSumRows = 16, kSumAhead = 8;
+// grad_w [dim] of the queries and of the keys: the workgroups' shares in binary64, each of 64 threads a 64th of them.
+constexpr int kSumColumns = 16, kSumRows = 64, kSumAhead = 8;
 
 template <typename W>
 __global__ __launch_bounds__(kSumColumns* kSumRows) void head_norm_weights_kernel(const float* partial, int32_t blocks, int32_t dim, W* grad_q, W* grad_k)
@@ -273,7 +273,7 @@ __global__ __launch_bounds__(kSumColumns* kSumRows) void head_norm_weights_kerne
     __shared__ double sums[kSumRows][kSumColumns];
     const int column = threadIdx.x % kSumColumns, row = threadIdx.x / kSumColumns, at = blockIdx.x * kSumColumns + column;
     double sum = 0.0;
-    // eight loads in flight: one after the other each of up to 32 costs a trip to memory
+    // all of a thread's loads in flight: one after the other each costs a trip to memory
     for (int b = row; b < blocks; b += kSumRows * kSumAhead) {
         float v[kSumAhead];
 #pragma unroll
@@ -286,9 +286,14 @@ __global__ __launch_bounds__(kSumColumns* kSumRows) void head_norm_weights_kerne
     }
     sums[row][column] = sum;
     __syncthreads();
+    for (int half = kSumRows / 2; half >= 1; half /= 2) {
+        if (row < half) {
+            sum += sums[row + half][column];
+            sums[row][column] = sum;
+        }
+        __syncthreads();
+    }
     if (row != 0) return;
-#pragma unroll
-    for (int r = 1; r < kSumRows; ++r) sum += sums[r][column];
     W* const out = at < dim ? grad_q : grad_k;
     if (out) out[at < dim ? at : at - dim] = static_cast<W>(static_cast<float>(sum));
 }

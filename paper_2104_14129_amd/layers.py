@@ -5,6 +5,8 @@ layer keeps a compressed context instead and computes its gradients from the deq
 context with the stock backward routine of the layer.  The forward results are those of the
 stock layer, so inference is unchanged.
 
+`QHeadNorm` (norm and rotation of attention heads) computes forward and backward in the library as well.
+
 Everything that touches the saved activations runs in libactq through `binding`: per-group
 statistics, sensitivities, the device-side bit allocator, quantize + pack, unpack + dequantize,
 the ReLU bit mask and the max-pooling positions.  torch supplies the layers' own arithmetic
@@ -24,7 +26,7 @@ import torch.nn.functional as F
 from . import binding as B
 
 __all__ = ["QConfig", "config", "set_optimization_level", "compress", "decompress", "SavedContext",
-           "QLinear", "QConv2d", "QBatchNorm2d", "QReLU", "QMaxPool2d", "convert"]
+           "QLinear", "QConv2d", "QBatchNorm2d", "QReLU", "QMaxPool2d", "QHeadNorm", "convert"]
 
 
 @dataclass
@@ -302,6 +304,48 @@ class _QMaxPool2dFn(torch.autograd.Function):
         return B.maxpool2d_backward(arg, grad_y.contiguous(), H, W, kernel, stride, padding, dilation), None, None, None, None
 
 
+class _QHeadNormFn(torch.autograd.Function):
+    """Norm and rotation of queries and keys by the library; the contexts are the compressed queries and keys.  What the codec does not
+    take (bfloat16, no tokens) is kept as it is."""
+
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, positions, cos, sin, eps, interleaved):
+        out = B.head_norm_rotate(q, k, q_weight, k_weight, positions, cos, sin, eps, interleaved)
+        ctx.options = eps, interleaved
+        ctx.contexts, saved = [], []
+        for x in (q, k):
+            if x.dtype in _DTYPES and x.numel() > 0:
+                c = compress(x)
+                streams = c.host if c.host is not None else (c.packed, c.header)
+                ctx.contexts.append((c.shape, c.dtype, c.N, c.D, c.hf, c.ready, c.host is not None))
+                saved += [c.bits, c.offsets, *streams]
+            else:
+                ctx.contexts.append(None)
+                saved += [x, None, None, None]
+        ctx.save_for_backward(*saved, q_weight, k_weight, positions, cos, sin)
+        return out
+
+    @staticmethod
+    def backward(ctx, grad_q, grad_k):
+        saved = ctx.saved_tensors
+        inputs = []
+        for i, meta in enumerate(ctx.contexts):
+            first, offsets, s0, s1 = saved[4 * i:4 * i + 4]
+            if meta is None:
+                inputs.append(first)
+                continue
+            c = SavedContext()
+            c.bits, c.offsets = first, offsets
+            c.shape, c.dtype, c.N, c.D, c.hf, c.ready, swapped = meta
+            c.host, c.packed, c.header = ((s0, s1), None, None) if swapped else (None, s0, s1)
+            inputs.append(decompress(c))
+        q_weight, k_weight, positions, cos, sin = saved[8:]
+        grad_q, grad_k = (g if g.stride(-1) == 1 else g.contiguous() for g in (grad_q, grad_k))
+        gradients = B.head_norm_rotate_backward(grad_q, grad_k, *inputs, q_weight, k_weight, positions, cos, sin, *ctx.options,
+                                                need_weights=ctx.needs_input_grad[2] or ctx.needs_input_grad[3])
+        return (*gradients, None, None, None, None, None)
+
+
 # ----------------------------------------------------------------------------- modules
 
 def _pair(v):
@@ -352,6 +396,25 @@ class QMaxPool2d(nn.MaxPool2d):
             window = k, _pair(self.stride if self.stride is not None else self.kernel_size), _pair(self.padding), _pair(self.dilation)
             return B._host.maxpool2d(x, *window) if _native(x) else _QMaxPool2dFn.apply(x, *window)
         return super().forward(x)
+
+
+class QHeadNorm(nn.Module):
+    """RMS norm of every query and key head with its own weight, and rotation by position (binding.head_norm_rotate).
+
+    q, k [tokens, heads, dim] (float32, float16 or bfloat16; heads contiguous); positions int32 [tokens], rows of the float32 tables
+    cos and sin [rows, rotated / 2], a position that is none of them being padding.  In training the backward pass starts from the
+    compressed queries and keys; bfloat16 ones, which the codec does not take, are kept as they are."""
+
+    def __init__(self, dim: int, eps: float = 1e-6, interleaved: bool = False, device=None, dtype=None):
+        super().__init__()
+        self.eps, self.interleaved = eps, interleaved
+        self.q_weight = nn.Parameter(torch.ones(dim, device=device, dtype=dtype))
+        self.k_weight = nn.Parameter(torch.ones(dim, device=device, dtype=dtype))
+
+    def forward(self, q, k, positions, cos, sin):
+        if torch.is_grad_enabled() and any(t.requires_grad for t in (q, k, self.q_weight, self.k_weight)):
+            return _QHeadNormFn.apply(q, k, self.q_weight, self.k_weight, positions, cos, sin, self.eps, self.interleaved)
+        return B.head_norm_rotate(q, k, self.q_weight, self.k_weight, positions, cos, sin, self.eps, self.interleaved)
 
 
 def convert(module: nn.Module) -> nn.Module:

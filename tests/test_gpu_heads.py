@@ -378,3 +378,50 @@ def test_attention_without_tokens_or_sequences():
     assert B.cache_attention(q[:0].to(DEV), *cache, *args).shape == (0, 4, 64)
     none = B.cache_attention(q[:0].to(DEV), *cache, table[:0].to(DEV), lengths[:0].to(DEV), start[:1].to(DEV), 0, 0)
     assert none.shape == (0, 4, 64)
+
+
+# ----------------------------------------------------------------------------- refusals of the binding
+
+def test_tensors_that_do_not_fit_are_refused():
+    q, k = torch.zeros((3, 4, 64), device=DEV), torch.zeros((3, 2, 64), device=DEV)
+    i, t = torch.zeros(3, dtype=torch.int32, device=DEV), torch.zeros((5, 32), device=DEV)
+    w = torch.ones(64, device=DEV)
+    ok = [q, k, w, w, i, t, t]
+    B.head_norm_rotate(*ok)
+    for at, bad, error in ((0, q[0], ValueError), (0, q.double(), TypeError), (0, q.transpose(1, 2), ValueError), (1, k[:2], ValueError), (1, k.half(), TypeError),
+                           (2, w[:32], ValueError), (2, w.half(), TypeError), (4, i.long(), TypeError), (4, i[:2], ValueError), (5, t[:, :16], ValueError),
+                           (5, t.double(), TypeError), (6, t.cpu(), ValueError), (0, q.cpu(), ValueError)):
+        args = list(ok)
+        args[at] = bad
+        with pytest.raises(error):
+            B.head_norm_rotate(*args)
+    with pytest.raises(ValueError, match="expanded"):
+        B.head_norm_rotate(*ok, q_out=torch.zeros((3, 1, 64), device=DEV).expand(3, 4, 64))
+    with pytest.raises(B.ActqError, match="eps"):
+        B.head_norm_rotate(*ok, eps=0.0)
+    with pytest.raises(ValueError, match="grad_k"):
+        B.head_norm_rotate_backward(q, None, *ok)
+    cache = H.make_cache(4, 2, 16, 64, 8, 4, 0, poison=False)
+    slots = torch.arange(3, device=DEV)
+    B.cache_write(k, k, slots, *cache)
+    for args, error in (((k, k[:2], slots, *cache), ValueError), ((k, k.half(), slots, *cache), TypeError), ((k, k, slots.int(), *cache), TypeError), ((q, q, slots, *cache), B.ActqError),
+                        ((k, k, slots, cache[0][:2], *cache[1:]), ValueError), ((k, k, slots, cache[0][..., :8], *cache[1:]), ValueError),
+                        ((k, k, slots, cache[0], cache[1].half(), *cache[2:]), TypeError)):
+        with pytest.raises(error):
+            B.cache_write(*args)
+    with pytest.raises(TypeError):
+        B.cache_read(slots, *cache, 64, torch.int32)
+    with pytest.raises(ValueError):
+        B.cache_read(slots, *cache, 64, torch.float32, k=torch.zeros((2, 2, 64), device=DEV))
+    table, lengths, start = i.view(3, 1), i, torch.zeros(4, dtype=torch.int32, device=DEV)
+    ok = [q, *cache, table, lengths, start, 1, 16]
+    B.cache_attention(*ok)
+    for at, bad, error in ((0, q[..., :32], ValueError), (5, table.long(), TypeError), (5, table[:2], ValueError), (7, start[:3], ValueError), (6, lengths.cpu(), ValueError),
+                           (8, -1, B.ActqError), (0, q[:, :3], B.ActqError)):
+        args = list(ok)
+        args[at] = bad
+        with pytest.raises(error):
+            B.cache_attention(*args)
+    for options in (dict(window=-1), dict(softcap=-1.0), dict(scale=float("inf")), dict(out=torch.zeros((3, 4, 64), dtype=F16, device=DEV))):
+        with pytest.raises((ValueError, TypeError, B.ActqError)):
+            B.cache_attention(*ok, **options)
