@@ -53,7 +53,7 @@ struct AttendArgs {
     FastDiv by_tiles, by_parts, by_heads;
     int32_t per_part;           // keys of a part, a multiple of the kernels' block of keys
     float* partial;             // [parts][tokens * q_heads][dim], null: one part
-    float* partial_lse;         // [parts][tokens * q_heads]
+    f32x2* partial_sums;        // [parts][tokens * q_heads]: running maximum and sum; no sum: nothing in sight, and no outputs written
 };
 
 __device__ __forceinline__ uint32_t divide(uint32_t n, FastDiv by) { return (__umulhi(n, by.m) + n) >> by.s; }
@@ -232,7 +232,8 @@ __device__ __forceinline__ uint32_t byte_pair(uint32_t low, uint32_t high)
 __device__ __forceinline__ int code_order(int bits, int j) { return bits == 8 ? j : (j >> 1) + 4 * (j & 1); }
 __device__ __forceinline__ int code_bits(int bits, int j) { return bits == 8 ? 0 : (j & 2) * 2; }   // to the left of where they belong
 
-template <int BITS>
+// CENTERED: (code - c) * 2^-9 instead, for binary32: scores are then sums of smaller terms, whose rounding is a third.
+template <int BITS, bool CENTERED>
 __device__ __forceinline__ f16x8 key_codes_of(const uint32_t* w)
 {
     u32x4 r;
@@ -247,6 +248,13 @@ __device__ __forceinline__ f16x8 key_codes_of(const uint32_t* w)
         r[1] = w[0] & 0x00f000f0u;
         r[2] = up & 0x000f000fu;
         r[3] = up & 0x00f000f0u;
+    }
+    if (CENTERED) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const _Float16 unit = BITS == 4 && i % 2 ? 2048.0f : 32768.0f, center = BITS == 8 ? -0.25f : -0.015625f;
+            r[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2, uint32_t(r[i])), f16x2{unit, unit}, f16x2{center, center}));
+        }
     }
     return __builtin_bit_cast(f16x8, r);
 }
@@ -286,10 +294,12 @@ struct Constants {
 
 // Constants of a key that some row sees, or (value header zero) of one that none does.  Where a value is no number, step is zero and
 // middle is none: nothing times an infinity is no number either, so rows that see the key are made none on their own.
-__device__ __forceinline__ f32x4 constants_of(f32x2 key_header, f32x2 value_header, const AttendArgs& a, int q_exponent, int E, int value_bits)
+template <bool CENTERED>
+__device__ __forceinline__ f32x4 constants_of(f32x2 key_header, f32x2 value_header, const AttendArgs& a, int q_exponent, int E, int key_bits, int value_bits)
 {
     const float middle = fmaf(value_bits == 8 ? 128.0f : 8.0f, value_header[1], value_header[0]);
-    return f32x4{ldexpf(key_header[1] * a.factor, 24 - 14 + q_exponent), key_header[0] * a.factor,
+    const float zero = CENTERED ? fmaf(key_bits == 8 ? 128.0f : 8.0f, key_header[1], key_header[0]) : key_header[0];
+    return f32x4{ldexpf(key_header[1] * a.factor, (CENTERED ? kUnitBits : 24) - 14 + q_exponent), zero * a.factor,
                  finite(middle) ? ldexpf(value_header[1], kStepBits - E) : 0.0f, middle};
 }
 
@@ -355,7 +365,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
         const int32_t position = w.first + token;
         const Span span = span_of(a, w, 16 * tile, 16, K::kBlock);
         if (a.partial && span.begin >= span.end) {   // a part beyond a short sequence's end
-            if (threadIdx.x < 16 && there) a.partial_lse[part_row_of(a, w, token, head)] = kNothing;
+            if (threadIdx.x < 16 && there) a.partial_sums[part_row_of(a, w, token, head)] = f32x2{kNothing, 0.0f};
             continue;
         }
 
@@ -425,7 +435,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
             for (int s = 0; s < K::kSteps; ++s)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float v = ldexpf(f[s][code_order(KEY_BITS, j)], 14 - q_exponent - code_bits(KEY_BITS, j));
+                    const float v = ldexpf(f[s][code_order(KEY_BITS, j)], 14 - q_exponent - (SPLIT == 2 ? 0 : code_bits(KEY_BITS, j)));
                     q[0][s][j] = static_cast<_Float16>(v);
                     if (SPLIT == 2) q[SPLIT - 1][s][j] = static_cast<_Float16>(v - static_cast<float>(q[0][s][j]));
                 }
@@ -437,7 +447,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
 #pragma unroll
         for (int i = 0; i < K::kColumns; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         // Codes are multiplied as they lie and centred at the end, by the sum of the very weights that they were multiplied with: one product
-        // more for one instruction less per pair of codes.
+        // more for one instruction less per pair of codes.  The sums are larger than centred ones, by 2.5 where a group is normal, and so is
+        // their rounding: far below that of a 16-bit result, but not for binary32, whose codes are centred at once.
         f32x4 weights = {0.0f, 0.0f, 0.0f, 0.0f};
         const _Float16 one = 1.0f;
         const f16x8 ones = {one, one, one, one, one, one, one, one};
@@ -456,7 +467,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
                 weights[0] = ldexpf(weights[0], E - top);
                 E = top;
             }
-            const f32x4 four = constants_of(b.key_header, value_header, a, q_exponent, E, VALUE_BITS);
+            const f32x4 four = constants_of<SPLIT == 2>(b.key_header, value_header, a, q_exponent, E, KEY_BITS, VALUE_BITS);
             Constants c = {four[0], four[1], four[2], four[3]};
             settled(c.key_zero);
             f32x4 x[K::kTiles];
@@ -465,7 +476,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
                 x[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
                 for (int s = 0; s < K::kSteps; ++s) {
-                    const f16x8 codes = key_codes_of<KEY_BITS>(&b.key[t][s / K::kPieceSteps][s % K::kPieceSteps * (KEY_BITS / 4)]);
+                    const f16x8 codes = key_codes_of<KEY_BITS, SPLIT == 2>(&b.key[t][s / K::kPieceSteps][s % K::kPieceSteps * (KEY_BITS / 4)]);
 #pragma unroll
                     for (int h = 0; h < SPLIT; ++h) x[t] = multiply(codes, q[h][s], x[t]);
                 }
@@ -519,22 +530,25 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
             }
             settled(c.middle);
             f16x8 p[SPLIT][K::kTiles / 2];
+            float block_sum = 0.0f, block_middle = 0.0f;   // of the block first: one sum over thousands of keys would gather their roundings
             each<K::kTiles>([&](auto t) {
                 each<4>([&](auto e) {
                     constexpr int i = e, kAt = kDppBroadcast + 4 * t + i;
                     const float v = __builtin_amdgcn_exp2f(x[t][i] - m);
-                    sum += v;
+                    block_sum += v;
                     const float weight = dpp<kAt>(c.step) * v;
-                    middle = add_broadcast<4 * t + i>(middle, c.middle, v, weight);
+                    block_middle = add_broadcast<4 * t + i>(block_middle, c.middle, v, weight);
                     const _Float16 high = static_cast<_Float16>(weight);
                     p[0][t / 2][4 * (t % 2) + i] = high;
                     if (SPLIT == 2) p[SPLIT - 1][t / 2][4 * (t % 2) + i] = static_cast<_Float16>(weight - static_cast<float>(high));
                 });
             });
+            sum += block_sum;
+            middle += block_middle;
+            if (SPLIT == 1) {
 #pragma unroll
-            for (int s = 0; s < K::kTiles / 2; ++s)
-#pragma unroll
-                for (int h = 0; h < SPLIT; ++h) weights = multiply(ones, p[h][s], weights);
+                for (int s = 0; s < K::kTiles / 2; ++s) weights = multiply(ones, p[0][s], weights);
+            }
 #pragma unroll
             for (int s = 0; s < K::kTiles / 2; ++s)
                 each<K::kColumns>([&](auto i) {
@@ -542,7 +556,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const uint32_t (&key)[4][K::kValueWords] = b.value[2 * s + k / 2];
-                        const f16x2 pair = __builtin_bit_cast(f16x2, raw_pair<VALUE_BITS, i>(key[2 * (k % 2)], key[2 * (k % 2) + 1]));
+                        const uint32_t *const low = key[2 * (k % 2)], *const high = key[2 * (k % 2) + 1];
+                        const f16x2 pair = SPLIT == 2 ? value_pair<VALUE_BITS, i>(low, high) : __builtin_bit_cast(f16x2, raw_pair<VALUE_BITS, i>(low, high));
                         values[2 * k] = pair[0];
                         values[2 * k + 1] = pair[1];
                     }
@@ -588,8 +603,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
         for (int i = 0; i < K::kColumns; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int unit = VALUE_BITS == 4 && i % 2 ? 20 : 24;
-                const float centered = fmaf(weights[0], VALUE_BITS == 8 ? -128.0f / (1 << 24) : -8.0f / (1 << unit), acc[i][r]);
+                const int unit = SPLIT == 2 ? kUnitBits : VALUE_BITS == 4 && i % 2 ? 20 : 24;
+                const float centered = SPLIT == 2 ? acc[i][r] : fmaf(weights[0], (VALUE_BITS == 8 ? -128.0f : -8.0f) / (1 << unit), acc[i][r]);
                 acc[i][r] = (ldexpf(centered, E + unit - kStepBits) + middle) * share;
             }
 #pragma unroll
@@ -607,6 +622,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
 #pragma unroll
                     for (int r = 0; r < 4; ++r) acc[i][r] += joined_out[wave][i][r][place];
             }
+            __syncthreads();   // read before the next step writes there
         }
         if (wave == 0 && there) {
             const float scale = is(total, 0.0f) ? 0.0f : 1.0f / total;   // nothing in sight: zeros
@@ -619,9 +635,8 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
                 if (a.partial) store_some(a.partial, ACTQ_F32, part_row_of(a, w, token, head) * DIM + at, f);
                 else store_some(a.out.p, a.dtype, (static_cast<int64_t>(w.start) + token) * a.out.token + head * a.out.head + at, f);
             }
-            if (a.partial && g == 0) a.partial_lse[part_row_of(a, w, token, head)] = is(total, 0.0f) ? kNothing : top + __builtin_amdgcn_logf(total);
+            if (a.partial && g == 0) a.partial_sums[part_row_of(a, w, token, head)] = f32x2{top, total};
         }
-        __syncthreads();   // the next tile writes the LDS again
     }
 }
 
@@ -700,7 +715,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
         if (a.partial && span.begin >= span.end) {   // a part beyond a short sequence's end
             for (int r = threadIdx.x; r < K::kRows && K::kRows * tile + r < w.rows; r += K::kThreads) {
                 const int32_t token = static_cast<int32_t>(divide(K::kRows * tile + r, a.by_group));
-                a.partial_lse[part_row_of(a, w, token, w.head * a.group + K::kRows * tile + r - token * a.group)] = kNothing;
+                a.partial_sums[part_row_of(a, w, token, w.head * a.group + K::kRows * tile + r - token * a.group)] = f32x2{kNothing, 0.0f};
             }
             continue;
         }
@@ -809,7 +824,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
                     load_eight(a.q.p, a.dtype, at(r, s), f);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const float v = ldexpf(a.key_bits == 8 ? f[j] : f[code_order(4, j)], 14 - q_exponent - (a.key_bits == 8 ? 0 : code_bits(4, j)));
+                        const float v = ldexpf(a.key_bits == 8 ? f[j] : f[code_order(4, j)], 14 - q_exponent - (a.key_bits == 8 || SPLIT == 2 ? 0 : code_bits(4, j)));
                         q[r][0][s][j] = static_cast<_Float16>(v);
                         if (SPLIT == 2) q[r][SPLIT - 1][s][j] = static_cast<_Float16>(v - static_cast<float>(q[r][0][s][j]));
                     }
@@ -844,8 +859,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
                 constexpr int kBits = decltype(bits)::value;
 #pragma unroll
                 for (int u = 0; u < K::kKeyUnits; ++u) {
-                    *reinterpret_cast<f16x8*>(&keys[to][K::key_place(key_of(u), chunk_of(u))]) = key_codes_of<kBits>(codes + 4 * u);
-                    *reinterpret_cast<f16x8*>(&keys[to][K::key_place(key_of(u), chunk_of(u) + DIM / 16)]) = key_codes_of<kBits>(codes + 4 * u + kBits / 4);
+                    *reinterpret_cast<f16x8*>(&keys[to][K::key_place(key_of(u), chunk_of(u))]) = key_codes_of<kBits, SPLIT == 2>(codes + 4 * u);
+                    *reinterpret_cast<f16x8*>(&keys[to][K::key_place(key_of(u), chunk_of(u) + DIM / 16)]) = key_codes_of<kBits, SPLIT == 2>(codes + 4 * u + kBits / 4);
                 }
             };
             if (of_values) a.value_bits == 8 ? store_values(eight) : store_values(four);
@@ -864,7 +879,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
 #pragma unroll
                 for (int o = 0; o < K::kOwn; ++o)
                     if (lane + 64 * o < K::kTile)
-                        constants[to][lane + 64 * o] = constants_of(key_header[o], f32x2{value_header[o][0], step[o]}, a, q_exponent, running, a.value_bits);
+                        constants[to][lane + 64 * o] = constants_of<SPLIT == 2>(key_header[o], f32x2{value_header[o][0], step[o]}, a, q_exponent, running, a.key_bits, a.value_bits);
                 if (lane == 0) exponents[to] = running;
             }
         };
@@ -970,16 +985,19 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
 #pragma unroll
             for (int r = 0; r < SETS; ++r) {
                 f16x8 p[SPLIT][2];
+                float part_sum = 0.0f, part_middle = 0.0f;   // of the part first: one sum over thousands of keys would gather their roundings
                 each<16>([&](auto e) {
                     constexpr int i = e, kAt = kDppBroadcast + i;
                     const float v = __builtin_amdgcn_exp2f(x[r][i] - m[r]);
-                    sum[r] += v;
+                    part_sum += v;
                     const float weight = dpp<kAt>(c.step) * v;
-                    middle[r] = add_broadcast<i>(middle[r], c.middle, v, weight);
+                    part_middle = add_broadcast<i>(part_middle, c.middle, v, weight);
                     const _Float16 high = static_cast<_Float16>(weight);
                     p[0][i / 8][i % 8] = high;
                     if (SPLIT == 2) p[SPLIT - 1][i / 8][i % 8] = static_cast<_Float16>(weight - static_cast<float>(high));
                 });
+                sum[r] += part_sum;
+                middle[r] += part_middle;
 #pragma unroll
                 for (int b = 0; b < K::kBlocks; ++b)
 #pragma unroll
@@ -1035,14 +1053,15 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
                     if (a.partial) store_some(a.partial, ACTQ_F32, part_row * DIM + column, f);
                     else store_some(a.out.p, a.dtype, (static_cast<int64_t>(w.start) + token) * a.out.token + head * a.out.head + column, f);
                 }
-            if (a.partial && h == 0) a.partial_lse[part_row] = is(sum[r], 0.0f) ? kNothing : m[r] + __builtin_amdgcn_logf(sum[r]);
+            if (a.partial && h == 0) a.partial_sums[part_row] = f32x2{m[r], sum[r]};
         }
+        __syncthreads();   // the next tile writes the LDS again
     }
 }
 
 // ----------------------------------------------------------------------------- joining parts
 
-// A workgroup per row: the parts' outputs weighted by 2^(lse - largest).  DIM / 4 threads take a part, four columns each, the others the
+// A workgroup per row: the parts' outputs weighted by their sums at the largest maximum.  DIM / 4 threads take a part, four columns each, the others the
 // next ones, with four parts' loads in flight; their sums meet in the LDS.  In a loop of one wavefront a part costs a trip to memory, 1.2 us.
 constexpr int kJoinThreads = 256;
 constexpr int kMostParts = 128;
@@ -1062,8 +1081,8 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a)
     const int64_t row = SHARED ? static_cast<int64_t>(blockIdx.x) : static_cast<int64_t>(blockIdx.x) * kTeams + team;
     const bool there = row < rows;
     const int own = SHARED ? static_cast<int>(threadIdx.x) : column;   // the part whose weight the thread works out
-    const float lse = there && own < parts ? a.partial_lse[own * rows + row] : kNothing;
-    float top = SHARED ? wave_max(lse) : over_lanes<16>(lse, [](float x, float y) { return fmaxf(x, y); });   // the first 16 threads of a team
+    const f32x2 none = {kNothing, 0.0f}, part = there && own < parts ? a.partial_sums[own * rows + row] : none;
+    float top = SHARED ? wave_max(part[0]) : over_lanes<16>(part[0], [](float x, float y) { return fmaxf(x, y); });   // the first 16 threads of a team
     if (SHARED) {
         if (threadIdx.x % 64 == 0) tops[threadIdx.x / 64] = top;
         __syncthreads();
@@ -1072,7 +1091,7 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a)
         for (int k = 1; k < kJoinThreads / 64; ++k) top = fmaxf(top, tops[k]);
     }
     float* const mine = weights[SHARED ? 0 : team];
-    if (own < parts) mine[own] = is(lse, kNothing) ? 0.0f : __builtin_amdgcn_exp2f(lse - top);
+    if (own < parts) mine[own] = part[1] * __builtin_amdgcn_exp2f(part[0] - top);
     __syncthreads();
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int p = SHARED ? team : 0; there && p < parts; p += kStride * kAhead) {
@@ -1156,7 +1175,7 @@ uint64_t cache_attention_workspace(const actq_cache* c, int32_t heads, int64_t t
 {
     if (tokens == 0 || sequences == 0) return 0;
     const Shape s = shape_of(c, heads, sequences, max_query, max_length, window);
-    return s.parts == 1 ? 0 : static_cast<uint64_t>(s.parts) * tokens * heads * (c->dim + 1) * sizeof(float);
+    return s.parts == 1 ? 0 : static_cast<uint64_t>(s.parts) * tokens * heads * (c->dim + 2) * sizeof(float);
 }
 
 int launch_cache_attention(const actq_cache* c, const actq_heads* q, int dtype, int64_t tokens, int64_t sequences, const int32_t* table, int32_t table_width,
@@ -1198,7 +1217,7 @@ int launch_cache_attention(const actq_cache* c, const actq_heads* q, int dtype, 
     a.per_part = static_cast<int32_t>(shape.per_part);
     if (shape.parts > 1) {
         a.partial = static_cast<float*>(workspace);
-        a.partial_lse = a.partial + shape.parts * tokens * q->heads * c->dim;
+        a.partial_sums = reinterpret_cast<f32x2*>(a.partial + shape.parts * tokens * q->heads * c->dim);
     }
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const unsigned blocks = static_cast<unsigned>(sequences * c->heads * shape.parts * shape.tiles);

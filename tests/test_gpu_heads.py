@@ -372,6 +372,18 @@ def test_attention_is_the_same_every_time_and_in_a_graph():
     assert torch.equal(B.cache_attention(*args, 1, 3000), eager)
 
 
+@pytest.mark.parametrize("new, length, sequences", [(1, 6000, 24), (40, 1500, 6)])
+def test_attention_of_many_workgroups_is_the_same_every_time(new, length, sequences):
+    """Workgroups that share a compute unit run at different paces: what they exchange inside must not depend on it."""
+    lengths = [length - 137 * i for i in range(sequences)]
+    case = _attention_case(lengths, [new] * sequences, 32, 8, 128, F16, 4, 4, 64, seed=19)
+    cache, table, lengths, start, q = case
+    args = [q.to(DEV), *cache, table.to(DEV), lengths.to(DEV), start.to(DEV), new, length]
+    first = B.cache_attention(*args)
+    for _ in range(8):
+        assert torch.equal(B.cache_attention(*args), first)
+
+
 def test_attention_without_tokens_or_sequences():
     cache, table, lengths, start, q = _attention_case([30], [3], 4, 2, 64, F16, 8, 8, 16, seed=17)
     args = (table.to(DEV), lengths.to(DEV), start.to(DEV), 3, 30)

@@ -80,7 +80,7 @@ def test_cache_refusals():
     assert L.actq_cache_attention(*none) == B.ACTQ_OK
     size = ctypes.c_uint64(7)
     assert L.actq_cache_attention_workspace(_cache(), 8, 3, 3, 1, 100, 0, ctypes.addressof(size)) == 0 and size.value == 0   # one part
-    assert L.actq_cache_attention_workspace(_cache(), 8, 3, 3, 1, 5000, 0, ctypes.addressof(size)) == 0 and size.value % (3 * 8 * 129 * 4) == 0 and size.value > 0
+    assert L.actq_cache_attention_workspace(_cache(), 8, 3, 3, 1, 5000, 0, ctypes.addressof(size)) == 0 and size.value % (3 * 8 * 130 * 4) == 0 and size.value > 0
     assert L.actq_cache_attention_workspace(_cache(), 8, 3, 3, 1, 5000, 0, None) == E
 
 
