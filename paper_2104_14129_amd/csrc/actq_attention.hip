@@ -15,6 +15,14 @@
 // probabilities are already laid out as the right operand of the second product, whose keys come in the same order.  A group's
 // constants lie in the lanes of the 16-lane row that needs them and are broadcast by the instruction that uses them (DPP).
 // The running maximum m moves only when a score passes it by 8 (p <= 2^8 then), so that sums are rarely rescaled.
+//
+// Where there are few rows the keys are cut into parts, whose outputs a second kernel joins.
+//
+// Measured on one MI355X (a large library product 1.1 PFLOP/s, a copy 5.2 TB/s).  Few rows are bound by memory where all compute units
+// have work: 64 sequences of 8192 tokens, 32 heads over 8 of 128, 8 bits 197 us (5.8 TB/s), 4 bits 121 us (5.0); 32 sequences of lengths up to
+// 16384 (4 bits) 78 + 5 us (4.0), the longest ones' workgroups being the last.  Many rows are bound by vector instructions and products that
+// hardly overlap (some 4150 of the 6200 cycles of a 64-key tile are vector instructions, of which a score costs 9): 2048 tokens over 32768, 8 bits, bfloat16
+// 1.35 ms (790 TFLOP/s).  The error against 64 bits is that of binary32 operations rounded once.
 #include "actq_heads.h"
 
 namespace actq {
@@ -308,8 +316,9 @@ __device__ __forceinline__ f32x4 constants_of(f32x2 key_header, f32x2 value_head
 // Sixteen rows, whose keys four wavefronts share out in turn, blocks of 16 * TILES keys each.  Codes go from memory to the matrix
 // instructions without the LDS: of a 16-key tile a lane loads its own pieces of one key, and for the values its own columns of eight
 // keys, which it transposes itself as it widens them.  The next block's codes are loaded while one is computed.
-constexpr int kFewWaves = 4;
+constexpr int kFewWaves = 4;   // [8, which need no join up to 1024 keys: one token over 1021 11.0 -> 12.4 us]
 
+// SPLIT: binary16 numbers for one of q and of the weights, 1 for 16-bit types, 2 for binary32.
 template <int DIM, int SPLIT, int KEY_BITS, int VALUE_BITS>
 struct Few {
     static constexpr int kTiles = DIM == 256 ? 2 : 4, kBlock = 16 * kTiles;
@@ -1137,7 +1146,8 @@ struct Shape {
     int64_t tiles, parts, per_part;
 };
 
-// Rows of a sequence and head of the cache from which on the kernel for many rows serves.
+// Rows of a sequence and head of the cache from which on the kernel for many rows serves: four tiles of 16 rows would each read and widen the
+// same keys.
 constexpr int64_t kManyRows = 64;
 
 Shape shape_of(const actq_cache* c, int32_t heads, int64_t sequences, int64_t max_query, int64_t max_length, int32_t window)
