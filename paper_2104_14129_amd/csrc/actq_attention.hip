@@ -82,7 +82,7 @@ __device__ __forceinline__ Work work_of(const AttendArgs& a, uint32_t id)
     w.head = static_cast<int32_t>(by_part - w.sequence * a.kv_heads);
     const int32_t start = a.query_start[w.sequence], end = a.query_start[w.sequence + 1];
     w.start = min(max(start, 0), a.tokens);
-    const int32_t count = max(min(end, a.tokens) - w.start, 0);
+    const int32_t count = min(max(end, w.start), a.tokens) - w.start;
     w.rows = count * a.group;
     w.length = static_cast<int32_t>(min(static_cast<int64_t>(max(a.lengths[w.sequence], 0)), static_cast<int64_t>(a.table_width) << a.page_shift));
     w.first = w.length - count;
