@@ -1146,15 +1146,19 @@ struct Shape {
     int64_t tiles, parts, per_part;
 };
 
-// Rows of a sequence and head of the cache from which on the kernel for many rows serves: four tiles of 16 rows would each read and widen the
-// same keys.
-constexpr int64_t kManyRows = 64;
+// Rows of a sequence and head of the cache from which on the kernel for many rows serves.  Below, tiles of 16 rows read and widen the same keys
+// again, but a workgroup begins sooner.  Few rows -> many rows, us, 8 bits, 32 heads over 8:
+//   16 sequences of 4096, 128, bfloat16   64 rows 87 -> 112, 96 rows 123 -> 115, 128 rows 167 -> 119
+//   one of 8192, 128, bfloat16            64 rows 23 -> 28, 96 rows 29 -> 31, 128 rows 32 -> 34
+//   16 of 4096, 64, binary32              64 rows 51 -> 90, 96 rows 72 -> 92, 128 rows 92 -> 97, 256 rows 154 -> 117
+//   4 of 4096, 256, binary16              64 rows 73 -> 107, 128 rows 122 -> 132, 256 rows 167 -> 197 (there the many need scratch memory)
+constexpr int64_t kManyRows = 97, kManyRowsWide = 321;
 
 Shape shape_of(const actq_cache* c, int32_t heads, int64_t sequences, int64_t max_query, int64_t max_length, int32_t window)
 {
     const int64_t group = heads / c->heads, groups = sequences * c->heads, rows = max_query < 1 ? group : max_query * group;
     Shape s;
-    s.rows = rows < kManyRows ? 16 : rows <= 128 || c->dim == 256 ? 128 : 256;
+    s.rows = rows < (c->dim == 256 ? kManyRowsWide : kManyRows) ? 16 : rows <= 128 || c->dim == 256 ? 128 : 256;
     s.tiles = ceil_div(rows, s.rows);
     if (s.tiles > kMostBlocks / groups) s.tiles = kMostBlocks / groups;
     // keys of a step; the fewest that are worth a workgroup; workgroups that are wanted, as many as are resident: two per compute unit, one of 256

@@ -275,6 +275,16 @@ def test_attention_of_every_kind(key_bits, value_bits, dim, dtype, new):
     _check(case, dim, dtype, new, 333)
 
 
+@pytest.mark.parametrize("key_bits, value_bits", [(8, 8), (8, 4), (4, 8), (4, 4)])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("new, options", [(50, {}), (190, dict(window=70)), (190, dict(softcap=4.0))])
+def test_attention_of_every_kind_in_chunks(key_bits, value_bits, dim, dtype, new, options):
+    """100 and 380 rows for a head of the cache."""
+    case = _attention_case([420], [new], 2, 1, dim, dtype, key_bits, value_bits, 16, seed=dim + key_bits + new)
+    _check(case, dim, dtype, new, 420, **options)
+
+
 @pytest.mark.parametrize("max_query, max_length", [(1, 1), (7, 100), (1000, 30), (2, 1 << 20)])
 def test_attention_bounds_that_are_wrong_only_shape_the_launch(max_query, max_length):
     case = _attention_case([700, 33], [61, 2], 4, 2, 128, F16, 8, 8, 16, seed=9)
@@ -313,6 +323,20 @@ def test_attention_does_not_look_past_a_window():
         header[inside, :, : first % 64] = float("nan")
     args = (table.to(DEV), lengths.to(DEV), start.to(DEV), 40, 640)
     assert torch.equal(B.cache_attention(q.to(DEV), *cache, *args, window=50), clean)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_attention_of_earlier_tokens_of_a_chunk_does_not_depend_on_later_ones(dtype, bad):
+    """The same for 120 rows."""
+    cache, table, lengths, start, q = _attention_case([300], [60], 2, 1, 128, dtype, 8, 8, 16, seed=20)
+    args = (table.to(DEV), lengths.to(DEV), start.to(DEV), 60, 300)
+    clean = B.cache_attention(q.to(DEV), *cache, *args)
+    for at in (290, 296, 299):
+        for header in (cache[1], cache[3]):
+            header[table[0, at // 16].long(), :, at % 16] = bad
+    out = B.cache_attention(q.to(DEV), *cache, *args)
+    assert torch.equal(out[:50], clean[:50]) and not torch.isfinite(out[50:]).any()
 
 
 @pytest.mark.parametrize("dtype", [F32, F16])
