@@ -193,6 +193,14 @@ __device__ __forceinline__ uint32_t bits_of(float v)
     return b;
 }
 
+// A number as it was rounded, which the operations on it see and not what it was computed from: a conversion of a product to binary16
+// may become one instruction, which rounds once where a conversion of the rounded product rounds twice.
+__device__ __forceinline__ float rounded(float v)
+{
+    asm("" : "+v"(v));
+    return v;
+}
+
 // A number whose uses are computed where it is asked for: what is computed from a lane's number alone would otherwise be held in
 // registers from the kernel's begin on, through the loop over the keys.
 __device__ __forceinline__ int here(int v)
@@ -545,7 +553,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
                     constexpr int i = e, kAt = kDppBroadcast + 4 * t + i;
                     const float v = __builtin_amdgcn_exp2f(x[t][i] - m);
                     block_sum += v;
-                    const float weight = dpp<kAt>(c.step) * v;
+                    const float weight = SPLIT == 2 ? rounded(dpp<kAt>(c.step) * v) : dpp<kAt>(c.step) * v;   // the same one for both of its numbers
                     block_middle = add_broadcast<4 * t + i>(block_middle, c.middle, v, weight);
                     const _Float16 high = static_cast<_Float16>(weight);
                     p[0][t / 2][4 * (t % 2) + i] = high;
@@ -999,7 +1007,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
                     constexpr int i = e, kAt = kDppBroadcast + i;
                     const float v = __builtin_amdgcn_exp2f(x[r][i] - m[r]);
                     part_sum += v;
-                    const float weight = dpp<kAt>(c.step) * v;
+                    const float weight = SPLIT == 2 ? rounded(dpp<kAt>(c.step) * v) : dpp<kAt>(c.step) * v;   // the same one for both of its numbers
                     part_middle = add_broadcast<i>(part_middle, c.middle, v, weight);
                     const _Float16 high = static_cast<_Float16>(weight);
                     p[0][i / 8][i % 8] = high;

@@ -1,0 +1,60 @@
+"""Every row of the attention by itself: against its own bound, and unmoved by what other rows of a tile hold."""
+import numpy as np
+import pytest
+import torch
+
+import _attention_rows as R
+import _heads as H
+from paper_2104_14129_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+
+
+def _case(lengths, news, q_heads, kv, dim, dtype, key_bits=8, value_bits=8, page=16, seed=0):
+    """Sequences whose pages lie anywhere, garbage with NaN headers in the slots that hold no token."""
+    per = (max(lengths) + page - 1) // page
+    pages = len(lengths) * per + 2
+    cache = H.make_cache(pages, kv, page, dim, key_bits, value_bits, seed)
+    g = torch.Generator().manual_seed(seed + 1)
+    table = torch.randperm(pages, generator=g)[:len(lengths) * per].view(len(lengths), per).int()
+    for n, length in enumerate(lengths):
+        j = torch.arange(length)
+        k, v = (torch.randn((length, kv, dim), generator=g) for _ in range(2))
+        H.fill(cache, (table[n].long()[j // page] * page + j % page).to(DEV), k + 1.5 * torch.randn((1, kv, dim), generator=g), v, key_bits, value_bits)
+    start = torch.tensor([0] + list(np.cumsum(news)), dtype=torch.int32)
+    return torch.randn((int(start[-1]), q_heads, dim), generator=g).to(dtype), cache, table, torch.tensor(lengths, dtype=torch.int32), start, dim
+
+
+def _attend(case, **options):
+    q, cache, table, lengths, start, _ = case
+    return B.cache_attention(q.to(DEV), *cache, table.to(DEV), lengths.to(DEV), start.to(DEV), int(start.diff().max()), int(lengths.max()), **options)
+
+
+def _within(out, case, **options):
+    want, bound = R.attention(*case, **options)
+    off = np.abs(out.cpu().double().numpy() - want)
+    assert (off <= bound).all(), float((off / np.maximum(bound, 1e-300)).max())
+
+
+SHAPES = [
+    # new tokens of 300, q heads, kv heads, dim, key bits, value bits: 6 rows, 80, and 104 and 300 for the kernel of many rows; heads of 256 in both
+    (3, 4, 2, 64, 8, 8), (40, 4, 2, 128, 4, 8), (52, 2, 1, 128, 8, 8), (150, 4, 2, 64, 8, 4), (5, 2, 1, 256, 8, 4), (170, 2, 1, 256, 4, 4),
+]
+
+
+@pytest.mark.parametrize("options", [{}, dict(softcap=5.0), dict(window=30)])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("at", range(len(SHAPES)))
+def test_rows_keep_to_their_own_bound(at, dtype, options):
+    new, q_heads, kv, dim, key_bits, value_bits = SHAPES[at]
+    case = _case([300], [new], q_heads, kv, dim, dtype, key_bits, value_bits, seed=at)
+    _within(_attend(case, **options), case, **options)
+
+
+@pytest.mark.parametrize("new", [1, 60])
+def test_binary32_is_held_in_two_numbers_of_binary16_in_every_row(new):
+    """Thousands of rows over few keys, where a single weight of which only one number counts shows."""
+    case = _case([64] * 24, [new] * 24, 4, 2, 64, F32, seed=60 + new)
+    _within(_attend(case), case)
