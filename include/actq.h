@@ -498,7 +498,8 @@ int actq_cache_read(const actq_cache* cache, const int64_t* slots, int64_t token
  * at offset j mod page_size.  Its new tokens are rows query_start[n] .. query_start[n + 1] - 1
  * of q, the last ones of the sequence: the last row is position lengths[n] - 1.  A row at
  * position i sees the positions j <= i, and with window > 0 only those with j > i - window.
- * A row that sees nothing (a position below zero) gives zeros.  Head h of q reads head
+ * A row that sees nothing (a position below zero) gives zeros, any other one whose q holds an
+ * infinity or NaN gives NaN.  No row depends on what another row of q holds.  Head h of q reads head
  * h div (heads / cache heads) of the cache.
  *
  * The device arrays cannot be checked by the host: a length is cut to what the table

@@ -5,8 +5,11 @@
 // with k_j = Zk_j + step_j code_j and v_j likewise.  The codes stay whole numbers: as they are, a byte or a nibble under zeros, they
 // are subnormal binary16 numbers code * 2^-24, which the matrix instructions multiply exactly, so that
 //   q . k_j = step_j 2^24 (q . code_j 2^-24) + Zk_j sum(q)
-// has no rounding but that of its binary32 sum.  q is scaled by a power of two so that its largest element fills binary16's range
-// (exact for 16-bit types; binary32 takes two binary16 numbers, 22 bits).  The values' codes are centred, u_j = code_j - c, and
+// has no rounding but that of its binary32 sum.  A row of q is scaled by a power of two of its own, so that its largest element fills
+// binary16's range: exact for 16-bit types but for elements below 2^-27 of the row's largest one (2^-23 beside keys of 4 bits), while binary32 takes two
+// binary16 numbers, 22 bits.  Its scores stay in the row's unit until the exponential, whose subtraction of m multiplies by the unit in the same
+// instruction.  What one row of q holds has so no part in another's; a row with an element that is no finite number is none.
+// The values' codes are centred, u_j = code_j - c, and
 //   sum_j p_j v_j = sum_j (p_j step_j) u_j + sum_j p_j (Zv_j + c step_j),
 // the second sum in binary32, one number per row.  p_j step_j is rounded to binary16 (to two of them for binary32 outputs) at a scale
 // 2^E of the largest step so far; centred codes keep that error at what rounding the values themselves would cost.
@@ -36,6 +39,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kSlack = 8.0f;         // by how much a score may pass the running maximum
 constexpr int kStepBits = 6;           // p * step is scaled to stay below 2^(kSlack + kStepBits + 1), inside binary16's range
 constexpr int kUnitBits = 9;           // centred codes are held as code * 2^-9
+constexpr float kMostCap = 1152921504606846976.0f;
+constexpr int kRowBits = 13;           // a row of q is scaled to a largest element of 2^13 to 2^14 (2^15 at the upper end of binary32's range)
 
 struct AttendArgs {
     const uint8_t* key_codes;
@@ -218,6 +223,22 @@ __device__ __forceinline__ float nan_where(bool bad)
 
 __device__ __forceinline__ int exponent(float v) { return static_cast<int>(bits_of(v) >> 23 & 255u) - 127; }
 
+// The magnitude of a value as a whole number, which orders infinities and NaN above all numbers.
+__device__ __forceinline__ uint32_t magnitude(float v) { return bits_of(v) & 0x7fffffffu; }
+
+// The row of q that a lane has a share of: the exponent of its largest element, and whether one is no finite number.
+struct RowScale {
+    int exponent;
+    bool bad;
+
+    __device__ __forceinline__ explicit RowScale(uint32_t largest)
+        : exponent(min(max(static_cast<int>(largest >> 23) - 127, -64), 126)), bad(largest >= 0x7f800000u) {}
+
+    // An element as it goes to the matrix instructions, zero in a row that is none.
+    __device__ __forceinline__ float scaled(float v) const { return bad ? 0.0f : ldexpf(v, kRowBits - exponent); }
+    __device__ __forceinline__ float unit() const { return ldexpf(1.0f, exponent); }
+};
+
 __device__ __forceinline__ bool finite(float v) { return exponent(v) != 128; }
 
 __device__ __forceinline__ bool is(float v, float constant) { return bits_of(v) == __builtin_bit_cast(uint32_t, constant); }
@@ -234,6 +255,13 @@ __device__ __forceinline__ float tanh_of(float x)
     if (FINE) return tanhf(x);
     const float e = __builtin_amdgcn_exp2f(x * (2.0f * kLog2e));
     return 1.0f - 2.0f * __builtin_amdgcn_rcpf(e + 1.0f);
+}
+
+// cap tanh(x / cap) of a score in units of a power of two, whose inverse is a matter of its exponent.
+template <bool FINE>
+__device__ __forceinline__ float capped(float x, float unit, float cap)
+{
+    return cap * __builtin_bit_cast(float, 0x7f000000u - __builtin_bit_cast(uint32_t, unit)) * tanh_of<FINE>(x * unit);
 }
 
 // f16 pair under zeros: byte B of `low` and of `high`.
@@ -303,7 +331,7 @@ __device__ __forceinline__ void each(F f)
 
 __device__ __forceinline__ f32x4 multiply(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// A group's constants, lane by lane: scores are key * (q . codes) + key_zero * sum(q); step and middle of the values.
+// A group's constants, lane by lane: scores are key * (q . codes) + key_zero * sum(q), in the row's unit; step and middle of the values.
 struct Constants {
     float key, key_zero, step, middle;
 };
@@ -311,11 +339,11 @@ struct Constants {
 // Constants of a key that some row sees, or (value header zero) of one that none does.  Where a value is no number, step is zero and
 // middle is none: nothing times an infinity is no number either, so rows that see the key are made none on their own.
 template <bool CENTERED>
-__device__ __forceinline__ f32x4 constants_of(f32x2 key_header, f32x2 value_header, const AttendArgs& a, int q_exponent, int E, int key_bits, int value_bits)
+__device__ __forceinline__ f32x4 constants_of(f32x2 key_header, f32x2 value_header, const AttendArgs& a, int E, int key_bits, int value_bits)
 {
     const float middle = fmaf(value_bits == 8 ? 128.0f : 8.0f, value_header[1], value_header[0]);
     const float zero = CENTERED ? fmaf(key_bits == 8 ? 128.0f : 8.0f, key_header[1], key_header[0]) : key_header[0];
-    return f32x4{ldexpf(key_header[1] * a.factor, (CENTERED ? kUnitBits : 24) - 14 + q_exponent), zero * a.factor,
+    return f32x4{key_header[1] * a.factor * (CENTERED ? 1.0f / (1 << (kRowBits - kUnitBits)) : 1 << (24 - kRowBits)), zero * a.factor,
                  finite(middle) ? ldexpf(value_header[1], kStepBits - E) : 0.0f, middle};
 }
 
@@ -430,35 +458,39 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
 
         // q, a lane's 8 elements of its row for every step
         f16x8 q[SPLIT][K::kSteps];
-        float q_sum = 0.0f;
-        int q_exponent;
+        float q_sum = 0.0f, unit, sum;
         {
             const int64_t at = (static_cast<int64_t>(w.start) + token) * a.q.token + head * a.q.head;
-            float f[K::kSteps][8], top = 0.0f;
+            float f[K::kSteps][8];
+            uint32_t largest = 0;
 #pragma unroll
             for (int s = 0; s < K::kSteps; ++s) {
                 const int piece = s / K::kPieceSteps, in_piece = s % K::kPieceSteps;
                 load_eight(a.q.p, a.dtype, at + (4 * piece + g) * (8 * K::kPieceSteps) + 8 * in_piece, f[s]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    top = fmaxf(top, fabsf(f[s][j]));
-                    q_sum += f[s][j];
-                }
+                for (int j = 0; j < 8; ++j) largest = max(largest, magnitude(f[s][j]));
             }
-            q_sum += __shfl_xor(q_sum, 16);
-            q_sum += __shfl_xor(q_sum, 32);
-            q_exponent = max(__builtin_amdgcn_readfirstlane(exponent(wave_max(top))), -100);
+            largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), 16)));
+            largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), 32)));
+            const RowScale row_scale(largest);
 #pragma unroll
             for (int s = 0; s < K::kSteps; ++s)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const float v = ldexpf(f[s][code_order(KEY_BITS, j)], 14 - q_exponent - (SPLIT == 2 ? 0 : code_bits(KEY_BITS, j)));
+                    const float whole = row_scale.scaled(f[s][code_order(KEY_BITS, j)]);
+                    q_sum += whole;
+                    const float v = ldexpf(whole, SPLIT == 2 ? 0 : -code_bits(KEY_BITS, j));
                     q[0][s][j] = static_cast<_Float16>(v);
                     if (SPLIT == 2) q[SPLIT - 1][s][j] = static_cast<_Float16>(v - static_cast<float>(q[0][s][j]));
                 }
+            q_sum += __shfl_xor(q_sum, 16);
+            q_sum += __shfl_xor(q_sum, 32);
+            q_sum *= 1.0f / (1 << kRowBits);
+            unit = row_scale.unit();
+            sum = nan_where(row_scale.bad && position >= 0);   // a row that sees something and is not finite
         }
 
-        float m = kNothing, sum = 0.0f, middle = 0.0f;
+        float m = kNothing, middle = 0.0f;
         int E = -126;
         f32x4 acc[K::kColumns];
 #pragma unroll
@@ -484,7 +516,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
                 weights[0] = ldexpf(weights[0], E - top);
                 E = top;
             }
-            const f32x4 four = constants_of<SPLIT == 2>(b.key_header, value_header, a, q_exponent, E, KEY_BITS, VALUE_BITS);
+            const f32x4 four = constants_of<SPLIT == 2>(b.key_header, value_header, a, E, KEY_BITS, VALUE_BITS);
             Constants c = {four[0], four[1], four[2], four[3]};
             settled(c.key_zero);
             f32x4 x[K::kTiles];
@@ -509,7 +541,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
 #pragma unroll
                 for (int t = 0; t < K::kTiles; ++t)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[t][i] = a.cap * tanh_of<SPLIT == 2>(x[t][i]);
+                    for (int i = 0; i < 4; ++i) x[t][i] = capped<SPLIT == 2>(x[t][i], unit, a.cap);
             }
             // f(tile, i, whether the row sees key i of it): key = base + 4 g + a constant, between the window's begin and the last one in sight
             const auto each_key = [&](auto f) {
@@ -526,6 +558,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
             for (int t = 0; t < K::kTiles; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, x[t][i]);
+            top *= unit;
             if (__any(top > m + kSlack)) {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
@@ -551,7 +584,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
             each<K::kTiles>([&](auto t) {
                 each<4>([&](auto e) {
                     constexpr int i = e, kAt = kDppBroadcast + 4 * t + i;
-                    const float v = __builtin_amdgcn_exp2f(x[t][i] - m);
+                    const float v = __builtin_amdgcn_exp2f(fmaf(x[t][i], unit, -m));
                     block_sum += v;
                     const float weight = SPLIT == 2 ? rounded(dpp<kAt>(c.step) * v) : dpp<kAt>(c.step) * v;   // the same one for both of its numbers
                     block_middle = add_broadcast<4 * t + i>(block_middle, c.middle, v, weight);
@@ -698,7 +731,6 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
     __shared__ __attribute__((aligned(16))) uint8_t values[2][16384];
     __shared__ f32x4 constants[2][K::kTile];   // as in Constants
     __shared__ int exponents[2];
-    __shared__ float tops[WAVES];
 
     const Work w = work_of(a, blockIdx.x);
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -802,59 +834,55 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
 
         // q, a lane's 8 elements of its rows for every step
         f16x8 q[SETS][SPLIT][K::kSteps];
-        float q_sum[SETS];
-        int q_exponent;
+        float q_sum[SETS], unit[SETS], sum[SETS];
         {
             // element of q in slot 0 of a step: the order of the chunks in the LDS
             const auto at = [&](int r, int s) {
                 const int chunk = 2 * s + h;
                 return (static_cast<int64_t>(w.start) + token_at(r)) * a.q.token + head_at(r) * a.q.head + (chunk < DIM / 16 ? 16 * chunk : 16 * chunk - DIM + 8);
             };
-            float top = 0.0f;
 #pragma unroll
             for (int r = 0; r < SETS; ++r) {
-                q_sum[r] = 0.0f;
+                uint32_t largest = 0;
 #pragma unroll
                 for (int s = 0; s < K::kSteps; ++s) {
                     float f[8];
                     load_eight(a.q.p, a.dtype, at(r, s), f);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        top = fmaxf(top, fabsf(f[j]));
-                        q_sum[r] += f[j];
-                    }
+                    for (int j = 0; j < 8; ++j) largest = max(largest, magnitude(f[j]));
                 }
-                q_sum[r] += __shfl_xor(q_sum[r], 32);
-            }
-            top = wave_max(top);
-            if (lane == 0) tops[wave] = top;
-            __syncthreads();
-#pragma unroll
-            for (int k = 0; k < WAVES; ++k) top = fmaxf(top, tops[k]);
-            q_exponent = max(__builtin_amdgcn_readfirstlane(exponent(top)), -100);
-            // once more, from the cache: held until here they would be twice the registers of everything else
-#pragma unroll
-            for (int r = 0; r < SETS; ++r)
+                largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), 32)));
+                const RowScale row_scale(largest);
+                q_sum[r] = 0.0f;
+                // once more, from the cache: held until here they would be twice the registers of everything else
 #pragma unroll
                 for (int s = 0; s < K::kSteps; ++s) {
                     float f[8];
                     load_eight(a.q.p, a.dtype, at(r, s), f);
 #pragma unroll
+                    for (int j = 0; j < 8; ++j) f[j] = row_scale.scaled(f[j]);
+#pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const float v = ldexpf(a.key_bits == 8 ? f[j] : f[code_order(4, j)], 14 - q_exponent - (a.key_bits == 8 || SPLIT == 2 ? 0 : code_bits(4, j)));
+                        q_sum[r] += f[j];
+                        const float v = ldexpf(a.key_bits == 8 ? f[j] : f[code_order(4, j)], a.key_bits == 8 || SPLIT == 2 ? 0 : -code_bits(4, j));
                         q[r][0][s][j] = static_cast<_Float16>(v);
                         if (SPLIT == 2) q[r][SPLIT - 1][s][j] = static_cast<_Float16>(v - static_cast<float>(q[r][0][s][j]));
                     }
                 }
+                q_sum[r] += __shfl_xor(q_sum[r], 32);
+                q_sum[r] *= 1.0f / (1 << kRowBits);
+                unit[r] = row_scale.unit();
+                sum[r] = nan_where(row_scale.bad && w.first + token_at(r) >= 0);   // a row that sees something and is not finite
+            }
         }
 
-        float m[SETS], sum[SETS], middle[SETS];
+        float m[SETS], middle[SETS];
         int E = -126, running = -126;   // of the sums; of the tiles prepared so far
         f32x16 acc[SETS][K::kBlocks];
 #pragma unroll
         for (int r = 0; r < SETS; ++r) {
             m[r] = kNothing;
-            sum[r] = middle[r] = 0.0f;
+            middle[r] = 0.0f;
 #pragma unroll
             for (int b = 0; b < K::kBlocks; ++b) acc[r][b] = f32x16{};
         }
@@ -896,7 +924,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
 #pragma unroll
                 for (int o = 0; o < K::kOwn; ++o)
                     if (lane + 64 * o < K::kTile)
-                        constants[to][lane + 64 * o] = constants_of<SPLIT == 2>(key_header[o], f32x2{value_header[o][0], step[o]}, a, q_exponent, running, a.key_bits, a.value_bits);
+                        constants[to][lane + 64 * o] = constants_of<SPLIT == 2>(key_header[o], f32x2{value_header[o][0], step[o]}, a, running, a.key_bits, a.value_bits);
                 if (lane == 0) exponents[to] = running;
             }
         };
@@ -947,7 +975,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
 #pragma unroll
                 for (int r = 0; r < SETS; ++r)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) x[r][i] = a.cap * tanh_of<SPLIT == 2>(x[r][i]);
+                    for (int i = 0; i < 16; ++i) x[r][i] = capped<SPLIT == 2>(x[r][i], unit[r], a.cap);
             }
             // f(i, whether the row sees key i): key = base + 4 h + a constant, between the window's begin and the last one in sight
             const auto each_key = [&](int r, auto f) {
@@ -973,6 +1001,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
                 top[r] = kNothing;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top[r] = fmaxf(top[r], x[r][i]);
+                top[r] *= unit[r];
                 over |= top[r] > m[r] + kSlack;
             }
             if (__any(over)) {
@@ -1005,7 +1034,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
                 float part_sum = 0.0f, part_middle = 0.0f;   // of the part first: one sum over thousands of keys would gather their roundings
                 each<16>([&](auto e) {
                     constexpr int i = e, kAt = kDppBroadcast + i;
-                    const float v = __builtin_amdgcn_exp2f(x[r][i] - m[r]);
+                    const float v = __builtin_amdgcn_exp2f(fmaf(x[r][i], unit[r], -m[r]));
                     part_sum += v;
                     const float weight = SPLIT == 2 ? rounded(dpp<kAt>(c.step) * v) : dpp<kAt>(c.step) * v;   // the same one for both of its numbers
                     part_middle = add_broadcast<i>(part_middle, c.middle, v, weight);
@@ -1228,8 +1257,10 @@ int launch_cache_attention(const actq_cache* c, const actq_heads* q, int dtype, 
     a.table_width = table_width;
     a.lengths = lengths;
     a.query_start = query_start;
-    a.factor = softcap > 0.0f ? scale / softcap : scale * kLog2e;
-    a.cap = softcap * kLog2e;
+    // A cap beyond 2^60 would overflow in the unit of a row of the smallest elements; any such one leaves the scores below it as they are.
+    const float cap = softcap < kMostCap ? softcap : kMostCap;
+    a.factor = cap > 0.0f ? scale / cap : scale * kLog2e;
+    a.cap = cap * kLog2e;
     a.window = window;
     a.tiles = static_cast<uint32_t>(shape.tiles);
     a.parts = static_cast<uint32_t>(shape.parts);

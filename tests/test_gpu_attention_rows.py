@@ -58,3 +58,42 @@ def test_binary32_is_held_in_two_numbers_of_binary16_in_every_row(new):
     """Thousands of rows over few keys, where a single weight of which only one number counts shows."""
     case = _case([64] * 24, [new] * 24, 4, 2, 64, F32, seed=60 + new)
     _within(_attend(case), case)
+
+
+@pytest.mark.parametrize("options", [{}, dict(softcap=5.0), dict(window=30)])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("at", range(len(SHAPES)))
+def test_a_row_of_q_that_is_not_finite_or_large_leaves_the_others_as_they_were(at, dtype, options):
+    """One element of one token's head: the row itself is NaN where it is no finite number, every other row is what it was, bit for bit."""
+    new, q_heads, kv, dim, key_bits, value_bits = SHAPES[at]
+    case = _case([300], [new], q_heads, kv, dim, dtype, key_bits, value_bits, seed=at)
+    clean = _attend(case, **options)
+    q = case[0]
+    for token, head, element, value in ((new - 1, 0, 5, float("inf")), (new // 2, q_heads - 1, dim - 1, float("-inf")), (0, 1, 0, float("nan")), (new - 1, q_heads - 1, 3, 2.0 ** (15 if dtype == F16 else 40))):
+        changed = q.clone()
+        changed[token, head, element] = value
+        out = _attend((changed, *case[1:]), **options)
+        if np.isfinite(value):
+            assert torch.isfinite(out[token, head]).all()
+        else:
+            assert torch.isnan(out[token, head]).all()
+        out[token, head] = clean[token, head]
+        assert torch.equal(out, clean), (token, head, value)
+
+
+@pytest.mark.parametrize("new", [2, 60])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_rows_of_very_different_sizes(new, dtype):
+    """Rows of 2^-30 to 2^3 and zeros side by side: each keeps to its own bound."""
+    q, *rest = case = _case([200], [new], 4, 2, 64, dtype, seed=40)
+    sizes = torch.tensor([2.0 ** -30, 1.0, 0.0, 8.0, 2.0 ** -12]).repeat(q.shape[0] * 4)[:q.shape[0] * 4].view(q.shape[0], 4, 1)
+    case = ((q.float() * sizes).to(dtype), *rest)
+    for options in ({}, dict(softcap=3.0)):
+        _within(_attend(case, **options), case, **options)
+
+
+def test_rows_before_the_first_position_are_zeros_whatever_they_hold():
+    q, *rest = _case([3], [5], 2, 1, 64, F16, seed=41)
+    q[0] = float("inf")
+    q[1] = float("nan")
+    assert (_attend((q, *rest))[:2] == 0).all()
