@@ -11,13 +11,16 @@
 // instruction.  What one row of q holds has so no part in another's; a row with an element that is no finite number is none.
 // The values' codes are centred, u_j = code_j - c, and
 //   sum_j p_j v_j = sum_j (p_j step_j) u_j + sum_j p_j (Zv_j + c step_j),
-// the second sum in binary32, one number per row.  p_j step_j is rounded to binary16 (to two of them for binary32 outputs) at a scale
-// 2^E of the largest step so far; centred codes keep that error at what rounding the values themselves would cost.
+// the second sum in binary32, one number per row.  p_j step_j is rounded to binary16 (to two of them for binary32 outputs); centred codes keep
+// that error at what rounding the values themselves would cost.  So that it fits, m is the row's running maximum not of x_j but of
+// x_j + log2(step_j), or log2 of a 128th of the value's middle where that is more (its sum then stays in range, and the step's share of the
+// result is the smaller): what a row does not see, or hardly weighs, takes no bits from what it does.
 //
 // Scores are computed transposed, keys by rows: a lane holds keys of one row, so that maximum and sum are per lane, and the
 // probabilities are already laid out as the right operand of the second product, whose keys come in the same order.  A group's
 // constants lie in the lanes of the 16-lane row that needs them and are broadcast by the instruction that uses them (DPP).
-// The running maximum m moves only when a score passes it by 8 (p <= 2^8 then), so that sums are rarely rescaled.
+// m moves only when a row's p_j step_j would pass 2^15, and then to where it is 2^7, so that sums are rarely rescaled.  Whether it has to is asked of the
+// largest score and the largest step of a block of keys; only where those two together would pass is it worked out key by key.
 //
 // Where there are few rows the keys are cut into parts, whose outputs a second kernel joins.
 //
@@ -36,8 +39,8 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr float kNothing = -3.0e38f;   // running maximum of a row that has seen no key
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kSlack = 8.0f;         // by how much a score may pass the running maximum
-constexpr int kStepBits = 6;           // p * step is scaled to stay below 2^(kSlack + kStepBits + 1), inside binary16's range
+constexpr float kMostWeight = 15.0f;   // p * step stays below 2^kMostWeight, inside binary16's range,
+constexpr float kNewWeight = 7.0f;     // and below 2^kNewWeight where the running maximum has just moved
 constexpr int kUnitBits = 9;           // centred codes are held as code * 2^-9
 constexpr float kMostCap = 1152921504606846976.0f;
 constexpr int kRowBits = 13;           // a row of q is scaled to a largest element of 2^13 to 2^14 (2^15 at the upper end of binary32's range)
@@ -62,6 +65,7 @@ struct AttendArgs {
     float factor;               // scale * log2(e); with a cap scale / cap
     float cap;                  // softcap * log2(e); 0: none
     int32_t window;             // 0: none
+    float least;                // log2 of the step that smaller ones count as, so that the sum of p stays inside binary32's range
     uint32_t tiles, parts;      // row tiles of the grid, parts of the keys
     FastDiv by_tiles, by_parts, by_heads;
     int32_t per_part;           // keys of a part, a multiple of the kernels' block of keys
@@ -339,13 +343,26 @@ struct Constants {
 // Constants of a key that some row sees, or (value header zero) of one that none does.  Where a value is no number, step is zero and
 // middle is none: nothing times an infinity is no number either, so rows that see the key are made none on their own.
 template <bool CENTERED>
-__device__ __forceinline__ f32x4 constants_of(f32x2 key_header, f32x2 value_header, const AttendArgs& a, int E, int key_bits, int value_bits)
+__device__ __forceinline__ f32x4 constants_of(f32x2 key_header, f32x2 value_header, const AttendArgs& a, int key_bits, int value_bits)
 {
     const float middle = fmaf(value_bits == 8 ? 128.0f : 8.0f, value_header[1], value_header[0]);
     const float zero = CENTERED ? fmaf(key_bits == 8 ? 128.0f : 8.0f, key_header[1], key_header[0]) : key_header[0];
     return f32x4{key_header[1] * a.factor * (CENTERED ? 1.0f / (1 << (kRowBits - kUnitBits)) : 1 << (24 - kRowBits)), zero * a.factor,
-                 finite(middle) ? ldexpf(value_header[1], kStepBits - E) : 0.0f, middle};
+                 finite(middle) ? value_header[1] : 0.0f, middle};
 }
+
+// log2 of a key's step, or of a 128th of its middle, from above.
+__device__ __forceinline__ float reach_of(const AttendArgs& a, float step, float middle)
+{
+    return fmaxf(static_cast<float>(exponent(fmaxf(fabsf(step), fabsf(middle) * 0.0078125f)) + 1), a.least);
+}
+
+// v * 2^x, where 2^x alone may be too small a number: the sums of two parts whose steps are 2^200 apart lie so far apart themselves.
+struct Shrink {
+    float half;
+    __device__ __forceinline__ explicit Shrink(float x) : half(__builtin_amdgcn_exp2f(0.5f * x)) {}
+    __device__ __forceinline__ float operator()(float v) const { return v * half * half; }
+};
 
 // ----------------------------------------------------------------------------- few rows
 
@@ -491,7 +508,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
         }
 
         float m = kNothing, middle = 0.0f;
-        int E = -126;
+        float ceiling = a.least;   // the largest reach of the wavefront's keys so far
         f32x4 acc[K::kColumns];
 #pragma unroll
         for (int i = 0; i < K::kColumns; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -506,18 +523,11 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
             const int32_t own = base + 16 * (n / 4 % K::kTiles) + 4 * g + n % 4;
             const bool seen = own >= span.from && own < span.end;   // by any row
             const f32x2 value_header = {seen ? b.value_header[0] : 0.0f, seen ? b.value_header[1] : 0.0f};
-            const float proper = finite(value_header[1]) ? value_header[1] : 0.0f;
-            if (__any(exponent(proper) > E)) {
-                const int top = __builtin_amdgcn_readfirstlane(exponent(wave_max(proper)));
-#pragma unroll
-                for (int i = 0; i < K::kColumns; ++i)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[i][r] = ldexpf(acc[i][r], E - top);
-                weights[0] = ldexpf(weights[0], E - top);
-                E = top;
-            }
-            const f32x4 four = constants_of<SPLIT == 2>(b.key_header, value_header, a, E, KEY_BITS, VALUE_BITS);
+            const f32x4 four = constants_of<SPLIT == 2>(b.key_header, value_header, a, KEY_BITS, VALUE_BITS);
             Constants c = {four[0], four[1], four[2], four[3]};
+            const bool bad = !finite(c.middle);
+            const float reach = reach_of(a, c.step, bad ? 0.0f : c.middle);
+            if (__any(reach > ceiling)) ceiling = wave_max(reach);
             settled(c.key_zero);
             f32x4 x[K::kTiles];
 #pragma unroll
@@ -559,18 +569,27 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = fmaxf(top, x[t][i]);
             top *= unit;
-            if (__any(top > m + kSlack)) {
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float now = top > m + kSlack ? top : m, less = __builtin_amdgcn_exp2f(m - now);   // a row's doing alone
+            if (__any(top + ceiling > m + kMostWeight)) {
+                float peak = kNothing;
+                each<K::kTiles>([&](auto t) {
+                    each<4>([&](auto e) {
+                        constexpr int i = e;
+                        peak = fmaxf(peak, fmaf(x[t][i], unit, dpp<kDppBroadcast + 4 * t + i>(reach)));
+                    });
+                });
+                peak = fmaxf(peak, __shfl_xor(peak, 16));
+                peak = fmaxf(peak, __shfl_xor(peak, 32));
+                const float now = peak > m + kMostWeight ? peak - kNewWeight : m;   // a row's doing alone
+                const Shrink less(m - now);
                 m = now;
-                sum *= less;
-                middle *= less;
+                sum = less(sum);
+                middle = less(middle);
 #pragma unroll
-                for (int i = 0; i < K::kColumns; ++i) acc[i] *= less;
-                weights[0] *= less;
+                for (int i = 0; i < K::kColumns; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[i][r] = less(acc[i][r]);
+                weights[0] = less(weights[0]);
             }
-            const bool bad = !finite(c.middle);
             if (__any(bad)) {
                 each_key([&](auto t, auto e, bool sees) {
                     const float none = dpp<kDppBroadcast + 4 * t + e>(nan_where(bad));
@@ -647,15 +666,15 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
         for (int k = 1; k < kFewWaves; ++k) top = fmaxf(top, joined_max[k][n]);
         float total = 0.0f;
 #pragma unroll
-        for (int k = 0; k < kFewWaves; ++k) total = fmaf(joined_sum[k][n], __builtin_amdgcn_exp2f(joined_max[k][n] - top), total);
-        const float share = __builtin_amdgcn_exp2f(m - top);
+        for (int k = 0; k < kFewWaves; ++k) total += Shrink(joined_max[k][n] - top)(joined_sum[k][n]);
+        const Shrink share(m - top);
 #pragma unroll
         for (int i = 0; i < K::kColumns; ++i)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 const int unit = SPLIT == 2 ? kUnitBits : VALUE_BITS == 4 && i % 2 ? 20 : 24;
                 const float centered = SPLIT == 2 ? acc[i][r] : fmaf(weights[0], (VALUE_BITS == 8 ? -128.0f : -8.0f) / (1 << unit), acc[i][r]);
-                acc[i][r] = (ldexpf(centered, E + unit - kStepBits) + middle) * share;
+                acc[i][r] = share(fmaf(centered, static_cast<float>(1 << unit), middle));
             }
 #pragma unroll
         for (int step = kFewWaves / 2; step >= 1; step /= 2) {
@@ -730,7 +749,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
     __shared__ __attribute__((aligned(16))) uint8_t keys[2][16384];
     __shared__ __attribute__((aligned(16))) uint8_t values[2][16384];
     __shared__ f32x4 constants[2][K::kTile];   // as in Constants
-    __shared__ int exponents[2];
+    __shared__ float ceilings[2];   // the largest reach of the tile's keys
 
     const Work w = work_of(a, blockIdx.x);
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
@@ -877,7 +896,6 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
         }
 
         float m[SETS], middle[SETS];
-        int E = -126, running = -126;   // of the sums; of the tiles prepared so far
         f32x16 acc[SETS][K::kBlocks];
 #pragma unroll
         for (int r = 0; r < SETS; ++r) {
@@ -911,21 +929,18 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
             if (of_values) a.value_bits == 8 ? store_values(eight) : store_values(four);
             else a.key_bits == 8 ? store_keys(eight) : store_keys(four);
             if (of_constants) {
-                float step[K::kOwn], top = 0.0f;
+                float top = a.least;
 #pragma unroll
                 for (int o = 0; o < K::kOwn; ++o) {
                     const int32_t own = base + (lane + 64 * o) % K::kTile;
                     const bool seen = own >= span.from && own < span.end;   // by any row
-                    step[o] = seen ? value_header[o][1] : 0.0f;
-                    value_header[o][0] = seen ? value_header[o][0] : 0.0f;
-                    top = fmaxf(top, finite(step[o]) ? step[o] : 0.0f);
+                    const f32x2 header = {seen ? value_header[o][0] : 0.0f, seen ? value_header[o][1] : 0.0f};
+                    const f32x4 c = constants_of<SPLIT == 2>(key_header[o], header, a, a.key_bits, a.value_bits);
+                    top = fmaxf(top, reach_of(a, c[2], finite(c[3]) ? c[3] : 0.0f));
+                    if (lane + 64 * o < K::kTile) constants[to][lane + 64 * o] = c;
                 }
-                if (__any(exponent(top) > running)) running = __builtin_amdgcn_readfirstlane(exponent(wave_max(top)));
-#pragma unroll
-                for (int o = 0; o < K::kOwn; ++o)
-                    if (lane + 64 * o < K::kTile)
-                        constants[to][lane + 64 * o] = constants_of<SPLIT == 2>(key_header[o], f32x2{value_header[o][0], step[o]}, a, running, a.key_bits, a.value_bits);
-                if (lane == 0) exponents[to] = running;
+                top = wave_max(top);
+                if (lane == 0) ceilings[to] = top;
             }
         };
 
@@ -939,7 +954,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
         // Scores and sums of the keys [base, base + 32), that part; the next part's keys are loaded behind the products that need these.
         const auto use = [&](int32_t base, int from, int s, bool more) {
             const f32x4 v = constants[from][32 * s + 8 * (lane % 16 / 4) + 4 * h + lane % 4];
-            const int now_read = exponents[from];
+            const float ceiling = ceilings[from];
             __builtin_amdgcn_sched_barrier(0);
             f32x16 x[SETS] = {};
 #pragma unroll
@@ -953,16 +968,6 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
             for (int b = 0; b < K::kBlocks; ++b)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) u[b][k] = *reinterpret_cast<const f16x8*>(&values[from][0] + (value_at ^ (2 * s + k) << 5) + b * (64 * K::kTile));
-            const int now = __builtin_amdgcn_readfirstlane(now_read);
-            if (now != E) {
-#pragma unroll
-                for (int r = 0; r < SETS; ++r)
-#pragma unroll
-                    for (int b = 0; b < K::kBlocks; ++b)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) acc[r][b][i] = ldexpf(acc[r][b][i], E - now);
-                E = now;
-            }
             Constants c = {v[0], v[1], v[2], v[3]};
             settled(c.key_zero);
 #pragma unroll
@@ -1002,18 +1007,27 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
 #pragma unroll
                 for (int i = 0; i < 16; ++i) top[r] = fmaxf(top[r], x[r][i]);
                 top[r] *= unit[r];
-                over |= top[r] > m[r] + kSlack;
+                over |= top[r] + ceiling > m[r] + kMostWeight;
             }
             if (__any(over)) {
+                const float reach = reach_of(a, c.step, finite(c.middle) ? c.middle : 0.0f);
 #pragma unroll
                 for (int r = 0; r < SETS; ++r) {
-                    top[r] = fmaxf(top[r], __shfl_xor(top[r], 32));
-                    const float now = top[r] > m[r] + kSlack ? top[r] : m[r], less = __builtin_amdgcn_exp2f(m[r] - now);   // a row's doing alone
+                    float peak = kNothing;
+                    each<16>([&](auto e) {
+                        constexpr int i = e;
+                        peak = fmaxf(peak, fmaf(x[r][i], unit[r], dpp<kDppBroadcast + i>(reach)));
+                    });
+                    peak = fmaxf(peak, __shfl_xor(peak, 32));
+                    const float now = peak > m[r] + kMostWeight ? peak - kNewWeight : m[r];   // a row's doing alone
+                    const Shrink less(m[r] - now);
                     m[r] = now;
-                    sum[r] *= less;
-                    middle[r] *= less;
+                    sum[r] = less(sum[r]);
+                    middle[r] = less(middle[r]);
 #pragma unroll
-                    for (int b = 0; b < K::kBlocks; ++b) acc[r][b] *= less;
+                    for (int b = 0; b < K::kBlocks; ++b)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[r][b][i] = less(acc[r][b][i]);
                 }
             }
             const bool bad = !finite(c.middle);
@@ -1094,7 +1108,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
                 for (int i = 0; i < 16; i += 4) {
                     float f[4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) f[j] = (ldexpf(acc[r][b][i + j], E + kUnitBits - kStepBits) + middle[r]) * scale;
+                    for (int j = 0; j < 4; ++j) f[j] = fmaf(acc[r][b][i + j], static_cast<float>(1 << kUnitBits), middle[r]) * scale;
                     const int column = 32 * b + 2 * i + 4 * (here(lane) / 32);
                     if (a.partial) store_some(a.partial, ACTQ_F32, part_row * DIM + column, f);
                     else store_some(a.out.p, a.dtype, (static_cast<int64_t>(w.start) + token) * a.out.token + head * a.out.head + column, f);
@@ -1137,7 +1151,7 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a)
         for (int k = 1; k < kJoinThreads / 64; ++k) top = fmaxf(top, tops[k]);
     }
     float* const mine = weights[SHARED ? 0 : team];
-    if (own < parts) mine[own] = part[1] * __builtin_amdgcn_exp2f(part[0] - top);
+    if (own < parts) mine[own] = Shrink(part[0] - top)(part[1]);
     __syncthreads();
     f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int p = SHARED ? team : 0; there && p < parts; p += kStride * kAhead) {
@@ -1177,6 +1191,7 @@ __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a)
 
 constexpr int64_t kMostBlocks = int64_t(1) << 22;
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int ceil_log2(int64_t n) { return n <= 1 ? 0 : 64 - __builtin_clzll(static_cast<unsigned long long>(n - 1)); }
 
 struct Shape {
     int rows;      // of a tile: 16, or 32 per wavefront of the kernel for many rows
@@ -1262,6 +1277,8 @@ int launch_cache_attention(const actq_cache* c, const actq_heads* q, int dtype, 
     a.factor = cap > 0.0f ? scale / cap : scale * kLog2e;
     a.cap = cap * kLog2e;
     a.window = window;
+    // p <= 2^(kMostWeight - least), and there are no more of them than the table has room for
+    a.least = static_cast<float>(ceil_log2(static_cast<int64_t>(table_width) << a.page_shift) - 111);
     a.tiles = static_cast<uint32_t>(shape.tiles);
     a.parts = static_cast<uint32_t>(shape.parts);
     a.by_tiles = make_fastdiv(a.tiles);

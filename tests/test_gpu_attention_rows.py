@@ -97,3 +97,42 @@ def test_rows_before_the_first_position_are_zeros_whatever_they_hold():
     q[0] = float("inf")
     q[1] = float("nan")
     assert (_attend((q, *rest))[:2] == 0).all()
+
+
+@pytest.mark.parametrize("ratio", [12, 20, 40])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("at", range(len(SHAPES)))
+def test_values_that_only_later_rows_see_leave_the_earlier_ones_as_they_were(at, dtype, ratio):
+    """The last two tokens' values are 2^ratio times larger: rows before them are what they were, bit for bit, and every row keeps to its own bound."""
+    new, q_heads, kv, dim, key_bits, value_bits = SHAPES[at]
+    q, cache, table, *rest = case = _case([300], [new], q_heads, kv, dim, dtype, key_bits, value_bits, seed=at)
+    clean = _attend(case)
+    for j in (298, 299):
+        cache[3][table[0, j // 16].long(), :, j % 16] *= 2.0 ** ratio
+    out = _attend(case)
+    assert torch.equal(out[:-2], clean[:-2])
+    if dtype != F16:   # the last rows' outputs are beyond binary16
+        _within(out, case)
+
+
+@pytest.mark.parametrize("ratio", [20, 30])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("new, dim", [(1, 64), (1, 128), (1, 256), (130, 128), (130, 64), (330, 256)])
+def test_a_large_value_of_no_weight_takes_no_bits_from_the_others(new, dim, dtype, ratio):
+    """One key's scores lie some 60 below the others (its weight is about e^-60) while its values are 2^ratio times theirs."""
+    q, cache, table, *rest = case = _case([400], [new], 1, 1, dim, dtype, seed=70)
+    q[:, 0] = q[:, 0].abs()
+    block, j = table[0, 7 // 16].long(), 7
+    cache[1][block, 0, j] = torch.tensor([-60.0 * dim ** 0.5 / (0.8 * dim), 0.0])
+    cache[3][block, 0, j] *= 2.0 ** ratio
+    _within(_attend(case), case)
+
+
+@pytest.mark.parametrize("new, dim", [(1, 64), (1, 128), (130, 64), (330, 256)])
+@pytest.mark.parametrize("factor", [-100, -60, 60, 100])
+def test_values_of_any_size(new, dim, factor):
+    """Half of a sequence's values, or all of them, are 2^factor times the others: binary32's range of steps on both sides."""
+    for some in (slice(0, 7), slice(0, None)):
+        q, cache, table, *rest = case = _case([400], [new], 2, 1, dim, F32, seed=71)
+        cache[3][table[0, some].long()] *= 2.0 ** factor
+        _within(_attend(case), case)
