@@ -42,7 +42,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kMostWeight = 15.0f;   // p * step stays below 2^kMostWeight, inside binary16's range,
 constexpr float kNewWeight = 7.0f;     // and below 2^kNewWeight where the running maximum has just moved
 constexpr int kUnitBits = 9;           // centred codes are held as code * 2^-9
-constexpr float kMostCap = 1152921504606846976.0f;
+constexpr float kMostCap = 0x1p60f, kLeastCap = 0x1p-60f;
 constexpr int kRowBits = 13;           // a row of q is scaled to a largest element of 2^13 to 2^14 (2^15 at the upper end of binary32's range)
 
 struct AttendArgs {
@@ -252,13 +252,15 @@ __device__ __forceinline__ float wave_max(float v)
     return over_lanes<64>(v, [](float a, float b) { return fmaxf(a, b); });
 }
 
-// tanh(x): for 16-bit outputs from one exponential, off by some 2^-23 of the cap; for binary32 the function's own.
+// tanh(x): for 16-bit outputs to 2^-22 of itself, from one exponential, whose cancellation below 1/2 a polynomial takes over: x + x u g(u), u = x^2, g the
+// interpolation of (tanh(x) / x - 1) / u at four Chebyshev nodes of [0, 1/4] (2^-23.4).  For binary32 the function's own.
 template <bool FINE>
 __device__ __forceinline__ float tanh_of(float x)
 {
     if (FINE) return tanhf(x);
-    const float e = __builtin_amdgcn_exp2f(x * (2.0f * kLog2e));
-    return 1.0f - 2.0f * __builtin_amdgcn_rcpf(e + 1.0f);
+    const float e = __builtin_amdgcn_exp2f(x * (2.0f * kLog2e)), u = x * x;
+    const float g = fmaf(fmaf(fmaf(0.01798874f, u, -0.05338711f), u, 0.13330476f), u, -0.33333311f);
+    return u < 0.25f ? fmaf(x * u, g, x) : 1.0f - 2.0f * __builtin_amdgcn_rcpf(e + 1.0f);
 }
 
 // cap tanh(x / cap) of a score in units of a power of two, whose inverse is a matter of its exponent.
@@ -1272,8 +1274,9 @@ int launch_cache_attention(const actq_cache* c, const actq_heads* q, int dtype, 
     a.table_width = table_width;
     a.lengths = lengths;
     a.query_start = query_start;
-    // A cap beyond 2^60 would overflow in the unit of a row of the smallest elements; any such one leaves the scores below it as they are.
-    const float cap = softcap < kMostCap ? softcap : kMostCap;
+    // A cap beyond 2^60 would overflow in the unit of a row of the smallest elements, and leaves the scores below it as they are; one below 2^-60 would
+    // in its inverse, and leaves all weights alike.
+    const float cap = softcap > kMostCap ? kMostCap : softcap > 0.0f && softcap < kLeastCap ? kLeastCap : softcap;
     a.factor = cap > 0.0f ? scale / cap : scale * kLog2e;
     a.cap = cap * kLog2e;
     a.window = window;

@@ -136,3 +136,13 @@ def test_values_of_any_size(new, dim, factor):
         q, cache, table, *rest = case = _case([400], [new], 2, 1, dim, F32, seed=71)
         cache[3][table[0, some].long()] *= 2.0 ** factor
         _within(_attend(case), case)
+
+
+@pytest.mark.parametrize("softcap", [1e-39, 1e-30, 0.01, 1.0, 30.0, 1e3, 1e4, 1e6, 1e12, 3e38])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("new, dim", [(1, 64), (2, 128), (130, 64), (330, 256)])
+def test_caps_of_any_size(new, dim, dtype, softcap):
+    """Scores of up to some tens under caps that hold nearly all of them, some, or none: the cap's own error is that of the score."""
+    q, *rest = _case([340], [new], 2, 1, dim, dtype, seed=80)
+    case = (q * 4, *rest)
+    _within(_attend(case, softcap=softcap), case, softcap=softcap)
