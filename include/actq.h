@@ -454,8 +454,9 @@ int actq_head_norm_rotate_backward(const actq_heads* grad_q, const actq_heads* g
  * Z = min, R = max - min, B = 2^bits - 1, step = R / B, and
  *   code = nearest(min((x - Z) * (B / R), B)), ties to even,
  * every operation rounded to binary32 (a group whose R is zero, or whose B / R
- * overflows, has step 0 and codes 0): the quantizer of actq_quantize_pack with rounding
- * to nearest, since a cache feeds no gradient.  A code stands for Z + code * step.
+ * overflows, has step 0 and codes 0; one with an element that is not finite, or whose R
+ * overflows, has Z and step NaN and codes 0): the quantizer of actq_quantize_pack with
+ * rounding to nearest, since a cache feeds no gradient.  A code stands for Z + code * step.
  *
  * Token slot s of the cache is offset s mod page_size of page s div page_size.
  *   key_codes   device [pages, heads, page_size, dim * key_bits / 8] bytes, LSB-first as above

@@ -193,15 +193,6 @@ __device__ __forceinline__ void store_some(void* p, int dtype, int64_t at, const
     else put(__bf16{});
 }
 
-// The bits of a value that may be no number.  The compiler takes it that floating-point data holds no NaN, and would fold a
-// question about the bits that it recognises as one about the number.
-__device__ __forceinline__ uint32_t bits_of(float v)
-{
-    uint32_t b = __builtin_bit_cast(uint32_t, v);
-    asm("" : "+v"(b));
-    return b;
-}
-
 // A number as it was rounded, which the operations on it see and not what it was computed from: a conversion of a product to binary16
 // may become one instruction, which rounds once where a conversion of the rounded product rounds twice.
 __device__ __forceinline__ float rounded(float v)
@@ -218,17 +209,7 @@ __device__ __forceinline__ int here(int v)
     return v;
 }
 
-__device__ __forceinline__ float nan_where(bool bad)
-{
-    uint32_t b = bad ? 0x7fc00000u : 0u;
-    asm("" : "+v"(b));
-    return __builtin_bit_cast(float, b);
-}
-
 __device__ __forceinline__ int exponent(float v) { return static_cast<int>(bits_of(v) >> 23 & 255u) - 127; }
-
-// The magnitude of a value as a whole number, which orders infinities and NaN above all numbers.
-__device__ __forceinline__ uint32_t magnitude(float v) { return bits_of(v) & 0x7fffffffu; }
 
 // The row of q that a lane has a share of: the exponent of its largest element, and whether one is no finite number.
 struct RowScale {

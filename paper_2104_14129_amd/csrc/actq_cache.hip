@@ -1,8 +1,9 @@
 // A paged cache of keys and values, quantised as it is written, and read back.
 //
 // A group is a token's head: Z = min, R = max - min, code = nearest((x - Z) (B / R)), ties to even, B = 2^bits - 1, and a code
-// stands for Z + code (R / B): the codec's quantizer with rounding to nearest in place of the stochastic one, since a cache feeds no
-// gradient that would have to be unbiased, and to nearest is half the error.
+// stands for Z + code (R / B); a group with an infinity or NaN, or whose R overflows, reads as NaN.  It is the codec's quantizer with
+// rounding to nearest in place of the stochastic one, since a cache feeds no gradient that would have to be unbiased, and to nearest is
+// half the error.
 //
 // What bounds it: memory.  A head is 8, 16 or 32 lanes of eight elements; a lane handles a token's key and value together, so that
 // the slot is looked up once and two loads are in flight.  Measured on one MI355X, whose copy of 1 GiB reaches 5.2 TB/s: 65536 tokens of 8 heads of 128
@@ -55,21 +56,29 @@ template <int LANES>
 __device__ __forceinline__ void quantise(const float (&x)[8], int bits, uint8_t* codes, float* header, bool held, int at)
 {
     float low = x[0], high = x[0];
+    uint32_t largest = magnitude(x[0]);
 #pragma unroll
     for (int i = 1; i < 8; ++i) {
         low = fminf(low, x[i]);
         high = fmaxf(high, x[i]);
+        largest = max(largest, magnitude(x[i]));
+    }
+    // an infinity or NaN (which a minimum passes over) gives the group an infinite range
+    if (largest >= 0x7f800000u) {
+        low = 0.0f;
+        high = INFINITY;
     }
     low = over_lanes<LANES>(low, [](float a, float b) { return fminf(a, b); });
     high = over_lanes<LANES>(high, [](float a, float b) { return fmaxf(a, b); });
     const float top = bits == 8 ? 255.0f : 15.0f;
     const float zero = low + 0.0f;   // -0 becomes +0
     const float range = high - zero;
+    const bool none = magnitude(range) >= 0x7f800000u;
     float inverse = top / range, step = range / top;
     if (range == 0.0f || isinf(inverse)) inverse = step = 0.0f;
     uint32_t code[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) code[i] = static_cast<uint32_t>(rintf(fminf((x[i] - zero) * inverse, top)));
+    for (int i = 0; i < 8; ++i) code[i] = none ? 0u : static_cast<uint32_t>(rintf(fminf((x[i] - zero) * inverse, top)));
     if (!held) return;
     if (bits == 8) {
         u32x2 w;
@@ -82,7 +91,10 @@ __device__ __forceinline__ void quantise(const float (&x)[8], int bits, uint8_t*
         for (int i = 1; i < 8; ++i) w |= code[i] << 4 * i;
         *reinterpret_cast<uint32_t*>(codes + 4 * at) = w;
     }
-    if (at == 0) *reinterpret_cast<f32x2*>(header) = f32x2{zero, step};
+    if (at == 0) {
+        const uint32_t nan = 0x7fc00000u;   // stored as bits: the compiler takes it that floating-point data holds no NaN
+        *reinterpret_cast<u32x2*>(header) = none ? u32x2{nan, nan} : u32x2{__builtin_bit_cast(uint32_t, zero), __builtin_bit_cast(uint32_t, step)};
+    }
 }
 
 template <typename T, int LANES>

@@ -53,6 +53,25 @@ struct Eight {
     }
 };
 
+// The bits of a value that may be no number.  The compiler takes it that floating-point data holds no NaN, and would fold a
+// question about the bits that it recognises as one about the number.
+__device__ __forceinline__ uint32_t bits_of(float v)
+{
+    uint32_t b = __builtin_bit_cast(uint32_t, v);
+    asm("" : "+v"(b));
+    return b;
+}
+
+// The magnitude of a value as a whole number, which orders infinities and NaN above all numbers.
+__device__ __forceinline__ uint32_t magnitude(float v) { return bits_of(v) & 0x7fffffffu; }
+
+__device__ __forceinline__ float nan_where(bool bad)
+{
+    uint32_t b = bad ? 0x7fc00000u : 0u;
+    asm("" : "+v"(b));
+    return __builtin_bit_cast(float, b);
+}
+
 // A value of another lane of the 16-lane row, by a DPP control: every lane has a source, so that the instruction which
 // uses the value can fetch it itself.
 template <int CONTROL>
