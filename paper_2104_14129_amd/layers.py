@@ -22,6 +22,7 @@ from dataclasses import dataclass
 import torch
 import torch.nn as nn
 import torch.nn.functional as F
+from torch.autograd import forward_ad
 
 from . import binding as B
 
@@ -304,6 +305,12 @@ class _QMaxPool2dFn(torch.autograd.Function):
         return B.maxpool2d_backward(arg, grad_y.contiguous(), H, W, kernel, stride, padding, dilation), None, None, None, None
 
 
+def _no_tangents(*tensors) -> None:
+    """Forward-mode tangents, which the library's calls would drop, are refused."""
+    if any(forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise NotImplementedError("QHeadNorm has no forward-mode derivative")
+
+
 class _QHeadNormFn(torch.autograd.Function):
     """Norm and rotation of queries and keys by the library; the contexts are the compressed queries and keys.  What the codec does not
     take (bfloat16, no tokens) is kept as it is."""
@@ -340,6 +347,8 @@ class _QHeadNormFn(torch.autograd.Function):
             c.host, c.packed, c.header = ((s0, s1), None, None) if swapped else (None, s0, s1)
             inputs.append(decompress(c))
         q_weight, k_weight, positions, cos, sin = saved[8:]
+        if not _native(grad_q, grad_k):
+            _no_tangents(grad_q, grad_k)
         grad_q, grad_k = (g if g.stride(-1) == 1 else g.contiguous() for g in (grad_q, grad_k))
         gradients = B.head_norm_rotate_backward(grad_q, grad_k, *inputs, q_weight, k_weight, positions, cos, sin, *ctx.options,
                                                 need_weights=ctx.needs_input_grad[2] or ctx.needs_input_grad[3])
@@ -403,7 +412,8 @@ class QHeadNorm(nn.Module):
 
     q, k [tokens, heads, dim] (float32, float16 or bfloat16; heads contiguous); positions int32 [tokens], rows of the float32 tables
     cos and sin [rows, rotated / 2], a position that is none of them being padding.  In training the backward pass starts from the
-    compressed queries and keys; bfloat16 ones, which the codec does not take, are kept as they are."""
+    compressed queries and keys; bfloat16 ones, which the codec does not take, are kept as they are.  The tables get no gradient, and
+    forward-mode tangents are refused."""
 
     def __init__(self, dim: int, eps: float = 1e-6, interleaved: bool = False, device=None, dtype=None):
         super().__init__()
@@ -412,9 +422,13 @@ class QHeadNorm(nn.Module):
         self.k_weight = nn.Parameter(torch.ones(dim, device=device, dtype=dtype))
 
     def forward(self, q, k, positions, cos, sin):
-        if torch.is_grad_enabled() and any(t.requires_grad for t in (q, k, self.q_weight, self.k_weight)):
-            return _QHeadNormFn.apply(q, k, self.q_weight, self.k_weight, positions, cos, sin, self.eps, self.interleaved)
-        return B.head_norm_rotate(q, k, self.q_weight, self.k_weight, positions, cos, sin, self.eps, self.interleaved)
+        q_weight, k_weight = self.q_weight, self.k_weight
+        if torch.is_grad_enabled() and any(t.requires_grad for t in (q, k, q_weight, k_weight)):
+            return _QHeadNormFn.apply(q, k, q_weight, k_weight, positions, cos, sin, self.eps, self.interleaved)
+        host = B._host or B.host()
+        if not host.plain(q, k, q_weight, k_weight):
+            _no_tangents(q, k, q_weight, k_weight)
+        return host.head_norm_rotate(q, k, q_weight, k_weight, positions, cos, sin, float(self.eps), bool(self.interleaved), None, None)
 
 
 def convert(module: nn.Module) -> nn.Module:
