@@ -311,6 +311,18 @@ def _no_tangents(*tensors) -> None:
         raise NotImplementedError("QHeadNorm has no forward-mode derivative")
 
 
+class _Last(torch.autograd.Function):
+    """A gradient that the library computed from `of` and that cannot be differentiated once more."""
+
+    @staticmethod
+    def forward(ctx, grad, *of):
+        return grad.view_as(grad)
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise NotImplementedError("QHeadNorm has no second derivative")
+
+
 class _QHeadNormFn(torch.autograd.Function):
     """Norm and rotation of queries and keys by the library; the contexts are the compressed queries and keys.  What the codec does not
     take (bfloat16, no tokens) is kept as it is."""
@@ -352,6 +364,8 @@ class _QHeadNormFn(torch.autograd.Function):
         grad_q, grad_k = (g if g.stride(-1) == 1 else g.contiguous() for g in (grad_q, grad_k))
         gradients = B.head_norm_rotate_backward(grad_q, grad_k, *inputs, q_weight, k_weight, positions, cos, sin, *ctx.options,
                                                 need_weights=ctx.needs_input_grad[2] or ctx.needs_input_grad[3])
+        if torch.is_grad_enabled():   # a graph of the gradients is being made, in which these would pass for constants
+            gradients = [None if g is None else _Last.apply(g.requires_grad_(), grad_q, grad_k, q_weight, k_weight) for g in gradients]
         return (*gradients, None, None, None, None, None)
 
 
@@ -412,8 +426,8 @@ class QHeadNorm(nn.Module):
 
     q, k [tokens, heads, dim] (float32, float16 or bfloat16; heads contiguous); positions int32 [tokens], rows of the float32 tables
     cos and sin [rows, rotated / 2], a position that is none of them being padding.  In training the backward pass starts from the
-    compressed queries and keys; bfloat16 ones, which the codec does not take, are kept as they are.  The tables get no gradient, and
-    forward-mode tangents are refused."""
+    compressed queries and keys; bfloat16 ones, which the codec does not take, are kept as they are.  The tables get no gradient;
+    forward-mode tangents and second derivatives are refused."""
 
     def __init__(self, dim: int, eps: float = 1e-6, interleaved: bool = False, device=None, dtype=None):
         super().__init__()

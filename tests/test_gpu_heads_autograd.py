@@ -93,3 +93,21 @@ def test_under_autocast(dtype):
         want, want_w, _ = H.norm_rotate_backward(r.float().cpu(), x1.detach().float().cpu(), w.detach().cpu(), *(t.cpu() for t in table), 1e-6, False)
         assert float((grad.cpu().double() - want).norm() / want.norm()) < 0.05
         assert float((w.grad.cpu().double() - want_w).norm() / want_w.norm()) < 0.05
+
+
+@pytest.mark.parametrize("linear", [True, False])
+@pytest.mark.parametrize("of", [0, 1, 2, 3])
+def test_second_derivatives_are_refused_and_not_taken_for_zeros(of, linear):
+    q, k, *table = _case()
+    q.requires_grad_(), k.requires_grad_()
+    layer = L.QHeadNorm(64).to(DEV)
+    inputs = [q, k, layer.q_weight, layer.k_weight]
+    loss = sum(t.sum() if linear else t.square().sum() for t in layer(q, k, *table))
+    plain = torch.autograd.grad(loss, inputs, retain_graph=True)
+    graph = torch.autograd.grad(loss, inputs, create_graph=True)
+    assert all(torch.equal(a, b) for a, b in zip(plain, graph))
+    again = graph[of].square().sum() + q.sum()
+    with pytest.raises(NotImplementedError, match="second derivative"):
+        torch.autograd.grad(again, layer.k_weight, retain_graph=True)
+    with pytest.raises(NotImplementedError, match="second derivative"):
+        again.backward()
