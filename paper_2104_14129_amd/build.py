@@ -3,6 +3,7 @@ binding's native half, with the host compiler against torch's headers."""
 from __future__ import annotations
 
 import os
+import re
 import shutil
 import subprocess
 import sys
@@ -28,6 +29,9 @@ HIPCC_FLAGS = [
     "-Wno-pass-failed",
 ]
 
+
+# sources with instructions of their own that read other lanes, for which the compiler does not wait
+LANE_READERS = ["actq_attention.hip"]
 
 HOST_LIB = os.path.join(_HERE, "actq_torch.so")
 HOST_SOURCE = "actq_torch.cpp"
@@ -75,6 +79,51 @@ def hipcc() -> str:
     return exe
 
 
+def _registers(operand: str) -> set:
+    """The vector registers that an operand names: v7, v[4:7], |v7|, -v7."""
+    m = re.fullmatch(r"[-|]*v(?:(\d+)|\[(\d+):(\d+)\])\|?", operand.strip())
+    if not m:
+        return set()
+    return {int(m[1])} if m[1] else set(range(int(m[2]), int(m[3]) + 1))
+
+
+def lane_read_hazards(assembly: str) -> list:
+    """What is too near to the DPP multiply-adds in an assembly listing.  The compiler waits for the results of its own instructions; of those written by hand
+    it knows the operands only.  A lane of another's register needs two wait states after a vector instruction has written it, the result of an exponential, a
+    reciprocal and the like one before anything reads it, that of a matrix instruction up to 18 (unless one of the compiler's own has used it in between, which
+    has waited for it), and lanes that a vector comparison has switched five.
+    An instruction is a wait state, s_nop n is n + 1; what lies before a label is not known and counts as a hazard."""
+    found, window = [], []   # of instructions since the last label: (wait states, mnemonic, registers written, registers used, whether it is one of ours)
+    label = True
+    for number, line in enumerate(assembly.splitlines(), 1):
+        text = line.split(";")[0].split("//")[0].strip()
+        if not text or text.startswith((".", "#")) and not text.endswith(":"):
+            continue
+        if text.endswith(":"):
+            window, label = [], True
+            continue
+        name, _, rest = text.partition(" ")
+        operands = re.split(r",\s*(?![^\[]*\])", rest.strip().split(" row_")[0]) if rest else []
+        ours = name == "v_fmac_f32_dpp" and "row_newbcast" in text
+        if ours:
+            target, source, factor = (_registers(o) for o in operands[:3])
+            waited, known = 0, set()
+            for states, other, written, used, by_hand in reversed(window):
+                trans = re.match(r"v_(exp|log|rcp|rsq|sqrt|sin|cos)_", other)
+                matrix = other.startswith(("v_mfma", "v_smfmac"))
+                if other.startswith("v_") and (waited < 2 and written & source or trans and waited < 1 and written & (source | factor | target)
+                                               or matrix and waited < 18 and (written & (source | factor | target)) - known or other.startswith("v_cmpx") and waited < 5):
+                    found.append(f"line {number}: {text}  behind {other}")
+                waited += states
+                known |= set() if by_hand else used
+            if label and waited < 2:
+                found.append(f"line {number}: {text}  behind a label")
+        states = int(operands[0], 0) + 1 if name == "s_nop" else 1
+        written = _registers(operands[0]) if name.startswith("v_") and operands else set()
+        window = (window + [(states, name, written, set().union(*map(_registers, operands)) if name.startswith("v_") else set(), ours)])[-18:]
+    return found
+
+
 def build(verbose: bool = False) -> str:
     """Compile every source of the library; always recompiles."""
     from concurrent.futures import ThreadPoolExecutor
@@ -96,8 +145,17 @@ def build(verbose: bool = False) -> str:
     with tempfile.TemporaryDirectory() as objects, ThreadPoolExecutor(min(len(SOURCES), os.cpu_count() or 1)) as pool:
         common = [hipcc(), *flags, f'-DACTQ_SOURCE_HASH="{source_hash()}"', "-I", os.path.join(ROOT, "include"), "-I", CSRC]
         made = [os.path.join(objects, s + ".o") for s in SOURCES]
-        for done in [pool.submit(run, [*common, "-x", "hip", "-c", os.path.join(CSRC, s), "-o", o]) for s, o in zip(SOURCES, made)]:
+        listing = {s: ["-save-temps=obj"] if s in LANE_READERS else [] for s in SOURCES}
+        for done in [pool.submit(run, [*common, *listing[s], "-x", "hip", "-c", os.path.join(CSRC, s), "-o", o]) for s, o in zip(SOURCES, made)]:
             done.result()
+        for s in LANE_READERS:
+            listings = [f for f in os.listdir(objects) if f.startswith(os.path.splitext(s)[0]) and "gfx950" in f and f.endswith(".s")]
+            if len(listings) != 1:
+                raise RuntimeError(f"{s}: no assembly listing to check")
+            with open(os.path.join(objects, listings[0])) as f:
+                hazards = lane_read_hazards(f.read())
+            if hazards:
+                raise RuntimeError(f"{s}: lanes read too early:\n" + "\n".join(hazards[:20]))
         run([hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", *made, "-o", tmp])
     os.replace(tmp, LIB)
     return LIB
