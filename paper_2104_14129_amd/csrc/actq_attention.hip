@@ -233,15 +233,16 @@ __device__ __forceinline__ float wave_max(float v)
     return over_lanes<64>(v, [](float a, float b) { return fmaxf(a, b); });
 }
 
-// tanh(x): for 16-bit outputs to 2^-22 of itself, from one exponential, whose cancellation below 1/2 a polynomial takes over: x + x u g(u), u = x^2, g the
-// interpolation of (tanh(x) / x - 1) / u at four Chebyshev nodes of [0, 1/4] (2^-23.4).  For binary32 the function's own.
+// tanh(x): for 16-bit outputs to 2^-21 of itself, from one exponential, whose cancellation below 1/2 a Pade approximant takes over (of order 5 over 4, off
+// by 2^-33); both end in the same reciprocal, and no constant has to be held in a register.  For binary32 the function's own.
 template <bool FINE>
 __device__ __forceinline__ float tanh_of(float x)
 {
     if (FINE) return tanhf(x);
     const float e = __builtin_amdgcn_exp2f(x * (2.0f * kLog2e)), u = x * x;
-    const float g = fmaf(fmaf(fmaf(0.01798874f, u, -0.05338711f), u, 0.13330476f), u, -0.33333311f);
-    return u < 0.25f ? fmaf(x * u, g, x) : 1.0f - 2.0f * __builtin_amdgcn_rcpf(e + 1.0f);
+    const bool small = u < 0.25f;
+    const float r = __builtin_amdgcn_rcpf(small ? fmaf(fmaf(15.0f, u, 420.0f), u, 945.0f) : e + 1.0f);
+    return small ? x * fmaf(u + 105.0f, u, 945.0f) * r : fmaf(-2.0f, r, 1.0f);
 }
 
 // cap tanh(x / cap) of a score in units of a power of two, whose inverse is a matter of its exponent.
