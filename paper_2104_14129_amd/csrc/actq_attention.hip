@@ -165,13 +165,6 @@ __device__ __forceinline__ void load_eight(const void* p, int dtype, int64_t at,
     }
 }
 
-__device__ __forceinline__ void store_element(void* p, int dtype, int64_t at, float v)
-{
-    if (dtype == ACTQ_F32) static_cast<float*>(p)[at] = v;
-    else if (dtype == ACTQ_F16) static_cast<_Float16*>(p)[at] = static_cast<_Float16>(v);
-    else static_cast<__bf16*>(p)[at] = static_cast<__bf16>(v);
-}
-
 template <int N>
 __device__ __forceinline__ void store_some(void* p, int dtype, int64_t at, const float (&f)[N])
 {
@@ -695,7 +688,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
 
 // ----------------------------------------------------------------------------- many rows
 
-// SETS times 32 rows per wavefront, WAVES of them over the same keys.  Tiles of keys are widened once per workgroup into the LDS (keys as
+// 32 rows per wavefront, WAVES of them over the same keys.  Tiles of keys are widened once per workgroup into the LDS (keys as
 // they lie, values transposed), twice buffered: while one is computed the next one's codes are on their way to registers.  Half of the wavefronts
 // widen keys and half values; the last one prepares the groups' constants.
 //
@@ -703,9 +696,9 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
 // steps of the second product take eight of them each, and the transposed values hold a step's sixteen keys in that order.
 // Rows of the LDS are 16-byte chunks; a chunk's place is its number XOR some bits of the row, so that neither the rows that eight lanes read
 // together nor those that they write share a bank.  Of sixteen neighbouring codes of a key the first eight go to the row's first half.
-template <int DIM, int SPLIT, int WAVES, int SETS>
+template <int DIM, int SPLIT, int WAVES>
 struct Many {
-    static constexpr int kThreads = 64 * WAVES, kOwnRows = 32 * SETS, kRows = kOwnRows * WAVES;
+    static constexpr int kThreads = 64 * WAVES, kOwnRows = 32, kRows = kOwnRows * WAVES;
     static constexpr int kTile = 8192 / DIM;           // keys of a tile
     static constexpr int kParts = kTile / 32;          // of 32 keys
     static constexpr int kSteps = DIM / 16;            // of the first product
@@ -726,10 +719,10 @@ struct Many {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-template <int DIM, int SPLIT, int WAVES, int SETS>
+template <int DIM, int SPLIT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_kernel(AttendArgs a)
 {
-    typedef Many<DIM, SPLIT, WAVES, SETS> K;
+    typedef Many<DIM, SPLIT, WAVES> K;
     __shared__ __attribute__((aligned(16))) uint8_t keys[2][16384];
     __shared__ __attribute__((aligned(16))) uint8_t values[2][16384];
     __shared__ f32x4 constants[2][K::kTile];   // as in Constants
@@ -777,10 +770,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
             mine.high = w.first + static_cast<int32_t>(divide(min(first_row + K::kOwnRows, w.rows) - 1, a.by_group));
             mine.from = a.window > 0 ? max(mine.low - a.window + 1, 0) : 0;
         }
-        // the lane's rows, one of each set; beyond the last one the last one again
-        const auto row_at = [&](int r) { return first_row + 32 * r + n; };
-        const auto token_at = [&](int r) { return static_cast<int32_t>(divide(min(row_at(r), w.rows - 1), a.by_group)); };
-        const auto head_at = [&](int r) { return w.head * a.group + min(row_at(r), w.rows - 1) - token_at(r) * a.group; };
+        // the lane's row; beyond the last one the last one again
+        const auto token_of_row = [&] { return static_cast<int32_t>(divide(min(first_row + n, w.rows - 1), a.by_group)); };
+        const auto head_of_row = [&] { return w.head * a.group + min(first_row + n, w.rows - 1) - token_of_row() * a.group; };
 
         int32_t pages[K::kKeyUnits], own_pages[K::kOwn];
         uint32_t codes[8 * K::kValueUnits];
@@ -836,58 +828,50 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
         }
 
         // q, a lane's 8 elements of its rows for every step
-        f16x8 q[SETS][SPLIT][K::kSteps];
-        float q_sum[SETS], unit[SETS], sum[SETS];
+        f16x8 q[SPLIT][K::kSteps];
+        float q_sum, unit, sum;
         {
             // element of q in slot 0 of a step: the order of the chunks in the LDS
-            const auto at = [&](int r, int s) {
+            const auto at = [&](int s) {
                 const int chunk = 2 * s + h;
-                return (static_cast<int64_t>(w.start) + token_at(r)) * a.q.token + head_at(r) * a.q.head + (chunk < DIM / 16 ? 16 * chunk : 16 * chunk - DIM + 8);
+                return (static_cast<int64_t>(w.start) + token_of_row()) * a.q.token + head_of_row() * a.q.head + (chunk < DIM / 16 ? 16 * chunk : 16 * chunk - DIM + 8);
             };
+            uint32_t largest = 0;
 #pragma unroll
-            for (int r = 0; r < SETS; ++r) {
-                uint32_t largest = 0;
+            for (int s = 0; s < K::kSteps; ++s) {
+                float f[8];
+                load_eight(a.q.p, a.dtype, at(s), f);
 #pragma unroll
-                for (int s = 0; s < K::kSteps; ++s) {
-                    float f[8];
-                    load_eight(a.q.p, a.dtype, at(r, s), f);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) largest = max(largest, magnitude(f[j]));
-                }
-                largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), 32)));
-                const RowScale row_scale(largest);
-                q_sum[r] = 0.0f;
-                // once more, from the cache: held until here they would be twice the registers of everything else
-#pragma unroll
-                for (int s = 0; s < K::kSteps; ++s) {
-                    float f[8];
-                    load_eight(a.q.p, a.dtype, at(r, s), f);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) f[j] = row_scale.scaled(f[j]);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        q_sum[r] += f[j];
-                        const float v = ldexpf(a.key_bits == 8 ? f[j] : f[code_order(4, j)], a.key_bits == 8 || SPLIT == 2 ? 0 : -code_bits(4, j));
-                        q[r][0][s][j] = static_cast<_Float16>(v);
-                        if (SPLIT == 2) q[r][SPLIT - 1][s][j] = static_cast<_Float16>(v - static_cast<float>(q[r][0][s][j]));
-                    }
-                }
-                q_sum[r] += __shfl_xor(q_sum[r], 32);
-                q_sum[r] *= 1.0f / (1 << kRowBits);
-                unit[r] = row_scale.unit();
-                sum[r] = nan_where(row_scale.bad && w.first + token_at(r) >= 0);   // a row that sees something and is not finite
+                for (int j = 0; j < 8; ++j) largest = max(largest, magnitude(f[j]));
             }
+            largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), 32)));
+            const RowScale row_scale(largest);
+            q_sum = 0.0f;
+            // once more, from the cache: held until here they would be twice the registers of everything else
+#pragma unroll
+            for (int s = 0; s < K::kSteps; ++s) {
+                float f[8];
+                load_eight(a.q.p, a.dtype, at(s), f);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[j] = row_scale.scaled(f[j]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    q_sum += f[j];
+                    const float v = ldexpf(a.key_bits == 8 ? f[j] : f[code_order(4, j)], a.key_bits == 8 || SPLIT == 2 ? 0 : -code_bits(4, j));
+                    q[0][s][j] = static_cast<_Float16>(v);
+                    if (SPLIT == 2) q[SPLIT - 1][s][j] = static_cast<_Float16>(v - static_cast<float>(q[0][s][j]));
+                }
+            }
+            q_sum += __shfl_xor(q_sum, 32);
+            q_sum *= 1.0f / (1 << kRowBits);
+            unit = row_scale.unit();
+            sum = nan_where(row_scale.bad && w.first + token_of_row() >= 0);   // a row that sees something and is not finite
         }
 
-        float m[SETS], middle[SETS];
-        f32x16 acc[SETS][K::kBlocks];
+        float m = kNothing, middle = 0.0f;
+        f32x16 acc[K::kBlocks];
 #pragma unroll
-        for (int r = 0; r < SETS; ++r) {
-            m[r] = kNothing;
-            middle[r] = 0.0f;
-#pragma unroll
-            for (int b = 0; b < K::kBlocks; ++b) acc[r][b] = f32x16{};
-        }
+        for (int b = 0; b < K::kBlocks; ++b) acc[b] = f32x16{};
 
         const auto store = [&](int32_t base, int to) {
             const auto store_values = [&](auto bits) {
@@ -940,13 +924,11 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
             const f32x4 v = constants[from][32 * s + 8 * (lane % 16 / 4) + 4 * h + lane % 4];
             const float ceiling = ceilings[from];
             __builtin_amdgcn_sched_barrier(0);
-            f32x16 x[SETS] = {};
+            f32x16 x = {};
 #pragma unroll
-            for (int r = 0; r < SETS; ++r)
+            for (int k = 0; k < K::kSteps; ++k)
 #pragma unroll
-                for (int k = 0; k < K::kSteps; ++k)
-#pragma unroll
-                    for (int i = 0; i < SPLIT; ++i) x[r] = __builtin_amdgcn_mfma_f32_32x32x16_f16(c_keys[k], q[r][i][k], x[r], 0, 0, 0);
+                for (int i = 0; i < SPLIT; ++i) x = __builtin_amdgcn_mfma_f32_32x32x16_f16(c_keys[k], q[i][k], x, 0, 0, 0);
             f16x8 u[K::kBlocks][2];
 #pragma unroll
             for (int b = 0; b < K::kBlocks; ++b)
@@ -954,21 +936,17 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
                 for (int k = 0; k < 2; ++k) u[b][k] = *reinterpret_cast<const f16x8*>(&values[from][0] + (value_at ^ (2 * s + k) << 5) + b * (64 * K::kTile));
             Constants c = {v[0], v[1], v[2], v[3]};
             settled(c.key_zero);
-#pragma unroll
-            for (int r = 0; r < SETS; ++r)
-                each<16>([&](auto e) {
-                    constexpr int i = e, kAt = kDppBroadcast + i;
-                    x[r][i] = add_broadcast<i>(dpp<kAt>(c.key) * x[r][i], c.key_zero, q_sum[r], q_sum[r]);
-                });
+            each<16>([&](auto e) {
+                constexpr int i = e, kAt = kDppBroadcast + i;
+                x[i] = add_broadcast<i>(dpp<kAt>(c.key) * x[i], c.key_zero, q_sum, q_sum);
+            });
             if (a.cap > 0.0f) {
 #pragma unroll
-                for (int r = 0; r < SETS; ++r)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[r][i] = capped<SPLIT == 2>(x[r][i], unit[r], a.cap);
+                for (int i = 0; i < 16; ++i) x[i] = capped<SPLIT == 2>(x[i], unit, a.cap);
             }
             // f(i, whether the row sees key i): key = base + 4 h + a constant, between the window's begin and the last one in sight
-            const auto each_key = [&](int r, auto f) {
-                const int32_t position = w.first + token_at(r);
+            const auto each_key = [&](auto f) {
+                const int32_t position = w.first + token_of_row();
                 const int32_t last = min(position, span.end - 1) - base - 4 * h, before = a.window > 0 ? position - a.window - base - 4 * h : -1;
                 each<16>([&](auto e) {
                     constexpr int kKey = 8 * (e / 4) + e % 4;
@@ -976,79 +954,63 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
                 });
             };
             if (mine.edge(base, 32, a.window)) {
-#pragma unroll
-                for (int r = 0; r < SETS; ++r)
-                    each_key(r, [&](auto e, bool sees) {
-                        constexpr int i = e;
-                        x[r][i] = sees ? x[r][i] : -INFINITY;
-                    });
+                each_key([&](auto e, bool sees) {
+                    constexpr int i = e;
+                    x[i] = sees ? x[i] : -INFINITY;
+                });
             }
-            float top[SETS];
-            bool over = false;
+            float top = kNothing;
 #pragma unroll
-            for (int r = 0; r < SETS; ++r) {
-                top[r] = kNothing;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) top[r] = fmaxf(top[r], x[r][i]);
-                top[r] *= unit[r];
-                over |= top[r] + ceiling > m[r] + kMostWeight;
-            }
-            if (__any(over)) {
+            for (int i = 0; i < 16; ++i) top = fmaxf(top, x[i]);
+            top *= unit;
+            if (__any(top + ceiling > m + kMostWeight)) {
                 const float reach = reach_of(a, c.step, finite(c.middle) ? c.middle : 0.0f);
+                float peak = kNothing;
+                each<16>([&](auto e) {
+                    constexpr int i = e;
+                    peak = fmaxf(peak, fmaf(x[i], unit, dpp<kDppBroadcast + i>(reach)));
+                });
+                peak = fmaxf(peak, __shfl_xor(peak, 32));
+                const float now = peak > m + kMostWeight ? peak - kNewWeight : m;   // a row's doing alone
+                const Shrink less(m - now);
+                m = now;
+                sum = less(sum);
+                middle = less(middle);
 #pragma unroll
-                for (int r = 0; r < SETS; ++r) {
-                    float peak = kNothing;
-                    each<16>([&](auto e) {
-                        constexpr int i = e;
-                        peak = fmaxf(peak, fmaf(x[r][i], unit[r], dpp<kDppBroadcast + i>(reach)));
-                    });
-                    peak = fmaxf(peak, __shfl_xor(peak, 32));
-                    const float now = peak > m[r] + kMostWeight ? peak - kNewWeight : m[r];   // a row's doing alone
-                    const Shrink less(m[r] - now);
-                    m[r] = now;
-                    sum[r] = less(sum[r]);
-                    middle[r] = less(middle[r]);
+                for (int b = 0; b < K::kBlocks; ++b)
 #pragma unroll
-                    for (int b = 0; b < K::kBlocks; ++b)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) acc[r][b][i] = less(acc[r][b][i]);
-                }
+                    for (int i = 0; i < 16; ++i) acc[b][i] = less(acc[b][i]);
             }
             const bool bad = !finite(c.middle);
             if (__any(bad)) {
-#pragma unroll
-                for (int r = 0; r < SETS; ++r)
-                    each_key(r, [&](auto e, bool sees) {
-                        const float none = dpp<kDppBroadcast + e>(nan_where(bad));
-                        sum[r] += sees ? none : 0.0f;
-                    });
+                each_key([&](auto e, bool sees) {
+                    const float none = dpp<kDppBroadcast + e>(nan_where(bad));
+                    sum += sees ? none : 0.0f;
+                });
                 c.middle = bad ? 0.0f : c.middle;
             }
             settled(c.middle);
             if (more) load_part(from, s + 1);
+            f16x8 p[SPLIT][2];
+            float part_sum = 0.0f, part_middle = 0.0f;   // of the part first: one sum over thousands of keys would gather their roundings
+            each<16>([&](auto e) {
+                constexpr int i = e, kAt = kDppBroadcast + i;
+                const float v = __builtin_amdgcn_exp2f(fmaf(x[i], unit, -m));
+                part_sum += v;
+                const float weight = SPLIT == 2 ? rounded(dpp<kAt>(c.step) * v) : dpp<kAt>(c.step) * v;   // the same one for both of its numbers
+                part_middle = add_broadcast<i>(part_middle, c.middle, v, weight);
+                const _Float16 high = static_cast<_Float16>(weight);
+                p[0][i / 8][i % 8] = high;
+                if (SPLIT == 2) p[SPLIT - 1][i / 8][i % 8] = static_cast<_Float16>(weight - static_cast<float>(high));
+            });
+            sum += part_sum;
+            middle += part_middle;
 #pragma unroll
-            for (int r = 0; r < SETS; ++r) {
-                f16x8 p[SPLIT][2];
-                float part_sum = 0.0f, part_middle = 0.0f;   // of the part first: one sum over thousands of keys would gather their roundings
-                each<16>([&](auto e) {
-                    constexpr int i = e, kAt = kDppBroadcast + i;
-                    const float v = __builtin_amdgcn_exp2f(fmaf(x[r][i], unit[r], -m[r]));
-                    part_sum += v;
-                    const float weight = SPLIT == 2 ? rounded(dpp<kAt>(c.step) * v) : dpp<kAt>(c.step) * v;   // the same one for both of its numbers
-                    part_middle = add_broadcast<i>(part_middle, c.middle, v, weight);
-                    const _Float16 high = static_cast<_Float16>(weight);
-                    p[0][i / 8][i % 8] = high;
-                    if (SPLIT == 2) p[SPLIT - 1][i / 8][i % 8] = static_cast<_Float16>(weight - static_cast<float>(high));
-                });
-                sum[r] += part_sum;
-                middle[r] += part_middle;
+            for (int b = 0; b < K::kBlocks; ++b)
 #pragma unroll
-                for (int b = 0; b < K::kBlocks; ++b)
+                for (int k = 0; k < 2; ++k)
 #pragma unroll
-                    for (int k = 0; k < 2; ++k)
-#pragma unroll
-                        for (int i = 0; i < SPLIT; ++i) acc[r][b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(u[b][k], p[i][k], acc[r][b], 0, 0, 0);
-            }
+                    for (int i = 0; i < SPLIT; ++i) acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(u[b][k], p[i][k], acc[b], 0, 0, 0);
         };
 
         if (span.begin < span.end) {
@@ -1078,13 +1040,11 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
             }
         }
 
-#pragma unroll
-        for (int r = 0; r < SETS; ++r) {
-            sum[r] += __shfl_xor(sum[r], 32);
-            middle[r] += __shfl_xor(middle[r], 32);
-            if (row_at(r) >= w.rows) continue;
-            const float scale = is(sum[r], 0.0f) ? 0.0f : 1.0f / sum[r];   // nothing in sight: zeros
-            const int32_t token = token_at(r), head = head_at(r);
+        sum += __shfl_xor(sum, 32);
+        middle += __shfl_xor(middle, 32);
+        if (first_row + n < w.rows) {
+            const float scale = is(sum, 0.0f) ? 0.0f : 1.0f / sum;   // nothing in sight: zeros
+            const int32_t token = token_of_row(), head = head_of_row();
             const int64_t part_row = part_row_of(a, w, token, head);
 #pragma unroll
             for (int b = 0; b < K::kBlocks; ++b)
@@ -1092,12 +1052,12 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
                 for (int i = 0; i < 16; i += 4) {
                     float f[4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) f[j] = fmaf(acc[r][b][i + j], static_cast<float>(1 << kUnitBits), middle[r]) * scale;
+                    for (int j = 0; j < 4; ++j) f[j] = fmaf(acc[b][i + j], static_cast<float>(1 << kUnitBits), middle) * scale;
                     const int column = 32 * b + 2 * i + 4 * (here(lane) / 32);
                     if (a.partial) store_some(a.partial, ACTQ_F32, part_row * DIM + column, f);
                     else store_some(a.out.p, a.dtype, (static_cast<int64_t>(w.start) + token) * a.out.token + head * a.out.head + column, f);
                 }
-            if (a.partial && h == 0) a.partial_sums[part_row] = f32x2{m[r], sum[r]};
+            if (a.partial && h == 0) a.partial_sums[part_row] = f32x2{m, sum};
         }
         __syncthreads();   // the next tile writes the LDS again
     }
@@ -1280,11 +1240,11 @@ int launch_cache_attention(const actq_cache* c, const actq_heads* q, int dtype, 
         constexpr int kDim = decltype(d)::value;
         if (shape.rows != 16) {
             if (shape.rows == 128) {
-                if (dtype == ACTQ_F32) launch(attend_many_kernel<kDim, 2, 4, 1>, blocks, 256, s, a);
-                else launch(attend_many_kernel<kDim, 1, 4, 1>, blocks, 256, s, a);
+                if (dtype == ACTQ_F32) launch(attend_many_kernel<kDim, 2, 4>, blocks, 256, s, a);
+                else launch(attend_many_kernel<kDim, 1, 4>, blocks, 256, s, a);
             } else if constexpr (kDim != 256) {
-                if (dtype == ACTQ_F32) launch(attend_many_kernel<kDim, 2, 8, 1>, blocks, 512, s, a);
-                else launch(attend_many_kernel<kDim, 1, 8, 1>, blocks, 512, s, a);
+                if (dtype == ACTQ_F32) launch(attend_many_kernel<kDim, 2, 8>, blocks, 512, s, a);
+                else launch(attend_many_kernel<kDim, 1, 8>, blocks, 512, s, a);
             }
             return launched(who);
         }
