@@ -146,3 +146,17 @@ def test_caps_of_any_size(new, dim, dtype, softcap):
     q, *rest = _case([340], [new], 2, 1, dim, dtype, seed=80)
     case = (q * 4, *rest)
     _within(_attend(case, softcap=softcap), case, softcap=softcap)
+
+
+@pytest.mark.parametrize("lengths, q_heads, dim, dtype, options", [
+    ([16384], 1, 256, F16, {}),                     # 128 parts, all with keys
+    ([16384, 300], 2, 256, F32, {}),                # the second sequence has keys in three of them
+    ([16384], 4, 128, BF16, {}),                    # 64
+    ([16384, 129, 5000], 1, 128, F32, {}),
+    ([9000, 1], 3, 128, F16, dict(window=6000)),    # parts before the window see nothing
+    ([16384, 77], 2, 64, F32, dict(softcap=5.0)),
+    ([4200], 1, 256, BF16, {}),                     # 33
+])
+def test_one_token_over_many_parts_that_are_joined(lengths, q_heads, dim, dtype, options):
+    case = _case(lengths, [1] * len(lengths), q_heads, 1, dim, dtype, page=64, seed=90 + dim)
+    _within(_attend(case, **options), case, **options)
