@@ -1142,19 +1142,39 @@ struct Shape {
     int64_t tiles, parts, per_part;
 };
 
-// Rows of a sequence and head of the cache from which on the kernel for many rows serves.  Below, tiles of 16 rows read and widen the same keys
-// again, but a workgroup begins sooner.  Few rows -> many rows, us, 8 bits, 32 heads over 8:
-//   16 sequences of 4096, 128, bfloat16   64 rows 87 -> 112, 96 rows 123 -> 115, 128 rows 167 -> 119
-//   one of 8192, 128, bfloat16            64 rows 23 -> 28, 96 rows 29 -> 31, 128 rows 32 -> 34
-//   16 of 4096, 64, binary32              64 rows 51 -> 90, 96 rows 72 -> 92, 128 rows 92 -> 97, 256 rows 154 -> 117
-//   4 of 4096, 256, binary16              64 rows 73 -> 107, 128 rows 122 -> 132, 256 rows 167 -> 197 (there the many need scratch memory)
-constexpr int64_t kManyRows = 97, kManyRowsWide = 321;
+// Which kernel serves, by the rows of a sequence and head of the cache.  The one for few reads and widens the same keys again for every 16 rows, but a
+// workgroup of it begins sooner and leaves room for a second; the one for many does so for every 128 or 256.  Few -> many, us, 8 bits, 32 heads over 8:
+//   heads of 128       64 rows  one sequence of 8192, bfloat16  24.5 -> 26.9, binary32 32.3 -> 29.6; 16 of 4096  90.7 -> 88.9, 121 -> 130
+//                      80 rows                                  28.3 -> 27.9,          37.9 -> 31.3;             120 -> 90.2,  191 -> 130
+//                     320 rows                                  46.4 -> 47.6,          77.9 -> 73.0;             264 -> 191,   494 -> 370
+//   heads of 64: the workgroups of 16 rows decide, kLoad of them half filling the card
+//                     256 rows  one of 8192 (128)               23.1 -> 30.5,          28.2 -> 34.5;   4 of 4096 (512)   32.3 -> 33.6, 41.7 -> 40.8
+//                     512 rows               (256)              34.2 -> 37.6,          44.0 -> 43.5             (1024)   57.3 -> 49.4, 76.0 -> 62.6
+//                     768 rows               (384)              54.6 -> 44.2,          73.2 -> 54.8;  16 of 4096, 80 rows (640)  66.0 -> 61.4, 71.9 -> 72.5
+//   heads of 256, 16-bit types: likewise above 128 rows
+//                      80 rows  one of 8192                     59.7 -> 55.4;  4 of 4096  92.0 -> 104;  16 of 4096  408 -> 308
+//                     256 rows               (128)              105 -> 121;               (512)  182 -> 175          886 -> 600
+//   heads of 256, binary32 (where the many need 600 bytes of scratch memory a lane): the sequences and heads of the cache decide
+//                     128 rows  one of 8192 (8)                 124 -> 127;  4 of 4096 (32)  228 -> 253;  16 of 4096 (128)  1027 -> 861
+//                    1024 rows                                  611 -> 803;                 1236 -> 1543                    6811 -> 6003
+constexpr int64_t kManyRows = 65, kLoad = 256, kManyGroups = 65;
 
-Shape shape_of(const actq_cache* c, int32_t heads, int64_t sequences, int64_t max_query, int64_t max_length, int32_t window)
+bool many_rows(int32_t dim, bool wide, int64_t groups, int64_t rows)
+{
+    if (rows < kManyRows) return false;
+    const bool loaded = groups * ceil_div(rows, 16) > kLoad;
+    return dim == 128 || (dim == 64 ? loaded : wide ? groups >= kManyGroups : rows <= 128 || loaded);
+}
+
+// Rows of a workgroup of it: 256 but where they need too many registers, in heads of 256, and for up to 128 rows of binary32 in heads of 128
+// (128 -> 256, us: 16 sequences of 4096, 128 rows 137 -> 154, 160 rows 243 -> 169; heads of 64 92 -> 74, bfloat16 in heads of 128 113 -> 94).
+int many_rows_of(int32_t dim, bool wide, int64_t rows) { return dim == 256 || (dim == 128 && wide && rows <= 128) ? 128 : 256; }
+
+Shape shape_of(const actq_cache* c, int32_t heads, int64_t sequences, int64_t max_query, int64_t max_length, int32_t window, bool wide)
 {
     const int64_t group = heads / c->heads, groups = sequences * c->heads, rows = max_query < 1 ? group : max_query * group;
     Shape s;
-    s.rows = rows < (c->dim == 256 ? kManyRowsWide : kManyRows) ? 16 : rows <= 128 || c->dim == 256 ? 128 : 256;
+    s.rows = many_rows(c->dim, wide, groups, rows) ? many_rows_of(c->dim, wide, rows) : 16;
     s.tiles = ceil_div(rows, s.rows);
     if (s.tiles > kMostBlocks / groups) s.tiles = kMostBlocks / groups;
     // keys of a step; the fewest that are worth a workgroup; workgroups that are wanted, as many as are resident: two per compute unit, one of 256
@@ -1184,8 +1204,12 @@ int by_bits(int bits, F f)
 uint64_t cache_attention_workspace(const actq_cache* c, int32_t heads, int64_t tokens, int64_t sequences, int64_t max_query, int64_t max_length, int32_t window)
 {
     if (tokens == 0 || sequences == 0) return 0;
-    const Shape s = shape_of(c, heads, sequences, max_query, max_length, window);
-    return s.parts == 1 ? 0 : static_cast<uint64_t>(s.parts) * tokens * heads * (c->dim + 2) * sizeof(float);
+    int64_t parts = 1;   // of either kind of type: the caller asks without one
+    for (const bool wide : {false, true}) {
+        const Shape s = shape_of(c, heads, sequences, max_query, max_length, window, wide);
+        if (s.parts > parts) parts = s.parts;
+    }
+    return parts == 1 ? 0 : static_cast<uint64_t>(parts) * tokens * heads * (c->dim + 2) * sizeof(float);
 }
 
 int launch_cache_attention(const actq_cache* c, const actq_heads* q, int dtype, int64_t tokens, int64_t sequences, const int32_t* table, int32_t table_width,
@@ -1193,7 +1217,8 @@ int launch_cache_attention(const actq_cache* c, const actq_heads* q, int dtype, 
                            const actq_heads* out, void* workspace, void* stream)
 {
     const char* who = "actq_cache_attention";
-    const Shape shape = shape_of(c, q->heads, sequences, max_query, max_length, window);
+    const bool wide = dtype == ACTQ_F32;
+    const Shape shape = shape_of(c, q->heads, sequences, max_query, max_length, window, wide);
     AttendArgs a = {};
     a.key_codes = c->key_codes;
     a.key_header = c->key_header;
@@ -1238,20 +1263,26 @@ int launch_cache_attention(const actq_cache* c, const actq_heads* q, int dtype, 
     const unsigned blocks = static_cast<unsigned>(sequences * c->heads * shape.parts * shape.tiles);
     const int rc = by_dim(c->dim, [&](auto d) {
         constexpr int kDim = decltype(d)::value;
-        if (shape.rows != 16) {
-            if (shape.rows == 128) {
-                if (dtype == ACTQ_F32) launch(attend_many_kernel<kDim, 2, 4>, blocks, 256, s, a);
-                else launch(attend_many_kernel<kDim, 1, 4>, blocks, 256, s, a);
-            } else if constexpr (kDim != 256) {
-                if (dtype == ACTQ_F32) launch(attend_many_kernel<kDim, 2, 8>, blocks, 512, s, a);
+        if (shape.rows == 256) {
+            if constexpr (kDim != 256) {
+                if (wide) launch(attend_many_kernel<kDim, 2, 8>, blocks, 512, s, a);
                 else launch(attend_many_kernel<kDim, 1, 8>, blocks, 512, s, a);
+            }
+            return launched(who);
+        }
+        if (shape.rows == 128) {
+            if constexpr (kDim == 256) {
+                if (wide) launch(attend_many_kernel<kDim, 2, 4>, blocks, 256, s, a);
+                else launch(attend_many_kernel<kDim, 1, 4>, blocks, 256, s, a);
+            } else if constexpr (kDim == 128) {
+                launch(attend_many_kernel<kDim, 2, 4>, blocks, 256, s, a);
             }
             return launched(who);
         }
         return by_bits(c->key_bits, [&](auto kb) {
             return by_bits(c->value_bits, [&](auto vb) {
                 constexpr int kKey = decltype(kb)::value, kValue = decltype(vb)::value;
-                if (dtype == ACTQ_F32) launch(attend_few_kernel<kDim, 2, kKey, kValue>, blocks, kFewWaves * 64, s, a);
+                if (wide) launch(attend_few_kernel<kDim, 2, kKey, kValue>, blocks, kFewWaves * 64, s, a);
                 else launch(attend_few_kernel<kDim, 1, kKey, kValue>, blocks, kFewWaves * 64, s, a);
                 return launched(who);
             });

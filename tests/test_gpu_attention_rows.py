@@ -27,9 +27,9 @@ def _case(lengths, news, q_heads, kv, dim, dtype, key_bits=8, value_bits=8, page
     return torch.randn((int(start[-1]), q_heads, dim), generator=g).to(dtype), cache, table, torch.tensor(lengths, dtype=torch.int32), start, dim
 
 
-def _attend(case, **options):
+def _attend(case, max_query=0, **options):
     q, cache, table, lengths, start, _ = case
-    return B.cache_attention(q.to(DEV), *cache, table.to(DEV), lengths.to(DEV), start.to(DEV), int(start.diff().max()), int(lengths.max()), **options)
+    return B.cache_attention(q.to(DEV), *cache, table.to(DEV), lengths.to(DEV), start.to(DEV), max(max_query, int(start.diff().max())), int(lengths.max()), **options)
 
 
 def _within(out, case, **options):
@@ -159,4 +159,29 @@ def test_caps_of_any_size(new, dim, dtype, softcap):
 ])
 def test_one_token_over_many_parts_that_are_joined(lengths, q_heads, dim, dtype, options):
     case = _case(lengths, [1] * len(lengths), q_heads, 1, dim, dtype, page=64, seed=90 + dim)
+    _within(_attend(case, **options), case, **options)
+
+
+@pytest.mark.parametrize("key_bits, value_bits", [(8, 8), (8, 4), (4, 8), (4, 4)])
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("new, options", [(50, {}), (190, dict(window=70)), (190, dict(softcap=4.0)), (9, {})])
+def test_heads_of_64_by_the_kernel_for_many_rows(new, options, dtype, key_bits, value_bits):
+    """It takes heads of 64 where workgroups are many; a most number of new tokens that is not reached makes them so.  Both kernels keep to the bound, and
+    what one row holds stays out of the others in this one too."""
+    q, cache, table, *rest = case = _case([420, 33], [new, 7], 4, 2, 64, dtype, key_bits, value_bits, seed=100)
+    out = _attend(case, max_query=4000, **options)
+    _within(out, case, **options)
+    _within(_attend(case, **options), case, **options)
+    changed = q.clone()
+    changed[new - 1, 0, 3] = float("inf")
+    cache[3][table[0, 419 // 16].long(), :, 419 % 16] *= 2.0 ** 20
+    again = _attend((changed, cache, table, *rest), max_query=4000, **options)
+    assert torch.isnan(again[new - 1, 0]).all() and torch.equal(again[:new - 1], out[:new - 1]) and torch.equal(again[new:], out[new:])
+
+
+@pytest.mark.parametrize("key_bits, value_bits", [(8, 8), (4, 4)])
+@pytest.mark.parametrize("options", [{}, dict(window=20, softcap=4.0)])
+def test_binary32_in_heads_of_256_by_the_kernel_for_many_rows(options, key_bits, value_bits):
+    """It takes them where sequences and heads of the cache are more than 64."""
+    case = _case([40 - n for n in range(33)], [36 - n for n in range(33)], 4, 2, 256, F32, key_bits, value_bits, seed=101)
     _within(_attend(case, **options), case, **options)
