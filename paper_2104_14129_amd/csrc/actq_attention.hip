@@ -1070,8 +1070,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
 constexpr int kJoinThreads = 256;
 constexpr int kMostParts = 128;
 
-// SHARED: all teams share a row; else each has its own, which is faster below kSharedParts parts.
-constexpr int kSharedParts = 16;
+// SHARED: all teams share a row; else each has its own, which is faster below kSharedParts parts (own -> shared, us of both kernels: one sequence, 32 rows of
+// 128, 2 parts 11.0 -> 11.3, 4 parts 11.1 -> 11.5, 8 parts 11.8 -> 11.6, 15 parts 13.2 -> 12.1; four sequences 4 parts 11.8 -> 12.0, 8 parts 12.7 -> 12.3).
+constexpr int kSharedParts = 8;
 
 template <int DIM, bool SHARED>
 __global__ __launch_bounds__(kJoinThreads) void attend_join_kernel(AttendArgs a)
