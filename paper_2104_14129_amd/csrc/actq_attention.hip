@@ -348,7 +348,7 @@ struct Shrink {
 // keys, which it transposes itself as it widens them.  The next block's codes are loaded while one is computed.
 constexpr int kFewWaves = 4;   // [8, which need no join up to 1024 keys: one token over 1021 11.0 -> 12.4 us]
 
-// SPLIT: binary16 numbers for one of q and of the weights, 1 for 16-bit types, 2 for binary32.
+// SPLIT: binary16 numbers for one of q, 1 for 16-bit types, 2 for binary32.
 template <int DIM, int SPLIT, int KEY_BITS, int VALUE_BITS>
 struct Few {
     static constexpr int kTiles = DIM == 256 ? 2 : 4, kBlock = 16 * kTiles;
@@ -386,7 +386,8 @@ __device__ __forceinline__ void load_words(const uint8_t* p, uint32_t* w)
     }
 }
 
-template <int DIM, int SPLIT, int KEY_BITS, int VALUE_BITS>
+// WEIGHTS: binary16 numbers for a weight (by_numbers).
+template <int DIM, int SPLIT, int WEIGHTS, int KEY_BITS, int VALUE_BITS>
 __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArgs a)
 {
     typedef Few<DIM, SPLIT, KEY_BITS, VALUE_BITS> K;
@@ -575,25 +576,27 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
                 c.middle = bad ? 0.0f : c.middle;
             }
             settled(c.middle);
-            f16x8 p[SPLIT][K::kTiles / 2];
+            f16x8 p[WEIGHTS][K::kTiles / 2];
             float block_sum = 0.0f, block_middle = 0.0f;   // of the block first: one sum over thousands of keys would gather their roundings
             each<K::kTiles>([&](auto t) {
                 each<4>([&](auto e) {
                     constexpr int i = e, kAt = kDppBroadcast + 4 * t + i;
                     const float v = __builtin_amdgcn_exp2f(fmaf(x[t][i], unit, -m));
                     block_sum += v;
-                    const float weight = SPLIT == 2 ? rounded(dpp<kAt>(c.step) * v) : dpp<kAt>(c.step) * v;   // the same one for both of its numbers
+                    const float weight = WEIGHTS == 2 ? rounded(dpp<kAt>(c.step) * v) : dpp<kAt>(c.step) * v;   // the same one for both of its numbers
                     block_middle = add_broadcast<4 * t + i>(block_middle, c.middle, v, weight);
                     const _Float16 high = static_cast<_Float16>(weight);
                     p[0][t / 2][4 * (t % 2) + i] = high;
-                    if (SPLIT == 2) p[SPLIT - 1][t / 2][4 * (t % 2) + i] = static_cast<_Float16>(weight - static_cast<float>(high));
+                    if (WEIGHTS == 2) p[WEIGHTS - 1][t / 2][4 * (t % 2) + i] = static_cast<_Float16>(weight - static_cast<float>(high));
                 });
             });
             sum += block_sum;
             middle += block_middle;
             if (SPLIT == 1) {
 #pragma unroll
-                for (int s = 0; s < K::kTiles / 2; ++s) weights = multiply(ones, p[0][s], weights);
+                for (int s = 0; s < K::kTiles / 2; ++s)
+#pragma unroll
+                    for (int h = 0; h < WEIGHTS; ++h) weights = multiply(ones, p[h][s], weights);
             }
 #pragma unroll
             for (int s = 0; s < K::kTiles / 2; ++s)
@@ -608,7 +611,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
                         values[2 * k + 1] = pair[1];
                     }
 #pragma unroll
-                    for (int h = 0; h < SPLIT; ++h) acc[i] = multiply(values, p[h][s], acc[i]);
+                    for (int h = 0; h < WEIGHTS; ++h) acc[i] = multiply(values, p[h][s], acc[i]);
                 });
         };
 
@@ -719,7 +722,7 @@ struct Many {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-template <int DIM, int SPLIT, int WAVES>
+template <int DIM, int SPLIT, int WEIGHTS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_kernel(AttendArgs a)
 {
     typedef Many<DIM, SPLIT, WAVES> K;
@@ -991,17 +994,17 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
             }
             settled(c.middle);
             if (more) load_part(from, s + 1);
-            f16x8 p[SPLIT][2];
+            f16x8 p[WEIGHTS][2];
             float part_sum = 0.0f, part_middle = 0.0f;   // of the part first: one sum over thousands of keys would gather their roundings
             each<16>([&](auto e) {
                 constexpr int i = e, kAt = kDppBroadcast + i;
                 const float v = __builtin_amdgcn_exp2f(fmaf(x[i], unit, -m));
                 part_sum += v;
-                const float weight = SPLIT == 2 ? rounded(dpp<kAt>(c.step) * v) : dpp<kAt>(c.step) * v;   // the same one for both of its numbers
+                const float weight = WEIGHTS == 2 ? rounded(dpp<kAt>(c.step) * v) : dpp<kAt>(c.step) * v;   // the same one for both of its numbers
                 part_middle = add_broadcast<i>(part_middle, c.middle, v, weight);
                 const _Float16 high = static_cast<_Float16>(weight);
                 p[0][i / 8][i % 8] = high;
-                if (SPLIT == 2) p[SPLIT - 1][i / 8][i % 8] = static_cast<_Float16>(weight - static_cast<float>(high));
+                if (WEIGHTS == 2) p[WEIGHTS - 1][i / 8][i % 8] = static_cast<_Float16>(weight - static_cast<float>(high));
             });
             sum += part_sum;
             middle += part_middle;
@@ -1010,7 +1013,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
 #pragma unroll
-                    for (int i = 0; i < SPLIT; ++i) acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(u[b][k], p[i][k], acc[b], 0, 0, 0);
+                    for (int i = 0; i < WEIGHTS; ++i) acc[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(u[b][k], p[i][k], acc[b], 0, 0, 0);
         };
 
         if (span.begin < span.end) {
@@ -1194,6 +1197,20 @@ Shape shape_of(const actq_cache* c, int32_t heads, int64_t sequences, int64_t ma
     return s;
 }
 
+// Numbers of binary16 for an element of q and for a weight.  One holds q exactly but for binary32.  A weight of one number costs a bfloat16 result 1 % of its
+// error.  A binary16 result it costs up to 70 % where few keys share the weight, so there it has two up to kFewKeys keys: beyond, a key's
+// rounding is a small part of a result that does not vanish, and twice the second products cost more (32 sequences of up to 16384, 4 bits
+// 81 -> 88 us; 2048 tokens over 32768 1340 -> 1730 us; one token over 1021 0.5 us).
+constexpr int64_t kFewKeys = 1024;
+
+template <typename F>
+int by_numbers(int dtype, int64_t keys, F f)
+{
+    constexpr std::integral_constant<int, 1> one;
+    constexpr std::integral_constant<int, 2> two;
+    return dtype == ACTQ_F32 ? f(two, two) : dtype == ACTQ_F16 && keys <= kFewKeys ? f(one, two) : f(one, one);
+}
+
 template <typename F>
 int by_bits(int bits, F f)
 {
@@ -1263,29 +1280,21 @@ int launch_cache_attention(const actq_cache* c, const actq_heads* q, int dtype, 
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const unsigned blocks = static_cast<unsigned>(sequences * c->heads * shape.parts * shape.tiles);
     const int rc = by_dim(c->dim, [&](auto d) {
-        constexpr int kDim = decltype(d)::value;
-        if (shape.rows == 256) {
-            if constexpr (kDim != 256) {
-                if (wide) launch(attend_many_kernel<kDim, 2, 8>, blocks, 512, s, a);
-                else launch(attend_many_kernel<kDim, 1, 8>, blocks, 512, s, a);
-            }
-            return launched(who);
-        }
-        if (shape.rows == 128) {
-            if constexpr (kDim == 256) {
-                if (wide) launch(attend_many_kernel<kDim, 2, 4>, blocks, 256, s, a);
-                else launch(attend_many_kernel<kDim, 1, 4>, blocks, 256, s, a);
-            } else if constexpr (kDim == 128) {
-                launch(attend_many_kernel<kDim, 2, 4>, blocks, 256, s, a);
-            }
-            return launched(who);
-        }
-        return by_bits(c->key_bits, [&](auto kb) {
-            return by_bits(c->value_bits, [&](auto vb) {
-                constexpr int kKey = decltype(kb)::value, kValue = decltype(vb)::value;
-                if (wide) launch(attend_few_kernel<kDim, 2, kKey, kValue>, blocks, kFewWaves * 64, s, a);
-                else launch(attend_few_kernel<kDim, 1, kKey, kValue>, blocks, kFewWaves * 64, s, a);
+        return by_numbers(dtype, window > 0 && window < max_length ? window : max_length, [&](auto split, auto weights) {
+            constexpr int kDim = decltype(d)::value, kSplit = decltype(split)::value, kWeights = decltype(weights)::value;
+            if (shape.rows == 256) {
+                if constexpr (kDim != 256) launch(attend_many_kernel<kDim, kSplit, kWeights, 8>, blocks, 512, s, a);
                 return launched(who);
+            }
+            if (shape.rows == 128) {
+                if constexpr (kDim == 256 || (kDim == 128 && kSplit == 2)) launch(attend_many_kernel<kDim, kSplit, kWeights, 4>, blocks, 256, s, a);
+                return launched(who);
+            }
+            return by_bits(c->key_bits, [&](auto kb) {
+                return by_bits(c->value_bits, [&](auto vb) {
+                    launch(attend_few_kernel<kDim, kSplit, kWeights, decltype(kb)::value, decltype(vb)::value>, blocks, kFewWaves * 64, s, a);
+                    return launched(who);
+                });
             });
         });
     });

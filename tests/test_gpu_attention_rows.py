@@ -185,3 +185,15 @@ def test_binary32_in_heads_of_256_by_the_kernel_for_many_rows(options, key_bits,
     """It takes them where sequences and heads of the cache are more than 64."""
     case = _case([40 - n for n in range(33)], [36 - n for n in range(33)], 4, 2, 256, F32, key_bits, value_bits, seed=101)
     _within(_attend(case, **options), case, **options)
+
+
+@pytest.mark.parametrize("lengths, news, max_query", [([1], [1], 0), ([2, 1, 3], [1, 1, 1], 0), ([15], [15], 0), ([100, 41], [1, 1], 0), ([1000], [3], 0), ([120], [120], 4000), ([60], [60], 0)])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_a_16_bit_result_over_few_keys_is_off_by_its_own_rounding(dtype, dim, lengths, news, max_query):
+    """The error is that of rounding the definition's result once, and 5 % for everything before that: a weight held in one binary16 number would add a half
+    to a binary16 result's, and 1 to 3 % (a 64th of the squares, at most 2.5 times that over one key) to a bfloat16 one's."""
+    case = _case(lengths, news, 8, 4, dim, dtype, seed=110)
+    want = torch.from_numpy(R.attention(*case)[0])
+    off = (_attend(case, max_query=max_query).cpu().double() - want).norm()
+    assert float(off / (want.to(dtype).double() - want).norm()) < 1.05
