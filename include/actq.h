@@ -388,7 +388,8 @@ int actq_linear_backward(const void* grad_y, const void* weight, const void* x, 
  * side in the output of one projection are passed as they are.  It is aligned to its
  * element size.  The descriptors live in HOST memory, the pointers inside are device
  * pointers.  tokens is at least 0 with tokens * heads < 2^26; no token is no work.
- * Every type of actq_dtype is taken; arithmetic is binary32, a result is rounded once.
+ * Every type of actq_dtype is taken; arithmetic is binary32 and a result is rounded once,
+ * but for two operands of the attention (see there).
  */
 typedef struct actq_heads {
     void* data;           /* element (0, 0, 0); may be NULL where tokens is 0 */
@@ -507,6 +508,13 @@ int actq_cache_read(const actq_cache* cache, const int64_t* slots, int64_t token
  * holds, a page to the cache's last, rows to [0, tokens); what such entries give is
  * unspecified, and nothing outside the buffers is read or written.  So is the output of a row of q
  * that belongs to no sequence.
+ *
+ * Scores, their statistics and all sums are binary32.  q is multiplied as one binary16 number
+ * an element, scaled by a power of two of its row (exact for 16-bit types), or as two of them
+ * (22 bits) for ACTQ_F32.  The weights p * step are rounded to two binary16 numbers for
+ * ACTQ_F32 and for ACTQ_F16 over at most 1024 keys (the smaller of max_length and window), else
+ * to one.  Against 64 bits a result is then off by 1e-7 to 4e-7 of its size (ACTQ_F32), or by what rounding
+ * it once costs and a few per cent more.  A cap of 16-bit types is exact to 2^-21 of the score.
  *
  * q, out       [tokens, heads, dim] of type dt, heads a multiple of the cache's, dim the cache's
  * table        device [sequences, table_width] int32

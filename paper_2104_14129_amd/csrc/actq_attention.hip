@@ -25,10 +25,11 @@
 // Where there are few rows the keys are cut into parts, whose outputs a second kernel joins.
 //
 // Measured on one MI355X (a large library product 1.1 PFLOP/s, a copy 5.2 TB/s).  Few rows are bound by memory where all compute units
-// have work: 64 sequences of 8192 tokens, 32 heads over 8 of 128, 8 bits 197 us (5.8 TB/s), 4 bits 121 us (5.0); 32 sequences of lengths up to
-// 16384 (4 bits) 78 + 5 us (4.0), the longest ones' workgroups being the last.  Many rows are bound by vector instructions and products that
-// hardly overlap (some 4150 of the 6200 cycles of a 64-key tile are vector instructions, of which a score costs 9): 2048 tokens over 32768, 8 bits, bfloat16
-// 1.35 ms (790 TFLOP/s).  The error against 64 bits is that of binary32 operations rounded once.
+// have work and registers suffice: 64 sequences of 8192 tokens, 32 heads over 8 of 128, 8 bits 208 us, 4 bits 110 us (both 5.5 TB/s); 32 sequences of lengths up
+// to 16384 (4 bits) 78 + 5 us (4.0), the longest ones' workgroups being the last; heads of 256 spill (32 sequences of 8192, 8 bits: bfloat16 318 us, 3.5 TB/s, binary32
+// 557 us, 2.0; binary32 of 128 182 us, 3.1).  Many rows are bound by vector instructions (53 % of a SIMD's cycles) and products (31 %) that hardly overlap:
+// 2048 tokens over 32768, 8 bits, bfloat16 1.35 ms (790 TFLOP/s).  The error against 64 bits: binary32 1e-7 to 4e-7 of the result; 16-bit types that
+// of the result's own rounding, up to 3 % more.
 #include "actq_heads.h"
 
 namespace actq {

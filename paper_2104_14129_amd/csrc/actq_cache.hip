@@ -7,7 +7,7 @@
 //
 // What bounds it: memory.  A head is 8, 16 or 32 lanes of eight elements; a lane handles a token's key and value together, so that
 // the slot is looked up once and two loads are in flight.  Measured on one MI355X, whose copy of 1 GiB reaches 5.2 TB/s: 65536 tokens of 8 heads of 128
-// read from 8 bits to bfloat16 83 us (5.0 TB/s), 8191 tokens written from binary16 to 4 bits 11.5 us (3.8 TB/s), 64 tokens 3 us.
+// read from 8 bits to bfloat16 83 us (5.0 TB/s), 8191 tokens written from binary16 to 4 bits 12.9 us (3.3 TB/s), 64 tokens 3 us.
 #include "actq_heads.h"
 
 namespace actq {

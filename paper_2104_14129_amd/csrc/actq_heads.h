@@ -86,7 +86,7 @@ constexpr int kDppXor1 = 0xB1, kDppXor2 = 0x4E, kDppHalfMirror = 0x141, kDppMirr
 // Of an instruction of ours it does not know what it has to wait for: a value that has just been written takes two cycles to be seen
 // by other lanes, so `settled` goes first; and the result of an exponential one cycle to be seen at all, so `after` is something that was
 // computed from it.  That nothing has come between is looked up in the assembly of every build, which fails otherwise: eight of them behind a wait in
-// one block of assembly would need no such check, but cost the schedule as much (1573 us), and a wait in each half of that (1452 us).
+// one block of assembly would need no such check, but cost the schedule nearly as much (1573 us); a wait in each costs less (1452 us).
 __device__ __forceinline__ void settled(float& v) { asm volatile("s_nop 1" : "+v"(v)); }
 
 template <int AT>
