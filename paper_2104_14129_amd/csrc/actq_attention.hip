@@ -210,8 +210,9 @@ struct RowScale {
     int exponent;
     bool bad;
 
-    __device__ __forceinline__ explicit RowScale(uint32_t largest)
-        : exponent(min(max(static_cast<int>(largest >> 23) - 127, -64), 126)), bad(largest >= 0x7f800000u) {}
+    // With a cap, the cap in the row's unit has to stay a number.
+    __device__ __forceinline__ RowScale(uint32_t largest, bool capped)
+        : exponent(min(max(static_cast<int>(largest >> 23) - 127, capped ? -64 : -100), 126)), bad(largest >= 0x7f800000u) {}
 
     // An element as it goes to the matrix instructions, zero in a row that is none.
     __device__ __forceinline__ float scaled(float v) const { return bad ? 0.0f : ldexpf(v, kRowBits - exponent); }
@@ -468,7 +469,7 @@ __global__ __launch_bounds__(kFewWaves * 64, 2) void attend_few_kernel(AttendArg
             }
             largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), 16)));
             largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), 32)));
-            const RowScale row_scale(largest);
+            const RowScale row_scale(largest, a.cap > 0.0f);
 #pragma unroll
             for (int s = 0; s < K::kSteps; ++s)
 #pragma unroll
@@ -849,7 +850,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 2 : 1) void attend_many_ke
                 for (int j = 0; j < 8; ++j) largest = max(largest, magnitude(f[j]));
             }
             largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), 32)));
-            const RowScale row_scale(largest);
+            const RowScale row_scale(largest, a.cap > 0.0f);
             q_sum = 0.0f;
             // once more, from the cache: held until here they would be twice the registers of everything else
 #pragma unroll

@@ -197,3 +197,14 @@ def test_a_16_bit_result_over_few_keys_is_off_by_its_own_rounding(dtype, dim, le
     want = torch.from_numpy(R.attention(*case)[0])
     off = (_attend(case, max_query=max_query).cpu().double() - want).norm()
     assert float(off / (want.to(dtype).double() - want).norm()) < 1.05
+
+
+@pytest.mark.parametrize("new, dim", [(1, 64), (130, 128), (330, 256)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("size", [-95, 60])
+def test_queries_of_any_size_under_a_scale_that_makes_up_for_it(new, dim, dtype, size):
+    """Powers of two on both sides: the scores, and so the outputs, are those of ordinary queries."""
+    q, *rest = case = _case([340], [new], 2, 1, dim, dtype, seed=120)
+    want = _attend(case)
+    out = _attend(((q.float() * 2.0 ** size).to(dtype), *rest), scale=dim ** -0.5 * 2.0 ** -size)
+    assert torch.equal(out, want)
