@@ -513,7 +513,8 @@ int actq_cache_read(const actq_cache* cache, const int64_t* slots, int64_t token
  * an element, scaled by a power of two of its row (exact for 16-bit types), or as two of them
  * (22 bits) for ACTQ_F32.  The weights p * step are rounded to two binary16 numbers for
  * ACTQ_F32 and for ACTQ_F16 over at most 1024 keys (the smaller of max_length and window), else
- * to one.  Against 64 bits a result is then off by 1e-7 to 4e-7 of its size (ACTQ_F32), or by what rounding
+ * to one; codes of 16-bit types are summed as they lie, off by up to 2^-19 (8 bits) or 2^-16 (4 bits) of
+ * the largest product.  Against 64 bits a result is then off by 1e-7 to 4e-7 of its size (ACTQ_F32), or by what rounding
  * it once costs and a few per cent more.  A cap of 16-bit types is exact to 2^-21 of the score.
  *
  * q, out       [tokens, heads, dim] of type dt, heads a multiple of the cache's, dim the cache's

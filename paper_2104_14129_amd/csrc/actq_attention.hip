@@ -3,12 +3,15 @@
 //   out = sum_j p_j v_j / sum_j p_j,  p_j = 2^(x_j - m),  x_j = log2(e) cap(scale q . k_j)
 //
 // with k_j = Zk_j + step_j code_j and v_j likewise.  The codes stay whole numbers: as they are, a byte or a nibble under zeros, they
-// are subnormal binary16 numbers code * 2^-24, which the matrix instructions multiply exactly, so that
+// are subnormal binary16 numbers code * 2^-24, whose products the matrix instructions round no further than in summing them, so that
 //   q . k_j = step_j 2^24 (q . code_j 2^-24) + Zk_j sum(q)
-// has no rounding but that of its binary32 sum.  A row of q is scaled by a power of two of its own, so that its largest element fills
-// binary16's range: exact for 16-bit types but for elements below 2^-27 of the row's largest one (2^-23 beside keys of 4 bits), while binary32 takes two
-// binary16 numbers, 22 bits.  Its scores stay in the row's unit until the exponential, whose subtraction of m multiplies by the unit in the same
-// instruction.  What one row of q holds has so no part in another's; a row with an element that is no finite number is none.
+// is off by that sum alone.  The terms of a sum are cut at so many bits below where the largest one could begin; a sum of 32 products of bytes is off by 2^-21
+// of the largest one (2^-19 at worst), of nibbles, with their leading zeros, by 2^-20 (2^-16): a sixteenth of what rounding a binary16 result costs, for which
+// moving every nibble up is too dear (32 sequences of up to 16384, 4 bits 81.5 -> 86 us).  A row of q is scaled by a power of two of its own, so that its
+// largest element fills binary16's range: exact for 16-bit types but for elements below 2^-27 of the row's largest one (2^-23 beside keys of 4 bits),
+// while binary32 takes two binary16 numbers, 22 bits, and centred codes, which have no leading zeros.  Scores stay in the row's unit until the exponential,
+// whose subtraction of m multiplies by the unit in the same instruction.  What one row of q holds has so no part in another's; a row with an element that is no
+// finite number is none.
 // The values' codes are centred, u_j = code_j - c, and
 //   sum_j p_j v_j = sum_j (p_j step_j) u_j + sum_j p_j (Zv_j + c step_j),
 // the second sum in binary32, one number per row.  p_j step_j is rounded to binary16 (to two of them for binary32 outputs); centred codes keep

@@ -208,3 +208,22 @@ def test_queries_of_any_size_under_a_scale_that_makes_up_for_it(new, dim, dtype,
     want = _attend(case)
     out = _attend(((q.float() * 2.0 ** size).to(dtype), *rest), scale=dim ** -0.5 * 2.0 ** -size)
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("key_bits, value_bits", [(8, 4), (4, 4), (8, 8)])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("seed", range(8))
+def test_columns_that_the_heaviest_key_leaves_alone(seed, dtype, key_bits, value_bits):
+    """Steps from 2^-12 to 2^12 of their size: in a column where the heaviest key's code is the middle one, the others' small values count.  A matrix
+    instruction's sum of bytes as they lie is off by 2^-19 of the largest product at worst, of nibbles by 2^-16, and a block of 64 keys takes two."""
+    q, cache, table, *rest = case = _case([16, 15, 64, 33], [1, 15, 2, 5], 4, 2, 64, dtype, key_bits, value_bits, seed=seed)
+    g = torch.Generator().manual_seed(seed)
+    cache[3].mul_(torch.exp2(torch.randint(-12, 12, cache[3].shape[:3], generator=g)).to(DEV)[..., None])
+    want, bound = R.attention(*case)
+    for token, head, ((kc, kz, ks, _), (_, _, vs, _)) in R._rows(q.double().numpy(), cache, table, *rest[:2], 64, 0):
+        s = (kz + ks * kc) @ q[token, head].double().numpy() / 8
+        p = np.exp(s - s.max())
+        bound[token, head] += 2.0 ** (-15 if value_bits == 4 else -18) * (p / p.sum() * vs[:, 0]).max() * (2 ** value_bits - 1)
+    off = np.abs(_attend(case).cpu().double().numpy() - want)
+    fits = np.abs(want) < (6e4 if dtype == F16 else 1e38)
+    assert (off <= bound)[fits].all(), float((off / bound)[fits].max())
