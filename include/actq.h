@@ -45,7 +45,7 @@ typedef enum actq_status {
 typedef enum actq_dtype {
     ACTQ_F32 = 0, /* IEEE binary32 */
     ACTQ_F16 = 1, /* IEEE binary16; widened exactly to binary32 before any arithmetic */
-    ACTQ_BF16 = 2 /* bfloat16: the calls for attention heads at the end of this file only */
+    ACTQ_BF16 = 2 /* bfloat16: the calls for attention heads and for a layer at the end of this file only */
 } actq_dtype;
 
 /* Per-group header kept beside the codes. */
@@ -535,6 +535,125 @@ int actq_cache_attention(const actq_cache* cache, const actq_heads* q, actq_dtyp
                          const int32_t* query_start, int64_t max_query, int64_t max_length, float scale,
                          float softcap, int32_t window, const actq_heads* out, void* workspace,
                          uint64_t workspace_bytes, void* stream);
+
+/*
+ * Appends new tokens to a cache: actq_head_norm_rotate of q and k and actq_cache_write of the
+ * keys it gives and of v, in one launch.  With norm = 0 queries and keys are rotated only (eps and the
+ * weights take no part).  Queries are those of actq_head_norm_rotate.  Keys are computed in
+ * binary64 and rounded once, to binary32, before they are quantised: they are not rounded to dt between, and
+ * their codes do not depend on the order of sums.
+ *
+ * q, q_out  NULL both: keys and values only.  q_out may be q; nothing written may overlap what
+ *           is read otherwise
+ * k, v      heads equal to the cache's
+ * A token whose position is none of the tables' rows gives zeros for its query and its key; a slot
+ * outside the cache is skipped.  The call must not name a slot twice.
+ */
+int actq_cache_append(const actq_cache* cache, const actq_heads* q, const actq_heads* k, const actq_heads* v,
+                      actq_dtype dt, int64_t tokens, const void* q_weight, const void* k_weight,
+                      actq_dtype weight_dt, const actq_rotation* rotation, int32_t norm, float eps,
+                      const int64_t* slots, const actq_heads* q_out, void* stream);
+
+/* ------------------------------------------------------------------ a layer around the attention */
+
+/* A matrix whose rows are contiguous. */
+typedef struct actq_rows {
+    void* data;     /* device, aligned to the element size */
+    int64_t stride; /* elements from a row to the next, |stride| < 2^36 */
+} actq_rows;
+
+/*
+ * The norms behind and before a block of a residual network, with its gate and scale:
+ *   n = h (mean(h^2) + eps)^(-1/2) post_weight    (n = h without post_weight)
+ *   r = x + scale * gate * n                      (r = x without h; then neither gate nor
+ *                                                  post_weight may be given, and r is not written)
+ *   y = r (mean(r^2) + eps)^(-1/2) weight
+ * in binary32, r and y each rounded once (y from the sum before it is rounded).  The gate is one
+ * vector for all tokens (`gate`), one of each token (`gates`) or none.
+ */
+typedef struct actq_block {
+    int64_t tokens;          /* at least 0, below 2^26 */
+    int32_t width;           /* in [1, 16384] */
+    actq_dtype dt;           /* of all rows */
+    actq_dtype weight_dt;    /* of weight, post_weight and gate: dt or ACTQ_F32 */
+    const void* weight;      /* device [width] */
+    const void* post_weight; /* device [width] or NULL */
+    const void* gate;        /* device [width] or NULL */
+    const actq_rows* gates;  /* [tokens, width] or NULL; not beside gate */
+    float scale;             /* finite */
+    float eps;               /* finite, above zero */
+} actq_block;
+
+/* x, h (or NULL), r (NULL without h), y: [tokens, width].  r or y may be x or h; nothing else that
+ * is written may overlap what is read. */
+int actq_block_norm(const actq_block* block, const actq_rows* x, const actq_rows* h, const actq_rows* r,
+                    const actq_rows* y, void* stream);
+
+/*
+ * Its gradients from those of r (NULL: zeros) and y, and from r and h.  Sums over the tokens have a fixed
+ * order.
+ *
+ * grad_x, grad_h     out; grad_h NULL without h.  They may be the memory of grad_r and grad_y
+ * grad_gates         out, with `gates` only
+ * grad_weight, grad_post_weight, grad_gate: device [width] of type weight_dt, out; NULL all, or
+ *                    given for every one that the block has
+ * workspace          device, actq_block_norm_workspace bytes, 16-byte aligned; may be NULL where no
+ *                    grad_weight is wanted
+ */
+int actq_block_norm_workspace(const actq_block* block, uint64_t* bytes_host);
+int actq_block_norm_backward(const actq_block* block, const actq_rows* grad_r, const actq_rows* grad_y,
+                             const actq_rows* r, const actq_rows* h, const actq_rows* grad_x,
+                             const actq_rows* grad_h, const actq_rows* grad_gates, void* grad_weight,
+                             void* grad_post_weight, void* grad_gate, void* workspace,
+                             uint64_t workspace_bytes, void* stream);
+
+/*
+ * Weights of a linear layer in 4 bits with a zero point and a step for `group` neighbouring inputs of
+ * an output.  A code stands for zero + step * code; groups = ceil(inputs / group).
+ *   codes   device [outputs, groups * group / 8] words of eight codes of neighbouring inputs: those of
+ *           inputs 8 j + 2 i and 8 j + 2 i + 1 are bits 4 i and 16 + 4 i, and up, of word j.  Codes beyond the
+ *           last input are ignored
+ *   header  device [outputs, groups, 2] bfloat16 bit patterns, (zero, step)
+ */
+typedef struct actq_weights4 {
+    const uint32_t* codes;  /* aligned to 4 bytes */
+    const uint16_t* header; /* aligned to 4 bytes */
+    int32_t inputs;         /* in [1, 2^20] */
+    int32_t outputs;        /* in [1, 2^20] */
+    int32_t group;          /* 32, 64 or 128 */
+} actq_weights4;
+
+/*
+ * Quantises w [outputs, inputs] into those codes and headers: zero = min and step =
+ * (max - min) / 15 of a group, each rounded to bfloat16, code = nearest((w - zero) (1 / step)) cut to
+ * [0, 15], every operation in binary32 (step 0 and codes 0 where step or its inverse overflows or is
+ * zero; NaN for a group with an element that is not finite, or whose zero or step overflows) / writes what
+ * the codes stand for, rounded to dt.
+ */
+int actq_weights4_quantize(const actq_rows* w, actq_dtype dt, const actq_weights4* to, void* stream);
+int actq_weights4_dequantize(const actq_weights4* w, const actq_rows* out, actq_dtype dt, void* stream);
+
+/*
+ * y = x W^T + bias.  Products are exact (of a binary32 x: of the three bfloat16 numbers that make it
+ * up), their sums binary32, a result is rounded once.  A row of x with an infinity or NaN gives NaN.
+ *
+ * x [rows, inputs], y [rows, outputs] of type dt; rows at least 0, below 2^20
+ * bias       device [outputs] of type dt or ACTQ_F32, or NULL
+ * workspace  device, actq_linear4_workspace bytes (may be 0: then NULL), 16-byte aligned
+ */
+int actq_linear4_workspace(const actq_weights4* w, actq_dtype dt, int64_t rows, uint64_t* bytes_host);
+int actq_linear4(const actq_weights4* w, const actq_rows* x, actq_dtype dt, int64_t rows, const void* bias,
+                 actq_dtype bias_dt, const actq_rows* y, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/*
+ * grad_x = grad_y W.  A weight is multiplied as two bfloat16 numbers (16 bits of zero + step * code;
+ * three, all of it, for ACTQ_F32).  Sums are binary32 in a fixed order, a result is rounded once.
+ *
+ * grad_y [rows, outputs], grad_x [rows, inputs] of type dt; workspace as above
+ */
+int actq_linear4_backward_workspace(const actq_weights4* w, actq_dtype dt, int64_t rows, uint64_t* bytes_host);
+int actq_linear4_backward(const actq_weights4* w, const actq_rows* grad_y, actq_dtype dt, int64_t rows,
+                          const actq_rows* grad_x, void* workspace, uint64_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -31,7 +31,9 @@ EXPORTS = ("actq_version", "actq_source_hash", "actq_last_error", "actq_packed_b
            "actq_pool2d_output_size", "actq_maxpool2d_forward", "actq_maxpool2d_backward", "actq_tensor_stats",
            "actq_group_stats_multi", "actq_quantize_pack_multi", "actq_unpack_dequantize_multi", "actq_linear_backward",
            "actq_head_norm_rotate", "actq_head_norm_workspace", "actq_head_norm_rotate_backward", "actq_cache_write", "actq_cache_read",
-           "actq_cache_attention_workspace", "actq_cache_attention")
+           "actq_cache_attention_workspace", "actq_cache_attention", "actq_cache_append", "actq_block_norm", "actq_block_norm_workspace",
+           "actq_block_norm_backward", "actq_weights4_quantize", "actq_weights4_dequantize", "actq_linear4_workspace", "actq_linear4",
+           "actq_linear4_backward_workspace", "actq_linear4_backward")
 
 
 class ActqError(RuntimeError):
@@ -56,6 +58,22 @@ class CacheDesc(ctypes.Structure):
     _fields_ = [("key_codes", ctypes.c_void_p), ("key_header", ctypes.c_void_p), ("value_codes", ctypes.c_void_p), ("value_header", ctypes.c_void_p),
                 ("pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("heads", ctypes.c_int32), ("dim", ctypes.c_int32),
                 ("key_bits", ctypes.c_int32), ("value_bits", ctypes.c_int32)]
+
+
+class RowsDesc(ctypes.Structure):
+    """Mirror of `actq_rows`."""
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64)]
+
+
+class BlockDesc(ctypes.Structure):
+    """Mirror of `actq_block`."""
+    _fields_ = [("tokens", ctypes.c_int64), ("width", ctypes.c_int32), ("dt", ctypes.c_int), ("weight_dt", ctypes.c_int), ("weight", ctypes.c_void_p),
+                ("post_weight", ctypes.c_void_p), ("gate", ctypes.c_void_p), ("gates", ctypes.POINTER(RowsDesc)), ("scale", ctypes.c_float), ("eps", ctypes.c_float)]
+
+
+class Weights4Desc(ctypes.Structure):
+    """Mirror of `actq_weights4`."""
+    _fields_ = [("codes", ctypes.c_void_p), ("header", ctypes.c_void_p), ("inputs", ctypes.c_int32), ("outputs", ctypes.c_int32), ("group", ctypes.c_int32)]
 
 
 _lib = None
@@ -168,6 +186,26 @@ def lib() -> ctypes.CDLL:
     L.actq_cache_attention_workspace.argtypes = [cache, i32, i64, i64, i64, i64, i32, vp]
     L.actq_cache_attention.restype = c.c_int
     L.actq_cache_attention.argtypes = [cache, heads, c.c_int, i64, i64, vp, i32, vp, vp, i64, i64, c_float, c_float, i32, heads, vp, u64, vp]
+    L.actq_cache_append.restype = c.c_int
+    L.actq_cache_append.argtypes = [cache, heads, heads, heads, c.c_int, i64, vp, vp, c.c_int, rotation, i32, c_float, vp, heads, vp]
+    rows, block, weights4 = c.POINTER(RowsDesc), c.POINTER(BlockDesc), c.POINTER(Weights4Desc)
+    L.actq_block_norm.restype = c.c_int
+    L.actq_block_norm.argtypes = [block, rows, rows, rows, rows, vp]
+    L.actq_block_norm_workspace.restype = c.c_int
+    L.actq_block_norm_workspace.argtypes = [block, vp]
+    L.actq_block_norm_backward.restype = c.c_int
+    L.actq_block_norm_backward.argtypes = [block] + [rows] * 7 + [vp, vp, vp, vp, u64, vp]
+    L.actq_weights4_quantize.restype = c.c_int
+    L.actq_weights4_quantize.argtypes = [rows, c.c_int, weights4, vp]
+    L.actq_weights4_dequantize.restype = c.c_int
+    L.actq_weights4_dequantize.argtypes = [weights4, rows, c.c_int, vp]
+    for workspace in (L.actq_linear4_workspace, L.actq_linear4_backward_workspace):
+        workspace.restype = c.c_int
+        workspace.argtypes = [weights4, c.c_int, i64, vp]
+    L.actq_linear4.restype = c.c_int
+    L.actq_linear4.argtypes = [weights4, rows, c.c_int, i64, vp, c.c_int, rows, vp, u64, vp]
+    L.actq_linear4_backward.restype = c.c_int
+    L.actq_linear4_backward.argtypes = [weights4, rows, c.c_int, i64, rows, vp, u64, vp]
     L.actq_allocate_bits_device.restype = c.c_int
     L.actq_allocate_bits_device.argtypes = [vp, vp, i64, i64, i32, i64, c.c_uint32, vp, vp, vp, vp]
     _lib = L
@@ -179,7 +217,9 @@ _host = None
 _ATTACHED = ("actq_last_error", "actq_group_stats", "actq_sample_sensitivity", "actq_allocate_bits_device", "actq_quantize_pack",
              "actq_unpack_dequantize", "actq_relu_mask_bytes", "actq_relu_forward", "actq_relu_backward", "actq_pool2d_output_size",
              "actq_maxpool2d_forward", "actq_maxpool2d_backward", "actq_linear_backward", "actq_head_norm_rotate", "actq_head_norm_workspace",
-             "actq_head_norm_rotate_backward", "actq_cache_write", "actq_cache_read", "actq_cache_attention_workspace", "actq_cache_attention")
+             "actq_head_norm_rotate_backward", "actq_cache_write", "actq_cache_read", "actq_cache_attention_workspace", "actq_cache_attention",
+             "actq_cache_append", "actq_block_norm", "actq_block_norm_workspace", "actq_block_norm_backward", "actq_weights4_quantize",
+             "actq_weights4_dequantize", "actq_linear4_workspace", "actq_linear4", "actq_linear4_backward_workspace", "actq_linear4_backward")
 
 
 def host():
@@ -429,6 +469,67 @@ def cache_attention(q, key_codes, key_header, value_codes, value_header, table, 
     tokens and the most tokens of a sequence, or more; scale defaults to dim ** -0.5."""
     return (_host or host()).cache_attention(q, key_codes, key_header, value_codes, value_header, table, lengths, query_start, int(max_query),
                                              int(max_length), scale, float(softcap), int(window), out)
+
+
+def cache_append(q, k, v, q_weight, k_weight, positions, cos, sin, slots, key_codes, key_header, value_codes, value_header, eps=1e-6, interleaved: bool = False,
+                 q_out=None):
+    """Device: head_norm_rotate of q and k and cache_write of the keys and v, in one launch; returns q_out (q_out = q works in place).
+    With eps None queries and keys are rotated only; q None appends keys and values alone.  Keys are quantised from binary32 values that are
+    rounded once, not from values of the tensors' type."""
+    return (_host or host()).cache_append(q, k, v, q_weight, k_weight, positions, cos, sin, slots, key_codes, key_header, value_codes, value_header,
+                                          None if eps is None else float(eps), bool(interleaved), q_out)
+
+
+# ----------------------------------------------------------------------------- a layer around the attention
+#
+# Matrices of rows are [rows, columns] (float32, float16 or bfloat16) with contiguous rows and any other stride.
+
+def block_norm(x, h, gate, weight, post_weight=None, scale: float = 1.0, eps: float = 1e-6, r=None, y=None):
+    """Device: the norms behind and before a block with the residual sum between, in one launch, x and h [tokens, width]:
+    r = x + scale * gate * norm(h) * post_weight and y = norm(r) * weight, norm(v) = v (mean(v^2) + eps)^(-1/2).  post_weight None: h goes
+    without a norm; gate None, [width] or [tokens, width]; h None: r is x.  Weights and a gate [width] have the rows' type or float32.  Returns
+    (r, y); r = x, y = h and the like work in place."""
+    return (_host or host()).block_norm(x, h, gate, weight, post_weight, float(scale), float(eps), r, y)
+
+
+def block_norm_backward(grad_r, grad_y, r, h, gate, weight, post_weight=None, scale: float = 1.0, eps: float = 1e-6, need_weights: bool = True):
+    """Device: gradients of block_norm's x, h, gate, weight and post_weight from those of r (None: zeros) and y (None for what is None, and for
+    the weights and a gate [width] unless need_weights)."""
+    return (_host or host()).block_norm_backward(grad_r, grad_y, r, h, gate, weight, post_weight, float(scale), float(eps), bool(need_weights))
+
+
+def quantize_weights(w, group: int = 128):
+    """Device: w [outputs, inputs] in 4 bits to nearest with a zero point and a step for `group` (32, 64 or 128) neighbouring inputs.  Returns
+    (codes int32 [outputs, groups * group / 8], header bfloat16 [outputs, groups, 2] = (zero, step)); pair i of a word's eight codes lies in
+    its bits 4 i and 16 + 4 i."""
+    torch = _torch()
+    if group not in (32, 64, 128):
+        raise ValueError("group must be 32, 64 or 128")
+    if w.dim() != 2 or w.shape[1] == 0:
+        raise ValueError("w must be [outputs, inputs]")
+    groups = (w.shape[1] + group - 1) // group
+    codes = torch.empty((w.shape[0], groups * group // 8), dtype=torch.int32, device=w.device)
+    header = torch.empty((w.shape[0], groups, 2), dtype=torch.bfloat16, device=w.device)
+    (_host or host()).weights4_quantize(w, codes, header)
+    return codes, header
+
+
+def dequantize_weights(codes, header, inputs: int, dtype):
+    """Device: what those codes stand for, [outputs, inputs] of type dtype."""
+    out = _torch().empty((codes.shape[0], int(inputs)), dtype=dtype, device=codes.device)
+    (_host or host()).weights4_dequantize(codes, header, out)
+    return out
+
+
+def linear4(x, codes, header, bias=None, out=None):
+    """Device: x [..., inputs] times the transpose of 4-bit weights (quantize_weights), plus bias [outputs]: [..., outputs] of x's type.
+    From one row, bound by the weights' memory, to thousands."""
+    return (_host or host()).linear4(x, codes, header, bias, out)
+
+
+def linear4_backward(grad_y, codes, header, inputs: int):
+    """Device: the gradient of linear4's x, grad_y [..., outputs] times the weights."""
+    return (_host or host()).linear4_backward(grad_y, codes, header, int(inputs))
 
 
 # ----------------------------------------------------------------------------- several tensors per launch

@@ -43,6 +43,11 @@ class PagedCache:
         """Quantises k and v [tokens, heads, dim] into the slots."""
         B.cache_write(k, v, slots, *self.buffers)
 
+    def append(self, q, k, v, q_weight, k_weight, positions, cos, sin, slots, **options):
+        """Norm and rotation of new queries and keys, keys and values quantised into the slots, in one launch; returns the queries
+        (binding.cache_append; options: eps, interleaved, q_out)."""
+        return B.cache_append(q, k, v, q_weight, k_weight, positions, cos, sin, slots, *self.buffers, **options)
+
     def read(self, slots, dtype, k=None, v=None):
         """(keys, values) [tokens, heads, dim] of the slots."""
         return B.cache_read(slots, *self.buffers, self.dim, dtype, k, v)

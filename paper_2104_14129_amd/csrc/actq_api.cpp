@@ -646,4 +646,188 @@ int actq_cache_attention(const actq_cache* cache, const actq_heads* q, actq_dtyp
                                   need > 0 ? workspace : nullptr, stream);
 }
 
+int actq_cache_append(const actq_cache* cache, const actq_heads* q, const actq_heads* k, const actq_heads* v, actq_dtype dt, int64_t tokens, const void* q_weight,
+                      const void* k_weight, actq_dtype weight_dt, const actq_rotation* rotation, int32_t norm, float eps, const int64_t* slots, const actq_heads* q_out,
+                      void* stream)
+{
+    const char* who = "actq_cache_append";
+    if (int rc = check_cached(who, cache, k, v, dt, tokens, slots)) return rc;
+    if (!q != !q_out) return fail(ACTQ_EINVAL, "%s: q goes with q_out", who);
+    if (norm != 0 && norm != 1) return fail(ACTQ_EINVAL, "%s: norm must be 0 or 1", who);
+    if (!norm && (q_weight || k_weight)) return fail(ACTQ_EINVAL, "%s: a weight without norm", who);
+    if (!q && q_weight) return fail(ACTQ_EINVAL, "%s: q_weight without q", who);
+    if (int rc = check_norm(who, q ? q : k, k, dt, tokens, cache->dim, q_weight, k_weight, weight_dt, rotation, norm ? eps : 1.0f)) return rc;
+    if (int rc = check_tokens(who, tokens, 2 * static_cast<int64_t>(cache->heads) + (q ? q->heads : 0))) return rc;
+    if (q)
+        if (int rc = check_heads(who, "q_out", q_out, dt, tokens, q->heads)) return rc;
+    return tokens == 0 ? ACTQ_OK : launch_cache_append(cache, q, k, v, dt, tokens, q_weight, k_weight, weight_dt, rotation, norm, eps, slots, q_out, stream);
+}
+
+// ----------------------------------------------------------------------------- a layer around the attention
+
+static int check_rows(const char* who, const char* name, const actq_rows* r, int dt, int64_t rows)
+{
+    if (!r) return fail(ACTQ_EINVAL, "%s: null %s", who, name);
+    if (rows == 0) return ACTQ_OK;
+    if (!r->data || !aligned(r->data, size_of(dt))) return fail(ACTQ_EINVAL, "%s: %s is null or not aligned to its element size", who, name);
+    if (r->stride <= -kMostStride || r->stride >= kMostStride) return fail(ACTQ_EINVAL, "%s: stride of %s out of range", who, name);
+    return ACTQ_OK;
+}
+
+static int check_block(const char* who, const actq_block* b, bool h)
+{
+    if (!b) return fail(ACTQ_EINVAL, "%s: null block", who);
+    if (int rc = check_heads_dtype(who, b->dt)) return rc;
+    if (b->weight_dt != b->dt && b->weight_dt != ACTQ_F32) return fail(ACTQ_EINVAL, "%s: weights must have the rows' type or ACTQ_F32", who);
+    if (b->tokens < 0 || b->tokens >= kMostHeads) return fail(ACTQ_EINVAL, "%s: tokens must be in [0, 2^26)", who);
+    if (b->width < 1 || b->width > 16384) return fail(ACTQ_EINVAL, "%s: width must be in [1, 16384], got %d", who, b->width);
+    if (!b->weight) return fail(ACTQ_EINVAL, "%s: null weight", who);
+    const uintptr_t size = size_of(b->weight_dt);
+    if (!aligned(b->weight, size) || !aligned(b->post_weight, size) || !aligned(b->gate, size)) return fail(ACTQ_EINVAL, "%s: a weight is not aligned to its element size", who);
+    if (b->gate && b->gates) return fail(ACTQ_EINVAL, "%s: gate beside gates", who);
+    if (!h && (b->post_weight || b->gate || b->gates)) return fail(ACTQ_EINVAL, "%s: post_weight or a gate without h", who);
+    if (b->gates)
+        if (int rc = check_rows(who, "gates", b->gates, b->dt, b->tokens)) return rc;
+    if (!finite(b->scale)) return fail(ACTQ_EINVAL, "%s: scale must be finite", who);
+    if (!finite(b->eps, true, false)) return fail(ACTQ_EINVAL, "%s: eps must be finite and above zero", who);
+    return ACTQ_OK;
+}
+
+int actq_block_norm(const actq_block* b, const actq_rows* x, const actq_rows* h, const actq_rows* r, const actq_rows* y, void* stream)
+{
+    const char* who = "actq_block_norm";
+    if (int rc = check_block(who, b, h != nullptr)) return rc;
+    if (!h != !r) return fail(ACTQ_EINVAL, "%s: h goes with r", who);
+    if (int rc = check_rows(who, "x", x, b->dt, b->tokens)) return rc;
+    if (h) {
+        if (int rc = check_rows(who, "h", h, b->dt, b->tokens)) return rc;
+        if (int rc = check_rows(who, "r", r, b->dt, b->tokens)) return rc;
+    }
+    if (int rc = check_rows(who, "y", y, b->dt, b->tokens)) return rc;
+    return b->tokens == 0 ? ACTQ_OK : launch_block_norm(b, x, h, r, y, stream);
+}
+
+int actq_block_norm_workspace(const actq_block* b, uint64_t* bytes_host)
+{
+    const char* who = "actq_block_norm_workspace";
+    if (int rc = check_block(who, b, true)) return rc;
+    if (!bytes_host) return fail(ACTQ_EINVAL, "%s: null output", who);
+    *bytes_host = block_norm_workspace(b);
+    return ACTQ_OK;
+}
+
+int actq_block_norm_backward(const actq_block* b, const actq_rows* grad_r, const actq_rows* grad_y, const actq_rows* r, const actq_rows* h, const actq_rows* grad_x,
+                             const actq_rows* grad_h, const actq_rows* grad_gates, void* grad_weight, void* grad_post_weight, void* grad_gate, void* workspace,
+                             uint64_t workspace_bytes, void* stream)
+{
+    const char* who = "actq_block_norm_backward";
+    if (int rc = check_block(who, b, h != nullptr)) return rc;
+    if (!h != !grad_h) return fail(ACTQ_EINVAL, "%s: h goes with grad_h", who);
+    if (!b->gates != !grad_gates) return fail(ACTQ_EINVAL, "%s: gates go with grad_gates", who);
+    if (grad_r)
+        if (int rc = check_rows(who, "grad_r", grad_r, b->dt, b->tokens)) return rc;
+    if (int rc = check_rows(who, "grad_y", grad_y, b->dt, b->tokens)) return rc;
+    if (int rc = check_rows(who, "r", r, b->dt, b->tokens)) return rc;
+    if (int rc = check_rows(who, "grad_x", grad_x, b->dt, b->tokens)) return rc;
+    if (h) {
+        if (int rc = check_rows(who, "h", h, b->dt, b->tokens)) return rc;
+        if (int rc = check_rows(who, "grad_h", grad_h, b->dt, b->tokens)) return rc;
+    }
+    if (grad_gates)
+        if (int rc = check_rows(who, "grad_gates", grad_gates, b->dt, b->tokens)) return rc;
+    const uintptr_t size = size_of(b->weight_dt);
+    if (!aligned(grad_weight, size) || !aligned(grad_post_weight, size) || !aligned(grad_gate, size))
+        return fail(ACTQ_EINVAL, "%s: a weight's gradient is not aligned to its element size", who);
+    if ((grad_post_weight != nullptr) != (grad_weight && b->post_weight) || (grad_gate != nullptr) != (grad_weight && b->gate))
+        return fail(ACTQ_EINVAL, "%s: grad_weight, grad_post_weight and grad_gate are given for all that the block has, or none", who);
+    if (grad_weight && b->tokens > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < block_norm_workspace(b)))
+        return fail(ACTQ_EINVAL, "%s: the workspace is null, misaligned or smaller than actq_block_norm_workspace says", who);
+    return launch_block_norm_backward(b, grad_r, grad_y, r, h, grad_x, grad_h, grad_gates, grad_weight, grad_post_weight, grad_gate, workspace, stream);
+}
+
+static int check_weights4(const char* who, const actq_weights4* w)
+{
+    if (!w) return fail(ACTQ_EINVAL, "%s: null weights", who);
+    if (w->group != 32 && w->group != 64 && w->group != 128) return fail(ACTQ_EINVAL, "%s: unsupported group of %d inputs (32, 64 or 128)", who, w->group);
+    constexpr int32_t kMost = 1 << 20;
+    if (w->inputs < 1 || w->outputs < 1 || w->inputs > kMost || w->outputs > kMost) return fail(ACTQ_EINVAL, "%s: inputs and outputs must be in [1, 2^20]", who);
+    if (!w->codes || !w->header || !aligned(w->codes, 4) || !aligned(w->header, 4)) return fail(ACTQ_EINVAL, "%s: codes or header is null or not aligned to 4 bytes", who);
+    return ACTQ_OK;
+}
+
+int actq_weights4_quantize(const actq_rows* w, actq_dtype dt, const actq_weights4* to, void* stream)
+{
+    const char* who = "actq_weights4_quantize";
+    if (int rc = check_weights4(who, to)) return rc;
+    if (int rc = check_heads_dtype(who, dt)) return rc;
+    if (int rc = check_rows(who, "w", w, dt, to->outputs)) return rc;
+    return launch_weights4_quantize(w, dt, to, stream);
+}
+
+int actq_weights4_dequantize(const actq_weights4* w, const actq_rows* out, actq_dtype dt, void* stream)
+{
+    const char* who = "actq_weights4_dequantize";
+    if (int rc = check_weights4(who, w)) return rc;
+    if (int rc = check_heads_dtype(who, dt)) return rc;
+    if (int rc = check_rows(who, "out", out, dt, w->outputs)) return rc;
+    return launch_weights4_dequantize(w, out, dt, stream);
+}
+
+// Sizes that shape the launch of a product.
+static int check_linear4(const char* who, const actq_weights4* w, int dt, int64_t rows)
+{
+    if (int rc = check_weights4(who, w)) return rc;
+    if (int rc = check_heads_dtype(who, dt)) return rc;
+    if (rows < 0 || rows >= (int64_t(1) << 20)) return fail(ACTQ_EINVAL, "%s: rows must be in [0, 2^20)", who);
+    return ACTQ_OK;
+}
+
+int actq_linear4_workspace(const actq_weights4* w, actq_dtype dt, int64_t rows, uint64_t* bytes_host)
+{
+    const char* who = "actq_linear4_workspace";
+    if (int rc = check_linear4(who, w, dt, rows)) return rc;
+    if (!bytes_host) return fail(ACTQ_EINVAL, "%s: null output", who);
+    *bytes_host = linear4_workspace(w, dt, rows);
+    return ACTQ_OK;
+}
+
+int actq_linear4(const actq_weights4* w, const actq_rows* x, actq_dtype dt, int64_t rows, const void* bias, actq_dtype bias_dt, const actq_rows* y, void* workspace,
+                 uint64_t workspace_bytes, void* stream)
+{
+    const char* who = "actq_linear4";
+    if (int rc = check_linear4(who, w, dt, rows)) return rc;
+    if (int rc = check_rows(who, "x", x, dt, rows)) return rc;
+    if (int rc = check_rows(who, "y", y, dt, rows)) return rc;
+    if (bias && bias_dt != dt && bias_dt != ACTQ_F32) return fail(ACTQ_EINVAL, "%s: the bias must have the rows' type or ACTQ_F32", who);
+    if (!aligned(bias, size_of(bias_dt))) return fail(ACTQ_EINVAL, "%s: the bias is not aligned to its element size", who);
+    if (rows == 0) return ACTQ_OK;
+    const uint64_t need = linear4_workspace(w, dt, rows);
+    if (need > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < need))
+        return fail(ACTQ_EINVAL, "%s: the workspace is null, misaligned or smaller than actq_linear4_workspace says", who);
+    return launch_linear4(w, x, dt, rows, bias, bias_dt, y, need > 0 ? workspace : nullptr, stream);
+}
+
+int actq_linear4_backward_workspace(const actq_weights4* w, actq_dtype dt, int64_t rows, uint64_t* bytes_host)
+{
+    const char* who = "actq_linear4_backward_workspace";
+    if (int rc = check_linear4(who, w, dt, rows)) return rc;
+    if (!bytes_host) return fail(ACTQ_EINVAL, "%s: null output", who);
+    *bytes_host = linear4_backward_workspace(w, dt, rows);
+    return ACTQ_OK;
+}
+
+int actq_linear4_backward(const actq_weights4* w, const actq_rows* grad_y, actq_dtype dt, int64_t rows, const actq_rows* grad_x, void* workspace, uint64_t workspace_bytes,
+                          void* stream)
+{
+    const char* who = "actq_linear4_backward";
+    if (int rc = check_linear4(who, w, dt, rows)) return rc;
+    if (int rc = check_rows(who, "grad_y", grad_y, dt, rows)) return rc;
+    if (int rc = check_rows(who, "grad_x", grad_x, dt, rows)) return rc;
+    if (rows == 0) return ACTQ_OK;
+    const uint64_t need = linear4_backward_workspace(w, dt, rows);
+    if (need > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < need))
+        return fail(ACTQ_EINVAL, "%s: the workspace is null, misaligned or smaller than actq_linear4_backward_workspace says", who);
+    return launch_linear4_backward(w, grad_y, dt, rows, grad_x, need > 0 ? workspace : nullptr, stream);
+}
+
 }  // extern "C"

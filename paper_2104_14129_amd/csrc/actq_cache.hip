@@ -51,52 +51,6 @@ struct Unit {
     }
 };
 
-// Codes of a lane's eight elements into the stream, the group's header by its first lane.
-template <int LANES>
-__device__ __forceinline__ void quantise(const float (&x)[8], int bits, uint8_t* codes, float* header, bool held, int at)
-{
-    float low = x[0], high = x[0];
-    uint32_t largest = magnitude(x[0]);
-#pragma unroll
-    for (int i = 1; i < 8; ++i) {
-        low = fminf(low, x[i]);
-        high = fmaxf(high, x[i]);
-        largest = max(largest, magnitude(x[i]));
-    }
-    // an infinity or NaN (which a minimum passes over) gives the group an infinite range
-    if (largest >= 0x7f800000u) {
-        low = 0.0f;
-        high = INFINITY;
-    }
-    low = over_lanes<LANES>(low, [](float a, float b) { return fminf(a, b); });
-    high = over_lanes<LANES>(high, [](float a, float b) { return fmaxf(a, b); });
-    const float top = bits == 8 ? 255.0f : 15.0f;
-    const float zero = low + 0.0f;   // -0 becomes +0
-    const float range = high - zero;
-    const bool none = magnitude(range) >= 0x7f800000u;
-    float inverse = top / range, step = range / top;
-    if (range == 0.0f || isinf(inverse)) inverse = step = 0.0f;
-    uint32_t code[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) code[i] = none ? 0u : static_cast<uint32_t>(rintf(fminf((x[i] - zero) * inverse, top)));
-    if (!held) return;
-    if (bits == 8) {
-        u32x2 w;
-        w[0] = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
-        w[1] = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
-        *reinterpret_cast<u32x2*>(codes + 8 * at) = w;
-    } else {
-        uint32_t w = code[0];
-#pragma unroll
-        for (int i = 1; i < 8; ++i) w |= code[i] << 4 * i;
-        *reinterpret_cast<uint32_t*>(codes + 4 * at) = w;
-    }
-    if (at == 0) {
-        const uint32_t nan = 0x7fc00000u;   // stored as bits: the compiler takes it that floating-point data holds no NaN
-        *reinterpret_cast<u32x2*>(header) = none ? u32x2{nan, nan} : u32x2{__builtin_bit_cast(uint32_t, zero), __builtin_bit_cast(uint32_t, step)};
-    }
-}
-
 template <typename T, int LANES>
 __global__ __launch_bounds__(kCacheBlock) void cache_write_kernel(CacheArgs<T> a)
 {

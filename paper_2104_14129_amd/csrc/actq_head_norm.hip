@@ -21,92 +21,6 @@ namespace {
 constexpr int kNormWaves = 4;
 constexpr int kNormBlock = kNormWaves * 64;
 
-struct Rotation {
-    const int32_t* positions;
-    const float* cos;
-    const float* sin;
-    int64_t rows;
-    int32_t half;          // pairs per head
-    int32_t interleaved;   // pairs (2p, 2p + 1) instead of (p, p + half)
-};
-
-struct Weights {
-    const void* q;   // null: ones
-    const void* k;
-    int32_t wide;    // binary32 beside a 16-bit type of the heads
-};
-
-// The lane's part of the rotation of one token.
-template <int LANES>
-struct Turn {
-    float c[8], s[8];
-    bool turned;   // whether the lane's elements are rotated
-    int partner;   // lane that holds the other elements of the pairs
-
-    // A lane's place among the LANES of its head.
-    __device__ __forceinline__ void load(const Rotation& r, int64_t position, int lane)
-    {
-        const int at = lane % LANES, first = kLaneValues * at;
-        turned = first < 2 * r.half;
-        partner = lane;
-        if (!turned) return;
-        if (r.interleaved) {
-            const float* const cs = r.cos + position * r.half + first / 2;
-            const float* const sn = r.sin + position * r.half + first / 2;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                c[2 * i] = c[2 * i + 1] = cs[i];
-                s[2 * i] = -sn[i];
-                s[2 * i + 1] = sn[i];
-            }
-        } else {
-            const bool low = first < r.half;
-            const int64_t entry = position * r.half + (low ? first : first - r.half);
-            partner = low ? lane + r.half / kLaneValues : lane - r.half / kLaneValues;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                c[i] = r.cos[entry + i];
-                const float sn = r.sin[entry + i];
-                s[i] = low ? -sn : sn;
-            }
-        }
-    }
-
-    // v rotated; BACK: by the opposite angle.
-    template <bool BACK>
-    __device__ __forceinline__ void apply(float (&v)[8], int interleaved) const
-    {
-        float other[8];
-        if (interleaved) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) other[i] = v[i ^ 1];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) other[i] = __shfl(v[i], partner);
-        }
-        if (!turned) return;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = fmaf(BACK ? -s[i] : s[i], other[i], v[i] * c[i]);
-    }
-};
-
-template <typename T>
-__device__ __forceinline__ void load_weight(const void* w, int wide, int first, float (&f)[8])
-{
-    if (!w) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = 1.0f;
-    } else if (wide) {
-        Eight<float> e;
-        e.load(static_cast<const float*>(w) + first);
-        e.widen(f);
-    } else {
-        Eight<T> e;
-        e.load(static_cast<const T*>(w) + first);
-        e.widen(f);
-    }
-}
-
 // The steps of a token: groups of 64 / LANES heads of the queries, then of the keys.
 struct Steps {
     int32_t q_heads, k_heads;
@@ -300,11 +214,6 @@ __global__ __launch_bounds__(kSumColumns* kSumRows) void head_norm_weights_kerne
     if (row != 0) return;
     W* const out = at < dim ? grad_q : grad_k;
     if (out) out[at < dim ? at : at - dim] = static_cast<W>(static_cast<float>(sum));
-}
-
-Rotation rotation_of(const actq_rotation* r)
-{
-    return {r->positions, r->cos, r->sin, r->rows, r->rotated / 2, r->interleaved};
 }
 
 Steps steps_of(const actq_heads* q, const actq_heads* k, int lanes)

@@ -1,4 +1,5 @@
-// What the kernels for attention heads share: tensors of heads, eight neighbouring elements of a head per lane, sums over the lanes of a head.
+// What the kernels for attention heads share: tensors of heads, eight neighbouring elements of a head per lane, sums over the lanes of a head,
+// the rotation by position, the quantizer of the cache.
 #ifndef ACTQ_HEADS_H
 #define ACTQ_HEADS_H
 
@@ -127,6 +128,143 @@ inline HeadsOf<T> heads_of(const actq_heads* h)
 {
     if (!h) return {nullptr, 0, 0};
     return {static_cast<T*>(h->data), h->token_stride, h->head_stride};
+}
+
+struct Rotation {
+    const int32_t* positions;
+    const float* cos;
+    const float* sin;
+    int64_t rows;
+    int32_t half;          // pairs per head
+    int32_t interleaved;   // pairs (2p, 2p + 1) instead of (p, p + half)
+};
+
+struct Weights {
+    const void* q;   // null: ones
+    const void* k;
+    int32_t wide;    // binary32 beside a 16-bit type of the heads
+};
+
+// The lane's part of the rotation of one token.
+template <int LANES>
+struct Turn {
+    float c[8], s[8];
+    bool turned;   // whether the lane's elements are rotated
+    int partner;   // lane that holds the other elements of the pairs
+
+    // A lane's place among the LANES of its head.
+    __device__ __forceinline__ void load(const Rotation& r, int64_t position, int lane)
+    {
+        const int at = lane % LANES, first = kLaneValues * at;
+        turned = first < 2 * r.half;
+        partner = lane;
+        if (!turned) return;
+        if (r.interleaved) {
+            const float* const cs = r.cos + position * r.half + first / 2;
+            const float* const sn = r.sin + position * r.half + first / 2;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                c[2 * i] = c[2 * i + 1] = cs[i];
+                s[2 * i] = -sn[i];
+                s[2 * i + 1] = sn[i];
+            }
+        } else {
+            const bool low = first < r.half;
+            const int64_t entry = position * r.half + (low ? first : first - r.half);
+            partner = low ? lane + r.half / kLaneValues : lane - r.half / kLaneValues;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                c[i] = r.cos[entry + i];
+                const float sn = r.sin[entry + i];
+                s[i] = low ? -sn : sn;
+            }
+        }
+    }
+
+    // v rotated; BACK: by the opposite angle.
+    template <bool BACK>
+    __device__ __forceinline__ void apply(float (&v)[8], int interleaved) const
+    {
+        float other[8];
+        if (interleaved) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) other[i] = v[i ^ 1];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) other[i] = __shfl(v[i], partner);
+        }
+        if (!turned) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = fmaf(BACK ? -s[i] : s[i], other[i], v[i] * c[i]);
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ void load_weight(const void* w, int wide, int first, float (&f)[8])
+{
+    if (!w) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = 1.0f;
+    } else if (wide) {
+        Eight<float> e;
+        e.load(static_cast<const float*>(w) + first);
+        e.widen(f);
+    } else {
+        Eight<T> e;
+        e.load(static_cast<const T*>(w) + first);
+        e.widen(f);
+    }
+}
+
+inline Rotation rotation_of(const actq_rotation* r)
+{
+    return {r->positions, r->cos, r->sin, r->rows, r->rotated / 2, r->interleaved};
+}
+
+// Codes of a lane's eight elements into the stream, the group's header by its first lane.
+template <int LANES>
+__device__ __forceinline__ void quantise(const float (&x)[8], int bits, uint8_t* codes, float* header, bool held, int at)
+{
+    float low = x[0], high = x[0];
+    uint32_t largest = magnitude(x[0]);
+#pragma unroll
+    for (int i = 1; i < 8; ++i) {
+        low = fminf(low, x[i]);
+        high = fmaxf(high, x[i]);
+        largest = max(largest, magnitude(x[i]));
+    }
+    // an infinity or NaN (which a minimum passes over) gives the group an infinite range
+    if (largest >= 0x7f800000u) {
+        low = 0.0f;
+        high = INFINITY;
+    }
+    low = over_lanes<LANES>(low, [](float a, float b) { return fminf(a, b); });
+    high = over_lanes<LANES>(high, [](float a, float b) { return fmaxf(a, b); });
+    const float top = bits == 8 ? 255.0f : 15.0f;
+    const float zero = low + 0.0f;   // -0 becomes +0
+    const float range = high - zero;
+    const bool none = magnitude(range) >= 0x7f800000u;
+    float inverse = top / range, step = range / top;
+    if (range == 0.0f || isinf(inverse)) inverse = step = 0.0f;
+    uint32_t code[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) code[i] = none ? 0u : static_cast<uint32_t>(rintf(fminf((x[i] - zero) * inverse, top)));
+    if (!held) return;
+    if (bits == 8) {
+        u32x2 w;
+        w[0] = code[0] | code[1] << 8 | code[2] << 16 | code[3] << 24;
+        w[1] = code[4] | code[5] << 8 | code[6] << 16 | code[7] << 24;
+        *reinterpret_cast<u32x2*>(codes + 8 * at) = w;
+    } else {
+        uint32_t w = code[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) w |= code[i] << 4 * i;
+        *reinterpret_cast<uint32_t*>(codes + 4 * at) = w;
+    }
+    if (at == 0) {
+        const uint32_t nan = 0x7fc00000u;   // stored as bits: the compiler takes it that floating-point data holds no NaN
+        *reinterpret_cast<u32x2*>(header) = none ? u32x2{nan, nan} : u32x2{__builtin_bit_cast(uint32_t, zero), __builtin_bit_cast(uint32_t, step)};
+    }
 }
 
 inline int launched(const char* who)

@@ -117,6 +117,20 @@ uint64_t cache_attention_workspace(const actq_cache* c, int32_t heads, int64_t t
 int launch_cache_attention(const actq_cache* c, const actq_heads* q, int dtype, int64_t tokens, int64_t sequences, const int32_t* table, int32_t table_width,
                            const int32_t* lengths, const int32_t* query_start, int64_t max_query, int64_t max_length, float scale, float softcap, int32_t window,
                            const actq_heads* out, void* workspace, void* stream);
+int launch_cache_append(const actq_cache* c, const actq_heads* q, const actq_heads* k, const actq_heads* v, int dtype, int64_t tokens, const void* q_weight,
+                        const void* k_weight, int weight_dtype, const actq_rotation* rotation, int norm, float eps, const int64_t* slots, const actq_heads* q_out, void* stream);
+
+// A layer around the attention (block norm and 4-bit linear kernels files).
+uint64_t block_norm_workspace(const actq_block* b);
+int launch_block_norm(const actq_block* b, const actq_rows* x, const actq_rows* h, const actq_rows* r, const actq_rows* y, void* stream);
+int launch_block_norm_backward(const actq_block* b, const actq_rows* grad_r, const actq_rows* grad_y, const actq_rows* r, const actq_rows* h, const actq_rows* grad_x,
+                               const actq_rows* grad_h, const actq_rows* grad_gates, void* grad_weight, void* grad_post_weight, void* grad_gate, void* workspace, void* stream);
+int launch_weights4_quantize(const actq_rows* w, int dtype, const actq_weights4* to, void* stream);
+int launch_weights4_dequantize(const actq_weights4* w, const actq_rows* out, int dtype, void* stream);
+uint64_t linear4_workspace(const actq_weights4* w, int dtype, int64_t rows);
+int launch_linear4(const actq_weights4* w, const actq_rows* x, int dtype, int64_t rows, const void* bias, int bias_dtype, const actq_rows* y, void* workspace, void* stream);
+uint64_t linear4_backward_workspace(const actq_weights4* w, int dtype, int64_t rows);
+int launch_linear4_backward(const actq_weights4* w, const actq_rows* grad_y, int dtype, int64_t rows, const actq_rows* grad_x, void* workspace, void* stream);
 
 }  // namespace actq
 

@@ -1,0 +1,519 @@
+// Products of rows with weights of 4 bits, and the gradient of those rows.
+//
+//   y[m, n] = sum over k of x[m, k] W[n, k] + b[n],   grad_x[m, k] = sum over n of grad_y[m, n] W[n, k]
+//   W[n, k] = zero[n, g] + step[n, g] code[n, k],  g = k div group
+//
+// A word holds eight codes of neighbouring k, pair i of them in bits 4 i and 16 + 4 i, so that a shift and a mask leave a pair in the halves of a register.
+// Under the bits of 128 that is a pair of bfloat16 numbers 128 + code, under zeros one of subnormal binary16 numbers code 2^-24: the matrix
+// instructions multiply both exactly.  So a group's sum of x code is a sum of exact products in binary32, to which step, and zero times the group's sum of
+// x (one more product, with ones), come afterwards.  A binary32 x goes as the three bfloat16 numbers that make it up, and its codes as converted numbers:
+// sums of 128 x would cost it 4 of its 24 bits.
+#include "actq_heads.h"
+
+namespace actq {
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ f32x4 multiply(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 multiply(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 multiply(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+// How a type of x meets the codes: a product is x (code kUnit + kShift).
+template <typename T>
+struct Meets;
+template <>
+struct Meets<__bf16> {
+    typedef bf16x8 vector;
+    static constexpr uint32_t kUnder = 0x43004300u, kOnes = 0x3f803f80u;
+    static constexpr float kUnit = 1.0f, kShift = 128.0f;
+};
+template <>
+struct Meets<_Float16> {
+    typedef f16x8 vector;
+    static constexpr uint32_t kUnder = 0u, kOnes = 0x3c003c00u;
+    static constexpr float kUnit = 0x1p-24f, kShift = 0.0f;
+};
+template <>
+struct Meets<float> {
+    typedef bf16x8 vector;
+    static constexpr uint32_t kOnes = 0x3f803f80u;
+    static constexpr float kUnit = 1.0f, kShift = 0.0f;
+};
+
+template <typename T>
+constexpr int kPieces = sizeof(T) == 4 ? 3 : 1;
+
+// The eight codes of a word in the order of their k.
+template <typename T>
+__device__ __forceinline__ typename Meets<T>::vector codes_of(uint32_t w)
+{
+    u32x4 v;
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (w >> 4 * i & 0x000f000fu) | Meets<T>::kUnder;
+    } else {
+        const uint32_t half[2] = {w & 0x0f0f0f0fu, w >> 4 & 0x0f0f0f0fu};   // bytes of the codes 0, 4, 1, 5 and 2, 6, 3, 7
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float low = static_cast<float>(half[i % 2] >> 8 * (i / 2) & 255u), high = static_cast<float>(half[i % 2] >> 8 * (i / 2 + 2) & 255u);
+            v[i] = __builtin_bit_cast(uint32_t, low) >> 16 | __builtin_bit_cast(uint32_t, high);   // whole numbers up to 15 end in zeros
+        }
+    }
+    return __builtin_bit_cast(typename Meets<T>::vector, v);
+}
+
+// Eight values of x as vectors for the matrix instructions.  Binary32: the upper 8 bits of a value's 24, of the rest, and what is left, each of them a
+// bfloat16 number.
+template <typename T>
+__device__ __forceinline__ void pieces_of(const Eight<T>& e, typename Meets<T>::vector (&v)[kPieces<T>])
+{
+    if constexpr (sizeof(T) == 2) {
+        v[0] = e.v;
+    } else {
+        u32x4 p[3];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t bits[3][2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const float x = e.v[2 * i + j];
+                bits[0][j] = __builtin_bit_cast(uint32_t, x) & 0xffff0000u;
+                const float rest = x - __builtin_bit_cast(float, bits[0][j]);
+                bits[1][j] = __builtin_bit_cast(uint32_t, rest) & 0xffff0000u;
+                bits[2][j] = __builtin_bit_cast(uint32_t, rest - __builtin_bit_cast(float, bits[1][j]));
+            }
+#pragma unroll
+            for (int k = 0; k < 3; ++k) p[k][i] = bits[k][0] >> 16 | (bits[k][1] & 0xffff0000u);
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) v[k] = __builtin_bit_cast(bf16x8, p[k]);
+    }
+}
+
+__device__ __forceinline__ float zero_of(uint32_t header) { return __builtin_bit_cast(float, header << 16); }
+__device__ __forceinline__ float step_of(uint32_t header) { return __builtin_bit_cast(float, header & 0xffff0000u); }
+
+struct Weights4 {
+    const uint32_t* codes;    // [outputs, groups * group / 8]
+    const uint32_t* header;   // [outputs, groups]: zero in the lower half, step in the upper one
+    int32_t inputs, outputs, groups;
+};
+
+Weights4 weights_of(const actq_weights4* w)
+{
+    return {w->codes, reinterpret_cast<const uint32_t*>(w->header), w->inputs, w->outputs, (w->inputs + w->group - 1) / w->group};
+}
+
+// ----------------------------------------------------------------------------- few rows
+
+// ROWS x 16 rows and COLUMNS x 16 outputs a workgroup, whose wavefronts take spans of 128 k in turn.  A lane's codes of a group are neighbours (a quarter
+// of the group), and so are its x.
+template <typename T>
+struct FewArgs {
+    Weights4 w;
+    const T* x;
+    int64_t x_stride;
+    const void* bias;
+    int32_t wide_bias;
+    T* y;
+    int64_t y_stride;
+    int64_t rows;
+};
+
+constexpr int kSpan = 128;
+
+template <typename T, int GROUP, int ROWS, int COLUMNS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void linear4_few_kernel(FewArgs<T> a)
+{
+    constexpr int kGroups = kSpan / GROUP, kWords = GROUP / 32;   // of a span; of a lane and group
+    typedef typename Meets<T>::vector V;
+    typedef uint32_t words __attribute__((ext_vector_type(kWords), aligned(4)));
+    __shared__ float joined[WAVES][ROWS * COLUMNS][256];
+    const int lane = threadIdx.x % 64, at = lane % 16, quarter = lane / 16;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t first_row = static_cast<int64_t>(blockIdx.y) * (16 * ROWS);
+    const int first_column = blockIdx.x * (16 * COLUMNS);
+    const int row_words = a.w.groups * (GROUP / 8);
+    const uint32_t* codes[COLUMNS];
+    const uint32_t* header[COLUMNS];
+    const T* x[ROWS];
+#pragma unroll
+    for (int c = 0; c < COLUMNS; ++c) {
+        const int64_t n = min(first_column + 16 * c + at, a.w.outputs - 1);
+        codes[c] = a.w.codes + n * row_words;
+        header[c] = a.w.header + n * a.w.groups;
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        const int64_t m = first_row + 16 * r + at;
+        x[r] = a.x + (m < a.rows ? m : a.rows - 1) * a.x_stride;
+    }
+    const V ones = __builtin_bit_cast(V, u32x4{Meets<T>::kOnes, Meets<T>::kOnes, Meets<T>::kOnes, Meets<T>::kOnes});
+    f32x4 total[ROWS][COLUMNS] = {};
+    for (int span = wave; span * kSpan < a.w.inputs; span += WAVES) {
+        uint32_t word[COLUMNS][kGroups * kWords], head[COLUMNS][kGroups];
+#pragma unroll
+        for (int c = 0; c < COLUMNS; ++c)
+#pragma unroll
+            for (int g = 0; g < kGroups; ++g) {
+                const int group = min(span * kGroups + g, a.w.groups - 1);   // beyond the last one x is zero
+                const words w = *reinterpret_cast<const words*>(codes[c] + group * (GROUP / 8) + quarter * kWords);
+#pragma unroll
+                for (int j = 0; j < kWords; ++j) word[c][g * kWords + j] = w[j];
+                head[c][g] = header[c][group];
+            }
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+            f32x4 sum[ROWS][COLUMNS] = {}, plain[ROWS] = {};
+#pragma unroll
+            for (int j = 0; j < kWords; ++j) {
+                const int k = span * kSpan + g * GROUP + quarter * (GROUP / 4) + 8 * j;
+                V code[COLUMNS];
+#pragma unroll
+                for (int c = 0; c < COLUMNS; ++c) code[c] = codes_of<T>(word[c][g * kWords + j]);
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) {
+                    Eight<T> e;
+                    if (k + kLaneValues <= a.w.inputs) {
+                        e.load(x[r] + k);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) e.v[i] = k + i < a.w.inputs ? x[r][k + i] : static_cast<T>(0.0f);
+                    }
+                    V p[kPieces<T>];
+                    pieces_of<T>(e, p);
+#pragma unroll
+                    for (int i = kPieces<T> - 1; i >= 0; --i) {
+                        plain[r] = multiply(p[i], ones, plain[r]);
+#pragma unroll
+                        for (int c = 0; c < COLUMNS; ++c) sum[r][c] = multiply(p[i], code[c], sum[r][c]);
+                    }
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < COLUMNS; ++c) {
+                const float step = step_of(head[c][g]), zero = fmaf(-Meets<T>::kShift, step, zero_of(head[c][g])), scaled = step * (1.0f / Meets<T>::kUnit);
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) total[r][c][i] = fmaf(zero, plain[r][i], fmaf(scaled, sum[r][c][i], total[r][c][i]));
+            }
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int c = 0; c < COLUMNS; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) joined[wave][r * COLUMNS + c][(4 * quarter + i) * 16 + at] = total[r][c][i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < ROWS * COLUMNS * 256; i += 64 * WAVES) {
+        const int column = i % (16 * COLUMNS), row = i / (16 * COLUMNS), tile = (row / 16) * COLUMNS + column / 16, place = row % 16 * 16 + column % 16;
+        const int64_t m = first_row + row;
+        const int n = first_column + column;
+        if (m >= a.rows || n >= a.w.outputs) continue;
+        float sum = joined[0][tile][place];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) sum += joined[w][tile][place];
+        if (a.bias) sum += a.wide_bias ? static_cast<const float*>(a.bias)[n] : static_cast<float>(static_cast<const T*>(a.bias)[n]);
+        a.y[m * a.y_stride + n] = static_cast<T>(sum);
+    }
+}
+
+// ----------------------------------------------------------------------------- the gradient
+
+// A workgroup's tile is kGradRows x 128 of grad_x, gathered over 64 outputs at a time from the LDS.  A weight goes there as two bfloat16 numbers (16 bits of
+// it; three for binary32), an element of grad_y as those that make it up (binary16: two, binary32: three): products below 2^-16 (2^-24) of the largest are left out.
+template <typename T>
+struct GradArgs {
+    Weights4 w;
+    const T* grad;
+    int64_t grad_stride;
+    T* out;
+    int64_t out_stride;
+    int64_t rows;
+};
+
+template <typename T>
+constexpr int kGradPieces = sizeof(T) == 4 ? 3 : std::is_same<T, _Float16>::value ? 2 : 1;   // of an element of grad_y
+template <typename T>
+constexpr int kWeightPieces = sizeof(T) == 4 ? 3 : 2;
+
+constexpr int kGradRows = 128, kGradColumns = 128, kGradDepth = 64;
+constexpr int kGradThreads = 256;
+
+// A row of the LDS is 128 bytes, eight chunks of 16, which lie at places that differ for neighbouring rows and for rows 8 apart: both kinds are accessed at once.
+__device__ __forceinline__ int chunk_place(int row, int chunk) { return row * 8 + (chunk ^ ((row ^ row >> 3) & 7)); }
+
+template <int N>
+__device__ __forceinline__ void split(float v, uint32_t (&bits)[N])   // bfloat16 numbers in the upper halves whose sum is v, but for what a last one leaves
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        bits[i] = __builtin_bit_cast(uint32_t, v);
+        if (i == N - 1) bits[i] += 0x7fffu + (bits[i] >> 16 & 1u);   // to nearest: what is left of 24 bits is exact, of 16 it is not
+        bits[i] &= 0xffff0000u;
+        v -= __builtin_bit_cast(float, bits[i]);
+    }
+}
+
+template <typename T, int GROUP>
+__global__ __launch_bounds__(kGradThreads) void linear4_backward_kernel(GradArgs<T> a)
+{
+    constexpr int kGP = kGradPieces<T>, kWP = kWeightPieces<T>, kHighest = kWP > kGP ? kWP - 1 : kGP - 1;
+    __shared__ u32x4 grads[kGP][kGradRows * 8];
+    __shared__ u32x4 weights[kWP][kGradColumns * 8];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int64_t first_row = static_cast<int64_t>(blockIdx.y) * kGradRows;
+    const int first_column = blockIdx.x * kGradColumns, row_words = a.w.groups * (GROUP / 8);
+    const int word = min(first_column / 8 + static_cast<int>(threadIdx.x % 16), row_words - 1), group = word / (GROUP / 8), quad = threadIdx.x / 16;
+    f32x16 sum[2][2] = {};
+    for (int from = 0; from < a.w.outputs; from += kGradDepth) {
+        // grad_y: chunks of eight outputs
+        for (int i = threadIdx.x; i < kGradRows * 8; i += kGradThreads) {
+            const int row = i / 8, chunk = i % 8, n = from + 8 * chunk;
+            const int64_t m = first_row + row;
+            const T* const g = a.grad + (m < a.rows ? m : a.rows - 1) * a.grad_stride;
+            Eight<T> e;
+            if (n + kLaneValues <= a.w.outputs) {
+                e.load(g + n);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) e.v[j] = n + j < a.w.outputs ? g[n + j] : static_cast<T>(0.0f);
+            }
+            if constexpr (kGP == 1) {
+                grads[0][chunk_place(row, chunk)] = __builtin_bit_cast(u32x4, e.v);
+            } else {
+                u32x4 p[kGP];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    uint32_t low[kGP], high[kGP];
+                    split(static_cast<float>(e.v[2 * j]), low);
+                    split(static_cast<float>(e.v[2 * j + 1]), high);
+#pragma unroll
+                    for (int k = 0; k < kGP; ++k) p[k][j] = low[k] >> 16 | high[k];
+                }
+#pragma unroll
+                for (int k = 0; k < kGP; ++k) grads[k][chunk_place(row, chunk)] = p[k];
+            }
+        }
+        // weights: a word of four outputs, turned so that the outputs are neighbours
+        {
+            float v[4][8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int n = from + 4 * quad + j;
+                const bool there = n < a.w.outputs;
+                const int64_t row = there ? n : 0;
+                const uint32_t w = there ? a.w.codes[row * row_words + word] : 0u, h = there ? a.w.header[row * a.w.groups + group] : 0u;
+                const float zero = zero_of(h), step = step_of(h);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[j][i] = fmaf(static_cast<float>(w >> (4 * (i / 2) + 16 * (i % 2)) & 15u), step, zero);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                uint32_t bits[4][kWP];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) split(v[j][i], bits[j]);
+                const int row = 8 * (threadIdx.x % 16) + i, place = chunk_place(row, quad / 2);
+#pragma unroll
+                for (int k = 0; k < kWP; ++k)
+                    reinterpret_cast<u32x2*>(&weights[k][place])[quad % 2] = u32x2{bits[0][k] >> 16 | bits[1][k], bits[2][k] >> 16 | bits[3][k]};
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int deep = 0; deep < kGradDepth / 16; ++deep) {
+            const int chunk = 2 * deep + lane / 32;
+            bf16x8 g[2][kGP], w[2][kWP];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+#pragma unroll
+                for (int k = 0; k < kGP; ++k) g[t][k] = __builtin_bit_cast(bf16x8, grads[k][chunk_place(64 * (wave / 2) + 32 * t + lane % 32, chunk)]);
+#pragma unroll
+                for (int k = 0; k < kWP; ++k) w[t][k] = __builtin_bit_cast(bf16x8, weights[k][chunk_place(64 * (wave % 2) + 32 * t + lane % 32, chunk)]);
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int p = kGP - 1; p >= 0; --p)
+#pragma unroll
+                        for (int q = kWP - 1; q >= 0; --q)
+                            if (p + q <= kHighest) sum[i][j] = multiply(g[i][p], w[j][q], sum[i][j]);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int k = first_column + 64 * (wave % 2) + 32 * j + lane % 32;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int64_t m = first_row + 64 * (wave / 2) + 32 * i + 8 * (r / 4) + 4 * (lane / 32) + r % 4;
+                if (m < a.rows && k < a.w.inputs) a.out[m * a.out_stride + k] = static_cast<T>(sum[i][j][r]);
+            }
+        }
+}
+
+// ----------------------------------------------------------------------------- the weights themselves
+
+// A thread is a word.  zero = min and step = (max - min) / 15 are rounded to bfloat16 before the codes are worked out with them; a group with an infinity or
+// NaN, or whose zero or step overflows, reads as NaN.
+template <typename T>
+__global__ __launch_bounds__(256) void weights4_quantize_kernel(const T* w, int64_t stride, int32_t inputs, int32_t group, int32_t row_words, int64_t words, uint32_t* codes, uint32_t* header)
+{
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const bool there = unit < words;
+    const int64_t n = there ? unit / row_words : 0;
+    const int word = there ? static_cast<int>(unit - n * row_words) : 0;
+    const T* const row = w + n * stride;
+    float x[8], low = INFINITY, high = -INFINITY;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int k = 8 * word + i;
+        x[i] = 0.0f;
+        if (k < inputs) x[i] = static_cast<float>(row[k]);
+        if (magnitude(x[i]) >= 0x7f800000u) {
+            bad = true;
+            x[i] = 0.0f;
+        }
+        if (k < inputs) {
+            low = fminf(low, x[i]);
+            high = fmaxf(high, x[i]);
+        }
+    }
+    int none = bad;
+    for (int step = 1; step < group / 8; step *= 2) {
+        low = fminf(low, __shfl_xor(low, step));
+        high = fmaxf(high, __shfl_xor(high, step));
+        none |= __shfl_xor(none, step);
+    }
+    const float zero = static_cast<float>(static_cast<__bf16>(low + 0.0f));
+    float step = static_cast<float>(static_cast<__bf16>((high - low) / 15.0f));
+    none = none || magnitude(zero) >= 0x7f800000u || magnitude(step) >= 0x7f800000u;
+    float inverse = 1.0f / step;
+    if (step == 0.0f || isinf(inverse)) inverse = step = 0.0f;
+    uint32_t out = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float code = none || 8 * word + i >= inputs ? 0.0f : rintf(fminf(fmaxf((x[i] - zero) * inverse, 0.0f), 15.0f));
+        out |= static_cast<uint32_t>(code) << (4 * (i / 2) + 16 * (i % 2));
+    }
+    if (!there) return;
+    codes[unit] = out;
+    if (word % (group / 8) == 0)
+        header[n * (row_words / (group / 8)) + word / (group / 8)] = none ? 0x7fc07fc0u : __builtin_bit_cast(uint32_t, zero) >> 16 | __builtin_bit_cast(uint32_t, step);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void weights4_dequantize_kernel(Weights4 w, int32_t group, int64_t words, T* out, int64_t stride)
+{
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (unit >= words) return;
+    const int row_words = w.groups * (group / 8);
+    const int64_t n = unit / row_words;
+    const int word = static_cast<int>(unit - n * row_words);
+    const uint32_t code = w.codes[unit], h = w.header[n * w.groups + word / (group / 8)];
+    Eight<T> e;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e.v[i] = static_cast<T>(fmaf(static_cast<float>(code >> (4 * (i / 2) + 16 * (i % 2)) & 15u), step_of(h), zero_of(h)));
+    T* const to = out + n * stride + 8 * word;
+    if (8 * word + 8 <= w.inputs) {
+        e.store(to);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (8 * word + i < w.inputs) to[i] = e.v[i];
+    }
+}
+
+template <typename F>
+int by_group(int32_t group, F f)
+{
+    return group == 32 ? f(std::integral_constant<int, 32>{}) : group == 64 ? f(std::integral_constant<int, 64>{}) : f(std::integral_constant<int, 128>{});
+}
+
+}  // namespace
+
+int launch_weights4_quantize(const actq_rows* w, int dtype, const actq_weights4* to, void* stream)
+{
+    return by_dtype(dtype, [&](auto type) {
+        typedef decltype(type) T;
+        const Weights4 v = weights_of(to);
+        const int32_t row_words = v.groups * (to->group / 8);
+        const int64_t words = static_cast<int64_t>(v.outputs) * row_words;
+        launch(weights4_quantize_kernel<T>, static_cast<unsigned>((words + 255) / 256), 256, static_cast<hipStream_t>(stream), static_cast<const T*>(w->data), w->stride, to->inputs,
+               to->group, row_words, words, const_cast<uint32_t*>(v.codes), const_cast<uint32_t*>(v.header));
+        return launched("actq_weights4_quantize");
+    });
+}
+
+int launch_weights4_dequantize(const actq_weights4* w, const actq_rows* out, int dtype, void* stream)
+{
+    return by_dtype(dtype, [&](auto type) {
+        typedef decltype(type) T;
+        const Weights4 v = weights_of(w);
+        const int64_t words = static_cast<int64_t>(v.outputs) * v.groups * (w->group / 8);
+        launch(weights4_dequantize_kernel<T>, static_cast<unsigned>((words + 255) / 256), 256, static_cast<hipStream_t>(stream), v, w->group, words, static_cast<T*>(out->data), out->stride);
+        return launched("actq_weights4_dequantize");
+    });
+}
+
+uint64_t linear4_workspace(const actq_weights4*, int, int64_t) { return 0; }
+uint64_t linear4_backward_workspace(const actq_weights4*, int, int64_t) { return 0; }
+
+int launch_linear4(const actq_weights4* w, const actq_rows* x, int dtype, int64_t rows, const void* bias, int bias_dtype, const actq_rows* y, void*, void* stream)
+{
+    return by_dtype(dtype, [&](auto type) {
+        return by_group(w->group, [&](auto g) {
+            typedef decltype(type) T;
+            constexpr int kGroup = decltype(g)::value;
+            FewArgs<T> a = {};
+            a.w = weights_of(w);
+            a.x = static_cast<const T*>(x->data);
+            a.x_stride = x->stride;
+            a.bias = bias;
+            a.wide_bias = bias_dtype == ACTQ_F32;
+            a.y = static_cast<T*>(y->data);
+            a.y_stride = y->stride;
+            a.rows = rows;
+            const auto go = [&](auto r, auto c, auto waves) {
+                constexpr int kRows = decltype(r)::value, kColumns = decltype(c)::value, kWaves = decltype(waves)::value;
+                const dim3 grid((a.w.outputs + 16 * kColumns - 1) / (16 * kColumns), static_cast<unsigned>((rows + 16 * kRows - 1) / (16 * kRows)));
+                launch(linear4_few_kernel<T, kGroup, kRows, kColumns, kWaves>, grid, 64 * kWaves, static_cast<hipStream_t>(stream), a);
+                return launched("actq_linear4");
+            };
+            return rows <= 16 ? go(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{}, std::integral_constant<int, 16>{})
+                              : go(std::integral_constant<int, 2>{}, std::integral_constant<int, 2>{}, std::integral_constant<int, 8>{});
+        });
+    });
+}
+
+int launch_linear4_backward(const actq_weights4* w, const actq_rows* grad_y, int dtype, int64_t rows, const actq_rows* grad_x, void*, void* stream)
+{
+    return by_dtype(dtype, [&](auto type) {
+        return by_group(w->group, [&](auto g) {
+            typedef decltype(type) T;
+            constexpr int kGroup = decltype(g)::value;
+            GradArgs<T> a = {};
+            a.w = weights_of(w);
+            a.grad = static_cast<const T*>(grad_y->data);
+            a.grad_stride = grad_y->stride;
+            a.out = static_cast<T*>(grad_x->data);
+            a.out_stride = grad_x->stride;
+            a.rows = rows;
+            const dim3 grid((w->inputs + kGradColumns - 1) / kGradColumns, static_cast<unsigned>((rows + kGradRows - 1) / kGradRows));
+            launch(linear4_backward_kernel<T, kGroup>, grid, kGradThreads, static_cast<hipStream_t>(stream), a);
+            return launched("actq_linear4_backward");
+        });
+    });
+}
+
+}  // namespace actq

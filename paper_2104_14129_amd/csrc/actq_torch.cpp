@@ -59,6 +59,16 @@ struct Api {
     decltype(&actq_cache_read) cache_read;
     decltype(&actq_cache_attention_workspace) cache_attention_workspace;
     decltype(&actq_cache_attention) cache_attention;
+    decltype(&actq_cache_append) cache_append;
+    decltype(&actq_block_norm) block_norm;
+    decltype(&actq_block_norm_workspace) block_norm_workspace;
+    decltype(&actq_block_norm_backward) block_norm_backward;
+    decltype(&actq_weights4_quantize) weights4_quantize;
+    decltype(&actq_weights4_dequantize) weights4_dequantize;
+    decltype(&actq_linear4_workspace) linear4_workspace;
+    decltype(&actq_linear4) linear4;
+    decltype(&actq_linear4_backward_workspace) linear4_backward_workspace;
+    decltype(&actq_linear4_backward) linear4_backward;
 };
 Api api = {};
 PyObject* actq_error = nullptr;   // the binding's exception class, called with (code, message)
@@ -903,6 +913,306 @@ PyObject* cache_attention_impl(PyObject* const* a)
 }
 ACTQ_ENTRY(cache_attention, 14)
 
+// (q or None, k, v, q_weight or None, k_weight or None, positions, cos, sin, slots, the cache's four, eps or None, interleaved, q_out or None) -> q_out or None
+PyObject* cache_append_impl(PyObject* const* a)
+{
+    const bool normed = a[13] != Py_None;
+    TORCH_CHECK_VALUE(normed || (a[3] == Py_None && a[4] == Py_None), "a weight without eps: without it nothing is normed");
+    TORCH_CHECK_VALUE(a[0] != Py_None || a[3] == Py_None, "q_weight without q");
+    TORCH_CHECK_VALUE(a[0] != Py_None || a[15] == Py_None, "q_out without q");
+    PyObject* const none_eps = normed ? nullptr : PyFloat_FromDouble(1.0);
+    // queries and keys are checked as those of the norm; keys alone stand in the queries' place
+    PyObject* const as_norm[9] = {a[0] == Py_None ? a[1] : a[0], a[0] == Py_None ? Py_None : a[1], a[0] == Py_None ? a[4] : a[3], a[0] == Py_None ? Py_None : a[4],
+                                  a[5], a[6], a[7], normed ? a[13] : none_eps, a[14]};
+    Norm n;
+    try {
+        norm_of(as_norm, n);
+    } catch (...) {
+        Py_XDECREF(none_eps);
+        throw;
+    }
+    Py_XDECREF(none_eps);
+    const bool queries = a[0] != Py_None;
+    const Tensor& k = tensor_of(a[1], "k");
+    const Tensor &v = tensor_of(a[2], "v"), &slots = tensor_of(a[8], "slots");
+    same_heads(v, k, "v");
+    const actq_heads hk = queries ? n.hk : n.hq, hv = heads_of(v, "v");
+    TORCH_CHECK_VALUE(slots.dim() == 1 && slots.size(0) == n.tokens, "slots must have an entry per token");
+    const Memory sp = contiguous_on_device(slots, at::kLong, "slots");
+    const actq_cache c = cache_of(a + 9, n.dim);
+    Tensor q_out;
+    actq_heads ho = {};
+    if (queries) {
+        q_out = heads_output(a[15], n.q, "q_out");
+        ho = heads_to(q_out, "q_out");
+    }
+    call(api.cache_append, &c, queries ? &n.hq : nullptr, &hk, &hv, n.dt, n.tokens, queries ? n.wq.p : nullptr, queries ? n.wk.p : n.wq.p, n.weight_dt, &n.rotation,
+         static_cast<int32_t>(normed), normed ? n.eps : 0.0f, sp, queries ? &ho : nullptr, current_stream());
+    return queries ? give(a[15], q_out) : wrap_or_none(q_out);
+}
+ACTQ_ENTRY(cache_append, 16)
+
+// ----------------------------------------------------------------------------- a layer around the attention
+
+// [rows, columns] as the library takes it.
+actq_rows rows_of(const Tensor& t, const char* name)
+{
+    on_current_device(t, name);
+    TORCH_CHECK_VALUE(t.dim() == 2, name, " must be [rows, columns]");
+    TORCH_CHECK_VALUE(t.stride(1) == 1 || t.size(1) <= 1 || t.numel() == 0, name, " must have contiguous rows");
+    return {t.data_ptr(), t.stride(0)};
+}
+
+// One that is written: elements do not share memory.
+actq_rows rows_to(const Tensor& t, const char* name)
+{
+    const actq_rows r = rows_of(t, name);
+    TORCH_CHECK_VALUE(t.size(0) <= 1 || std::abs(t.stride(0)) >= t.size(1), name, " must not have rows that overlap");
+    return r;
+}
+
+Tensor rows_output(PyObject* passed, const Tensor& like, const char* name)
+{
+    if (passed == Py_None) return empty_on(like, like.sizes(), like.scalar_type());
+    const Tensor& t = tensor_of(passed, name);
+    same_heads(t, like, name);
+    return t;
+}
+
+struct Block {
+    Tensor x;   // or r
+    std::optional<Tensor> h, gates;
+    actq_block b;
+    actq_rows hx, hh, hg;
+    at::ScalarType weight_type;
+    const actq_rows* h_rows;   // null without h
+};
+
+// (x or r, h or None, gate or None, weight, post_weight or None, scale, eps)
+void block_of(PyObject* const* a, const char* name, Block& k)
+{
+    k.x = tensor_of(a[0], name);
+    k.h = optional_tensor(a[1], "h");
+    const std::optional<Tensor> gate = optional_tensor(a[2], "gate"), post = optional_tensor(a[4], "post_weight");
+    const Tensor& weight = tensor_of(a[3], "weight");
+    actq_block& b = k.b;
+    b.dt = heads_dtype(k.x, name);
+    k.hx = rows_of(k.x, name);
+    b.tokens = k.x.size(0);
+    TORCH_CHECK_VALUE(k.x.size(1) <= INT32_MAX, name, " is too wide");
+    b.width = static_cast<int32_t>(k.x.size(1));
+    k.h_rows = nullptr;
+    if (k.h) {
+        same_heads(*k.h, k.x, "h");
+        k.hh = rows_of(*k.h, "h");
+        k.h_rows = &k.hh;
+    }
+    k.weight_type = weight.scalar_type();
+    TORCH_CHECK_TYPE(k.weight_type == at::kFloat || k.weight_type == k.x.scalar_type(), "weights must have the rows' dtype or torch.float32");
+    b.weight_dt = k.weight_type == at::kFloat ? ACTQ_F32 : b.dt;
+    TORCH_CHECK_VALUE(weight.numel() == b.width, "weight must have width entries");
+    b.weight = contiguous_on_device(weight, k.weight_type, "weight").p;
+    b.post_weight = b.gate = nullptr;
+    b.gates = nullptr;
+    if (post) {
+        TORCH_CHECK_VALUE(post->numel() == b.width, "post_weight must have width entries");
+        b.post_weight = contiguous_on_device(*post, k.weight_type, "post_weight").p;
+    }
+    if (gate && gate->dim() == 2) {
+        same_heads(*gate, k.x, "gate");
+        k.gates = gate;
+        k.hg = rows_of(*gate, "gate");
+        b.gates = &k.hg;
+    } else if (gate) {
+        TORCH_CHECK_VALUE(gate->numel() == b.width, "gate must be [width] or [tokens, width]");
+        b.gate = contiguous_on_device(*gate, k.weight_type, "gate").p;
+    }
+    b.scale = static_cast<float>(PyFloat_AsDouble(a[5]));
+    if (PyErr_Occurred()) throw python_error();
+    b.eps = static_cast<float>(PyFloat_AsDouble(a[6]));
+    if (PyErr_Occurred()) throw python_error();
+}
+
+// (x, h or None, gate or None, weight, post_weight or None, scale, eps, r or None, y or None) -> (r, y); without h r is x
+PyObject* block_norm_impl(PyObject* const* a)
+{
+    Block k;
+    block_of(a, "x", k);
+    TORCH_CHECK_VALUE(k.h || a[7] == Py_None, "r without h");
+    Tensor r;
+    actq_rows hr = {};
+    if (k.h) {
+        r = rows_output(a[7], k.x, "r");
+        hr = rows_to(r, "r");
+    }
+    const Tensor y = rows_output(a[8], k.x, "y");
+    const actq_rows hy = rows_to(y, "y");
+    call(api.block_norm, &k.b, &k.hx, k.h_rows, k.h ? &hr : nullptr, &hy, current_stream());
+    return tuple_of({k.h ? give(a[7], r) : give(a[0], k.x), give(a[8], y)});
+}
+ACTQ_ENTRY(block_norm, 9)
+
+// (grad_r or None, grad_y), block_of's seven with r, whether the weights need theirs -> gradients of x, h, gate, weight, post_weight (None for what is None)
+PyObject* block_norm_backward_impl(PyObject* const* a)
+{
+    Block k;
+    block_of(a + 2, "r", k);
+    const std::optional<Tensor> grad_r = optional_tensor(a[0], "grad_r");
+    const Tensor& grad_y = tensor_of(a[1], "grad_y");
+    actq_rows er = {}, xo = {}, ho = {}, go = {};
+    if (grad_r) {
+        same_heads(*grad_r, k.x, "grad_r");
+        er = rows_of(*grad_r, "grad_r");
+    }
+    same_heads(grad_y, k.x, "grad_y");
+    const actq_rows ey = rows_of(grad_y, "grad_y");
+    const Tensor x = empty_on(k.x, k.x.sizes(), k.x.scalar_type());
+    xo = rows_of(x, "grad_x");
+    Tensor h, gates, weight, post, gate, workspace;
+    if (k.h) {
+        h = empty_on(k.x, k.x.sizes(), k.x.scalar_type());
+        ho = rows_of(h, "grad_h");
+    }
+    if (k.gates) {
+        gates = empty_on(k.x, k.x.sizes(), k.x.scalar_type());
+        go = rows_of(gates, "grad_gate");
+    }
+    uint64_t bytes = 0;
+    if (a[9] == Py_True) {
+        const std::vector<int64_t> shape = {k.b.width};
+        weight = empty_on(k.x, shape, k.weight_type);
+        if (k.b.post_weight) post = empty_on(k.x, shape, k.weight_type);
+        if (k.b.gate) gate = empty_on(k.x, shape, k.weight_type);
+        call(api.block_norm_workspace, &k.b, &bytes);
+        workspace = empty_on(k.x, {static_cast<int64_t>(bytes)}, at::kByte);
+    }
+    const auto pointer = [](const Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; };
+    call(api.block_norm_backward, &k.b, grad_r ? &er : nullptr, &ey, &k.hx, k.h_rows, &xo, k.h ? &ho : nullptr, k.gates ? &go : nullptr, pointer(weight), pointer(post),
+         pointer(gate), pointer(workspace), bytes, current_stream());
+    return tuple_of({wrap_or_none(x), wrap_or_none(h), wrap_or_none(k.gates ? gates : gate), wrap_or_none(weight), wrap_or_none(post)});
+}
+ACTQ_ENTRY(block_norm_backward, 10)
+
+// (codes, header) of weights with `inputs` inputs
+actq_weights4 weights4_of(PyObject* const* a, int64_t inputs)
+{
+    const Tensor &codes = tensor_of(a[0], "codes"), &header = tensor_of(a[1], "header");
+    actq_weights4 w;
+    w.codes = contiguous_on_device(codes, at::kInt, "codes");
+    w.header = contiguous_on_device(header, at::kBFloat16, "header");
+    TORCH_CHECK_VALUE(codes.dim() == 2 && header.dim() == 3 && header.size(0) == codes.size(0) && header.size(2) == 2, "codes must be [outputs, groups * group / 8], header [outputs, groups, 2]");
+    const int64_t groups = header.size(1), words = codes.size(1), outputs = codes.size(0);
+    TORCH_CHECK_VALUE(groups > 0 && words % groups == 0 && words / groups <= 1024 && groups <= INT32_MAX / 128, "codes and header do not go together");
+    const int64_t group = 8 * (words / groups);
+    TORCH_CHECK_VALUE(inputs > (groups - 1) * group && inputs <= groups * group, inputs, " inputs are not those of ", groups, " groups of ", group);
+    TORCH_CHECK_VALUE(outputs <= INT32_MAX, "too many outputs");
+    w.inputs = static_cast<int32_t>(inputs);
+    w.outputs = static_cast<int32_t>(outputs);
+    w.group = static_cast<int32_t>(group);
+    return w;
+}
+
+// (w, codes, header)
+PyObject* weights4_quantize_impl(PyObject* const* a)
+{
+    const Tensor& w = tensor_of(a[0], "w");
+    const actq_dtype dt = heads_dtype(w, "w");
+    const actq_rows r = rows_of(w, "w");
+    const actq_weights4 to = weights4_of(a + 1, w.size(1));
+    TORCH_CHECK_VALUE(w.size(0) == to.outputs, "w must have a row for each output");
+    call(api.weights4_quantize, &r, dt, &to, current_stream());
+    Py_RETURN_NONE;
+}
+ACTQ_ENTRY(weights4_quantize, 3)
+
+// (codes, header, out)
+PyObject* weights4_dequantize_impl(PyObject* const* a)
+{
+    const Tensor& out = tensor_of(a[2], "out");
+    const actq_dtype dt = heads_dtype(out, "out");
+    const actq_rows r = rows_to(out, "out");
+    const actq_weights4 w = weights4_of(a, out.size(1));
+    TORCH_CHECK_VALUE(out.size(0) == w.outputs, "out must have a row for each output");
+    call(api.weights4_dequantize, &w, &r, dt, current_stream());
+    Py_RETURN_NONE;
+}
+ACTQ_ENTRY(weights4_dequantize, 3)
+
+// Rows of a tensor [..., columns]: as it lies where its leading dimensions are one, else contiguous.
+Tensor as_rows(const Tensor& t, const char* name)
+{
+    TORCH_CHECK_VALUE(t.dim() >= 1, name, " must have at least one dimension");
+    if (t.dim() == 2) return t;
+    int64_t rows = 1;
+    for (int64_t i = 0; i + 1 < t.dim(); ++i) rows *= t.size(i);
+    return t.reshape({rows, t.size(t.dim() - 1)});
+}
+
+std::vector<int64_t> with_columns(const Tensor& t, int64_t columns)
+{
+    std::vector<int64_t> shape = t.sizes().vec();
+    shape.back() = columns;
+    return shape;
+}
+
+// (x [..., inputs], codes, header, bias or None, out [..., outputs] or None) -> out
+PyObject* linear4_impl(PyObject* const* a)
+{
+    const Tensor& given = tensor_of(a[0], "x");
+    on_current_device(given, "x");
+    const actq_dtype dt = heads_dtype(given, "x");
+    const Tensor x = as_rows(given, "x");
+    const actq_rows hx = rows_of(x, "x");
+    const actq_weights4 w = weights4_of(a + 1, x.size(1));
+    const std::optional<Tensor> bias = optional_tensor(a[3], "bias");
+    Memory bp = {nullptr};
+    actq_dtype bias_dt = dt;
+    if (bias) {
+        TORCH_CHECK_TYPE(bias->scalar_type() == given.scalar_type() || bias->scalar_type() == at::kFloat, "bias must have the rows' dtype or torch.float32");
+        TORCH_CHECK_VALUE(bias->numel() == w.outputs, "bias must have an entry per output");
+        bp = contiguous_on_device(*bias, bias->scalar_type(), "bias");
+        bias_dt = bias->scalar_type() == at::kFloat ? ACTQ_F32 : dt;
+    }
+    const std::vector<int64_t> shape = with_columns(given, w.outputs);
+    const Tensor out = a[4] == Py_None ? empty_on(given, shape, given.scalar_type()) : tensor_of(a[4], "out");
+    TORCH_CHECK_VALUE(out.sizes() == at::IntArrayRef(shape), "out has another shape than expected");
+    TORCH_CHECK_TYPE(out.scalar_type() == given.scalar_type(), "out must be ", dtype_name(given.scalar_type()), ", got ", dtype_name(out.scalar_type()));
+    TORCH_CHECK_VALUE(out.dim() == 2 || out.is_contiguous(), "out must be contiguous or have two dimensions");
+    const Tensor y = as_rows(out, "out");
+    const actq_rows hy = rows_to(y, "out");
+    uint64_t bytes = 0;
+    call(api.linear4_workspace, &w, dt, x.size(0), &bytes);
+    Tensor workspace;
+    if (bytes > 0) workspace = empty_on(given, {static_cast<int64_t>(bytes)}, at::kByte);
+    void* const wp = bytes > 0 ? workspace.data_ptr() : nullptr;
+    call(api.linear4, &w, &hx, dt, x.size(0), bp, bias_dt, &hy, wp, bytes, current_stream());
+    return give(a[4], out);
+}
+ACTQ_ENTRY(linear4, 5)
+
+// (grad_y [..., outputs], codes, header, inputs) -> grad_x [..., inputs]
+PyObject* linear4_backward_impl(PyObject* const* a)
+{
+    const Tensor& given = tensor_of(a[0], "grad_y");
+    on_current_device(given, "grad_y");
+    const actq_dtype dt = heads_dtype(given, "grad_y");
+    const Tensor g = as_rows(given, "grad_y");
+    const actq_rows hg = rows_of(g, "grad_y");
+    const actq_weights4 w = weights4_of(a + 1, integer(a[3]));
+    TORCH_CHECK_VALUE(g.size(1) == w.outputs, "grad_y must have an entry per output");
+    const Tensor out = empty_on(given, with_columns(given, w.inputs), given.scalar_type());
+    const Tensor x = as_rows(out, "grad_x");
+    const actq_rows hx = rows_of(x, "grad_x");
+    uint64_t bytes = 0;
+    call(api.linear4_backward_workspace, &w, dt, g.size(0), &bytes);
+    Tensor workspace;
+    if (bytes > 0) workspace = empty_on(given, {static_cast<int64_t>(bytes)}, at::kByte);
+    void* const wp = bytes > 0 ? workspace.data_ptr() : nullptr;
+    call(api.linear4_backward, &w, &hg, dt, g.size(0), &hx, wp, bytes, current_stream());
+    return THPVariable_Wrap(out);
+}
+ACTQ_ENTRY(linear4_backward, 4)
+
 // ----------------------------------------------------------------------------- autograd
 
 using torch::autograd::AutogradContext;
@@ -1175,6 +1485,8 @@ PyMethodDef methods[] = {
     ACTQ_METHOD(quantize_pack), ACTQ_METHOD(unpack_dequantize), ACTQ_METHOD(compress_mixed), ACTQ_METHOD(relu_forward), ACTQ_METHOD(relu_backward),
     ACTQ_METHOD(maxpool2d_forward), ACTQ_METHOD(maxpool2d_backward), ACTQ_METHOD(linear_one_launch), ACTQ_METHOD(linear_gradients), ACTQ_METHOD(linear), ACTQ_METHOD(relu), ACTQ_METHOD(maxpool2d),
     ACTQ_METHOD(head_norm_rotate), ACTQ_METHOD(head_norm_rotate_backward), ACTQ_METHOD(cache_write), ACTQ_METHOD(cache_read), ACTQ_METHOD(cache_attention),
+    ACTQ_METHOD(cache_append), ACTQ_METHOD(block_norm), ACTQ_METHOD(block_norm_backward), ACTQ_METHOD(weights4_quantize), ACTQ_METHOD(weights4_dequantize),
+    ACTQ_METHOD(linear4), ACTQ_METHOD(linear4_backward),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "actq_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,0 +1,131 @@
+"""Appending new tokens to the cache: norm, rotation and quantizer in one launch."""
+import numpy as np
+import pytest
+import torch
+
+import _heads as H
+from paper_2104_14129_amd import binding as B
+from paper_2104_14129_amd.cache import PagedCache
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+
+# tokens, q_heads, heads, dim, dtype, rotated, wide, interleaved, norm, key_bits, value_bits, page
+CASES = [
+    (1, 1, 1, 64, F32, 64, True, False, True, 8, 8, 16), (1, 32, 8, 128, BF16, 128, False, False, True, 8, 8, 64), (7, 0, 3, 64, F16, 32, True, True, True, 4, 4, 16),
+    (33, 5, 5, 256, BF16, 64, True, True, True, 8, 4, 32), (200, 12, 4, 64, F32, 32, True, True, False, 8, 4, 16), (3, 9, 2, 128, F16, 16, False, False, False, 4, 8, 1024),
+    (1025, 4, 1, 128, F16, 128, False, False, True, 4, 4, 64), (2051, 2, 2, 64, BF16, 64, True, False, True, 8, 8, 128), (5, 64, 8, 256, F32, 256, True, False, True, 8, 8, 16),
+    (64, 3, 17, 64, F32, 48, True, False, True, 4, 8, 16),
+]
+
+
+def _case(tokens, q_heads, heads, dim, dtype, rotated, wide, interleaved, norm, key_bits, value_bits, page, paddings=True):
+    g = torch.Generator().manual_seed(7 * tokens + dim)
+    x = (2 * torch.randn((tokens, (q_heads + 2 * heads) * dim), generator=g)).to(dtype)
+    rows = 101
+    angle = torch.rand((rows, rotated // 2), generator=g) * 6.3
+    positions = torch.randint(-1 if paddings else 0, rows + 1 if paddings else rows, (tokens,), generator=g, dtype=torch.int32)
+    weights = [(1 + 0.3 * torch.randn(dim, generator=g)).to(F32 if wide else dtype) if norm else None for _ in range(2)]
+    pages = tokens // page + 3
+    slots = torch.randperm(pages * page, generator=g)[:tokens]
+    return x, positions, torch.cos(angle), torch.sin(angle), weights, pages, slots
+
+
+def _views(x, q_heads, heads, dim):
+    return tuple(x[:, a * dim:b * dim].view(len(x), b - a, dim) for a, b in ((0, q_heads), (q_heads, q_heads + heads), (q_heads + heads, q_heads + 2 * heads)))
+
+
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_append(case):
+    """Codes and headers bit for bit: values as they are, keys from 64 bits rounded to binary32 (those of a 64-bit value within 2^-52 of a border between two binary32
+    numbers may be either; none is, at these sizes).  Queries as the norm of heads gives them; slots that are not named keep what they hold."""
+    tokens, q_heads, heads, dim, dtype, rotated, wide, interleaved, norm, key_bits, value_bits, page = case
+    x, positions, cos, sin, (qw, kw), pages, slots = _case(*case)
+    slots = slots.clone()
+    if tokens > 4:
+        slots[1], slots[3] = -1, pages * page   # outside the cache
+    q, k, v = _views(x, q_heads, heads, dim)
+    dq, dk, dv = _views(x.to(DEV), q_heads, heads, dim)
+    table = positions.to(DEV), cos.to(DEV), sin.to(DEV)
+    cache, want = H.make_cache(pages, heads, page, dim, key_bits, value_bits, 3), H.make_cache(pages, heads, page, dim, key_bits, value_bits, 3, device="cpu")
+    on = lambda t: None if t is None else t.to(DEV)   # noqa: E731
+    out = B.cache_append(dq if q_heads else None, dk, dv, on(qw) if q_heads else None, on(kw), *table, slots.to(DEV), *cache, eps=1e-5 if norm else None, interleaved=interleaved)
+    there = (slots >= 0) & (slots < pages * page)
+    exact = H.norm_rotate(k, kw, positions, cos, sin, 1e-5, interleaved) if norm else H.rotate(k.double(), positions, cos, sin, interleaved)
+    H.fill(want, slots[there], exact[there].float(), v[there], key_bits, value_bits)
+    for name, a, b in zip(("key codes", "key header", "value codes", "value header"), cache, want):
+        assert torch.equal(a.cpu().view(torch.uint8), b.view(torch.uint8)), name
+    if not q_heads:
+        assert out is None
+    elif norm:
+        assert torch.equal(out, B.head_norm_rotate(dq, None, on(qw), None, *table, 1e-5, interleaved)[0])
+    else:
+        turned = H.rotate(q.double(), positions, cos, sin, interleaved)
+        assert ((out.cpu().double() - turned).abs() <= H.ROUNDOFF[dtype] * turned.abs() + 4 * 2.0 ** -24 * q.double().abs().amax(-1, keepdim=True) + 2.0 ** -25).all()
+
+
+def test_keys_that_are_not_finite_read_as_nan():
+    case = (6, 2, 2, 64, F32, 64, True, False, True, 8, 4, 16)
+    x, positions, cos, sin, (qw, kw), pages, slots = _case(*case, paddings=False)
+    x[2, 130], x[4, 64 * 5] = float("nan"), float("inf")   # the first head's key of token 2, the second head's value of token 4
+    q, k, v = _views(x.to(DEV), 2, 2, 64)
+    cache = H.make_cache(pages, 2, 16, 64, 8, 4, 1, poison=False)
+    B.cache_append(q, k, v, qw.to(DEV), kw.to(DEV), positions.to(DEV), cos.to(DEV), sin.to(DEV), slots.to(DEV), *cache)
+    keys, values = B.cache_read(slots.to(DEV), *cache, 64, F32)
+    bad = torch.isnan(keys).any(-1).cpu()
+    assert bad.nonzero().tolist() == [[2, 0]] and torch.isnan(keys[2, 0]).all()
+    assert torch.isnan(values).any(-1).cpu().nonzero().tolist() == [[4, 1]] and torch.isnan(values[4, 1]).all()
+
+
+def test_object_in_place_and_captured():
+    """PagedCache.append; queries in place; one graph replayed with other tokens and eager calls between."""
+    tokens, q_heads, heads, dim = 9, 4, 2, 128
+    g = torch.Generator().manual_seed(2)
+    cache, eager = (PagedCache(4, 16, heads, dim, 8, 4, device=DEV) for _ in range(2))
+    x = torch.randn((tokens, (q_heads + 2 * heads) * dim), generator=g).to(BF16).to(DEV)
+    q, k, v = _views(x, q_heads, heads, dim)
+    w = torch.randn((2, dim), generator=g).to(BF16).to(DEV)
+    angle = torch.rand((50, dim // 2), generator=g).to(DEV)
+    positions, slots = torch.arange(tokens, dtype=torch.int32, device=DEV), torch.randperm(64, generator=g)[:tokens].to(DEV)
+    args = (w[0], w[1], positions, torch.cos(angle), torch.sin(angle), slots)
+    want = eager.append(q, k, v, *args)
+    mine = q.clone()
+    out = cache.append(mine, k, v, *args, q_out=mine)
+    assert out is mine and torch.equal(mine, want) and all(torch.equal(a, b) for a, b in zip(cache.buffers, eager.buffers))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            out = cache.append(q, k, v, *args)
+    torch.cuda.current_stream().wait_stream(side)
+    for _ in range(3):
+        x.copy_(torch.randn(x.shape, generator=g).to(BF16))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager.append(q, k, v, *args)) and all(torch.equal(a, b) for a, b in zip(cache.buffers, eager.buffers))
+
+
+def test_refused_by_the_binding():
+    case = (6, 2, 2, 64, F32, 64, True, False, True, 8, 4, 16)
+    x, positions, cos, sin, (qw, kw), pages, slots = _case(*case, paddings=False)
+    q, k, v = _views(x.to(DEV), 2, 2, 64)
+    cache = H.make_cache(pages, 2, 16, 64, 8, 4, 1, poison=False)
+    table, slots = (positions.to(DEV), cos.to(DEV), sin.to(DEV)), slots.to(DEV)
+    qw, kw = qw.to(DEV), kw.to(DEV)
+    with pytest.raises(ValueError, match="eps"):
+        B.cache_append(q, k, v, qw, kw, *table, slots, *cache, eps=None)
+    with pytest.raises(ValueError, match="without q"):
+        B.cache_append(None, k, v, qw, kw, *table, slots, *cache)
+    with pytest.raises(ValueError, match="q_out without q"):
+        B.cache_append(None, k, v, None, kw, *table, slots, *cache, q_out=q)
+    for args, error in (((q, k.half(), v, qw, kw), TypeError), ((q, k, v.half(), qw, kw), TypeError), ((q, k, v[:5], qw, kw), ValueError), ((q[:5], k, v, qw, kw), ValueError),
+                        ((q, k, v, qw[:5], kw), ValueError), ((q, k, v, qw, kw.half()), TypeError)):
+        with pytest.raises(error):
+            B.cache_append(*args, *table, slots, *cache)
+    with pytest.raises(ValueError, match="per token"):
+        B.cache_append(q, k, v, qw, kw, *table, slots[:3], *cache)
+    with pytest.raises(ValueError, match="expanded"):
+        B.cache_append(q, k, v, qw, kw, *table, slots, *cache, q_out=torch.zeros((1, 2, 64), device=DEV).expand(6, 2, 64))
+    assert np.isfinite(B.cache_append(q, k, v, qw, kw, *table, slots, *cache).cpu().numpy()).all()

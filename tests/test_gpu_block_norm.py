@@ -1,0 +1,203 @@
+"""The norms around a block with gate, scale and residual sum, and their gradients, against their definitions in 64 bits."""
+import pytest
+import torch
+
+import _heads as H
+import _layer as Y
+from paper_2104_14129_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+EPS = 1e-5
+
+# tokens, width, dtype, wide weights, post, gate, scale
+CASES = [
+    (1, 1, F32, True, True, "channel", 1.0), (1, 64, BF16, False, True, "token", 0.5), (3, 7, F16, False, False, "none", 1.0), (2, 511, BF16, True, True, "channel", 1.0),
+    (9, 512, F32, True, False, "token", -2.0), (600, 513, F16, False, True, "none", 0.3), (5, 1000, BF16, False, True, "channel", 1.0), (700, 1024, BF16, True, True, "token", 1.0),
+    (513, 1025, F32, True, True, "channel", 1.0), (4, 2048, F16, True, True, "channel", 1.0), (530, 2047, F16, False, True, "token", 0.7), (3, 2049, F32, True, False, "channel", 1.0),
+    (8, 4096, BF16, False, True, "channel", 1.0), (1031, 4096, F16, False, False, "none", 0.5), (2, 4097, BF16, False, True, "token", 1.0), (515, 8191, BF16, True, True, "channel", 1.0),
+    (1, 8192, F32, True, True, "none", 1.0), (3, 8200, F16, False, True, "token", 1.0), (517, 16384, BF16, False, True, "channel", 1.0), (2, 16383, F32, True, True, "token", 1.0),
+    (4100, 64, F32, True, True, "channel", 1.0), (2100, 200, BF16, False, True, "channel", 1.0),
+]
+
+
+def _case(tokens, width, dtype, wide, post, gate, scale):
+    g = torch.Generator().manual_seed(17 * tokens + width)
+    randn = lambda *shape: torch.randn(shape, generator=g)   # noqa: E731
+    wdt = F32 if wide else dtype
+    x, h = (randn(tokens, width) * (0.1 + 2 * torch.rand(width, generator=g))).to(dtype), (3 * randn(tokens, width)).to(dtype)
+    weight, post = (1 + 0.3 * randn(width)).to(wdt), (0.5 + 0.2 * randn(width)).to(wdt) if post else None
+    gate = {"none": None, "channel": randn(width).to(wdt), "token": randn(tokens, width).to(dtype)}[gate]
+    return x, h, gate, weight, post, scale, EPS
+
+
+def _on(t):
+    return t.to(DEV) if isinstance(t, torch.Tensor) else t
+
+
+def _close(got, want, bound, dtype):
+    assert got.dtype == dtype and got.shape == want.shape
+    limit = H.ROUNDOFF[dtype] * want.abs() + bound + 2.0 ** -25   # of subnormal binary16
+    off = (got.cpu().double() - want).abs()
+    assert (off <= limit).all(), float((off / limit).max())
+
+
+@pytest.mark.parametrize("case", CASES, ids=str)
+def test_forward(case):
+    args = _case(*case)
+    got = B.block_norm(*map(_on, args))
+    want = Y.block_norm(*args)
+    bounds = Y.block_norm_bounds(*args, *want)
+    _close(got[0], want[0], bounds[0], case[2])
+    _close(got[1], want[1], bounds[1], case[2])
+
+
+@pytest.mark.parametrize("case", CASES, ids=str)
+@pytest.mark.parametrize("with_r", [True, False])
+def test_backward(case, with_r):
+    """Binary32 sums along a row are within 54 roundings of the sum of magnitudes, and an element is made of up to two of them, the second out of the
+    first: 96 and 192.  A channel's gradient is added up over a team's tokens (a 512th of them) in binary32, then in 64 bits."""
+    x, h, gate, weight, post, scale, eps = _case(*case)
+    g = torch.Generator().manual_seed(5)
+    grad_r, grad_y = (torch.randn(x.shape, generator=g).to(x.dtype) for _ in range(2))
+    r = x
+    args = grad_r if with_r else None, grad_y, r, h, gate, weight, post, scale, eps
+    got = B.block_norm_backward(*map(_on, args))
+    again = B.block_norm_backward(*map(_on, args))
+    assert all(a is b or torch.equal(a, b) for a, b in zip(got, again)), "the order of the sums is fixed"
+    want = Y.block_norm_backward(*args)
+    names = dict(zip(("x", "h", "gate", "weight", "post"), got))
+    assert {k for k, v in names.items() if v is not None} == set(want)
+    steps = 192 + x.shape[0] // 512 + 1
+    for name, (value, magnitude) in want.items():
+        like = {"x": x, "h": x, "gate": gate, "weight": weight, "post": weight}[name]
+        _close(names[name], value, steps * Y.UNIT * magnitude, like.dtype)
+    none = B.block_norm_backward(*map(_on, args), need_weights=False)
+    assert torch.equal(none[0], got[0]) and torch.equal(none[1], got[1]) and none[3] is None and none[4] is None
+
+
+def test_gradients_by_differences():
+    """The directional derivative along random directions; central differences of the definition itself are off by step^2 of it."""
+    x, h, gate, weight, post, scale, eps = _case(6, 96, F32, True, True, "token", 0.8)
+    g = torch.Generator().manual_seed(9)
+    u, e = (torch.randn(x.shape, generator=g) for _ in range(2))
+    r, _, _ = Y.block_norm(x, h, gate, weight, post, scale, eps)
+    got = B.block_norm_backward(*map(_on, (e, u, r.float(), h, gate, weight, post, scale, eps)))
+    inputs = [x, h, gate, weight, post]
+    for i, grad in enumerate(got):
+        direction = torch.randn(inputs[i].shape, generator=g).double()
+        step = 1e-5
+
+        def value(sign):
+            moved = [t.double() + sign * step * direction if j == i else t.double() for j, t in enumerate(inputs)]
+            r, y, _ = Y.block_norm(moved[0], moved[1], moved[2], moved[3], moved[4], scale, eps)
+            return float((r * e.double()).sum() + (y * u.double()).sum())
+
+        want = (value(1) - value(-1)) / (2 * step)
+        have = float((grad.cpu().double() * direction).sum())
+        size = float((grad.cpu().double() * direction).abs().sum())
+        assert abs(want - have) < 1e-5 * size + 1e-6, (i, want, have)
+
+
+def test_norm_alone():
+    x = torch.randn((5, 300), generator=torch.Generator().manual_seed(1))
+    w = torch.randn(300, generator=torch.Generator().manual_seed(2))
+    dx = x.to(DEV)
+    r, y = B.block_norm(dx, None, None, w.to(DEV), eps=EPS)
+    assert r is dx
+    want = Y.block_norm(x, None, None, w, None, 1.0, EPS)
+    _close(y, want[1], Y.block_norm_bounds(x, None, None, w, None, 1.0, EPS, *want)[1], F32)
+    u = torch.randn((5, 300), generator=torch.Generator().manual_seed(3))
+    got = B.block_norm_backward(None, u.to(DEV), dx, None, None, w.to(DEV), eps=EPS)
+    want = Y.block_norm_backward(None, u, x, None, None, w, None, 1.0, EPS)
+    assert got[1] is None and got[2] is None and got[4] is None
+    _close(got[0], want["x"][0], 192 * Y.UNIT * want["x"][1], F32)
+    _close(got[3], want["weight"][0], 192 * Y.UNIT * want["weight"][1], F32)
+
+
+@pytest.mark.parametrize("width", [96, 4096, 8192])
+def test_strides_in_place_and_neighbours(width):
+    """Rows inside a wider matrix, backwards, expanded (read only); r over x and y over h; nothing beside the rows is written."""
+    tokens = 5
+    g = torch.Generator().manual_seed(width)
+    flat = torch.randn((2, tokens, width + 3), generator=g).to(F16).to(DEV)
+    before = flat.clone()
+    x, h = flat[0, :, 1:1 + width], flat[1, :, 2:2 + width]
+    w = torch.ones(width, device=DEV)
+    gate = torch.randn((1, width), generator=g).to(F16).to(DEV).expand(tokens, width)
+    want = B.block_norm(x.clone(), h.clone(), gate.contiguous(), w, w)
+    odd = torch.empty((2 * tokens, width + 1), dtype=F16, device=DEV)[::2, :width]
+    got = B.block_norm(x, h, gate, w, w, r=odd)
+    assert got[0] is odd and torch.equal(odd, want[0]) and torch.equal(got[1], want[1])
+    r, y = B.block_norm(x, h, gate, w, w, r=x, y=h)
+    assert torch.equal(x, want[0]) and torch.equal(h, want[1]) and r.data_ptr() == x.data_ptr() and y.data_ptr() == h.data_ptr()
+    assert torch.equal(flat[0, :, 0], before[0, :, 0]) and torch.equal(flat[0, :, 1 + width:], before[0, :, 1 + width:])
+    assert torch.equal(flat[1, :, :2], before[1, :, :2]) and torch.equal(flat[1, :, 2 + width:], before[1, :, 2 + width:])
+
+
+def test_no_tokens_zeros_and_rows_that_are_not_finite():
+    w = torch.ones(128, device=DEV)
+    none = torch.zeros((0, 128), device=DEV)
+    r, y = B.block_norm(none, none, w, w, w)
+    assert r.shape == y.shape == (0, 128)
+    got = B.block_norm_backward(none, none, none, none, w, w, w)
+    assert got[0].shape == (0, 128) and all((t == 0).all() for t in got[2:])
+    zero = torch.zeros((3, 128), device=DEV)
+    r, y = B.block_norm(zero, zero, w, w, w)
+    assert (r == 0).all() and (y == 0).all()
+    assert all(torch.isfinite(t).all() for t in B.block_norm_backward(zero, zero + 1, zero, zero, w, w, w))
+    for width in (128, 4096):
+        w = torch.ones(width, device=DEV)
+        x = torch.randn((9, width), generator=torch.Generator().manual_seed(4)).to(DEV)
+        fine = B.block_norm(x, x, None, w, w)
+        bad = x.clone()
+        bad[3, 5], bad[6, 0] = float("nan"), float("inf")
+        got = B.block_norm(bad, x, None, w, w)
+        keep = [i for i in range(9) if i not in (3, 6)]
+        assert torch.equal(got[1][keep], fine[1][keep]) and torch.equal(got[0][keep], fine[0][keep])
+        assert torch.isnan(got[1][3]).all() and torch.isnan(got[1][6, 0])
+
+
+def test_refused_by_the_binding():
+    x, w = torch.zeros((4, 64), device=DEV), torch.ones(64, device=DEV)
+    for args, error in (((x, x.half(), None, w), TypeError), ((x, x[:3], None, w), ValueError), ((x, x, w[:3], w), ValueError), ((x, x, None, w.half()), TypeError),
+                        ((x.half(), x.half(), None, w.half(), w), TypeError), ((x.t(), x.t(), None, w[:4]), ValueError), ((x.double(), x, None, w), TypeError),
+                        ((x, x, None, w[:63]), ValueError), ((x[0], x[0], None, w), ValueError)):
+        with pytest.raises(error):
+            B.block_norm(*args)
+    with pytest.raises(ValueError, match="overlap"):
+        B.block_norm(x, x, None, w, r=x[:1].expand(4, 64))
+    with pytest.raises(ValueError, match="without h"):
+        B.block_norm(x, None, None, w, r=x)
+    with pytest.raises(B.ActqError):
+        B.block_norm(x, None, w, w)
+    with pytest.raises(B.ActqError, match="width"):
+        B.block_norm(torch.zeros((1, 16385), device=DEV), None, None, torch.ones(16385, device=DEV))
+
+
+def test_captured_and_replayed_on_another_stream():
+    """One graph with forward and backward, replayed with other inputs and with eager calls between."""
+    tokens, width = 37, 1000
+    g = torch.Generator().manual_seed(8)
+    x, h, u = (torch.randn((tokens, width), generator=g).to(BF16).to(DEV) for _ in range(3))
+    w, p, gate = (torch.randn(width, generator=g).to(BF16).to(DEV) for _ in range(3))
+
+    def both():
+        r, y = B.block_norm(x, h, gate, w, p, 0.5)
+        return (r, y, *B.block_norm_backward(None, u, r, h, gate, w, p, 0.5))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            out = both()
+    torch.cuda.current_stream().wait_stream(side)
+    for i in range(4):
+        x.copy_(torch.randn((tokens, width), generator=g).to(BF16))
+        h.copy_(torch.randn((tokens, width), generator=g).to(BF16))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(out, both())), i
