@@ -616,7 +616,7 @@ int actq_block_norm_backward(const actq_block* block, const actq_rows* grad_r, c
  *   header  device [outputs, groups, 2] bfloat16 bit patterns, (zero, step)
  */
 typedef struct actq_weights4 {
-    const uint32_t* codes;  /* aligned to 4 bytes */
+    const uint32_t* codes;  /* aligned to 16 bytes */
     const uint16_t* header; /* aligned to 4 bytes */
     int32_t inputs;         /* in [1, 2^20] */
     int32_t outputs;        /* in [1, 2^20] */

@@ -751,7 +751,7 @@ static int check_weights4(const char* who, const actq_weights4* w)
     if (w->group != 32 && w->group != 64 && w->group != 128) return fail(ACTQ_EINVAL, "%s: unsupported group of %d inputs (32, 64 or 128)", who, w->group);
     constexpr int32_t kMost = 1 << 20;
     if (w->inputs < 1 || w->outputs < 1 || w->inputs > kMost || w->outputs > kMost) return fail(ACTQ_EINVAL, "%s: inputs and outputs must be in [1, 2^20]", who);
-    if (!w->codes || !w->header || !aligned(w->codes, 4) || !aligned(w->header, 4)) return fail(ACTQ_EINVAL, "%s: codes or header is null or not aligned to 4 bytes", who);
+    if (!w->codes || !w->header || !aligned(w->codes, 16) || !aligned(w->header, 4)) return fail(ACTQ_EINVAL, "%s: codes or header is null or not aligned to 16 and 4 bytes", who);
     return ACTQ_OK;
 }
 

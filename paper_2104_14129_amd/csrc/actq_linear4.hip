@@ -19,6 +19,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ f32x4 multiply(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 multiply(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 multiply(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 multiply(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 
 // How a type of x meets the codes: a product is x (code kUnit + kShift).
@@ -52,8 +53,10 @@ __device__ __forceinline__ typename Meets<T>::vector codes_of(uint32_t w)
 {
     u32x4 v;
     if constexpr (sizeof(T) == 2) {
+        uint32_t under = Meets<T>::kUnder;
+        if (under) asm("" : "+v"(under));   // in a vector register: one instruction takes one constant from elsewhere, and so masks and sets at once
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = (w >> 4 * i & 0x000f000fu) | Meets<T>::kUnder;
+        for (int i = 0; i < 4; ++i) v[i] = (w >> 4 * i & 0x000f000fu) | under;
     } else {
         const uint32_t half[2] = {w & 0x0f0f0f0fu, w >> 4 & 0x0f0f0f0fu};   // bytes of the codes 0, 4, 1, 5 and 2, 6, 3, 7
 #pragma unroll
@@ -93,6 +96,18 @@ __device__ __forceinline__ void pieces_of(const Eight<T>& e, typename Meets<T>::
     }
 }
 
+template <int N>
+__device__ __forceinline__ void split(float v, uint32_t (&bits)[N])   // bfloat16 numbers in the upper halves whose sum is v, but for what a last one leaves
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        bits[i] = __builtin_bit_cast(uint32_t, v);
+        if (i == N - 1) bits[i] += 0x7fffu + (bits[i] >> 16 & 1u);   // to nearest: what is left of 24 bits is exact, of 16 it is not
+        bits[i] &= 0xffff0000u;
+        v -= __builtin_bit_cast(float, bits[i]);
+    }
+}
+
 __device__ __forceinline__ float zero_of(uint32_t header) { return __builtin_bit_cast(float, header << 16); }
 __device__ __forceinline__ float step_of(uint32_t header) { return __builtin_bit_cast(float, header & 0xffff0000u); }
 
@@ -105,6 +120,32 @@ struct Weights4 {
 Weights4 weights_of(const actq_weights4* w)
 {
     return {w->codes, reinterpret_cast<const uint32_t*>(w->header), w->inputs, w->outputs, (w->inputs + w->group - 1) / w->group};
+}
+
+template <typename T>
+__device__ __forceinline__ float bias_of(const void* bias, int wide, int n)
+{
+    if (!bias) return 0.0f;
+    return wide ? static_cast<const float*>(bias)[n] : static_cast<float>(static_cast<const T*>(bias)[n]);
+}
+
+// The parts of a sum over a long axis, joined in their order.
+template <typename T>
+__global__ __launch_bounds__(256) void linear4_join_kernel(const float* parts, int32_t count, int64_t rows, int32_t columns, const void* bias, int wide_bias, T* out, int64_t stride)
+{
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, all = rows * columns;
+    if (unit >= all) return;
+    const int64_t m = unit / columns;
+    const int n = static_cast<int>(unit - m * columns);
+    float sum = bias_of<T>(bias, wide_bias, n);
+    for (int i = 0; i < count; i += 8) {
+        float v[8];   // all in flight
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = i + j < count ? parts[(i + j) * all + unit] : 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += v[j];
+    }
+    out[m * stride + n] = static_cast<T>(sum);
 }
 
 // ----------------------------------------------------------------------------- few rows
@@ -218,9 +259,376 @@ __global__ __launch_bounds__(64 * WAVES) void linear4_few_kernel(FewArgs<T> a)
         float sum = joined[0][tile][place];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) sum += joined[w][tile][place];
-        if (a.bias) sum += a.wide_bias ? static_cast<const float*>(a.bias)[n] : static_cast<float>(static_cast<const T*>(a.bias)[n]);
+        sum += bias_of<T>(a.bias, a.wide_bias, n);
         a.y[m * a.y_stride + n] = static_cast<T>(sum);
     }
+}
+
+// ----------------------------------------------------------------------------- many rows
+
+// What x looks like for the kernel below: 16-bit numbers, whole spans of k, zeros beyond the last input.  16-bit rows that are like that already are taken
+// as they lie; others are copied (binary32: split into the bfloat16 numbers that make it up).  Beside it the sums of every group of a row, as
+// three bfloat16 numbers each.
+template <typename T>
+struct PrepareArgs {
+    const T* x;
+    int64_t stride;
+    int32_t inputs, padded;   // whole spans
+    int64_t rows;
+    u32x4* copy;              // [pieces][rows][padded / 8]; null: none
+    u32x2* sums;              // [padded / group][rows]
+};
+
+template <typename T, int GROUP>
+__global__ __launch_bounds__(256) void linear4_prepare_kernel(PrepareArgs<T> a)
+{
+    const int chunks = a.padded / 8;
+    const int64_t unit = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const bool there = unit < a.rows * chunks;
+    const int64_t m = there ? unit / chunks : 0;
+    const int chunk = there ? static_cast<int>(unit - m * chunks) : 0, k = 8 * chunk;
+    const T* const x = a.x + m * a.stride + k;
+    Eight<T> e;
+    if (k + kLaneValues <= a.inputs) {
+        e.load(x);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e.v[i] = k + i < a.inputs ? x[i] : static_cast<T>(0.0f);
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += static_cast<float>(e.v[i]);
+#pragma unroll
+    for (int step = 1; step < GROUP / 8; step *= 2) sum += __shfl_xor(sum, step);
+    if (!there) return;
+    if (a.copy) {
+        typename Meets<T>::vector p[kPieces<T>];
+        pieces_of<T>(e, p);
+#pragma unroll
+        for (int i = 0; i < kPieces<T>; ++i) a.copy[(i * a.rows + m) * chunks + chunk] = __builtin_bit_cast(u32x4, p[i]);
+    }
+    if (chunk % (GROUP / 8) != 0) return;
+    uint32_t bits[3];
+    split(sum, bits);
+    a.sums[chunk / (GROUP / 8) * a.rows + m] = u32x2{bits[0] >> 16 | bits[1], bits[2] >> 16};
+}
+
+template <typename T>
+struct ManyArgs {
+    Weights4 w;
+    const uint16_t* x;        // [pieces][rows][x_stride], 16-byte aligned rows
+    int64_t x_stride, x_piece;
+    const u32x2* sums;
+    int32_t padded;
+    const void* bias;
+    int32_t wide_bias;
+    T* y;
+    int64_t y_stride;
+    int64_t rows;
+    int32_t row_tiles, column_tiles;
+    int32_t share;            // k of a part; whole spans
+    float* parts;             // [parts][rows][outputs]; null: the only part writes y
+};
+
+// Sixteen or four bytes of every lane from memory to neighbouring places in the LDS, `to` being the first lane's, without registers between.
+typedef const __attribute__((address_space(1))) void* InMemory;
+typedef __attribute__((address_space(3))) void* InLds;
+
+__device__ __forceinline__ void to_lds(const void* from, u32x4* to) { __builtin_amdgcn_global_load_lds((InMemory) reinterpret_cast<uintptr_t>(from), (InLds)to, 16, 0, 0); }
+__device__ __forceinline__ void to_lds(const void* from, uint32_t* to) { __builtin_amdgcn_global_load_lds((InMemory) reinterpret_cast<uintptr_t>(from), (InLds)to, 4, 0, 0); }
+
+// Until all but the last COUNT of a wavefront's loads have arrived, in all wavefronts of the workgroup.
+template <int COUNT>
+__device__ __forceinline__ void arrived()
+{
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(COUNT) : "memory");
+}
+
+// A workgroup's tile is 128 rows x 256 outputs, a wavefront's 64 x 64: blocks of 32 x 32.  A group's sums of products and the total are both what ordinary instructions
+// work with, so they share the 256 registers that these see, and two wavefronts a SIMD.  x, codes and headers go from memory to the LDS without registers, two
+// stages of 128 k ahead (binary32, three times the bytes: one of 64); a wavefront turns the codes of its outputs into numbers in registers.
+template <typename T, int GROUP>
+__global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
+{
+    typedef typename Meets<T>::vector V;
+    constexpr int kP = kPieces<T>, kRing = kP == 1 ? 3 : 2, kDepth = kP == 1 ? 128 : 64, kRows = 128, kColumns = 256;
+    constexpr int kChunks = kDepth / 8, kSlots = kDepth / 32;   // 16 bytes of a row of x, of an output's codes
+    constexpr int kScaled = GROUP < kDepth ? GROUP : kDepth, kHeads = kDepth / kScaled, kSteps = kScaled / 16;
+    constexpr int kMoves = kRows * kChunks / 512, kCodeMoves = kColumns * kSlots / 512, kHeadMoves = kHeads == 4 ? 2 : 1;
+    constexpr int kLoads = kP * kMoves + kCodeMoves + kHeadMoves;   // of a wavefront and stage
+    // one array: of several the compiler knows which of them a load to the LDS writes, and waits for it before the next read of that one
+    constexpr int kTile = kRows * kChunks, kCodes = kP * kTile, kHeadsAt = kCodes + kColumns * kSlots, kStage = kHeadsAt + kHeadMoves * 128;
+    __shared__ u32x4 lds[kRing * kStage];
+    const int lane = threadIdx.x % 64, at = lane % 32, half = lane / 32;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    // each XCD (workgroups go to them in turn) takes a run of tiles, bands of 4 row tiles through all column tiles: their rows and codes stay in its L2
+    const int tiles = a.row_tiles * a.column_tiles, share = (tiles + 7) / 8, unit = blockIdx.x % 8 * share + blockIdx.x / 8;
+    if (unit >= tiles || static_cast<int>(blockIdx.x / 8) >= share) return;
+    const int band = unit / (4 * a.column_tiles), in_band = unit - band * 4 * a.column_tiles, high = min(4, a.row_tiles - 4 * band);
+    const int64_t first_row = static_cast<int64_t>(4 * band + in_band % high) * kRows;
+    const int first_column = (in_band / high) * kColumns, row_words = a.w.groups * (GROUP / 8);
+    const auto code_swizzle = [](int column) { return kSlots == 4 ? column >> 2 & 3 : 0; };
+
+    // where the lane's loads come from: the place in the LDS goes by the lane, so what lies there is chosen here
+    const uint16_t* x_from[kMoves];
+#pragma unroll
+    for (int i = 0; i < kMoves; ++i) {
+        const int row = (i * 512 + threadIdx.x) / kChunks, chunk = threadIdx.x % kChunks ^ (row & (kChunks - 1));
+        const int64_t m = first_row + row;
+        x_from[i] = a.x + (m < a.rows ? m : a.rows - 1) * a.x_stride + 8 * chunk;
+    }
+    const uint32_t* codes_from[kCodeMoves];
+    int code_chunk[kCodeMoves];
+#pragma unroll
+    for (int i = 0; i < kCodeMoves; ++i) {
+        const int column = (i * 512 + threadIdx.x) / kSlots;
+        const int64_t n = min(first_column + column, a.w.outputs - 1);
+        codes_from[i] = a.w.codes + n * row_words;
+        code_chunk[i] = threadIdx.x % kSlots ^ code_swizzle(column);
+    }
+    const uint32_t* const heads_from = a.w.header + static_cast<int64_t>(min(first_column + static_cast<int>(threadIdx.x % 256), a.w.outputs - 1)) * a.w.groups;
+    const auto load = [&](int k, int to) {
+#pragma unroll
+        for (int p = 0; p < kP; ++p)
+#pragma unroll
+            for (int i = 0; i < kMoves; ++i) to_lds(x_from[i] + p * a.x_piece + k, lds + to * kStage + p * kTile + i * 512 + wave * 64);
+        // beyond the last group x is zero, whatever the codes are
+#pragma unroll
+        for (int i = 0; i < kCodeMoves; ++i) to_lds(codes_from[i] + 4 * min(k / 32 + code_chunk[i], row_words / 4 - 1), lds + to * kStage + kCodes + i * 512 + wave * 64);
+#pragma unroll
+        for (int i = 0; i < kHeadMoves; ++i) {
+            const int group = k / GROUP + (kHeads == 1 ? 0 : 2 * i + static_cast<int>(threadIdx.x) / 256);
+            to_lds(heads_from + min(group, a.w.groups - 1), reinterpret_cast<uint32_t*>(lds + to * kStage + kHeadsAt) + i * 512 + wave * 64);
+        }
+    };
+    const int begin = blockIdx.y * a.share, end = min(begin + a.share, a.padded);   // the part's k
+    load(begin, 0);
+    if (kRing > 2 && begin + kDepth < end) load(begin + kDepth, 1);
+
+    // zero times the groups' sums of x, and what the codes' shift leaves: products of the parts of both.  A lane takes four neighbouring groups at a time.
+    const int columns = wave % 4 * 64, rows = wave / 4 * 64;   // the wavefront's place in the tile
+    f32x16 total[2][2] = {};
+    {
+        const u32x2* sums[2];
+        const uint32_t* header[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int64_t m = first_row + rows + 32 * r + at;
+            sums[r] = a.sums + (m < a.rows ? m : a.rows - 1);
+            header[r] = a.w.header + static_cast<int64_t>(min(first_column + columns + 32 * r + at, a.w.outputs - 1)) * a.w.groups;
+        }
+        constexpr int kTogether = Meets<T>::kShift != 0.0f ? 1 : 2;   // groups of a lane in a product
+        const int groups = min(end / GROUP, a.w.groups);
+        for (int g = begin / GROUP; g < groups; g += 8) {
+            const int mine = g + 4 * half;
+            u32x2 v[2][4];
+            u32x4 h[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                if (g + 8 <= groups) {
+                    typedef u32x4 any __attribute__((aligned(4)));
+                    h[r] = *reinterpret_cast<const any*>(header[r] + mine);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) h[r][j] = mine + j < groups ? header[r][mine + j] : 0u;
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[r][j] = sums[r][min(mine + j, groups - 1) * a.rows];
+            }
+#pragma unroll
+            for (int q = 0; q < 4; q += kTogether) {
+                u32x4 s[2], z[2];
+#pragma unroll
+                for (int j = 0; j < kTogether; ++j) {
+                    const uint32_t there = mine + q + j < groups ? ~0u : 0u;   // no NaN times zero
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+                        const uint32_t head = h[r][q + j], zero = head & 0xffffu;
+                        s[r][2 * j] = v[r][q + j][0] & there;
+                        s[r][2 * j + 1] = v[r][q + j][1] & there;
+                        z[r][2 * j] = zero | zero << 16;
+                        z[r][2 * j + 1] = zero;
+                        if (kTogether == 1) {
+                            s[r][2] = s[r][0];
+                            s[r][3] = s[r][1];
+                            const uint32_t shifted = __builtin_bit_cast(uint32_t, step_of(head) * -Meets<T>::kShift);
+                            z[r][2] = shifted | shifted >> 16;
+                            z[r][3] = shifted >> 16;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) total[r][c] = multiply(__builtin_bit_cast(bf16x8, s[r]), __builtin_bit_cast(bf16x8, z[c]), total[r][c]);
+            }
+        }
+    }
+    const auto place = [](int row, int chunk) { return row * kChunks + (chunk ^ (row & (kChunks - 1))); };
+    arrived<0>();
+    int buffer = 0;
+    for (int k = begin; k < end; k += kDepth) {
+        const int ahead = k + (kRing - 1) * kDepth;
+        if (ahead < end) load(ahead, buffer == 0 ? kRing - 1 : buffer - 1);
+        const u32x4* const tile = lds + buffer * kStage;
+        const u32x4* const codes = tile + kCodes;
+        const uint32_t* const heads = reinterpret_cast<const uint32_t*>(tile + kHeadsAt);
+#pragma unroll 1   // two groups' sums at once do not fit the registers
+        for (int g = 0; g < kHeads; ++g) {
+            f32x16 sum[2][2];
+            uint32_t word[2][kSteps];
+            float scaled[2];
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const int column = columns + 32 * c + at;
+                scaled[c] = step_of(heads[256 * g + column]) * (1.0f / Meets<T>::kUnit);
+                if constexpr (GROUP == 32) {   // a group is 16 bytes of an output, a half of them this lane's
+                    const u32x2 v = reinterpret_cast<const u32x2*>(&codes[column * kSlots + (g ^ code_swizzle(column))])[half];
+                    word[c][0] = v[0];
+                    word[c][1] = v[1];
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kSteps / 4; ++j) {
+                        const u32x4 v = codes[column * kSlots + ((g * (kScaled / 32) + 2 * j + half) ^ code_swizzle(column))];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) word[c][4 * j + i] = v[i];
+                    }
+                }
+            }
+#pragma unroll
+            for (int step = 0; step < kSteps; ++step) {
+                const int chunk = GROUP == 32 ? 4 * g + 2 * half + step : g * (kScaled / 8) + step / 4 * 8 + 4 * half + step % 4;
+                V w[2];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) w[c] = codes_of<T>(word[c][step]);
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int p = kP - 1; p >= 0; --p) {
+                        const V v = __builtin_bit_cast(V, tile[p * kTile + place(rows + 32 * r + at, chunk)]);
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            if (step == 0 && p == kP - 1) sum[r][c] = f32x16{};
+                            sum[r][c] = multiply(v, w[c], sum[r][c]);
+                        }
+                    }
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) total[r][c][i] = fmaf(scaled[c], sum[r][c][i], total[r][c][i]);
+        }
+        // the next stage; what lies behind it may still be on its way
+        if (ahead < end)
+            arrived<(kRing - 2) * kLoads>();
+        else
+            arrived<0>();
+        buffer = buffer == kRing - 1 ? 0 : buffer + 1;
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        const int n = first_column + columns + 32 * c + at;
+        if (n >= a.w.outputs) continue;
+        const int64_t m = first_row + rows + 4 * half;
+        if (a.parts) {
+            float* const to = a.parts + (blockIdx.y * a.rows + m) * a.w.outputs + n;
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int down = 32 * r + 8 * (i / 4) + i % 4;
+                    if (m + down < a.rows) to[down * static_cast<int64_t>(a.w.outputs)] = total[r][c][i];
+                }
+            continue;
+        }
+        const float bias = bias_of<T>(a.bias, a.wide_bias, n);
+        T* const to = a.y + m * a.y_stride + n;
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int down = 32 * r + 8 * (i / 4) + i % 4;
+                if (m + down < a.rows) to[down * a.y_stride] = static_cast<T>(total[r][c][i] + bias);
+            }
+    }
+}
+
+// Whether rows of x can be taken as they lie.
+bool as_they_lie(const actq_weights4* w, int dtype, const actq_rows* x)
+{
+    return dtype != ACTQ_F32 && w->inputs % kSpan == 0 && x->stride % 8 == 0 && reinterpret_cast<uintptr_t>(x->data) % 16 == 0;
+}
+
+int32_t padded_inputs(const actq_weights4* w) { return (w->inputs + kSpan - 1) / kSpan * kSpan; }
+
+// The sums, then the copy of x.
+uint64_t sums_bytes(const actq_weights4* w, int64_t rows) { return (static_cast<uint64_t>(rows) * (padded_inputs(w) / w->group) * sizeof(u32x2) + 15) / 16 * 16; }
+uint64_t copy_bytes(const actq_weights4* w, int dtype, int64_t rows) { return static_cast<uint64_t>(rows) * padded_inputs(w) * (dtype == ACTQ_F32 ? 6 : 2); }
+
+// Parts of the inputs: where the tiles are fewer than the compute units, as many as make one workgroup for each, of two spans at least.
+struct Parts {
+    int32_t row_tiles, column_tiles, count, share;
+};
+
+Parts parts_of(const actq_weights4* w, int64_t rows)
+{
+    Parts p;
+    p.row_tiles = static_cast<int32_t>((rows + 127) / 128);
+    p.column_tiles = (w->outputs + 255) / 256;
+    const int64_t tiles = static_cast<int64_t>(p.row_tiles) * p.column_tiles, spans = padded_inputs(w) / kSpan;
+    const int64_t most = 256 / tiles < spans / 2 ? 256 / tiles : spans / 2, share = most > 1 ? (spans + most - 1) / most : spans;
+    p.share = static_cast<int32_t>(share * kSpan);
+    p.count = static_cast<int32_t>((spans + share - 1) / share);
+    return p;
+}
+
+uint64_t parts_bytes(const actq_weights4* w, int64_t rows)
+{
+    const Parts p = parts_of(w, rows);
+    return p.count > 1 ? static_cast<uint64_t>(p.count) * rows * w->outputs * sizeof(float) : 0;
+}
+
+template <typename T, int GROUP>
+int launch_many(const actq_weights4* w, const actq_rows* x, int64_t rows, const void* bias, int bias_dtype, const actq_rows* y, void* workspace, hipStream_t stream)
+{
+    const int dtype = sizeof(T) == 4 ? ACTQ_F32 : ACTQ_F16;
+    const bool copied = !as_they_lie(w, dtype, x);
+    const int32_t padded = padded_inputs(w);
+    u32x2* const sums = static_cast<u32x2*>(workspace);
+    u32x4* const copy = copied ? reinterpret_cast<u32x4*>(static_cast<char*>(workspace) + sums_bytes(w, rows)) : nullptr;
+    PrepareArgs<T> p = {};
+    p.x = static_cast<const T*>(x->data);
+    p.stride = x->stride;
+    p.inputs = w->inputs;
+    p.padded = padded;
+    p.rows = rows;
+    p.copy = copy;
+    p.sums = sums;
+    launch(linear4_prepare_kernel<T, GROUP>, static_cast<unsigned>((rows * (padded / 8) + 255) / 256), 256, stream, p);
+    ManyArgs<T> a = {};
+    a.w = weights_of(w);
+    a.x = copied ? reinterpret_cast<const uint16_t*>(copy) : static_cast<const uint16_t*>(x->data);
+    a.x_stride = copied ? padded : x->stride;
+    a.x_piece = rows * padded;
+    a.sums = sums;
+    a.padded = padded;
+    a.bias = bias;
+    a.wide_bias = bias_dtype == ACTQ_F32;
+    a.y = static_cast<T*>(y->data);
+    a.y_stride = y->stride;
+    a.rows = rows;
+    const Parts parts = parts_of(w, rows);
+    a.row_tiles = parts.row_tiles;
+    a.column_tiles = parts.column_tiles;
+    a.share = parts.share;
+    if (parts.count > 1) a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + sums_bytes(w, rows) + copy_bytes(w, dtype, rows));
+    launch(linear4_many_kernel<T, GROUP>, dim3(static_cast<unsigned>((a.row_tiles * a.column_tiles + 7) / 8 * 8), static_cast<unsigned>(parts.count)), 512, stream, a);
+    if (parts.count > 1)
+        launch(linear4_join_kernel<T>, static_cast<unsigned>((rows * w->outputs + 255) / 256), 256, stream, static_cast<const float*>(a.parts), parts.count, rows, w->outputs, bias,
+               a.wide_bias, a.y, a.y_stride);
+    return launched("actq_linear4");
 }
 
 // ----------------------------------------------------------------------------- the gradient
@@ -247,18 +655,6 @@ constexpr int kGradThreads = 256;
 
 // A row of the LDS is 128 bytes, eight chunks of 16, which lie at places that differ for neighbouring rows and for rows 8 apart: both kinds are accessed at once.
 __device__ __forceinline__ int chunk_place(int row, int chunk) { return row * 8 + (chunk ^ ((row ^ row >> 3) & 7)); }
-
-template <int N>
-__device__ __forceinline__ void split(float v, uint32_t (&bits)[N])   // bfloat16 numbers in the upper halves whose sum is v, but for what a last one leaves
-{
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        bits[i] = __builtin_bit_cast(uint32_t, v);
-        if (i == N - 1) bits[i] += 0x7fffu + (bits[i] >> 16 & 1u);   // to nearest: what is left of 24 bits is exact, of 16 it is not
-        bits[i] &= 0xffff0000u;
-        v -= __builtin_bit_cast(float, bits[i]);
-    }
-}
 
 template <typename T, int GROUP>
 __global__ __launch_bounds__(kGradThreads) void linear4_backward_kernel(GradArgs<T> a)
@@ -434,6 +830,9 @@ __global__ __launch_bounds__(256) void weights4_dequantize_kernel(Weights4 w, in
     }
 }
 
+// The most rows that go to the kernel for few.
+constexpr int64_t kFewRows = 64;
+
 template <typename F>
 int by_group(int32_t group, F f)
 {
@@ -466,15 +865,16 @@ int launch_weights4_dequantize(const actq_weights4* w, const actq_rows* out, int
     });
 }
 
-uint64_t linear4_workspace(const actq_weights4*, int, int64_t) { return 0; }
+uint64_t linear4_workspace(const actq_weights4* w, int dtype, int64_t rows) { return rows > kFewRows ? sums_bytes(w, rows) + copy_bytes(w, dtype, rows) + parts_bytes(w, rows) : 0; }
 uint64_t linear4_backward_workspace(const actq_weights4*, int, int64_t) { return 0; }
 
-int launch_linear4(const actq_weights4* w, const actq_rows* x, int dtype, int64_t rows, const void* bias, int bias_dtype, const actq_rows* y, void*, void* stream)
+int launch_linear4(const actq_weights4* w, const actq_rows* x, int dtype, int64_t rows, const void* bias, int bias_dtype, const actq_rows* y, void* workspace, void* stream)
 {
     return by_dtype(dtype, [&](auto type) {
         return by_group(w->group, [&](auto g) {
             typedef decltype(type) T;
             constexpr int kGroup = decltype(g)::value;
+            if (rows > kFewRows) return launch_many<T, kGroup>(w, x, rows, bias, bias_dtype, y, workspace, static_cast<hipStream_t>(stream));
             FewArgs<T> a = {};
             a.w = weights_of(w);
             a.x = static_cast<const T*>(x->data);

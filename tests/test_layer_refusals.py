@@ -61,7 +61,7 @@ def test_block_norm_refusals():
 
 def test_linear4_refusals():
     L_ = B.lib()
-    bad = [None, _weights(codes=None), _weights(codes=FAKE + 2), _weights(header=None), _weights(header=FAKE + 2), _weights(inputs=0), _weights(inputs=(1 << 20) + 1),
+    bad = [None, _weights(codes=None), _weights(codes=FAKE + 2), _weights(codes=FAKE + 8), _weights(header=None), _weights(header=FAKE + 2), _weights(inputs=0), _weights(inputs=(1 << 20) + 1),
            _weights(outputs=0), _weights(outputs=(1 << 20) + 1), _weights(group=16), _weights(group=256), _weights(group=96)]
     # weights, x, dt, rows, bias, bias_dt, y, workspace, bytes, stream
     ok = [_weights(), _rows(), 1, 5, FAKE, 0, _rows(), FAKE, 1 << 40, None]
