@@ -8,6 +8,7 @@
 // instructions multiply both exactly.  So a group's sum of x code is a sum of exact products in binary32, to which step, and zero times the group's sum of
 // x (one more product, with ones), come afterwards.  A binary32 x goes as the three bfloat16 numbers that make it up, and its codes as converted numbers:
 // sums of 128 x would cost it 4 of its 24 bits.
+#include <cstdlib>
 #include "actq_heads.h"
 
 namespace actq {
@@ -344,21 +345,24 @@ __device__ __forceinline__ void arrived()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(COUNT) : "memory");
 }
 
-// A workgroup's tile is 128 rows x 256 outputs, a wavefront's 64 x 64: blocks of 32 x 32.  A group's sums of products and the total are both what ordinary instructions
-// work with, so they share the 256 registers that these see, and two wavefronts a SIMD.  x, codes and headers go from memory to the LDS without registers, two
-// stages of 128 k ahead (binary32, three times the bytes: one of 64); a wavefront turns the codes of its outputs into numbers in registers.
-template <typename T, int GROUP>
-__global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
+// A workgroup's tile is ROWS rows x 256 outputs, made of blocks of 32 x 32: 128 rows, two by two blocks a wavefront, or 32, one.  A group's sums of products
+// and the total are both what ordinary instructions work with, so they share the 256 registers that these see, and 128 rows take two wavefronts a SIMD.  x, codes and headers
+// go from memory to the LDS without registers, two stages of 128 k ahead (binary32, three times the bytes: 64 k, and one ahead with 128 rows); a wavefront turns the codes of its outputs
+// into numbers in registers.  Under 32 rows, where memory is what counts, the groups' sums of x are one more product, with ones.
+template <typename T, int GROUP, int ROWS>
+__global__ __launch_bounds__(512, ROWS == 128 ? 2 : 4) void linear4_many_kernel(ManyArgs<T> a)
 {
     typedef typename Meets<T>::vector V;
-    constexpr int kP = kPieces<T>, kRing = kP == 1 ? 3 : 2, kDepth = kP == 1 ? 128 : 64, kRows = 128, kColumns = 256;
+    constexpr int kP = kPieces<T>, kB = ROWS == 128 ? 2 : 1, kRing = kP == 1 || kB == 1 ? 3 : 2, kDepth = kP == 1 ? 128 : 64, kRows = ROWS, kColumns = 256;
     constexpr int kChunks = kDepth / 8, kSlots = kDepth / 32;   // 16 bytes of a row of x, of an output's codes
     constexpr int kScaled = GROUP < kDepth ? GROUP : kDepth, kHeads = kDepth / kScaled, kSteps = kScaled / 16;
-    constexpr int kMoves = kRows * kChunks / 512, kCodeMoves = kColumns * kSlots / 512, kHeadMoves = kHeads == 4 ? 2 : 1;
-    constexpr int kLoads = kP * kMoves + kCodeMoves + kHeadMoves;   // of a wavefront and stage
+    constexpr int kMoves = kRows * kChunks >= 512 ? kRows * kChunks / 512 : 1, kCodeMoves = kColumns * kSlots / 512;
+    constexpr int kLoads = kP * kMoves + kCodeMoves;   // of a wavefront and stage, beside headers
+    constexpr int kHeadGroups = 8;                     // headers of so many groups are fetched at a time: one by one they would take as many lines of the caches as the codes
     // one array: of several the compiler knows which of them a load to the LDS writes, and waits for it before the next read of that one
-    constexpr int kTile = kRows * kChunks, kCodes = kP * kTile, kHeadsAt = kCodes + kColumns * kSlots, kStage = kHeadsAt + kHeadMoves * 128;
-    __shared__ u32x4 lds[kRing * kStage];
+    constexpr int kTilePlace = kRows * kChunks < 512 ? 512 : kRows * kChunks, kCodes = kP * kTilePlace, kStage = kCodes + kColumns * kSlots, kHeadPlace = kColumns * kHeadGroups;
+    __shared__ u32x4 lds[kRing * kStage + 2 * kHeadPlace / 4];
+    uint32_t* const heads = reinterpret_cast<uint32_t*>(lds + kRing * kStage);   // [2][outputs][kHeadGroups]
     const int lane = threadIdx.x % 64, at = lane % 32, half = lane / 32;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     // each XCD (workgroups go to them in turn) takes a run of tiles, bands of 4 row tiles through all column tiles: their rows and codes stay in its L2
@@ -373,7 +377,7 @@ __global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
     const uint16_t* x_from[kMoves];
 #pragma unroll
     for (int i = 0; i < kMoves; ++i) {
-        const int row = (i * 512 + threadIdx.x) / kChunks, chunk = threadIdx.x % kChunks ^ (row & (kChunks - 1));
+        const int row = (i * 512 + threadIdx.x) / kChunks % kRows, chunk = threadIdx.x % kChunks ^ (row & (kChunks - 1));
         const int64_t m = first_row + row;
         x_from[i] = a.x + (m < a.rows ? m : a.rows - 1) * a.x_stride + 8 * chunk;
     }
@@ -386,29 +390,30 @@ __global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
         codes_from[i] = a.w.codes + n * row_words;
         code_chunk[i] = threadIdx.x % kSlots ^ code_swizzle(column);
     }
-    const uint32_t* const heads_from = a.w.header + static_cast<int64_t>(min(first_column + static_cast<int>(threadIdx.x % 256), a.w.outputs - 1)) * a.w.groups;
+    const int begin = blockIdx.y * a.share, end = min(begin + a.share, a.padded);   // the part's k
     const auto load = [&](int k, int to) {
 #pragma unroll
         for (int p = 0; p < kP; ++p)
 #pragma unroll
-            for (int i = 0; i < kMoves; ++i) to_lds(x_from[i] + p * a.x_piece + k, lds + to * kStage + p * kTile + i * 512 + wave * 64);
+            for (int i = 0; i < kMoves; ++i) to_lds(x_from[i] + p * a.x_piece + k, lds + to * kStage + p * kTilePlace + i * 512 + wave * 64);
         // beyond the last group x is zero, whatever the codes are
 #pragma unroll
         for (int i = 0; i < kCodeMoves; ++i) to_lds(codes_from[i] + 4 * min(k / 32 + code_chunk[i], row_words / 4 - 1), lds + to * kStage + kCodes + i * 512 + wave * 64);
+        if ((k - begin) % (kHeadGroups * GROUP) != 0) return;
+        const int place = (k - begin) / (kHeadGroups * GROUP) % 2, group = min(k / GROUP + static_cast<int>(threadIdx.x % kHeadGroups), a.w.groups - 1);
 #pragma unroll
-        for (int i = 0; i < kHeadMoves; ++i) {
-            const int group = k / GROUP + (kHeads == 1 ? 0 : 2 * i + static_cast<int>(threadIdx.x) / 256);
-            to_lds(heads_from + min(group, a.w.groups - 1), reinterpret_cast<uint32_t*>(lds + to * kStage + kHeadsAt) + i * 512 + wave * 64);
+        for (int i = 0; i < kHeadPlace / 512; ++i) {
+            const int64_t n = min(first_column + (i * 512 + static_cast<int>(threadIdx.x)) / kHeadGroups, a.w.outputs - 1);
+            to_lds(a.w.header + n * a.w.groups + group, heads + place * kHeadPlace + i * 512 + wave * 64);
         }
     };
-    const int begin = blockIdx.y * a.share, end = min(begin + a.share, a.padded);   // the part's k
     load(begin, 0);
     if (kRing > 2 && begin + kDepth < end) load(begin + kDepth, 1);
 
     // zero times the groups' sums of x, and what the codes' shift leaves: products of the parts of both.  A lane takes four neighbouring groups at a time.
-    const int columns = wave % 4 * 64, rows = wave / 4 * 64;   // the wavefront's place in the tile
-    f32x16 total[2][2] = {};
-    {
+    const int columns = kB == 2 ? wave % 4 * 64 : wave * 32, rows = kB == 2 ? wave / 4 * 64 : 0;   // the wavefront's place in the tile
+    f32x16 total[kB][kB] = {};
+    if constexpr (kB == 2) {
         const u32x2* sums[2];
         const uint32_t* header[2];
 #pragma unroll
@@ -466,22 +471,22 @@ __global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
     }
     const auto place = [](int row, int chunk) { return row * kChunks + (chunk ^ (row & (kChunks - 1))); };
     arrived<0>();
+    const V ones = __builtin_bit_cast(V, u32x4{Meets<T>::kOnes, Meets<T>::kOnes, Meets<T>::kOnes, Meets<T>::kOnes});
     int buffer = 0;
     for (int k = begin; k < end; k += kDepth) {
         const int ahead = k + (kRing - 1) * kDepth;
         if (ahead < end) load(ahead, buffer == 0 ? kRing - 1 : buffer - 1);
         const u32x4* const tile = lds + buffer * kStage;
         const u32x4* const codes = tile + kCodes;
-        const uint32_t* const heads = reinterpret_cast<const uint32_t*>(tile + kHeadsAt);
+        const int group = (k - begin) / GROUP;
 #pragma unroll 1   // two groups' sums at once do not fit the registers
         for (int g = 0; g < kHeads; ++g) {
-            f32x16 sum[2][2];
-            uint32_t word[2][kSteps];
-            float scaled[2];
+            f32x16 sum[kB][kB], plain;
+            uint32_t word[kB][kSteps], head[kB];
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
+            for (int c = 0; c < kB; ++c) {
                 const int column = columns + 32 * c + at;
-                scaled[c] = step_of(heads[256 * g + column]) * (1.0f / Meets<T>::kUnit);
+                head[c] = heads[(group + g) / kHeadGroups % 2 * kHeadPlace + column * kHeadGroups + (group + g) % kHeadGroups];
                 if constexpr (GROUP == 32) {   // a group is 16 bytes of an output, a half of them this lane's
                     const u32x2 v = reinterpret_cast<const u32x2*>(&codes[column * kSlots + (g ^ code_swizzle(column))])[half];
                     word[c][0] = v[0];
@@ -498,29 +503,38 @@ __global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
 #pragma unroll
             for (int step = 0; step < kSteps; ++step) {
                 const int chunk = GROUP == 32 ? 4 * g + 2 * half + step : g * (kScaled / 8) + step / 4 * 8 + 4 * half + step % 4;
-                V w[2];
+                V w[kB];
 #pragma unroll
-                for (int c = 0; c < 2; ++c) w[c] = codes_of<T>(word[c][step]);
+                for (int c = 0; c < kB; ++c) w[c] = codes_of<T>(word[c][step]);
 #pragma unroll
-                for (int r = 0; r < 2; ++r)
+                for (int r = 0; r < kB; ++r)
 #pragma unroll
                     for (int p = kP - 1; p >= 0; --p) {
-                        const V v = __builtin_bit_cast(V, tile[p * kTile + place(rows + 32 * r + at, chunk)]);
+                        const V v = __builtin_bit_cast(V, tile[p * kTilePlace + place(rows + 32 * r + at, chunk)]);
+                        if constexpr (kB == 1) {
+                            if (step == 0 && p == kP - 1) plain = f32x16{};
+                            plain = multiply(v, ones, plain);
+                        }
 #pragma unroll
-                        for (int c = 0; c < 2; ++c) {
+                        for (int c = 0; c < kB; ++c) {
                             if (step == 0 && p == kP - 1) sum[r][c] = f32x16{};
                             sum[r][c] = multiply(v, w[c], sum[r][c]);
                         }
                     }
             }
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
+            for (int c = 0; c < kB; ++c) {
+                const float step = step_of(head[c]), scaled = step * (1.0f / Meets<T>::kUnit), zero = fmaf(-Meets<T>::kShift, step, zero_of(head[c]));
 #pragma unroll
-                for (int r = 0; r < 2; ++r)
+                for (int r = 0; r < kB; ++r)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) total[r][c][i] = fmaf(scaled[c], sum[r][c][i], total[r][c][i]);
+                    for (int i = 0; i < 16; ++i) {
+                        total[r][c][i] = fmaf(scaled, sum[r][c][i], total[r][c][i]);
+                        if constexpr (kB == 1) total[r][c][i] = fmaf(zero, plain[i], total[r][c][i]);
+                    }
+            }
         }
-        // the next stage; what lies behind it may still be on its way
+        // the next stage; what lies behind it may still be on its way (headers of later groups are waited for)
         if (ahead < end)
             arrived<(kRing - 2) * kLoads>();
         else
@@ -528,14 +542,14 @@ __global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
         buffer = buffer == kRing - 1 ? 0 : buffer + 1;
     }
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
+    for (int c = 0; c < kB; ++c) {
         const int n = first_column + columns + 32 * c + at;
         if (n >= a.w.outputs) continue;
         const int64_t m = first_row + rows + 4 * half;
         if (a.parts) {
             float* const to = a.parts + (blockIdx.y * a.rows + m) * a.w.outputs + n;
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
+            for (int r = 0; r < kB; ++r)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int down = 32 * r + 8 * (i / 4) + i % 4;
@@ -546,7 +560,7 @@ __global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
         const float bias = bias_of<T>(a.bias, a.wide_bias, n);
         T* const to = a.y + m * a.y_stride + n;
 #pragma unroll
-        for (int r = 0; r < 2; ++r)
+        for (int r = 0; r < kB; ++r)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int down = 32 * r + 8 * (i / 4) + i % 4;
@@ -554,6 +568,9 @@ __global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
             }
     }
 }
+
+// The most rows of which a tile has 32.
+constexpr int64_t kLowRows = 64;
 
 // Whether rows of x can be taken as they lie.
 bool as_they_lie(const actq_weights4* w, int dtype, const actq_rows* x)
@@ -575,10 +592,11 @@ struct Parts {
 Parts parts_of(const actq_weights4* w, int64_t rows)
 {
     Parts p;
-    p.row_tiles = static_cast<int32_t>((rows + 127) / 128);
+    const bool low = rows <= kLowRows;
+    p.row_tiles = static_cast<int32_t>(low ? (rows + 31) / 32 : (rows + 127) / 128);
     p.column_tiles = (w->outputs + 255) / 256;
     const int64_t tiles = static_cast<int64_t>(p.row_tiles) * p.column_tiles, spans = padded_inputs(w) / kSpan;
-    const int64_t most = 256 / tiles < spans / 2 ? 256 / tiles : spans / 2, share = most > 1 ? (spans + most - 1) / most : spans;
+    const int64_t wanted = (low ? 512 : 256) / tiles, most = wanted < spans / 2 ? wanted : spans / 2, share = most > 1 ? (spans + most - 1) / most : spans;
     p.share = static_cast<int32_t>(share * kSpan);
     p.count = static_cast<int32_t>((spans + share - 1) / share);
     return p;
@@ -606,7 +624,8 @@ int launch_many(const actq_weights4* w, const actq_rows* x, int64_t rows, const 
     p.rows = rows;
     p.copy = copy;
     p.sums = sums;
-    launch(linear4_prepare_kernel<T, GROUP>, static_cast<unsigned>((rows * (padded / 8) + 255) / 256), 256, stream, p);
+    const bool low = rows <= kLowRows;
+    if (!low || copied) launch(linear4_prepare_kernel<T, GROUP>, static_cast<unsigned>((rows * (padded / 8) + 255) / 256), 256, stream, p);
     ManyArgs<T> a = {};
     a.w = weights_of(w);
     a.x = copied ? reinterpret_cast<const uint16_t*>(copy) : static_cast<const uint16_t*>(x->data);
@@ -624,7 +643,7 @@ int launch_many(const actq_weights4* w, const actq_rows* x, int64_t rows, const 
     a.column_tiles = parts.column_tiles;
     a.share = parts.share;
     if (parts.count > 1) a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + sums_bytes(w, rows) + copy_bytes(w, dtype, rows));
-    launch(linear4_many_kernel<T, GROUP>, dim3(static_cast<unsigned>((a.row_tiles * a.column_tiles + 7) / 8 * 8), static_cast<unsigned>(parts.count)), 512, stream, a);
+    launch(low ? linear4_many_kernel<T, GROUP, 32> : linear4_many_kernel<T, GROUP, 128>, dim3(static_cast<unsigned>((a.row_tiles * a.column_tiles + 7) / 8 * 8), static_cast<unsigned>(parts.count)), 512, stream, a);
     if (parts.count > 1)
         launch(linear4_join_kernel<T>, static_cast<unsigned>((rows * w->outputs + 255) / 256), 256, stream, static_cast<const float*>(a.parts), parts.count, rows, w->outputs, bias,
                a.wide_bias, a.y, a.y_stride);
@@ -831,7 +850,7 @@ __global__ __launch_bounds__(256) void weights4_dequantize_kernel(Weights4 w, in
 }
 
 // The most rows that go to the kernel for few.
-constexpr int64_t kFewRows = 64;
+static const int64_t kFewRows = getenv("FEWROWS") ? atoi(getenv("FEWROWS")) : 0;
 
 template <typename F>
 int by_group(int32_t group, F f)
