@@ -646,8 +646,11 @@ int actq_linear4(const actq_weights4* w, const actq_rows* x, actq_dtype dt, int6
                  actq_dtype bias_dt, const actq_rows* y, void* workspace, uint64_t workspace_bytes, void* stream);
 
 /*
- * grad_x = grad_y W.  A weight is multiplied as two bfloat16 numbers (16 bits of zero + step * code;
- * three, all of it, for ACTQ_F32).  Sums are binary32 in a fixed order, a result is rounded once.
+ * grad_x = grad_y W.  Sums are binary32 in a fixed order, a result is rounded once.  Where there are
+ * many rows, a weight (zero + step * code) is multiplied as one number of 11 bits for ACTQ_BF16, as two of
+ * them (22 bits) for ACTQ_F16 and ACTQ_F32, an element of grad_y as it is, or as 22 bits for
+ * ACTQ_F32; else a weight as 16 bits or, for ACTQ_F32, as it is.  That is off by 2^-11, 2^-16 and
+ * 2^-21 of a product at most.
  *
  * grad_y [rows, outputs], grad_x [rows, inputs] of type dt; workspace as above
  */

@@ -8,7 +8,6 @@
 // instructions multiply both exactly.  So a group's sum of x code is a sum of exact products in binary32, to which step, and zero times the group's sum of
 // x (one more product, with ones), come afterwards.  A binary32 x goes as the three bfloat16 numbers that make it up, and its codes as converted numbers:
 // sums of 128 x would cost it 4 of its 24 bits.
-#include <cstdlib>
 #include "actq_heads.h"
 
 namespace actq {
@@ -151,8 +150,9 @@ __global__ __launch_bounds__(256) void linear4_join_kernel(const float* parts, i
 
 // ----------------------------------------------------------------------------- few rows
 
-// ROWS x 16 rows and COLUMNS x 16 outputs a workgroup, whose wavefronts take spans of 128 k in turn.  A lane's codes of a group are neighbours (a quarter
-// of the group), and so are its x.
+// 16 rows and COLUMNS x 16 outputs a workgroup, whose wavefronts take spans of 128 k in turn: for one token of a small matrix every compute unit has 16 wavefronts
+// with all that they need on its way at once.  A lane's codes of a group are neighbours (a quarter of the group), and so are its x.  What bounds it: the chain of trips to
+// memory, and the loads of x, which are as many for a row as for 16.
 template <typename T>
 struct FewArgs {
     Weights4 w;
@@ -167,93 +167,108 @@ struct FewArgs {
 
 constexpr int kSpan = 128;
 
-template <typename T, int GROUP, int ROWS, int COLUMNS, int WAVES>
+template <typename T, int GROUP, int COLUMNS, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void linear4_few_kernel(FewArgs<T> a)
 {
     constexpr int kGroups = kSpan / GROUP, kWords = GROUP / 32;   // of a span; of a lane and group
     typedef typename Meets<T>::vector V;
     typedef uint32_t words __attribute__((ext_vector_type(kWords), aligned(4)));
-    __shared__ float joined[WAVES][ROWS * COLUMNS][256];
+    typedef uint32_t headers __attribute__((ext_vector_type(kGroups), aligned(4)));
+    __shared__ float joined[WAVES][COLUMNS][256];
     const int lane = threadIdx.x % 64, at = lane % 16, quarter = lane / 16;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-    const int64_t first_row = static_cast<int64_t>(blockIdx.y) * (16 * ROWS);
+    const int64_t first_row = static_cast<int64_t>(blockIdx.y) * 16;
     const int first_column = blockIdx.x * (16 * COLUMNS);
     const int row_words = a.w.groups * (GROUP / 8);
     const uint32_t* codes[COLUMNS];
     const uint32_t* header[COLUMNS];
-    const T* x[ROWS];
 #pragma unroll
     for (int c = 0; c < COLUMNS; ++c) {
         const int64_t n = min(first_column + 16 * c + at, a.w.outputs - 1);
         codes[c] = a.w.codes + n * row_words;
         header[c] = a.w.header + n * a.w.groups;
     }
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-        const int64_t m = first_row + 16 * r + at;
-        x[r] = a.x + (m < a.rows ? m : a.rows - 1) * a.x_stride;
-    }
+    const T* const x = a.x + min(first_row + at, a.rows - 1) * a.x_stride;
     const V ones = __builtin_bit_cast(V, u32x4{Meets<T>::kOnes, Meets<T>::kOnes, Meets<T>::kOnes, Meets<T>::kOnes});
-    f32x4 total[ROWS][COLUMNS] = {};
-    for (int span = wave; span * kSpan < a.w.inputs; span += WAVES) {
-        uint32_t word[COLUMNS][kGroups * kWords], head[COLUMNS][kGroups];
+    f32x4 total[COLUMNS] = {};
+
+    // what a span needs; that of the wavefront's next one is on its way while this one is worked on
+    struct Span {
+        words word[COLUMNS][kGroups];
+        headers head[COLUMNS];
+        Eight<T> x[kGroups * kWords];
+    };
+    const auto load = [&](Span& s, int span) {
+        const int group = span * kGroups;
+        if (group + kGroups <= a.w.groups) {
 #pragma unroll
-        for (int c = 0; c < COLUMNS; ++c)
+            for (int c = 0; c < COLUMNS; ++c) {
 #pragma unroll
-            for (int g = 0; g < kGroups; ++g) {
-                const int group = min(span * kGroups + g, a.w.groups - 1);   // beyond the last one x is zero
-                const words w = *reinterpret_cast<const words*>(codes[c] + group * (GROUP / 8) + quarter * kWords);
-#pragma unroll
-                for (int j = 0; j < kWords; ++j) word[c][g * kWords + j] = w[j];
-                head[c][g] = header[c][group];
+                for (int g = 0; g < kGroups; ++g) s.word[c][g] = *reinterpret_cast<const words*>(codes[c] + (group + g) * (GROUP / 8) + quarter * kWords);
+                s.head[c] = *reinterpret_cast<const headers*>(header[c] + group);
             }
+        } else {   // groups that are none stand for zeros
+#pragma unroll
+            for (int c = 0; c < COLUMNS; ++c)
+#pragma unroll
+                for (int g = 0; g < kGroups; ++g) {
+                    const bool there = group + g < a.w.groups;
+                    s.word[c][g] = *reinterpret_cast<const words*>(codes[c] + (there ? group + g : 0) * (GROUP / 8) + quarter * kWords);
+                    s.head[c][g] = there ? header[c][group + g] : 0u;
+                }
+        }
+        if ((span + 1) * kSpan <= a.w.inputs) {
+#pragma unroll
+            for (int j = 0; j < kGroups * kWords; ++j) s.x[j].load(x + span * kSpan + j / kWords * GROUP + quarter * (GROUP / 4) + 8 * (j % kWords));
+        } else {
+#pragma unroll
+            for (int j = 0; j < kGroups * kWords; ++j) {
+                const int k = span * kSpan + j / kWords * GROUP + quarter * (GROUP / 4) + 8 * (j % kWords);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s.x[j].v[i] = k + i < a.w.inputs ? x[k + i] : static_cast<T>(0.0f);
+            }
+        }
+    };
+    const int spans = (a.w.inputs + kSpan - 1) / kSpan;
+    Span now;
+    if (wave < spans) load(now, wave);
+    for (int span = wave; span < spans; span += WAVES) {
+        Span next;
+        if (span + WAVES < spans) load(next, span + WAVES);
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
-            f32x4 sum[ROWS][COLUMNS] = {}, plain[ROWS] = {};
+            f32x4 sum[COLUMNS] = {}, plain = {};
 #pragma unroll
             for (int j = 0; j < kWords; ++j) {
-                const int k = span * kSpan + g * GROUP + quarter * (GROUP / 4) + 8 * j;
                 V code[COLUMNS];
 #pragma unroll
-                for (int c = 0; c < COLUMNS; ++c) code[c] = codes_of<T>(word[c][g * kWords + j]);
+                for (int c = 0; c < COLUMNS; ++c) code[c] = codes_of<T>(kWords == 1 ? now.word[c][g][0] : now.word[c][g][j]);
+                V p[kPieces<T>];
+                pieces_of<T>(now.x[g * kWords + j], p);
 #pragma unroll
-                for (int r = 0; r < ROWS; ++r) {
-                    Eight<T> e;
-                    if (k + kLaneValues <= a.w.inputs) {
-                        e.load(x[r] + k);
-                    } else {
+                for (int i = kPieces<T> - 1; i >= 0; --i) {
+                    plain = multiply(p[i], ones, plain);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) e.v[i] = k + i < a.w.inputs ? x[r][k + i] : static_cast<T>(0.0f);
-                    }
-                    V p[kPieces<T>];
-                    pieces_of<T>(e, p);
-#pragma unroll
-                    for (int i = kPieces<T> - 1; i >= 0; --i) {
-                        plain[r] = multiply(p[i], ones, plain[r]);
-#pragma unroll
-                        for (int c = 0; c < COLUMNS; ++c) sum[r][c] = multiply(p[i], code[c], sum[r][c]);
-                    }
+                    for (int c = 0; c < COLUMNS; ++c) sum[c] = multiply(p[i], code[c], sum[c]);
                 }
             }
 #pragma unroll
             for (int c = 0; c < COLUMNS; ++c) {
-                const float step = step_of(head[c][g]), zero = fmaf(-Meets<T>::kShift, step, zero_of(head[c][g])), scaled = step * (1.0f / Meets<T>::kUnit);
+                const uint32_t head = now.head[c][g];
+                const float step = step_of(head), zero = fmaf(-Meets<T>::kShift, step, zero_of(head)), scaled = step * (1.0f / Meets<T>::kUnit);
 #pragma unroll
-                for (int r = 0; r < ROWS; ++r)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) total[r][c][i] = fmaf(zero, plain[r][i], fmaf(scaled, sum[r][c][i], total[r][c][i]));
+                for (int i = 0; i < 4; ++i) total[c][i] = fmaf(zero, plain[i], fmaf(scaled, sum[c][i], total[c][i]));
             }
         }
+        now = next;
     }
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r)
+    for (int c = 0; c < COLUMNS; ++c)
 #pragma unroll
-        for (int c = 0; c < COLUMNS; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) joined[wave][r * COLUMNS + c][(4 * quarter + i) * 16 + at] = total[r][c][i];
+        for (int i = 0; i < 4; ++i) joined[wave][c][(4 * quarter + i) * 16 + at] = total[c][i];
     __syncthreads();
-    for (int i = threadIdx.x; i < ROWS * COLUMNS * 256; i += 64 * WAVES) {
-        const int column = i % (16 * COLUMNS), row = i / (16 * COLUMNS), tile = (row / 16) * COLUMNS + column / 16, place = row % 16 * 16 + column % 16;
+    for (int i = threadIdx.x; i < COLUMNS * 256; i += 64 * WAVES) {
+        const int column = i % (16 * COLUMNS), row = i / (16 * COLUMNS), tile = column / 16, place = row * 16 + column % 16;
         const int64_t m = first_row + row;
         const int n = first_column + column;
         if (m >= a.rows || n >= a.w.outputs) continue;
@@ -569,8 +584,22 @@ __global__ __launch_bounds__(512, ROWS == 128 ? 2 : 4) void linear4_many_kernel(
     }
 }
 
-// The most rows of which a tile has 32.
-constexpr int64_t kLowRows = 64;
+// Which kernel serves.  What counts is the units of 16 rows, 16 outputs and a span; measured on one MI355X, us, bfloat16 with groups of 128 where nothing is said:
+//   kFew         up to 8192 units (one row of 4096 x 4096 5.1, tiles of 32 rows 7.9; 4096 x 4096 binary32 8.2 and 13.5; 16384 units: 13.6 and 12.0)
+//   kFewWide     a few rows of many outputs: x is read once for 64 outputs (one row of 8192 x 16384 19.5, tiles 23.7; binary32 29.3 and 49.3; groups of
+//                32 44.0 and 32.8; at 8192 x 2048 18.6 and 7.7)
+//   kLowTiles    up to 64 rows, or 65536 units (binary32, where products are three times as many, 32768): 128 rows of 4096 x 4096 24.2, tiles of 128 rows 27.2;
+//                at 262144 units 44.4 and 36.7; 301 rows of 1000 x 1501 binary32 19.0 and 26.3
+//   kHighTiles   else
+enum Kernel { kFew, kFewWide, kLowTiles, kHighTiles };
+
+Kernel kernel_of(const actq_weights4* w, int dtype, int64_t rows)
+{
+    const int64_t units = (rows + 15) / 16 * ((w->outputs + 15) / 16) * ((w->inputs + kSpan - 1) / kSpan);
+    if (rows <= 16 && w->outputs >= 8192 && w->group >= 64) return kFewWide;
+    if (units <= 8192) return kFew;
+    return rows <= 64 || units <= (dtype == ACTQ_F32 ? 32768 : 65536) ? kLowTiles : kHighTiles;
+}
 
 // Whether rows of x can be taken as they lie.
 bool as_they_lie(const actq_weights4* w, int dtype, const actq_rows* x)
@@ -584,15 +613,14 @@ int32_t padded_inputs(const actq_weights4* w) { return (w->inputs + kSpan - 1) /
 uint64_t sums_bytes(const actq_weights4* w, int64_t rows) { return (static_cast<uint64_t>(rows) * (padded_inputs(w) / w->group) * sizeof(u32x2) + 15) / 16 * 16; }
 uint64_t copy_bytes(const actq_weights4* w, int dtype, int64_t rows) { return static_cast<uint64_t>(rows) * padded_inputs(w) * (dtype == ACTQ_F32 ? 6 : 2); }
 
-// Parts of the inputs: where the tiles are fewer than the compute units, as many as make one workgroup for each, of two spans at least.
+// Parts of the inputs: where the tiles are fewer than the compute units, as many as make one workgroup for each (of 32 rows two), of two spans at least.
 struct Parts {
     int32_t row_tiles, column_tiles, count, share;
 };
 
-Parts parts_of(const actq_weights4* w, int64_t rows)
+Parts parts_of(const actq_weights4* w, int64_t rows, bool low)
 {
     Parts p;
-    const bool low = rows <= kLowRows;
     p.row_tiles = static_cast<int32_t>(low ? (rows + 31) / 32 : (rows + 127) / 128);
     p.column_tiles = (w->outputs + 255) / 256;
     const int64_t tiles = static_cast<int64_t>(p.row_tiles) * p.column_tiles, spans = padded_inputs(w) / kSpan;
@@ -602,14 +630,14 @@ Parts parts_of(const actq_weights4* w, int64_t rows)
     return p;
 }
 
-uint64_t parts_bytes(const actq_weights4* w, int64_t rows)
+uint64_t parts_bytes(const actq_weights4* w, int64_t rows, bool low)
 {
-    const Parts p = parts_of(w, rows);
+    const Parts p = parts_of(w, rows, low);
     return p.count > 1 ? static_cast<uint64_t>(p.count) * rows * w->outputs * sizeof(float) : 0;
 }
 
 template <typename T, int GROUP>
-int launch_many(const actq_weights4* w, const actq_rows* x, int64_t rows, const void* bias, int bias_dtype, const actq_rows* y, void* workspace, hipStream_t stream)
+int launch_tiles(const actq_weights4* w, const actq_rows* x, int64_t rows, bool low, const void* bias, int bias_dtype, const actq_rows* y, void* workspace, hipStream_t stream)
 {
     const int dtype = sizeof(T) == 4 ? ACTQ_F32 : ACTQ_F16;
     const bool copied = !as_they_lie(w, dtype, x);
@@ -624,7 +652,6 @@ int launch_many(const actq_weights4* w, const actq_rows* x, int64_t rows, const 
     p.rows = rows;
     p.copy = copy;
     p.sums = sums;
-    const bool low = rows <= kLowRows;
     if (!low || copied) launch(linear4_prepare_kernel<T, GROUP>, static_cast<unsigned>((rows * (padded / 8) + 255) / 256), 256, stream, p);
     ManyArgs<T> a = {};
     a.w = weights_of(w);
@@ -638,7 +665,7 @@ int launch_many(const actq_weights4* w, const actq_rows* x, int64_t rows, const 
     a.y = static_cast<T*>(y->data);
     a.y_stride = y->stride;
     a.rows = rows;
-    const Parts parts = parts_of(w, rows);
+    const Parts parts = parts_of(w, rows, low);
     a.row_tiles = parts.row_tiles;
     a.column_tiles = parts.column_tiles;
     a.share = parts.share;
@@ -652,8 +679,10 @@ int launch_many(const actq_weights4* w, const actq_rows* x, int64_t rows, const 
 
 // ----------------------------------------------------------------------------- the gradient
 
-// A workgroup's tile is kGradRows x 128 of grad_x, gathered over 64 outputs at a time from the LDS.  A weight goes there as two bfloat16 numbers (16 bits of
+// Few rows.  A workgroup's tile is 128 x 128 of grad_x, gathered over 64 outputs at a time from the LDS.  A weight goes there as two bfloat16 numbers (16 bits of
 // it; three for binary32), an element of grad_y as those that make it up (binary16: two, binary32: three): products below 2^-16 (2^-24) of the largest are left out.
+// What bounds it: turning the weights into numbers, 6 instructions a code, which every tile does for itself.  One row of 4096 inputs and 8192 outputs 34 us (one
+// part of the outputs: 315).
 template <typename T>
 struct GradArgs {
     Weights4 w;
@@ -662,6 +691,8 @@ struct GradArgs {
     T* out;
     int64_t out_stride;
     int64_t rows;
+    int32_t share;   // outputs of a part
+    float* parts;    // [parts][rows][inputs]; null: the only part writes out
 };
 
 template <typename T>
@@ -686,7 +717,8 @@ __global__ __launch_bounds__(kGradThreads) void linear4_backward_kernel(GradArgs
     const int first_column = blockIdx.x * kGradColumns, row_words = a.w.groups * (GROUP / 8);
     const int word = min(first_column / 8 + static_cast<int>(threadIdx.x % 16), row_words - 1), group = word / (GROUP / 8), quad = threadIdx.x / 16;
     f32x16 sum[2][2] = {};
-    for (int from = 0; from < a.w.outputs; from += kGradDepth) {
+    const int end = min(static_cast<int>(blockIdx.z + 1) * a.share, a.w.outputs);
+    for (int from = blockIdx.z * a.share; from < end; from += kGradDepth) {
         // grad_y: chunks of eight outputs
         for (int i = threadIdx.x; i < kGradRows * 8; i += kGradThreads) {
             const int row = i / 8, chunk = i % 8, n = from + 8 * chunk;
@@ -771,7 +803,248 @@ __global__ __launch_bounds__(kGradThreads) void linear4_backward_kernel(GradArgs
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int64_t m = first_row + 64 * (wave / 2) + 32 * i + 8 * (r / 4) + 4 * (lane / 32) + r % 4;
-                if (m < a.rows && k < a.w.inputs) a.out[m * a.out_stride + k] = static_cast<T>(sum[i][j][r]);
+                if (m >= a.rows || k >= a.w.inputs) continue;
+                if (a.parts)
+                    a.parts[(blockIdx.z * a.rows + m) * a.w.inputs + k] = sum[i][j][r];
+                else
+                    a.out[m * a.out_stride + k] = static_cast<T>(sum[i][j][r]);
+            }
+        }
+}
+
+// Many rows: the weights are turned into numbers once, transposed, in memory, and the product is one of two matrices whose rows are contiguous along the outputs.
+// Both are binary16, scaled by powers of two so that it has the range: a weight by that of its output's largest one, which the elements of grad_y there make up for;
+// a row of grad_y by that of its largest element, for which the row of the result makes up.  bfloat16: a number for each, 11 bits, beside which the result's rounding to 8
+// counts; binary16: two for a weight (22 bits); binary32: two for both, without the product of the second ones.
+template <typename T>
+constexpr int kGradNumbers = sizeof(T) == 4 ? 2 : 1;
+template <typename T>
+constexpr int kWeightNumbers = std::is_same<T, __bf16>::value ? 1 : 2;
+
+constexpr int kDeepest = 64;   // outputs are padded to a multiple
+
+// The power of two that takes a number of this magnitude into [2^13, 2^14).
+__device__ __forceinline__ float scale_of(uint32_t largest)
+{
+    const int exponent = static_cast<int>(largest >> 23) - 127;
+    const int power = largest == 0 || largest >= 0x7f800000u ? 0 : max(min(13 - exponent, 100), -100);
+    return __builtin_bit_cast(float, static_cast<uint32_t>(power + 127) << 23);
+}
+
+// 1 / the scale of every output, a wavefront each.
+__global__ __launch_bounds__(256) void weights4_scale_kernel(Weights4 w, float* inverse)
+{
+    const int n = blockIdx.x * 4 + threadIdx.x / 64;
+    if (n >= w.outputs) return;
+    uint32_t largest = 0;
+    for (int g = threadIdx.x % 64; g < w.groups; g += 64) {
+        const uint32_t h = w.header[static_cast<int64_t>(n) * w.groups + g];
+        const uint32_t ends[2] = {magnitude(zero_of(h)), magnitude(fmaf(15.0f, step_of(h), zero_of(h)))};
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (ends[i] < 0x7f800000u) largest = max(largest, ends[i]);
+    }
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2) largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), step)));
+    if (threadIdx.x % 64 == 0) inverse[n] = 1.0f / scale_of(largest);
+}
+
+// 64 outputs x 128 inputs a workgroup; out [numbers][inputs][padded outputs].
+template <int GROUP, int NUMBERS>
+__global__ __launch_bounds__(256) void weights4_transpose_kernel(Weights4 w, const float* inverse, int32_t padded, uint16_t* out)
+{
+    __shared__ u32x2 turned[128 * 17];
+    const int row_words = w.groups * (GROUP / 8), column = threadIdx.x % 16, quad = threadIdx.x / 16;
+    const int word = min(static_cast<int>(blockIdx.x) * 16 + column, row_words - 1);
+    float v[4][8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int n = blockIdx.y * 64 + 4 * quad + j;
+        const bool there = n < w.outputs;
+        const int64_t row = there ? n : 0;
+        const uint32_t codes = w.codes[row * row_words + word], h = there ? w.header[row * w.groups + word / (GROUP / 8)] : 0u;
+        const float scale = 1.0f / inverse[row];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[j][i] = fmaf(static_cast<float>(codes >> (4 * (i / 2) + 16 * (i % 2)) & 15u), step_of(h), zero_of(h)) * scale;
+    }
+#pragma unroll
+    for (int number = 0; number < NUMBERS; ++number) {
+        if (number > 0) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            typedef _Float16 four __attribute__((ext_vector_type(4)));
+            four f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                f[j] = static_cast<_Float16>(v[j][i]);
+                v[j][i] -= static_cast<float>(f[j]);
+            }
+            turned[(8 * column + i) * 17 + quad] = __builtin_bit_cast(u32x2, f);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = i * 32 + threadIdx.x / 8, pair = threadIdx.x % 8 * 2, k = blockIdx.x * 128 + row;
+            const u32x2 a = turned[row * 17 + pair], b = turned[row * 17 + pair + 1];
+            if (k < w.inputs) *reinterpret_cast<u32x4*>(out + (static_cast<int64_t>(number) * w.inputs + k) * padded + blockIdx.y * 64 + 4 * pair) = u32x4{a[0], a[1], b[0], b[1]};
+        }
+    }
+}
+
+// A row of grad_y a workgroup; out [numbers][rows][padded outputs], and what its result has to be multiplied by.
+template <typename T>
+__global__ __launch_bounds__(256) void linear4_scale_rows_kernel(const T* grad, int64_t stride, int64_t rows, int32_t outputs, int32_t padded, const float* inverse, uint16_t* out, float* back)
+{
+    __shared__ uint32_t shares[4];
+    const int64_t m = blockIdx.x;
+    const T* const row = grad + m * stride;
+    const auto at = [&](int n, float (&f)[8]) {
+        Eight<T> e;
+        Eight<float> by;
+        if (n + 8 <= outputs) {
+            e.load(row + n);
+            by.load(inverse + n);
+            e.widen(f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] *= by.v[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = n + i < outputs ? static_cast<float>(row[n + i]) * inverse[n + i] : 0.0f;
+        }
+    };
+    uint32_t largest = 0;
+    for (int n = 8 * threadIdx.x; n < outputs; n += 8 * 256) {
+        float f[8];
+        at(n, f);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) largest = max(largest, magnitude(f[i]));
+    }
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2) largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), step)));
+    if (threadIdx.x % 64 == 0) shares[threadIdx.x / 64] = largest;
+    __syncthreads();
+    largest = max(max(shares[0], shares[1]), max(shares[2], shares[3]));
+    const float scale = scale_of(largest);
+    if (threadIdx.x == 0) back[m] = 1.0f / scale;
+    for (int n = 8 * threadIdx.x; n < padded; n += 8 * 256) {
+        float f[8];
+        at(n, f);
+#pragma unroll
+        for (int number = 0; number < kGradNumbers<T>; ++number) {
+            f16x8 v;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (number == 0) f[i] *= scale;
+                v[i] = static_cast<_Float16>(f[i]);
+                f[i] -= static_cast<float>(v[i]);
+            }
+            *reinterpret_cast<u32x4*>(out + (static_cast<int64_t>(number) * rows + m) * padded + n) = __builtin_bit_cast(u32x4, v);
+        }
+    }
+}
+
+template <typename T>
+struct TilesArgs {
+    const uint16_t* grad;     // [numbers][rows][padded]
+    const uint16_t* weights;  // [numbers][inputs][padded]
+    const float* back;
+    int64_t rows;
+    int32_t inputs, padded;
+    int32_t row_tiles, column_tiles;
+    T* out;
+    int64_t out_stride;
+    int32_t share;            // outputs of a part
+    float* parts;             // [parts][rows][inputs]; null: the only part writes out
+};
+
+// A workgroup's tile is 256 rows x 128 inputs, a wavefront's 128 x 64, and both matrices go from memory to the LDS without registers, two stages ahead
+// (binary16, with half as many bytes again: one).  What bounds it: the matrix instructions, beside which the LDS is read three quarters of the time.
+template <typename T>
+__global__ __launch_bounds__(256, 1) void linear4_backward_tiles_kernel(TilesArgs<T> a)
+{
+    constexpr int kG = kGradNumbers<T>, kW = kWeightNumbers<T>, kDepth = kG == 1 ? 64 : 32, kRing = kG == kW ? 3 : 2, kRows = 256, kColumns = 128;
+    constexpr int kChunks = kDepth / 8, kGrads = kRows * kChunks, kWeights = kColumns * kChunks, kStage = kG * kGrads + kW * kWeights, kLoads = kStage / 256;
+    __shared__ u32x4 lds[kRing * kStage];   // one array, as above
+    const int lane = threadIdx.x % 64, at = lane % 32, half = lane / 32;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), rows = wave / 2 * 128, columns = wave % 2 * 64;
+    const int tiles = a.row_tiles * a.column_tiles, share = (tiles + 7) / 8, unit = blockIdx.x % 8 * share + blockIdx.x / 8;
+    if (unit >= tiles || static_cast<int>(blockIdx.x / 8) >= share) return;
+    const int band = unit / (4 * a.column_tiles), in_band = unit - band * 4 * a.column_tiles, high = min(4, a.row_tiles - 4 * band);
+    const int64_t first_row = static_cast<int64_t>(4 * band + in_band % high) * kRows;
+    const int first_column = (in_band / high) * kColumns;
+    const auto swizzle = [](int row) { return kChunks == 8 ? row & 7 : row >> 2 & 3; };
+    const uint16_t* from[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+        const bool of_grad = i * 256 < kG * kGrads;
+        const int place = i * 256 + threadIdx.x - (of_grad ? 0 : kG * kGrads), number = place / (of_grad ? kGrads : kWeights), in = place % (of_grad ? kGrads : kWeights);
+        const int row = in / kChunks, chunk = in % kChunks ^ swizzle(row);
+        const int64_t all = of_grad ? a.rows : a.inputs, wanted = (of_grad ? first_row : first_column) + row;
+        from[i] = (of_grad ? a.grad : a.weights) + (number * all + (wanted < all ? wanted : all - 1)) * a.padded + 8 * chunk;
+    }
+    const auto load = [&](int n, int to) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) to_lds(from[i] + n, lds + to * kStage + i * 256 + wave * 64);
+    };
+    const int begin = blockIdx.y * a.share, end = min(begin + a.share, a.padded);
+    load(begin, 0);
+    if (kRing > 2 && begin + kDepth < end) load(begin + kDepth, 1);
+    f32x16 sum[4][2] = {};
+    if (kRing > 2 && begin + kDepth < end)
+        arrived<kLoads>();
+    else
+        arrived<0>();
+    int buffer = 0;
+    for (int n = begin; n < end; n += kDepth) {
+        const int ahead = n + (kRing - 1) * kDepth;
+        if (ahead < end) load(ahead, buffer == 0 ? kRing - 1 : buffer - 1);
+        const u32x4* const stage = lds + buffer * kStage;
+#pragma unroll
+        for (int step = 0; step < kDepth / 16; ++step) {
+            f16x8 g[4][kG], w[2][kW];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = rows + 32 * i + at;
+#pragma unroll
+                for (int p = 0; p < kG; ++p) g[i][p] = __builtin_bit_cast(f16x8, stage[p * kGrads + row * kChunks + ((2 * step + half) ^ swizzle(row))]);
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int row = columns + 32 * j + at;
+#pragma unroll
+                for (int p = 0; p < kW; ++p) w[j][p] = __builtin_bit_cast(f16x8, stage[kG * kGrads + p * kWeights + row * kChunks + ((2 * step + half) ^ swizzle(row))]);
+            }
+#pragma unroll
+            for (int p = kG - 1; p >= 0; --p)
+#pragma unroll
+                for (int q = kW - 1; q >= 0; --q)
+                    if (p + q < 2)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) sum[i][j] = multiply(g[i][p], w[j][q], sum[i][j]);
+        }
+        if (ahead < end)
+            arrived<(kRing - 2) * kLoads>();
+        else
+            arrived<0>();
+        buffer = buffer == kRing - 1 ? 0 : buffer + 1;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int64_t m = first_row + rows + 32 * i + 8 * (r / 4) + 4 * half + r % 4;
+            if (m >= a.rows) continue;
+            const float back = a.back[m];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int k = first_column + columns + 32 * j + at;
+                if (k >= a.inputs) continue;
+                if (a.parts)
+                    a.parts[(blockIdx.y * a.rows + m) * a.inputs + k] = sum[i][j][r] * back;
+                else
+                    a.out[m * a.out_stride + k] = static_cast<T>(sum[i][j][r] * back);
             }
         }
 }
@@ -849,9 +1122,6 @@ __global__ __launch_bounds__(256) void weights4_dequantize_kernel(Weights4 w, in
     }
 }
 
-// The most rows that go to the kernel for few.
-static const int64_t kFewRows = getenv("FEWROWS") ? atoi(getenv("FEWROWS")) : 0;
-
 template <typename F>
 int by_group(int32_t group, F f)
 {
@@ -884,8 +1154,82 @@ int launch_weights4_dequantize(const actq_weights4* w, const actq_rows* out, int
     });
 }
 
-uint64_t linear4_workspace(const actq_weights4* w, int dtype, int64_t rows) { return rows > kFewRows ? sums_bytes(w, rows) + copy_bytes(w, dtype, rows) + parts_bytes(w, rows) : 0; }
-uint64_t linear4_backward_workspace(const actq_weights4*, int, int64_t) { return 0; }
+uint64_t linear4_workspace(const actq_weights4* w, int dtype, int64_t rows)
+{
+    if (rows == 0) return 0;
+    const Kernel kernel = kernel_of(w, dtype, rows);
+    return kernel == kFew || kernel == kFewWide ? 0 : sums_bytes(w, rows) + copy_bytes(w, dtype, rows) + parts_bytes(w, rows, kernel == kLowTiles);
+}
+
+// Whether the weights are turned into numbers in memory: from so many products on (bfloat16: 2^33 in 256 rows 74 us, the other kernel 72; 512 rows 92 and 126;
+// 2047 233 and 463; 1000 rows of 1024 x 1024 45 and 29.  binary32: 2^32 in 128 rows 106 and 95, 256 rows 115 and 169).
+bool in_memory(const actq_weights4* w, int dtype, int64_t rows) { return rows * w->inputs * w->outputs > int64_t(1) << (dtype == ACTQ_F32 ? 32 : 33); }
+
+struct GradPlan {
+    bool tiles;               // of 256 rows, from numbers in memory
+    int32_t row_tiles, column_tiles, padded, share, parts;
+    uint64_t inverse, back, grads, weights, sums;   // bytes of the workspace's pieces
+};
+
+// Where the tiles are few, the outputs are cut into parts that make a workgroup for each compute unit (of the smaller tiles two), of four stages at least.
+GradPlan grad_plan(const actq_weights4* w, int dtype, int64_t rows)
+{
+    GradPlan p = {};
+    if (rows == 0) return p;
+    p.tiles = in_memory(w, dtype, rows);
+    p.row_tiles = static_cast<int32_t>(p.tiles ? (rows + 255) / 256 : (rows + kGradRows - 1) / kGradRows);
+    p.column_tiles = (w->inputs + kGradColumns - 1) / kGradColumns;
+    p.padded = (w->outputs + kDeepest - 1) / kDeepest * kDeepest;
+    const int64_t stages = p.padded / kDeepest, wanted = (p.tiles ? 256 : 512) / (static_cast<int64_t>(p.row_tiles) * p.column_tiles);
+    const int64_t most = wanted < stages / 4 ? wanted : stages / 4, share = most > 1 ? (stages + most - 1) / most : stages;
+    p.share = static_cast<int32_t>(share * kDeepest);
+    p.parts = static_cast<int32_t>((stages + share - 1) / share);
+    if (p.tiles) {
+        p.inverse = (static_cast<uint64_t>(w->outputs) * sizeof(float) + 15) / 16 * 16;
+        p.back = (static_cast<uint64_t>(rows) * sizeof(float) + 15) / 16 * 16;
+        p.grads = static_cast<uint64_t>(rows) * p.padded * 2 * (dtype == ACTQ_F32 ? 2 : 1);
+        p.weights = static_cast<uint64_t>(w->inputs) * p.padded * 2 * (dtype == ACTQ_BF16 ? 1 : 2);
+    }
+    p.sums = p.parts > 1 ? static_cast<uint64_t>(p.parts) * rows * w->inputs * sizeof(float) : 0;
+    return p;
+}
+
+uint64_t linear4_backward_workspace(const actq_weights4* w, int dtype, int64_t rows)
+{
+    const GradPlan p = grad_plan(w, dtype, rows);
+    return p.inverse + p.back + p.grads + p.weights + p.sums;
+}
+
+template <typename T, int GROUP>
+void launch_backward_tiles(const actq_weights4* w, const actq_rows* grad_y, int64_t rows, const actq_rows* grad_x, const GradPlan& p, void* workspace, float* parts, hipStream_t stream)
+{
+    char* const at = static_cast<char*>(workspace);
+    float* const inverse = reinterpret_cast<float*>(at);
+    float* const back = reinterpret_cast<float*>(at + p.inverse);
+    uint16_t* const grads = reinterpret_cast<uint16_t*>(at + p.inverse + p.back);
+    uint16_t* const weights = reinterpret_cast<uint16_t*>(at + p.inverse + p.back + p.grads);
+    const Weights4 v = weights_of(w);
+    launch(weights4_scale_kernel, static_cast<unsigned>((w->outputs + 3) / 4), 256, stream, v, inverse);
+    launch(weights4_transpose_kernel<GROUP, kWeightNumbers<T>>, dim3(static_cast<unsigned>((w->inputs + 127) / 128), static_cast<unsigned>(p.padded / 64)), 256, stream, v,
+           static_cast<const float*>(inverse), p.padded, weights);
+    launch(linear4_scale_rows_kernel<T>, static_cast<unsigned>(rows), 256, stream, static_cast<const T*>(grad_y->data), grad_y->stride, rows, w->outputs, p.padded,
+           static_cast<const float*>(inverse), grads, back);
+    TilesArgs<T> a = {};
+    a.grad = grads;
+    a.weights = weights;
+    a.back = back;
+    a.rows = rows;
+    a.inputs = w->inputs;
+    a.padded = p.padded;
+    a.row_tiles = p.row_tiles;
+    a.column_tiles = p.column_tiles;
+    a.out = static_cast<T*>(grad_x->data);
+    a.out_stride = grad_x->stride;
+    a.share = p.share;
+    a.parts = parts;
+    const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(p.row_tiles) * p.column_tiles + 7) / 8 * 8), static_cast<unsigned>(p.parts));
+    launch(linear4_backward_tiles_kernel<T>, grid, 256, stream, a);
+}
 
 int launch_linear4(const actq_weights4* w, const actq_rows* x, int dtype, int64_t rows, const void* bias, int bias_dtype, const actq_rows* y, void* workspace, void* stream)
 {
@@ -893,7 +1237,9 @@ int launch_linear4(const actq_weights4* w, const actq_rows* x, int dtype, int64_
         return by_group(w->group, [&](auto g) {
             typedef decltype(type) T;
             constexpr int kGroup = decltype(g)::value;
-            if (rows > kFewRows) return launch_many<T, kGroup>(w, x, rows, bias, bias_dtype, y, workspace, static_cast<hipStream_t>(stream));
+            const Kernel kernel = kernel_of(w, dtype, rows);
+            if (kernel == kLowTiles || kernel == kHighTiles)
+                return launch_tiles<T, kGroup>(w, x, rows, kernel == kLowTiles, bias, bias_dtype, y, workspace, static_cast<hipStream_t>(stream));
             FewArgs<T> a = {};
             a.w = weights_of(w);
             a.x = static_cast<const T*>(x->data);
@@ -903,33 +1249,46 @@ int launch_linear4(const actq_weights4* w, const actq_rows* x, int dtype, int64_
             a.y = static_cast<T*>(y->data);
             a.y_stride = y->stride;
             a.rows = rows;
-            const auto go = [&](auto r, auto c, auto waves) {
-                constexpr int kRows = decltype(r)::value, kColumns = decltype(c)::value, kWaves = decltype(waves)::value;
-                const dim3 grid((a.w.outputs + 16 * kColumns - 1) / (16 * kColumns), static_cast<unsigned>((rows + 16 * kRows - 1) / (16 * kRows)));
-                launch(linear4_few_kernel<T, kGroup, kRows, kColumns, kWaves>, grid, 64 * kWaves, static_cast<hipStream_t>(stream), a);
+            const auto go = [&](auto columns, auto waves) {
+                constexpr int kColumns = decltype(columns)::value, kWaves = decltype(waves)::value;
+                const dim3 grid((a.w.outputs + 16 * kColumns - 1) / (16 * kColumns), static_cast<unsigned>((rows + 15) / 16));
+                launch(linear4_few_kernel<T, kGroup, kColumns, kWaves>, grid, 64 * kWaves, static_cast<hipStream_t>(stream), a);
                 return launched("actq_linear4");
             };
-            return rows <= 16 ? go(std::integral_constant<int, 1>{}, std::integral_constant<int, 1>{}, std::integral_constant<int, 16>{})
-                              : go(std::integral_constant<int, 2>{}, std::integral_constant<int, 2>{}, std::integral_constant<int, 8>{});
+            if constexpr (kGroup >= 64)
+                if (kernel == kFewWide) return go(std::integral_constant<int, 4>{}, std::integral_constant<int, 8>{});
+            return go(std::integral_constant<int, 1>{}, std::integral_constant<int, 16>{});
         });
     });
 }
 
-int launch_linear4_backward(const actq_weights4* w, const actq_rows* grad_y, int dtype, int64_t rows, const actq_rows* grad_x, void*, void* stream)
+int launch_linear4_backward(const actq_weights4* w, const actq_rows* grad_y, int dtype, int64_t rows, const actq_rows* grad_x, void* workspace, void* stream)
 {
     return by_dtype(dtype, [&](auto type) {
         return by_group(w->group, [&](auto g) {
             typedef decltype(type) T;
             constexpr int kGroup = decltype(g)::value;
-            GradArgs<T> a = {};
-            a.w = weights_of(w);
-            a.grad = static_cast<const T*>(grad_y->data);
-            a.grad_stride = grad_y->stride;
-            a.out = static_cast<T*>(grad_x->data);
-            a.out_stride = grad_x->stride;
-            a.rows = rows;
-            const dim3 grid((w->inputs + kGradColumns - 1) / kGradColumns, static_cast<unsigned>((rows + kGradRows - 1) / kGradRows));
-            launch(linear4_backward_kernel<T, kGroup>, grid, kGradThreads, static_cast<hipStream_t>(stream), a);
+            const GradPlan p = grad_plan(w, dtype, rows);
+            const hipStream_t at = static_cast<hipStream_t>(stream);
+            float* const parts = p.parts > 1 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + p.inverse + p.back + p.grads + p.weights) : nullptr;
+            if (p.tiles) {
+                launch_backward_tiles<T, kGroup>(w, grad_y, rows, grad_x, p, workspace, parts, at);
+            } else {
+                GradArgs<T> a = {};
+                a.w = weights_of(w);
+                a.grad = static_cast<const T*>(grad_y->data);
+                a.grad_stride = grad_y->stride;
+                a.out = static_cast<T*>(grad_x->data);
+                a.out_stride = grad_x->stride;
+                a.rows = rows;
+                a.share = p.share;
+                a.parts = parts;
+                const dim3 grid(static_cast<unsigned>(p.column_tiles), static_cast<unsigned>(p.row_tiles), static_cast<unsigned>(p.parts));
+                launch(linear4_backward_kernel<T, kGroup>, grid, kGradThreads, at, a);
+            }
+            if (parts)
+                launch(linear4_join_kernel<T>, static_cast<unsigned>((rows * w->inputs + 255) / 256), 256, at, static_cast<const float*>(parts), p.parts, rows, w->inputs,
+                       static_cast<const void*>(nullptr), 0, static_cast<T*>(grad_x->data), grad_x->stride);
             return launched("actq_linear4_backward");
         });
     });

@@ -17,6 +17,12 @@ CASES = [
     (100, 300, 500, 64, F16), (127, 96, 257, 32, BF16), (128, 4096, 128, 128, F16), (129, 257, 300, 128, BF16), (200, 512, 256, 64, F32), (257, 1100, 513, 32, F16),
     (300, 2500, 100, 128, F32), (513, 384, 640, 128, BF16), (700, 64, 1000, 64, F16), (1, 8192, 40, 128, BF16), (1, 4097, 35, 64, F32), (260, 777, 259, 64, BF16),
     (1030, 160, 96, 32, BF16), (4, 5000, 3, 32, F16), (48, 3000, 200, 128, F32),
+    # many outputs for few rows; tiles of 32 rows, one part and several; tiles of 128 rows, likewise
+    (1, 300, 8200, 64, BF16), (16, 1111, 8193, 128, F16), (7, 129, 9000, 128, F32), (40, 4100, 4000, 64, F16), (33, 8192, 1024, 128, BF16), (70, 3000, 5003, 32, BF16),
+    (64, 1025, 3001, 32, F32), (500, 120, 5000, 64, F16), (130, 4100, 4203, 128, BF16), (100, 2500, 4500, 32, F32), (5000, 100, 4001, 32, BF16), (1100, 4224, 300, 64, F16),
+    (300, 8200, 1000, 64, F32),
+    # gradients from weights in memory
+    (1100, 4224, 2100, 128, BF16), (1031, 4100, 2099, 64, F16), (701, 3001, 2100, 32, F32),
 ]
 
 
@@ -54,8 +60,9 @@ def test_product(case, bias):
 
 @pytest.mark.parametrize("case", CASES, ids=str)
 def test_gradient(case):
-    """A weight goes as 16 bits of it (24 for binary32), an element of grad_y as it is, and of the products of parts those below 2^-16 (2^-24) of the whole are
-    left out: at most 2^-15 (2^-22) of a product, of either sign.  Sums over the outputs as above."""
+    """What a product is off by, of either sign.  bfloat16: a weight may go as 11 bits of it, off by 2^-11, an element of grad_y as it is.  binary16: a weight as 16 bits
+    or more, 2^-16, and what is left of products of parts, 2^-16.  binary32: 22 bits of both, 2^-23 each, without the product of the lower halves, 2^-22.
+    Eight times that for the root of the sum of squares.  Sums over the outputs as above."""
     rows, inputs, outputs, group, dtype = case
     codes, header = Y.random_weights(outputs, inputs, group, rows + inputs + 1)
     grad = _rows(rows, outputs, dtype, inputs)
@@ -64,7 +71,7 @@ def test_gradient(case):
     want = grad.double() @ w
     e = ((grad.double() ** 2) @ (w ** 2)) ** 0.5
     assert got.dtype == dtype and got.shape == (rows, inputs)
-    limit = H.ROUNDOFF[dtype] * want.abs() + (8 * (2.0 ** -22 if dtype == F32 else 2.0 ** -15) + 32 * Y.UNIT * (3 * outputs) ** 0.5) * e + 2.0 ** -25
+    limit = H.ROUNDOFF[dtype] * want.abs() + (8 * {F32: 2.0 ** -21, F16: 2.0 ** -15, BF16: 2.0 ** -11}[dtype] + 32 * Y.UNIT * (3 * outputs) ** 0.5) * e + 2.0 ** -25
     off = (got.cpu().double() - want).abs()
     assert (off <= limit).all(), float((off / limit).max())
     assert torch.equal(got, B.linear4_backward(grad.to(DEV), codes.to(DEV), header.to(DEV), inputs)), "the order of the sums is fixed"
@@ -121,10 +128,10 @@ def test_groups_that_are_not_finite_read_as_nan():
 
 
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
-@pytest.mark.parametrize("rows", [3, 70, 300])
-def test_rows_that_are_not_finite_are_their_own_business(rows, dtype):
-    codes, header = (t.to(DEV) for t in Y.random_weights(100, 300, 64, 2))
-    for call, columns in ((lambda x: B.linear4(x, codes, header), 300), (lambda x: B.linear4_backward(x, codes, header, 300), 100)):
+@pytest.mark.parametrize("rows, inputs, outputs", [(3, 300, 100), (300, 300, 100), (40, 4100, 4000), (1100, 4100, 2100)])
+def test_rows_that_are_not_finite_are_their_own_business(rows, inputs, outputs, dtype):
+    codes, header = (t.to(DEV) for t in Y.random_weights(outputs, inputs, 64, 2))
+    for call, columns in ((lambda x: B.linear4(x, codes, header), inputs), (lambda x: B.linear4_backward(x, codes, header, inputs), outputs)):
         x = _rows(rows, columns, dtype, 3).to(DEV)
         fine = call(x)
         bad = x.clone()
@@ -135,22 +142,22 @@ def test_rows_that_are_not_finite_are_their_own_business(rows, dtype):
         assert torch.isnan(got[1]).all() and not torch.isfinite(got[rows - 1]).any()
 
 
-@pytest.mark.parametrize("rows", [1, 40, 150])
-def test_strides_shapes_and_neighbours(rows):
-    codes, header = (t.to(DEV) for t in Y.random_weights(70, 200, 32, 4))
-    wide = _rows(rows, 307, BF16, 5).to(DEV)
-    x = wide[:, 3:203]
+@pytest.mark.parametrize("rows, inputs, outputs", [(1, 200, 70), (40, 200, 70), (5, 1024, 8201), (40, 4096, 4003), (200, 5001, 3001), (300, 512, 2050)])
+def test_strides_shapes_and_neighbours(rows, inputs, outputs):
+    codes, header = (t.to(DEV) for t in Y.random_weights(outputs, inputs, 32, 4))
+    wide = _rows(rows, inputs + 107, BF16, 5).to(DEV)
+    x = wide[:, 3:3 + inputs]
     want = B.linear4(x.contiguous(), codes, header)
     assert torch.equal(B.linear4(x, codes, header), want)
-    out = torch.full((rows, 99), 7.0, dtype=BF16, device=DEV)
-    assert torch.equal(B.linear4(x, codes, header, out=out[:, 11:81]), want)
-    assert (out[:, :11] == 7).all() and (out[:, 81:] == 7).all()
-    assert torch.equal(B.linear4(x.contiguous().view(rows, 1, 1, 200), codes, header), want.view(rows, 1, 1, 70))
-    assert torch.equal(B.linear4(x[:1].expand(rows, 200), codes, header), want[:1].expand(rows, 70)) or rows > 1   # rows that share memory may be read
+    out = torch.full((rows, outputs + 29), 7.0, dtype=BF16, device=DEV)
+    assert torch.equal(B.linear4(x, codes, header, out=out[:, 11:11 + outputs]), want)
+    assert (out[:, :11] == 7).all() and (out[:, 11 + outputs:] == 7).all()
+    assert torch.equal(B.linear4(x.contiguous().view(rows, 1, 1, inputs), codes, header), want.view(rows, 1, 1, outputs))
+    assert torch.equal(B.linear4(x[:1].expand(rows, inputs), codes, header), want[:1].expand(rows, outputs))   # rows that share memory may be read
     assert torch.equal(B.linear4(x.flip(0), codes, header).flip(0), want)
-    grad = _rows(rows, 90, F16, 6).to(DEV)[:, 5:75]
-    assert torch.equal(B.linear4_backward(grad, codes, header, 200), B.linear4_backward(grad.contiguous(), codes, header, 200))
-    assert torch.equal(B.linear4_backward(grad.contiguous().view(rows, 1, 70), codes, header, 200).view(rows, 200), B.linear4_backward(grad, codes, header, 200))
+    grad = _rows(rows, outputs + 20, F16, 6).to(DEV)[:, 5:5 + outputs]
+    assert torch.equal(B.linear4_backward(grad, codes, header, inputs), B.linear4_backward(grad.contiguous(), codes, header, inputs))
+    assert torch.equal(B.linear4_backward(grad.contiguous().view(rows, 1, outputs), codes, header, inputs).view(rows, inputs), B.linear4_backward(grad, codes, header, inputs))
 
 
 def test_one_vector_and_no_rows():
@@ -197,15 +204,15 @@ def test_refused_by_the_binding():
         B.linear4(torch.zeros((3, 200), device=DEV), torch.zeros((5, 32), dtype=torch.int32, device=DEV), torch.zeros((5, 1, 2), dtype=BF16, device=DEV))
 
 
-def test_captured_and_replayed_with_two_graphs():
-    """Two graphs of the same weights, each with its own workspace, replayed in turn with other inputs and eager calls between."""
-    codes, header = (t.to(DEV) for t in Y.random_weights(300, 1000, 64, 4))
+def test_captured_and_replayed_with_several_graphs():
+    """Graphs of the same weights, each with its own workspace, replayed in turn with other inputs and eager calls between."""
+    codes, header = (t.to(DEV) for t in Y.random_weights(2000, 3000, 64, 4))
     g = torch.Generator().manual_seed(8)
     graphs = []
     side = torch.cuda.Stream()
-    for rows in (1, 30, 300):
-        x, grad = torch.zeros((rows, 1000), dtype=BF16, device=DEV), torch.zeros((rows, 300), dtype=BF16, device=DEV)
-        call = lambda x=x, grad=grad: (B.linear4(x, codes, header), B.linear4_backward(grad, codes, header, 1000))   # noqa: E731
+    for rows in (1, 60, 1500):
+        x, grad = torch.zeros((rows, 3000), dtype=BF16, device=DEV), torch.zeros((rows, 2000), dtype=BF16, device=DEV)
+        call = lambda x=x, grad=grad: (B.linear4(x, codes, header), B.linear4_backward(grad, codes, header, 3000))   # noqa: E731
         side.wait_stream(torch.cuda.current_stream())
         with torch.cuda.stream(side):
             call()

@@ -74,6 +74,10 @@ def test_linear4_refusals():
     size = ctypes.c_uint64()
     for f, call, args in ((L_.actq_linear4_workspace, L_.actq_linear4, lambda w, n: [w, _rows(), 1, 5000, FAKE, 0, _rows(), FAKE, n, None]),
                           (L_.actq_linear4_backward_workspace, L_.actq_linear4_backward, lambda w, n: [w, _rows(), 1, 5000, _rows(), FAKE, n, None])):
+        for rows in (0, 1, 200, 5000):
+            for dt in (0, 1, 2):
+                for w in (_weights(), _weights(inputs=1, outputs=1), _weights(inputs=1 << 20, outputs=1 << 20)):
+                    assert f(w, dt, rows, ctypes.addressof(size)) == 0 and (size.value == 0 or rows > 0)
         assert f(_weights(), 1, 5000, ctypes.addressof(size)) == 0
         if size.value:   # one byte less, none, or misaligned
             assert call(*args(_weights(), size.value - 1)) == E
