@@ -80,7 +80,7 @@ __device__ __forceinline__ void exact_key(float (&x)[8], const float (&w)[8], co
 constexpr int kAhead = 4;
 
 template <typename T, int LANES>
-__global__ __launch_bounds__(kAppendBlock) void cache_append_kernel(AppendArgs<T> a)
+__global__ __launch_bounds__(kAppendBlock, 4) void cache_append_kernel(AppendArgs<T> a)
 {
     constexpr int kSide = 64 / LANES, kDim = LANES * kLaneValues;
     const int lane = threadIdx.x % 64, at = lane % LANES, first = kLaneValues * at, side = lane / LANES;

@@ -209,126 +209,159 @@ struct BlockGradArgs {
     int32_t of_post, of_gate, vectors;   // their places (post_weight, gate: -1 without one), how many there are
 };
 
-// A team goes through the tokens with the grid's stride and keeps its share of the channels' gradients in registers; the teams of a workgroup
-// join theirs in the LDS in a fixed order, a second kernel those of the workgroups.
+// A team goes through the tokens with the grid's stride and keeps its share of the channels' gradients in registers, beside the channels themselves and the next
+// token's rows, which are on their way while one is worked on (but for teams of 16 wavefronts, which have half the registers); the teams of a workgroup join theirs in the LDS in a fixed order, a second kernel those of the workgroups.
 template <typename T, int WAVES, int PARTS>
-__global__ __launch_bounds__(kBlockThreads<WAVES>) void block_norm_backward_kernel(BlockGradArgs<T> a)
+__global__ __launch_bounds__(kBlockThreads<WAVES>, WAVES == 16 ? 4 : 2) void block_norm_backward_kernel(BlockGradArgs<T> a)
 {
     constexpr int kTeams = WAVES == 1 ? kSmallTeams : 1;
     __shared__ Team<WAVES, 3> team;
     __shared__ float joined[WAVES == 1 ? kSmallTeams * 64 * PARTS * 8 : 1];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int lane = WAVES == 1 ? threadIdx.x % 64 : threadIdx.x;
+    const bool gated = a.gates.p || a.gate;
     int turn = 0;
-    float grad_w[PARTS][8], grad_p[PARTS][8], grad_g[PARTS][8];
+    float grad_w[PARTS][8], grad_p[PARTS][8], grad_g[PARTS][8], weight[PARTS][8], post[PARTS][8], gate[PARTS][8];
+    constexpr bool kHeld = WAVES < 16;
+    const auto channels = [&] {
+#pragma unroll
+        for (int c = 0; c < PARTS; ++c) {
+            const int first = kLaneValues * (lane + c * 64 * WAVES);
+            load_channels<T>(a.weight, a.wide, first, a.width, weight[c]);
+            if (a.gate) load_channels<T>(a.gate, a.wide, first, a.width, gate[c]);
+            if (a.post_weight) {
+                load_channels<T>(a.post_weight, a.wide, first, a.width, post[c]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) post[c][i] = 1.0f;
+            }
+        }
+    };
+    if (kHeld) channels();
 #pragma unroll
     for (int c = 0; c < PARTS; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i) grad_w[c][i] = grad_p[c][i] = grad_g[c][i] = 0.0f;
-    for (int64_t token = static_cast<int64_t>(blockIdx.x) * kTeams + (WAVES == 1 ? wave : 0); token < a.tokens; token += static_cast<int64_t>(gridDim.x) * kTeams) {
-        Eight<T> ee[PARTS], eu[PARTS], er[PARTS], eh[PARTS], eg[PARTS];
+    struct Token {
+        Eight<T> e[PARTS], u[PARTS], r[PARTS], h[PARTS], g[PARTS];
+    };
+    const auto load = [&](Token& t, int64_t token) {
 #pragma unroll
         for (int c = 0; c < PARTS; ++c) {
             const int first = kLaneValues * (lane + c * 64 * WAVES);
-            ee[c].v = {};
-            eh[c].v = {};
-            load_part(eu[c], a.ey.p + token * a.ey.stride, first, a.width);
-            load_part(er[c], a.r.p + token * a.r.stride, first, a.width);
-            if (a.er.p) load_part(ee[c], a.er.p + token * a.er.stride, first, a.width);
-            if (a.h.p) load_part(eh[c], a.h.p + token * a.h.stride, first, a.width);
-            if (a.gates.p) load_part(eg[c], a.gates.p + token * a.gates.stride, first, a.width);
+            t.e[c].v = {};
+            t.h[c].v = {};
+            load_part(t.u[c], a.ey.p + token * a.ey.stride, first, a.width);
+            load_part(t.r[c], a.r.p + token * a.r.stride, first, a.width);
+            if (a.er.p) load_part(t.e[c], a.er.p + token * a.er.stride, first, a.width);
+            if (a.h.p) load_part(t.h[c], a.h.p + token * a.h.stride, first, a.width);
+            if (a.gates.p) load_part(t.g[c], a.gates.p + token * a.gates.stride, first, a.width);
+        }
+    };
+    const int64_t stride = static_cast<int64_t>(gridDim.x) * kTeams;
+    int64_t token = static_cast<int64_t>(blockIdx.x) * kTeams + (WAVES == 1 ? wave : 0);
+    Token now;
+    if (kHeld && token < a.tokens) load(now, token);
+    for (; token < a.tokens; token += stride) {
+        Token next;
+        if (kHeld) {
+            if (token + stride < a.tokens) load(next, token + stride);
+        } else {
+            load(now, token);
+            channels();
         }
         float s[PARTS][8];
         float sums[3] = {0.0f, 0.0f, 0.0f};   // of r^2, u w r, h^2
-        // s holds u w, then the gradient of x times the scale
 #pragma unroll
         for (int c = 0; c < PARTS; ++c) {
-            float u[8], r[8], h[8], w[8];
-            eu[c].widen(u);
-            er[c].widen(r);
-            eh[c].widen(h);
-            load_channels<T>(a.weight, a.wide, kLaneValues * (lane + c * 64 * WAVES), a.width, w);
+            float u[8], r[8], h[8];
+            now.u[c].widen(u);
+            now.r[c].widen(r);
+            now.h[c].widen(h);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                s[c][i] = u[i] * w[i];
                 sums[0] = fmaf(r[i], r[i], sums[0]);
-                sums[1] = fmaf(s[c][i], r[i], sums[1]);
+                sums[1] = fmaf(u[i] * weight[c][i], r[i], sums[1]);
                 sums[2] = fmaf(h[i], h[i], sums[2]);
             }
         }
         team.sum(sums, turn);
         const float q = 1.0f / sqrtf(fmaf(sums[0], a.mean, a.eps));
         const float back = sums[1] * a.mean * q * q;
-        const float t = 1.0f / sqrtf(fmaf(sums[2], a.mean, a.eps));
+        const float t = a.post_weight ? 1.0f / sqrtf(fmaf(sums[2], a.mean, a.eps)) : 1.0f;
+        // the gradient of x, and s: times the scale
 #pragma unroll
         for (int c = 0; c < PARTS; ++c) {
-            const int first = kLaneValues * (lane + c * 64 * WAVES);
             float u[8], r[8], e[8];
-            eu[c].widen(u);
-            er[c].widen(r);
-            ee[c].widen(e);
+            now.u[c].widen(u);
+            now.r[c].widen(r);
+            now.e[c].widen(e);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 grad_w[c][i] = fmaf(u[i], r[i] * q, grad_w[c][i]);
-                e[i] = fmaf(q, fmaf(-r[i], back, s[c][i]), e[i]);
+                e[i] = fmaf(q, fmaf(-r[i], back, u[i] * weight[c][i]), e[i]);
                 s[c][i] = a.scale * e[i];
             }
-            ee[c].round(e);
-            store_part(ee[c], a.x_out.p + token * a.x_out.stride, first, a.width);
+            Eight<T> out;
+            out.round(e);
+            store_part(out, a.x_out.p + token * a.x_out.stride, kLaneValues * (lane + c * 64 * WAVES), a.width);
         }
-        if (!a.h.p) continue;
-        const bool gated = a.gates.p || a.gate;
-        float along[1] = {0.0f};   // of s g p h
-#pragma unroll
-        for (int c = 0; c < PARTS; ++c) {
-            const int first = kLaneValues * (lane + c * 64 * WAVES);
-            float h[8], p[8];
-            eh[c].widen(h);
-            if (a.post_weight) load_channels<T>(a.post_weight, a.wide, first, a.width, p);
-            if (gated) {
-                float g[8], gradient[8];
-                if (a.gates.p)
-                    eg[c].widen(g);
-                else
-                    load_channels<T>(a.gate, a.wide, first, a.width, g);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    gradient[i] = s[c][i] * (a.post_weight ? h[i] * t * p[i] : h[i]);
-                    s[c][i] *= g[i];
-                }
-                if (a.gates.p) {
-                    eg[c].round(gradient);
-                    store_part(eg[c], a.gates_out.p + token * a.gates_out.stride, first, a.width);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) grad_g[c][i] += gradient[i];
-                }
-            }
-            if (a.post_weight) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    grad_p[c][i] = fmaf(s[c][i], h[i] * t, grad_p[c][i]);
-                    s[c][i] *= p[i];
-                    along[0] = fmaf(s[c][i], h[i], along[0]);
-                }
-            }
-        }
-        if (a.post_weight) {
-            team.sum(along, turn);
-            const float towards = along[0] * a.mean * t * t;
+        if (a.h.p) {
+            float along[1] = {0.0f};   // of s g p h
 #pragma unroll
             for (int c = 0; c < PARTS; ++c) {
                 float h[8];
-                eh[c].widen(h);
+                now.h[c].widen(h);
+                if (gated) {
+                    float g[8], gradient[8];
+                    if (a.gates.p) {
+                        now.g[c].widen(g);
+                    } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s[c][i] = t * fmaf(-h[i], towards, s[c][i]);
+                        for (int i = 0; i < 8; ++i) g[i] = gate[c][i];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        gradient[i] = s[c][i] * (h[i] * t * post[c][i]);
+                        s[c][i] *= g[i];
+                    }
+                    if (a.gates.p) {
+                        Eight<T> out;
+                        out.round(gradient);
+                        store_part(out, a.gates_out.p + token * a.gates_out.stride, kLaneValues * (lane + c * 64 * WAVES), a.width);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) grad_g[c][i] += gradient[i];
+                    }
+                }
+                if (a.post_weight) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        grad_p[c][i] = fmaf(s[c][i], h[i] * t, grad_p[c][i]);
+                        s[c][i] *= post[c][i];
+                        along[0] = fmaf(s[c][i], h[i], along[0]);
+                    }
+                }
+            }
+            if (a.post_weight) {
+                team.sum(along, turn);
+                const float towards = along[0] * a.mean * t * t;
+#pragma unroll
+                for (int c = 0; c < PARTS; ++c) {
+                    float h[8];
+                    now.h[c].widen(h);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[c][i] = t * fmaf(-h[i], towards, s[c][i]);
+                }
+            }
+#pragma unroll
+            for (int c = 0; c < PARTS; ++c) {
+                Eight<T> out;
+                out.round(s[c]);
+                store_part(out, a.h_out.p + token * a.h_out.stride, kLaneValues * (lane + c * 64 * WAVES), a.width);
             }
         }
-#pragma unroll
-        for (int c = 0; c < PARTS; ++c) {
-            eh[c].round(s[c]);
-            store_part(eh[c], a.h_out.p + token * a.h_out.stride, kLaneValues * (lane + c * 64 * WAVES), a.width);
-        }
+        if (kHeld) now = next;
     }
     if (!a.partial) return;
     const auto keep = [&](const float (&grad)[PARTS][8], int place) {
@@ -358,38 +391,50 @@ __global__ __launch_bounds__(kBlockThreads<WAVES>) void block_norm_backward_kern
     if (a.of_gate >= 0) keep(grad_g, a.of_gate);
 }
 
-// The channels' gradients: the workgroups' shares in binary64, each of 64 threads a 64th of them, all of a thread's loads in flight.
-constexpr int kSumColumns = 16, kSumRows = 64, kSumAhead = 8;
+// The channels' gradients: the workgroups' shares in binary64.  A thread takes four columns of a 16th or 64th of the shares, all of its loads in flight: 64 columns a
+// workgroup where there are many, 16 else (12288 columns of 512 shares 6.4 us, with 16 columns in steps of 4 bytes 12.7; 4094 columns 12.4 and 7).
+constexpr int kSumThreads = 256;
 
-template <typename W>
-__global__ __launch_bounds__(kSumColumns* kSumRows) void block_channels_kernel(const float* partial, int32_t blocks, int32_t width, int32_t columns, W* first, W* second, W* third)
+template <typename W, int kSumColumns>
+__global__ __launch_bounds__(kSumThreads) void block_channels_kernel(const float* partial, int32_t blocks, int32_t width, int32_t columns, W* first, W* second, W* third)
 {
+    constexpr int kSumRows = kSumThreads * 4 / kSumColumns, kSumAhead = 512 / kSumRows < 16 ? 512 / kSumRows : 16;
     __shared__ double sums[kSumRows][kSumColumns];
-    const int column = threadIdx.x % kSumColumns, row = threadIdx.x / kSumColumns, at = blockIdx.x * kSumColumns + column;
-    double sum = 0.0;
+    const int quad = threadIdx.x % (kSumColumns / 4) * 4, row = threadIdx.x / (kSumColumns / 4), at = blockIdx.x * kSumColumns + quad;
+    double sum[4] = {};
     for (int b = row; b < blocks; b += kSumRows * kSumAhead) {
-        float v[kSumAhead];
+        f32x4 v[kSumAhead];
 #pragma unroll
         for (int k = 0; k < kSumAhead; ++k) {
+            typedef f32x4 any __attribute__((aligned(4)));
             const int from = b + k * kSumRows;
-            v[k] = from < blocks && at < columns ? partial[static_cast<int64_t>(from) * columns + at] : 0.0f;
+            const float* const p = partial + static_cast<int64_t>(from) * columns + at;
+            v[k] = f32x4{};
+            if (from < blocks && at + 4 <= columns) {
+                v[k] = *reinterpret_cast<const any*>(p);
+            } else if (from < blocks) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (at + i < columns) v[k][i] = p[i];
+            }
         }
 #pragma unroll
-        for (int k = 0; k < kSumAhead; ++k) sum += static_cast<double>(v[k]);
+        for (int k = 0; k < kSumAhead; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] += static_cast<double>(v[k][i]);
     }
-    sums[row][column] = sum;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums[row][quad + i] = sum[i];
     __syncthreads();
-    for (int half = kSumRows / 2; half >= 1; half /= 2) {
-        if (row < half) {
-            sum += sums[row + half][column];
-            sums[row][column] = sum;
-        }
-        __syncthreads();
-    }
-    if (row != 0 || at >= columns) return;
-    const int vector = at / width;
+    if (threadIdx.x >= kSumColumns) return;
+    const int column = blockIdx.x * kSumColumns + threadIdx.x;
+    if (column >= columns) return;
+    double all = 0.0;
+#pragma unroll
+    for (int r = 0; r < kSumRows; ++r) all += sums[r][threadIdx.x];
+    const int vector = column / width;
     W* const out = vector == 0 ? first : vector == 1 ? second : third;
-    out[at - vector * width] = static_cast<W>(static_cast<float>(sum));
+    out[column - vector * width] = static_cast<W>(static_cast<float>(all));
 }
 
 template <int N>
@@ -407,12 +452,15 @@ int by_width(int32_t width, bool few, F f)
     return width <= 4096 ? f(Number<4>{}, Number<2>{}) : width <= 8192 ? f(Number<4>{}, Number<4>{}) : f(Number<16>{}, Number<2>{});
 }
 
-template <typename F>
+// A team's registers hold 16 columns a lane of 16-bit types, 8 of binary32.
+template <typename T, typename F>
 int by_width_backward(int32_t width, F f)
 {
     if (width <= 512) return f(Number<1>{}, Number<1>{});
-    if (width <= 1024) return f(Number<1>{}, Number<2>{});
-    return width <= 2048 ? f(Number<4>{}, Number<1>{}) : width <= 4096 ? f(Number<4>{}, Number<2>{}) : width <= 8192 ? f(Number<8>{}, Number<2>{}) : f(Number<16>{}, Number<2>{});
+    if (width <= 2048) return f(Number<4>{}, Number<1>{});
+    if (width > 8192) return f(Number<16>{}, Number<2>{});
+    if constexpr (sizeof(T) == 4) return width <= 4096 ? f(Number<8>{}, Number<1>{}) : f(Number<16>{}, Number<1>{});
+    else return width <= 4096 ? f(Number<4>{}, Number<2>{}) : f(Number<8>{}, Number<2>{});
 }
 
 constexpr int64_t kFewRows = 512;
@@ -422,7 +470,7 @@ constexpr int64_t kGradBlocks = 512;
 
 int64_t grad_blocks(const actq_block* b)
 {
-    const int64_t teams = b->width <= 1024 ? kSmallTeams : 1, need = (b->tokens + teams - 1) / teams;
+    const int64_t teams = b->width <= 512 ? kSmallTeams : 1, need = (b->tokens + teams - 1) / teams;
     return need < kGradBlocks ? need : kGradBlocks;
 }
 
@@ -469,8 +517,8 @@ int launch_block_norm_backward(const actq_block* b, const actq_rows* grad_r, con
     const int vectors = vectors_of(b);
     if (blocks > 0) {
         const int rc = by_dtype(b->dt, [&](auto type) {
-            return by_width_backward(b->width, [&](auto waves, auto parts) {
-                typedef decltype(type) T;
+            typedef decltype(type) T;
+            return by_width_backward<T>(b->width, [&](auto waves, auto parts) {
                 constexpr int kWaves = decltype(waves)::value, kParts = decltype(parts)::value;
                 BlockGradArgs<T> a = {};
                 a.er = rows_of<T>(grad_r);
@@ -505,8 +553,15 @@ int launch_block_norm_backward(const actq_block* b, const actq_rows* grad_r, con
         typedef decltype(type) W;
         W* const outs[3] = {static_cast<W*>(grad_weight), static_cast<W*>(b->post_weight ? grad_post_weight : grad_gate), static_cast<W*>(grad_gate)};
         const int32_t columns = vectors * b->width;
-        launch(block_channels_kernel<W>, static_cast<unsigned>((columns + kSumColumns - 1) / kSumColumns), kSumColumns * kSumRows, s, static_cast<const float*>(workspace),
-               static_cast<int32_t>(blocks), b->width, columns, outs[0], outs[1], outs[2]);
+        const auto sum = [&](auto wide) {
+            constexpr int kColumns = decltype(wide)::value;
+            launch(block_channels_kernel<W, kColumns>, static_cast<unsigned>((columns + kColumns - 1) / kColumns), kSumThreads, s, static_cast<const float*>(workspace),
+                   static_cast<int32_t>(blocks), b->width, columns, outs[0], outs[1], outs[2]);
+        };
+        if (columns >= 8192)
+            sum(Number<64>{});
+        else
+            sum(Number<16>{});
         return launched(who);
     });
 }
