@@ -5,7 +5,8 @@ layer keeps a compressed context instead and computes its gradients from the deq
 context with the stock backward routine of the layer.  The forward results are those of the
 stock layer, so inference is unchanged.
 
-`QHeadNorm` (norm and rotation of attention heads) computes forward and backward in the library as well.
+`QHeadNorm` (norm and rotation of attention heads), `QBlockNorm` (the norms around a block with gate and residual sum) and `Linear4` (a linear
+layer whose weights are frozen in 4 bits, which needs no context) compute forward and backward in the library as well.
 
 Everything that touches the saved activations runs in libactq through `binding`: per-group
 statistics, sensitivities, the device-side bit allocator, quantize + pack, unpack + dequantize,
@@ -27,7 +28,7 @@ from torch.autograd import forward_ad
 from . import binding as B
 
 __all__ = ["QConfig", "config", "set_optimization_level", "compress", "decompress", "SavedContext",
-           "QLinear", "QConv2d", "QBatchNorm2d", "QReLU", "QMaxPool2d", "QHeadNorm", "convert"]
+           "QLinear", "QConv2d", "QBatchNorm2d", "QReLU", "QMaxPool2d", "QHeadNorm", "QBlockNorm", "Linear4", "convert"]
 
 
 @dataclass
@@ -305,22 +306,39 @@ class _QMaxPool2dFn(torch.autograd.Function):
         return B.maxpool2d_backward(arg, grad_y.contiguous(), H, W, kernel, stride, padding, dilation), None, None, None, None
 
 
-def _no_tangents(*tensors) -> None:
+def _no_tangents(*tensors, who: str = "QHeadNorm") -> None:
     """Forward-mode tangents, which the library's calls would drop, are refused."""
-    if any(forward_ad.unpack_dual(t).tangent is not None for t in tensors):
-        raise NotImplementedError("QHeadNorm has no forward-mode derivative")
+    if any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise NotImplementedError(f"{who} has no forward-mode derivative")
 
 
 class _Last(torch.autograd.Function):
     """A gradient that the library computed from `of` and that cannot be differentiated once more."""
+    who = "QHeadNorm"
 
     @staticmethod
     def forward(ctx, grad, *of):
         return grad.view_as(grad)
 
-    @staticmethod
-    def backward(ctx, *_):
-        raise NotImplementedError("QHeadNorm has no second derivative")
+    @classmethod
+    def backward(cls, ctx, *_):
+        raise NotImplementedError(f"{cls.who} has no second derivative")
+
+
+class _LastOfBlockNorm(_Last):
+    who = "QBlockNorm"
+
+
+class _LastOfLinear4(_Last):
+    who = "Linear4"
+
+
+def _last(kind, gradients, *of):
+    """The gradients, marked as such where a graph of them is being made, in which they would pass for constants."""
+    if not torch.is_grad_enabled():
+        return gradients
+    of = [t for t in of if t is not None]
+    return [None if g is None else kind.apply(g.requires_grad_(), *of) for g in gradients]
 
 
 class _QHeadNormFn(torch.autograd.Function):
@@ -367,6 +385,93 @@ class _QHeadNormFn(torch.autograd.Function):
         if torch.is_grad_enabled():   # a graph of the gradients is being made, in which these would pass for constants
             gradients = [None if g is None else _Last.apply(g.requires_grad_(), grad_q, grad_k, q_weight, k_weight) for g in gradients]
         return (*gradients, None, None, None, None, None)
+
+
+def _kept(x, contexts: list, saved: list) -> None:
+    """Keeps `x` for the backward pass, compressed if the codec takes it."""
+    if x.dtype in _DTYPES and x.numel() > 0:
+        c = compress(x)
+        streams = c.host if c.host is not None else (c.packed, c.header)
+        contexts.append((c.shape, c.dtype, c.N, c.D, c.hf, c.ready, c.host is not None))
+        saved += [c.bits, c.offsets, *streams]
+    else:
+        contexts.append(None)
+        saved += [x, None, None, None]
+
+
+def _again(meta, first, offsets, s0, s1):
+    """What _kept was given, or its approximation."""
+    if meta is None:
+        return first
+    c = SavedContext()
+    c.bits, c.offsets = first, offsets
+    c.shape, c.dtype, c.N, c.D, c.hf, c.ready, swapped = meta
+    c.host, c.packed, c.header = ((s0, s1), None, None) if swapped else (None, s0, s1)
+    return decompress(c)
+
+
+def _in_rows(g, width: int):
+    """[rows, width] with contiguous rows."""
+    g = g.reshape(-1, width)
+    return g if g.stride(-1) == 1 else g.contiguous()
+
+
+class _QBlockNormFn(torch.autograd.Function):
+    """The norms around a block by the library; the contexts are the compressed residual sum, the block's output and the tokens' gates."""
+
+    @staticmethod
+    def forward(ctx, x, h, gate, weight, post_weight, scale, eps):
+        ctx.set_materialize_grads(False)
+        r, y = B.block_norm(x, h, gate, weight, post_weight, scale, eps)
+        ctx.options = scale, eps
+        ctx.contexts, saved = [], []
+        for t in (r, h, gate if gate is not None and gate.dim() == 2 else None):
+            if t is None:
+                ctx.contexts.append(None)
+                saved += [None, None, None, None]
+            else:
+                _kept(t, ctx.contexts, saved)
+        ctx.save_for_backward(*saved, gate if gate is not None and gate.dim() == 1 else None, weight, post_weight)
+        return y if h is None else (r, y)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        saved = ctx.saved_tensors
+        r, h, gates = (_again(meta, *saved[4 * i:4 * i + 4]) for i, meta in enumerate(ctx.contexts))
+        gate, weight, post_weight = saved[12:]
+        grad_r, grad_y = (None, *grads) if h is None else grads
+        if grad_r is None and grad_y is None:
+            return (None,) * 7
+        given = grad_r, grad_y
+        if not _native(*(g for g in given if g is not None)):
+            _no_tangents(*given, who="QBlockNorm")
+        grad_y = torch.zeros_like(r) if grad_y is None else _in_rows(grad_y, r.shape[1])
+        grad_r = None if grad_r is None else _in_rows(grad_r, r.shape[1])
+        scale, eps = ctx.options
+        gradients = B.block_norm_backward(grad_r, grad_y, r, h, gate if gates is None else gates, weight, post_weight, scale, eps,
+                                          need_weights=ctx.needs_input_grad[3] or ctx.needs_input_grad[4] or (gates is None and ctx.needs_input_grad[2]))
+        return (*_last(_LastOfBlockNorm, gradients, *given, weight, post_weight, gate), None, None)
+
+
+class _Linear4Fn(torch.autograd.Function):
+    """A product with frozen weights: the gradient of x needs nothing that the forward pass computed."""
+
+    @staticmethod
+    def forward(ctx, x, codes, header, bias):
+        ctx.save_for_backward(codes, header, bias)
+        ctx.inputs = x.shape[-1]
+        return B.linear4(x, codes, header, bias)
+
+    @staticmethod
+    def backward(ctx, grad_y):
+        codes, header, bias = ctx.saved_tensors
+        if not _native(grad_y):
+            _no_tangents(grad_y, who="Linear4")
+        rows = _in_rows(grad_y, grad_y.shape[-1])
+        grad_x = B.linear4_backward(rows, codes, header, ctx.inputs).view(*grad_y.shape[:-1], ctx.inputs) if ctx.needs_input_grad[0] else None
+        grad_b = rows.sum(0, dtype=torch.float32).to(bias.dtype) if bias is not None and ctx.needs_input_grad[3] else None
+        grad_x, grad_b = _last(_LastOfLinear4, [grad_x, grad_b], grad_y)
+        return grad_x, None, None, grad_b
 
 
 # ----------------------------------------------------------------------------- modules
@@ -443,6 +548,70 @@ class QHeadNorm(nn.Module):
         if not host.plain(q, k, q_weight, k_weight):
             _no_tangents(q, k, q_weight, k_weight)
         return host.head_norm_rotate(q, k, q_weight, k_weight, positions, cos, sin, float(self.eps), bool(self.interleaved), None, None)
+
+
+class QBlockNorm(nn.Module):
+    """The norms behind and before a block of a residual network with its gate and scale (binding.block_norm): of the residual stream x and
+    the block's output h, [..., width], the sum r = x + scale * gate * norm(h) * post_weight and y = norm(r) * weight, what the next block reads.
+
+    post: whether there is a norm behind the block; gate: whether a gate per channel is learned.  A gate of every token [..., width] may be passed
+    instead.  Without h r is x.  In training the backward pass starts from compressed contexts (bfloat16, which the codec does not take, is kept as it is);
+    forward-mode tangents and second derivatives are refused."""
+
+    def __init__(self, width: int, post: bool = True, gate: bool = False, scale: float = 1.0, eps: float = 1e-6, device=None, dtype=None):
+        super().__init__()
+        self.width, self.scale, self.eps = width, scale, eps
+        self.weight = nn.Parameter(torch.ones(width, device=device, dtype=dtype))
+        self.post_weight = nn.Parameter(torch.ones(width, device=device, dtype=dtype)) if post else None
+        self.gate = nn.Parameter(torch.ones(width, device=device, dtype=dtype)) if gate else None
+
+    def forward(self, x, h=None, gate=None):
+        if gate is not None and (self.gate is not None or h is None):
+            raise ValueError("a gate of every token goes with h and without a learned gate")
+        weight, post, gate = self.weight, None if h is None else self.post_weight, gate if h is None or self.gate is None else self.gate
+        shape = x.shape
+        rows = [None if t is None else t if t is self.gate else t.reshape(-1, self.width) for t in (x, h, gate)]
+        inputs = [t for t in (*rows, weight, post) if t is not None]
+        if torch.is_grad_enabled() and any(t.requires_grad for t in inputs):
+            out = _QBlockNormFn.apply(*rows, weight, post, float(self.scale), float(self.eps))
+            r, y = (x, out) if h is None else out
+        else:
+            if not (B._host or B.host()).plain(*inputs):
+                _no_tangents(*inputs, who="QBlockNorm")
+            r, y = B.block_norm(*rows, weight, post, self.scale, self.eps)
+            r = x if h is None else r
+        return r.view(shape), y.view(shape)
+
+
+class Linear4(nn.Module):
+    """A linear layer with frozen weights of 4 bits (binding.quantize_weights, linear4).  Gradients flow to its input and its bias; nothing of the
+    input is kept for them.  forward-mode tangents and second derivatives are refused."""
+
+    def __init__(self, codes, header, inputs: int, bias=None):
+        super().__init__()
+        self.inputs = inputs
+        self.register_buffer("codes", codes)
+        self.register_buffer("header", header.view(torch.int16))   # as bits: a module's type may change, the format's not
+        self.bias = None if bias is None else nn.Parameter(bias)
+
+    @classmethod
+    def from_linear(cls, linear: nn.Linear, group: int = 128) -> "Linear4":
+        """Quantises the weights of a linear layer that lives on the GPU."""
+        codes, header = B.quantize_weights(linear.weight.detach(), group)
+        return cls(codes, header, linear.in_features, None if linear.bias is None else linear.bias.detach().clone())
+
+    def weight(self, dtype=torch.float32):
+        """[outputs, inputs]: what the codes stand for."""
+        return B.dequantize_weights(self.codes, self.header.view(torch.bfloat16), self.inputs, dtype)
+
+    def forward(self, x):
+        header, bias = self.header.view(torch.bfloat16), self.bias
+        if torch.is_grad_enabled() and (x.requires_grad or bias is not None and bias.requires_grad):
+            return _Linear4Fn.apply(x, self.codes, header, bias)
+        host = B._host or B.host()
+        if not host.plain(x, bias):
+            _no_tangents(x, bias, who="Linear4")
+        return host.linear4(x, self.codes, header, bias, None)
 
 
 def convert(module: nn.Module) -> nn.Module:
