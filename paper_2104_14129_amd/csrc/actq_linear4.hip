@@ -362,10 +362,10 @@ __device__ __forceinline__ void arrived()
 
 // A workgroup's tile is ROWS rows x 256 outputs, made of blocks of 32 x 32: 128 rows, two by two blocks a wavefront, or 32, one.  A group's sums of products
 // and the total are both what ordinary instructions work with, so they share the 256 registers that these see, and 128 rows take two wavefronts a SIMD.  x, codes and headers
-// go from memory to the LDS without registers, two stages of 128 k ahead (binary32, three times the bytes: 64 k, and one ahead with 128 rows); a wavefront turns the codes of its outputs
+// go from memory to the LDS without registers, two stages of 128 k ahead (binary32, three times the bytes: one of 64 with 128 rows; four stages ahead under 32 rows give nothing); a wavefront turns the codes of its outputs
 // into numbers in registers.  Under 32 rows, where memory is what counts, the groups' sums of x are one more product, with ones.
 template <typename T, int GROUP, int ROWS>
-__global__ __launch_bounds__(512, ROWS == 128 ? 2 : 4) void linear4_many_kernel(ManyArgs<T> a)
+__global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
 {
     typedef typename Meets<T>::vector V;
     constexpr int kP = kPieces<T>, kB = ROWS == 128 ? 2 : 1, kRing = kP == 1 || kB == 1 ? 3 : 2, kDepth = kP == 1 ? 128 : 64, kRows = ROWS, kColumns = 256;
@@ -376,8 +376,10 @@ __global__ __launch_bounds__(512, ROWS == 128 ? 2 : 4) void linear4_many_kernel(
     constexpr int kHeadGroups = 8;                     // headers of so many groups are fetched at a time: one by one they would take as many lines of the caches as the codes
     // one array: of several the compiler knows which of them a load to the LDS writes, and waits for it before the next read of that one
     constexpr int kTilePlace = kRows * kChunks < 512 ? 512 : kRows * kChunks, kCodes = kP * kTilePlace, kStage = kCodes + kColumns * kSlots, kHeadPlace = kColumns * kHeadGroups;
-    __shared__ u32x4 lds[kRing * kStage + 2 * kHeadPlace / 4];
-    uint32_t* const heads = reinterpret_cast<uint32_t*>(lds + kRing * kStage);   // [2][outputs][kHeadGroups]
+    // as many places for headers as the stages on their way can need beside the one that is worked on
+    constexpr int kHeadStages = kHeadGroups * GROUP / kDepth, kHeadPlaces = 1 + (kRing - 1 + kHeadStages - 1) / kHeadStages;
+    __shared__ u32x4 lds[kRing * kStage + kHeadPlaces * kHeadPlace / 4];
+    uint32_t* const heads = reinterpret_cast<uint32_t*>(lds + kRing * kStage);   // [kHeadPlaces][outputs][kHeadGroups]
     const int lane = threadIdx.x % 64, at = lane % 32, half = lane / 32;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     // each XCD (workgroups go to them in turn) takes a run of tiles, bands of 4 row tiles through all column tiles: their rows and codes stay in its L2
@@ -415,15 +417,16 @@ __global__ __launch_bounds__(512, ROWS == 128 ? 2 : 4) void linear4_many_kernel(
 #pragma unroll
         for (int i = 0; i < kCodeMoves; ++i) to_lds(codes_from[i] + 4 * min(k / 32 + code_chunk[i], row_words / 4 - 1), lds + to * kStage + kCodes + i * 512 + wave * 64);
         if ((k - begin) % (kHeadGroups * GROUP) != 0) return;
-        const int place = (k - begin) / (kHeadGroups * GROUP) % 2, group = min(k / GROUP + static_cast<int>(threadIdx.x % kHeadGroups), a.w.groups - 1);
+        const int place = (k - begin) / (kHeadGroups * GROUP) % kHeadPlaces, group = min(k / GROUP + static_cast<int>(threadIdx.x % kHeadGroups), a.w.groups - 1);
 #pragma unroll
         for (int i = 0; i < kHeadPlace / 512; ++i) {
             const int64_t n = min(first_column + (i * 512 + static_cast<int>(threadIdx.x)) / kHeadGroups, a.w.outputs - 1);
             to_lds(a.w.header + n * a.w.groups + group, heads + place * kHeadPlace + i * 512 + wave * 64);
         }
     };
-    load(begin, 0);
-    if (kRing > 2 && begin + kDepth < end) load(begin + kDepth, 1);
+#pragma unroll
+    for (int i = 0; i < kRing - 1; ++i)
+        if (begin + i * kDepth < end) load(begin + i * kDepth, i);
 
     // zero times the groups' sums of x, and what the codes' shift leaves: products of the parts of both.  A lane takes four neighbouring groups at a time.
     const int columns = kB == 2 ? wave % 4 * 64 : wave * 32, rows = kB == 2 ? wave / 4 * 64 : 0;   // the wavefront's place in the tile
@@ -485,7 +488,10 @@ __global__ __launch_bounds__(512, ROWS == 128 ? 2 : 4) void linear4_many_kernel(
         }
     }
     const auto place = [](int row, int chunk) { return row * kChunks + (chunk ^ (row & (kChunks - 1))); };
-    arrived<0>();
+    if (begin + (kRing - 2) * kDepth < end)
+        arrived<(kRing - 2) * kLoads>();
+    else
+        arrived<0>();
     const V ones = __builtin_bit_cast(V, u32x4{Meets<T>::kOnes, Meets<T>::kOnes, Meets<T>::kOnes, Meets<T>::kOnes});
     int buffer = 0;
     for (int k = begin; k < end; k += kDepth) {
@@ -501,7 +507,7 @@ __global__ __launch_bounds__(512, ROWS == 128 ? 2 : 4) void linear4_many_kernel(
 #pragma unroll
             for (int c = 0; c < kB; ++c) {
                 const int column = columns + 32 * c + at;
-                head[c] = heads[(group + g) / kHeadGroups % 2 * kHeadPlace + column * kHeadGroups + (group + g) % kHeadGroups];
+                head[c] = heads[(group + g) / kHeadGroups % kHeadPlaces * kHeadPlace + column * kHeadGroups + (group + g) % kHeadGroups];
                 if constexpr (GROUP == 32) {   // a group is 16 bytes of an output, a half of them this lane's
                     const u32x2 v = reinterpret_cast<const u32x2*>(&codes[column * kSlots + (g ^ code_swizzle(column))])[half];
                     word[c][0] = v[0];
@@ -613,7 +619,8 @@ int32_t padded_inputs(const actq_weights4* w) { return (w->inputs + kSpan - 1) /
 uint64_t sums_bytes(const actq_weights4* w, int64_t rows) { return (static_cast<uint64_t>(rows) * (padded_inputs(w) / w->group) * sizeof(u32x2) + 15) / 16 * 16; }
 uint64_t copy_bytes(const actq_weights4* w, int dtype, int64_t rows) { return static_cast<uint64_t>(rows) * padded_inputs(w) * (dtype == ACTQ_F32 ? 6 : 2); }
 
-// Parts of the inputs: where the tiles are fewer than the compute units, as many as make one workgroup for each (of 32 rows two), of two spans at least.
+// Parts of the inputs: where the tiles are fewer than the compute units, as many as make one workgroup for each, of two spans at
+// least (of 32 rows two for each: 32 rows of 8192 x 16384 25.8 -> 31.0 us, four 38.7).
 struct Parts {
     int32_t row_tiles, column_tiles, count, share;
 };
@@ -624,7 +631,7 @@ Parts parts_of(const actq_weights4* w, int64_t rows, bool low)
     p.row_tiles = static_cast<int32_t>(low ? (rows + 31) / 32 : (rows + 127) / 128);
     p.column_tiles = (w->outputs + 255) / 256;
     const int64_t tiles = static_cast<int64_t>(p.row_tiles) * p.column_tiles, spans = padded_inputs(w) / kSpan;
-    const int64_t wanted = (low ? 512 : 256) / tiles, most = wanted < spans / 2 ? wanted : spans / 2, share = most > 1 ? (spans + most - 1) / most : spans;
+    const int64_t wanted = 256 / tiles, most = wanted < spans / 2 ? wanted : spans / 2, share = most > 1 ? (spans + most - 1) / most : spans;
     p.share = static_cast<int32_t>(share * kSpan);
     p.count = static_cast<int32_t>((spans + share - 1) / share);
     return p;
