@@ -593,7 +593,8 @@ int actq_block_norm(const actq_block* block, const actq_rows* x, const actq_rows
  * Its gradients from those of r (NULL: zeros) and y, and from r and h.  Sums over the tokens have a fixed
  * order.
  *
- * grad_x, grad_h     out; grad_h NULL without h.  They may be the memory of grad_r and grad_y
+ * grad_x, grad_h     out; grad_h NULL without h.  They may be the memory of grad_r and grad_y with the same
+ *                    strides
  * grad_gates         out, with `gates` only
  * grad_weight, grad_post_weight, grad_gate: device [width] of type weight_dt, out; NULL all, or
  *                    given for every one that the block has
@@ -637,7 +638,7 @@ int actq_weights4_dequantize(const actq_weights4* w, const actq_rows* out, actq_
  * y = x W^T + bias.  Products are exact (of a binary32 x: of the three bfloat16 numbers that make it
  * up), their sums binary32, a result is rounded once.  A row of x with an infinity or NaN gives NaN.
  *
- * x [rows, inputs], y [rows, outputs] of type dt; rows at least 0, below 2^20
+ * x [rows, inputs], y [rows, outputs] of type dt; rows at least 0, below 2^20; y may not overlap x
  * bias       device [outputs] of type dt or ACTQ_F32, or NULL
  * workspace  device, actq_linear4_workspace bytes (may be 0: then NULL), 16-byte aligned
  */
@@ -652,7 +653,7 @@ int actq_linear4(const actq_weights4* w, const actq_rows* x, actq_dtype dt, int6
  * ACTQ_F32; else a weight as 16 bits or, for ACTQ_F32, as it is.  That is off by 2^-11, 2^-16 and
  * 2^-21 of a product at most.
  *
- * grad_y [rows, outputs], grad_x [rows, inputs] of type dt; workspace as above
+ * grad_y [rows, outputs], grad_x [rows, inputs] of type dt, which may not overlap; workspace as above
  */
 int actq_linear4_backward_workspace(const actq_weights4* w, actq_dtype dt, int64_t rows, uint64_t* bytes_host);
 int actq_linear4_backward(const actq_weights4* w, const actq_rows* grad_y, actq_dtype dt, int64_t rows,

@@ -21,6 +21,7 @@
 
 #include <torch/extension.h>
 
+#include <ATen/MemoryOverlap.h>
 #include <ATen/TensorSubclassLikeUtils.h>
 #include <ATen/autocast_mode.h>
 #include <c10/core/GradMode.h>
@@ -1047,6 +1048,14 @@ PyObject* block_norm_impl(PyObject* const* a)
     }
     const Tensor y = rows_output(a[8], k.x, "y");
     const actq_rows hy = rows_to(y, "y");
+    // over an input element by element or beside it
+    for (const Tensor* out : std::initializer_list<const Tensor*>{&r, &y})
+        if (out->defined()) {
+            at::assert_no_partial_overlap(*out, k.x);
+            if (k.h) at::assert_no_partial_overlap(*out, *k.h);
+            if (k.gates) at::assert_no_partial_overlap(*out, *k.gates);
+        }
+    if (r.defined()) at::assert_no_overlap(r, y);
     call(api.block_norm, &k.b, &k.hx, k.h_rows, k.h ? &hr : nullptr, &hy, current_stream());
     return tuple_of({k.h ? give(a[7], r) : give(a[0], k.x), give(a[8], y)});
 }
@@ -1180,6 +1189,7 @@ PyObject* linear4_impl(PyObject* const* a)
     TORCH_CHECK_VALUE(out.dim() == 2 || out.is_contiguous(), "out must be contiguous or have two dimensions");
     const Tensor y = as_rows(out, "out");
     const actq_rows hy = rows_to(y, "out");
+    at::assert_no_overlap(y, x);
     uint64_t bytes = 0;
     call(api.linear4_workspace, &w, dt, x.size(0), &bytes);
     Tensor workspace;

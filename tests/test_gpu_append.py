@@ -128,4 +128,6 @@ def test_refused_by_the_binding():
         B.cache_append(q, k, v, qw, kw, *table, slots[:3], *cache)
     with pytest.raises(ValueError, match="expanded"):
         B.cache_append(q, k, v, qw, kw, *table, slots, *cache, q_out=torch.zeros((1, 2, 64), device=DEV).expand(6, 2, 64))
+    none = B.cache_append(q[:0], k[:0], v[:0], qw, kw, table[0][:0], *table[1:], slots[:0], *cache)
+    assert none.shape == (0, 2, 64) and all(torch.equal(a, b) for a, b in zip(cache, H.make_cache(pages, 2, 16, 64, 8, 4, 1, poison=False)))
     assert np.isfinite(B.cache_append(q, k, v, qw, kw, *table, slots, *cache).cpu().numpy()).all()

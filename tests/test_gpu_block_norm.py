@@ -168,6 +168,12 @@ def test_refused_by_the_binding():
             B.block_norm(*args)
     with pytest.raises(ValueError, match="overlap"):
         B.block_norm(x, x, None, w, r=x[:1].expand(4, 64))
+    both = torch.zeros((5, 64), device=DEV)
+    for r, y in ((both[:4], both[:4]), (both[:4], both[1:])):   # r and y are two
+        with pytest.raises(RuntimeError):
+            B.block_norm(x, x, None, w, r=r, y=y)
+    with pytest.raises(RuntimeError):   # a row is written before another team reads it
+        B.block_norm(both[:4], x, None, w, r=both[1:])
     with pytest.raises(ValueError, match="without h"):
         B.block_norm(x, None, None, w, r=x)
     with pytest.raises(B.ActqError):

@@ -127,6 +127,20 @@ def test_groups_that_are_not_finite_read_as_nan():
     assert torch.isfinite(g).all()
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("rows, inputs, outputs", [(5, 2560, 8200), (40, 2560, 5000), (700, 2560, 5000)])
+def test_groups_of_many_that_are_not_finite(rows, inputs, outputs, dtype):
+    """In every kernel such a group is seen by its output, and in the gradient by its inputs, alone."""
+    codes, header = (t.to(DEV) for t in Y.random_weights(outputs, inputs, 64, 2))
+    header[17, 3, 0], header[outputs - 1, 39, 1] = float("nan"), float("inf")
+    y = B.linear4(_rows(rows, inputs, dtype, 3).to(DEV), codes, header)
+    bad = ~torch.isfinite(y)
+    assert bad[:, 17].all() and bad[:, outputs - 1].all() and int(bad.sum()) == 2 * rows
+    g = B.linear4_backward(_rows(rows, outputs, dtype, 4).to(DEV), codes, header, inputs)
+    bad = ~torch.isfinite(g)
+    assert bad[:, 192:256].all() and int(bad[:, :2496].sum()) == 64 * rows   # of the last group a code of zero times infinity is what its column has
+
+
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
 @pytest.mark.parametrize("rows, inputs, outputs", [(3, 300, 100), (300, 300, 100), (40, 4100, 4000), (1100, 4100, 2100)])
 def test_rows_that_are_not_finite_are_their_own_business(rows, inputs, outputs, dtype):
@@ -198,6 +212,9 @@ def test_refused_by_the_binding():
             B.linear4(*args)
     with pytest.raises(ValueError, match="overlap"):
         B.linear4(x, codes, header, None, torch.zeros((1, 70), device=DEV).expand(3, 70))
+    square = torch.zeros((40, 200), device=DEV)
+    with pytest.raises(RuntimeError):   # a result over what others still read
+        B.linear4(square, *(t.to(DEV) for t in Y.random_weights(200, 200, 32, 5)), None, square)
     with pytest.raises(ValueError, match="per output"):
         B.linear4_backward(x, codes, header, 200)
     with pytest.raises(B.ActqError, match="group"):
