@@ -8,6 +8,10 @@
 // instructions multiply both exactly.  So a group's sum of x code is a sum of exact products in binary32, to which step, and zero times the group's sum of
 // x (one more product, with ones), come afterwards.  A binary32 x goes as the three bfloat16 numbers that make it up, and its codes as converted numbers:
 // sums of 128 x would cost it 4 of its 24 bits.
+//
+// Measured on one MI355X, whose copy of 1 GiB reaches 5.1 TB/s and whose library product of 8192^3 1.21 PFLOP/s in bfloat16: one row of 4096 x 4096 in groups of 128
+// 4.9 us, 23 rows of 8192 x 16384 in binary16 and groups of 64 26 us (3.0 TB/s), 4096 rows of 8192 x 8192 in bfloat16 541 us (1.02 PFLOP/s), the gradient of 2047 rows of
+// 4096 inputs and 8192 outputs 204 us (675 TFLOP/s).
 #include "actq_heads.h"
 
 namespace actq {
@@ -591,20 +595,21 @@ __global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
 }
 
 // Which kernel serves.  What counts is the units of 16 rows, 16 outputs and a span; measured on one MI355X, us, bfloat16 with groups of 128 where nothing is said:
-//   kFew         up to 8192 units (one row of 4096 x 4096 5.1, tiles of 32 rows 7.9; 4096 x 4096 binary32 8.2 and 13.5; 16384 units: 13.6 and 12.0)
-//   kFewWide     a few rows of many outputs: x is read once for 64 outputs (one row of 8192 x 16384 19.5, tiles 23.7; binary32 29.3 and 49.3; groups of
-//                32 44.0 and 32.8; at 8192 x 2048 18.6 and 7.7)
-//   kLowTiles    up to 64 rows, or 65536 units (binary32, where products are three times as many, 32768): 128 rows of 4096 x 4096 24.2, tiles of 128 rows 27.2;
-//                at 262144 units 44.4 and 36.7; 301 rows of 1000 x 1501 binary32 19.0 and 26.3
+//   kFew         small matrices: up to 8192 units, 4096 of groups of 32 (one row of 4096 x 4096 5.5, tiles of 32 rows 8.2; 16 rows 7.8 and 9.8; at 16384 units 13.8
+//                and 12.1; groups of 32, 64 rows of 2048 x 2048 10.7 and 8.5), unless a wavefront had more than two spans (16 rows of 8192 x 2048 12.8 and 8.7)
+//   kFewWide     a few rows of many outputs: x is read once for 64 outputs (one row of 8192 x 16384 19.7, tiles 23.0; binary32 29.5 and 48.4; groups of
+//                32 44 and 30)
+//   kLowTiles    up to 64 rows, or 131072 units (binary32, where products are three times as many, 32768): 128 rows of 4096 x 4096 18.1, tiles of 128 rows 26.6;
+//                192 23.7 and 26.4; 301 33.3 and 31.1; 128 of 8192 x 8192 39.7 and 35.6; binary32, 301 rows of 1000 x 1501 18.8 and 26.1, 300 of 2048 x 2048 29.7 and 27.8
 //   kHighTiles   else
 enum Kernel { kFew, kFewWide, kLowTiles, kHighTiles };
 
 Kernel kernel_of(const actq_weights4* w, int dtype, int64_t rows)
 {
-    const int64_t units = (rows + 15) / 16 * ((w->outputs + 15) / 16) * ((w->inputs + kSpan - 1) / kSpan);
+    const int64_t spans = (w->inputs + kSpan - 1) / kSpan, units = (rows + 15) / 16 * ((w->outputs + 15) / 16) * spans;
     if (rows <= 16 && w->outputs >= 8192 && w->group >= 64) return kFewWide;
-    if (units <= 8192) return kFew;
-    return rows <= 64 || units <= (dtype == ACTQ_F32 ? 32768 : 65536) ? kLowTiles : kHighTiles;
+    if (spans <= 32 && units <= (w->group == 32 ? 4096 : 8192)) return kFew;
+    return rows <= 64 || units <= (dtype == ACTQ_F32 ? 32768 : 131072) ? kLowTiles : kHighTiles;
 }
 
 // Whether rows of x can be taken as they lie.

@@ -20,7 +20,7 @@ CASES = [
     # many outputs for few rows; tiles of 32 rows, one part and several; tiles of 128 rows, likewise
     (1, 300, 8200, 64, BF16), (16, 1111, 8193, 128, F16), (7, 129, 9000, 128, F32), (40, 4100, 4000, 64, F16), (33, 8192, 1024, 128, BF16), (70, 3000, 5003, 32, BF16),
     (64, 1025, 3001, 32, F32), (500, 120, 5000, 64, F16), (130, 4100, 4203, 128, BF16), (100, 2500, 4500, 32, F32), (5000, 100, 4001, 32, BF16), (1100, 4224, 300, 64, F16),
-    (300, 8200, 1000, 64, F32),
+    (300, 8200, 1000, 64, F32), (9000, 100, 4001, 32, BF16), (130, 4100, 8203, 128, BF16), (9, 4200, 500, 64, F16),
     # gradients from weights in memory
     (1100, 4224, 2100, 128, BF16), (1031, 4100, 2099, 64, F16), (701, 3001, 2100, 32, F32),
 ]
