@@ -835,11 +835,13 @@ constexpr int kWeightNumbers = std::is_same<T, __bf16>::value ? 1 : 2;
 
 constexpr int kDeepest = 64;   // outputs are padded to a multiple
 
-// The power of two that takes a number of this magnitude into [2^13, 2^14).
+// The power of two that takes a number of this magnitude into [2^13, 2^14).  Zero counts as
+// the smallest: an output without weights, whose element of grad_y adds nothing, must not
+// be its row's largest.
 __device__ __forceinline__ float scale_of(uint32_t largest)
 {
     const int exponent = static_cast<int>(largest >> 23) - 127;
-    const int power = largest == 0 || largest >= 0x7f800000u ? 0 : max(min(13 - exponent, 100), -100);
+    const int power = largest >= 0x7f800000u ? 0 : max(min(13 - exponent, 100), -100);
     return __builtin_bit_cast(float, static_cast<uint32_t>(power + 127) << 23);
 }
 

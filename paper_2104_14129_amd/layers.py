@@ -585,7 +585,7 @@ class QBlockNorm(nn.Module):
 
 class Linear4(nn.Module):
     """A linear layer with frozen weights of 4 bits (binding.quantize_weights, linear4).  Gradients flow to its input and its bias; nothing of the
-    input is kept for them.  forward-mode tangents and second derivatives are refused."""
+    input is kept for them.  Forward-mode tangents and second derivatives are refused."""
 
     def __init__(self, codes, header, inputs: int, bias=None):
         super().__init__()

@@ -77,6 +77,26 @@ def test_gradient(case):
     assert torch.equal(got, B.linear4_backward(grad.to(DEV), codes.to(DEV), header.to(DEV), inputs)), "the order of the sums is fixed"
 
 
+@pytest.mark.parametrize("rows, inputs, outputs", [(20, 640, 400), (1100, 4224, 2100)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_gradients_past_outputs_without_weights_and_of_very_different_ones(rows, inputs, outputs, dtype):
+    """Outputs whose weights are all zero take no part, however large grad_y is there; others'
+    weights differ by 2^12 and grad_y makes up for it.  Errors as above."""
+    codes, header = Y.random_weights(outputs, inputs, 128, 3)
+    header[::3] = 0
+    grad = _rows(rows, outputs, dtype, 4)
+    grad[:, ::3] *= 2.0 ** 20
+    header[1::3] *= 2.0 ** 12
+    grad[:, 1::3] *= 2.0 ** -12
+    got = B.linear4_backward(grad.to(DEV), codes.to(DEV), header.to(DEV), inputs)
+    w, _ = Y.weights(codes, header, inputs)
+    want, e = grad.double() @ w, ((grad.double() ** 2) @ (w ** 2)) ** 0.5
+    limit = H.ROUNDOFF[dtype] * want.abs() + (8 * {F32: 2.0 ** -21, BF16: 2.0 ** -11}[dtype] + 32 * Y.UNIT * (3 * outputs) ** 0.5) * e
+    off = (got.cpu().double() - want).abs()
+    assert (off <= limit).all(), float((off / limit).max())
+    assert float((got.cpu().double() - want).norm() / want.norm()) <= (2.0 ** -21 if dtype == F32 else 1.1 * H.ROUNDOFF[dtype] / 3 ** 0.5)
+
+
 @pytest.mark.parametrize("rows", [1, 40, 300])
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
 def test_errors_as_a_whole(rows, dtype):
