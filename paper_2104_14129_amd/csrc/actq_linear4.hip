@@ -4,10 +4,11 @@
 //   W[n, k] = zero[n, g] + step[n, g] code[n, k],  g = k div group
 //
 // A word holds eight codes of neighbouring k, pair i of them in bits 4 i and 16 + 4 i, so that a shift and a mask leave a pair in the halves of a register.
-// Under the bits of 128 that is a pair of bfloat16 numbers 128 + code, under zeros one of subnormal binary16 numbers code 2^-24: the matrix
+// Under the bits of 2^-8 that is a pair of bfloat16 numbers 2^-8 (1 + code / 128), under zeros one of subnormal binary16 numbers code 2^-24: the matrix
 // instructions multiply both exactly.  So a group's sum of x code is a sum of exact products in binary32, to which step, and zero times the group's sum of
-// x (one more product, with ones), come afterwards.  A binary32 x goes as the three bfloat16 numbers that make it up, and its codes as converted numbers:
-// sums of 128 x would cost it 4 of its 24 bits.
+// x (one more product, with a constant), come afterwards.  A binary32 x goes as the three bfloat16 numbers that make it up, and its codes as converted numbers
+// code / 2048: sums of 128 x beside those of x code would cost it 4 of its 24 bits.  All of these are so small that no group's sum is larger than its largest x, and none of
+// finite x overflows; the total is kept in their unit until the end.
 //
 // Measured on one MI355X, whose copy of 1 GiB reaches 5.1 TB/s and whose library product of 8192^3 1.21 PFLOP/s in bfloat16: one row of 4096 x 4096 in groups of 128
 // 4.9 us, 23 rows of 8192 x 16384 in binary16 and groups of 64 26 us (3.0 TB/s), 4096 rows of 8192 x 8192 in bfloat16 541 us (1.02 PFLOP/s), the gradient of 2047 rows of
@@ -26,26 +27,27 @@ __device__ __forceinline__ f32x4 multiply(f16x8 a, f16x8 b, f32x4 c) { return __
 __device__ __forceinline__ f32x16 multiply(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 multiply(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 
-// How a type of x meets the codes: a product is x (code kUnit + kShift).
+// How a type of x meets the codes.  With sums of x times what stands for its code and of x times the plain number (kPlain as a pair of bits, kSum),
+// zero x + step x code = kBack (step sum + (kZero zero - kShift step) plain).
 template <typename T>
 struct Meets;
 template <>
 struct Meets<__bf16> {
     typedef bf16x8 vector;
-    static constexpr uint32_t kUnder = 0x43004300u, kOnes = 0x3f803f80u;
-    static constexpr float kUnit = 1.0f, kShift = 128.0f;
+    static constexpr uint32_t kUnder = 0x3b803b80u, kPlain = 0x3b803b80u;   // 2^-8
+    static constexpr float kSum = 0x1p-8f, kZero = 0x1p-7f, kShift = 1.0f, kBack = 0x1p15f;
 };
 template <>
 struct Meets<_Float16> {
     typedef f16x8 vector;
-    static constexpr uint32_t kUnder = 0u, kOnes = 0x3c003c00u;
-    static constexpr float kUnit = 0x1p-24f, kShift = 0.0f;
+    static constexpr uint32_t kUnder = 0u, kPlain = 0x04000400u;   // 2^-14, the smallest with all its bits: sums of products with smaller ones are less exact
+    static constexpr float kSum = 0x1p-14f, kZero = 0x1p-10f, kShift = 0.0f, kBack = 0x1p24f;
 };
 template <>
 struct Meets<float> {
     typedef bf16x8 vector;
-    static constexpr uint32_t kOnes = 0x3f803f80u;
-    static constexpr float kUnit = 1.0f, kShift = 0.0f;
+    static constexpr uint32_t kPlain = 0x3a003a00u;   // 2^-11, and so are the codes
+    static constexpr float kSum = 0x1p-11f, kZero = 1.0f, kShift = 0.0f, kBack = 0x1p11f;
 };
 
 template <typename T>
@@ -65,7 +67,7 @@ __device__ __forceinline__ typename Meets<T>::vector codes_of(uint32_t w)
         const uint32_t half[2] = {w & 0x0f0f0f0fu, w >> 4 & 0x0f0f0f0fu};   // bytes of the codes 0, 4, 1, 5 and 2, 6, 3, 7
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float low = static_cast<float>(half[i % 2] >> 8 * (i / 2) & 255u), high = static_cast<float>(half[i % 2] >> 8 * (i / 2 + 2) & 255u);
+            const float low = Meets<T>::kSum * static_cast<float>(half[i % 2] >> 8 * (i / 2) & 255u), high = Meets<T>::kSum * static_cast<float>(half[i % 2] >> 8 * (i / 2 + 2) & 255u);
             v[i] = __builtin_bit_cast(uint32_t, low) >> 16 | __builtin_bit_cast(uint32_t, high);   // whole numbers up to 15 end in zeros
         }
     }
@@ -114,6 +116,13 @@ __device__ __forceinline__ void split(float v, uint32_t (&bits)[N])   // bfloat1
 
 __device__ __forceinline__ float zero_of(uint32_t header) { return __builtin_bit_cast(float, header << 16); }
 __device__ __forceinline__ float step_of(uint32_t header) { return __builtin_bit_cast(float, header & 0xffff0000u); }
+
+// What a group's plain sum is multiplied by.
+template <typename T>
+__device__ __forceinline__ float plain_factor(uint32_t header)
+{
+    return fmaf(-Meets<T>::kShift, step_of(header), Meets<T>::kZero * zero_of(header));
+}
 
 struct Weights4 {
     const uint32_t* codes;    // [outputs, groups * group / 8]
@@ -193,7 +202,7 @@ __global__ __launch_bounds__(64 * WAVES) void linear4_few_kernel(FewArgs<T> a)
         header[c] = a.w.header + n * a.w.groups;
     }
     const T* const x = a.x + min(first_row + at, a.rows - 1) * a.x_stride;
-    const V ones = __builtin_bit_cast(V, u32x4{Meets<T>::kOnes, Meets<T>::kOnes, Meets<T>::kOnes, Meets<T>::kOnes});
+    const V plainly = __builtin_bit_cast(V, u32x4{Meets<T>::kPlain, Meets<T>::kPlain, Meets<T>::kPlain, Meets<T>::kPlain});
     f32x4 total[COLUMNS] = {};
 
     // what a span needs; that of the wavefront's next one is on its way while this one is worked on
@@ -251,7 +260,7 @@ __global__ __launch_bounds__(64 * WAVES) void linear4_few_kernel(FewArgs<T> a)
                 pieces_of<T>(now.x[g * kWords + j], p);
 #pragma unroll
                 for (int i = kPieces<T> - 1; i >= 0; --i) {
-                    plain = multiply(p[i], ones, plain);
+                    plain = multiply(p[i], plainly, plain);
 #pragma unroll
                     for (int c = 0; c < COLUMNS; ++c) sum[c] = multiply(p[i], code[c], sum[c]);
                 }
@@ -259,9 +268,9 @@ __global__ __launch_bounds__(64 * WAVES) void linear4_few_kernel(FewArgs<T> a)
 #pragma unroll
             for (int c = 0; c < COLUMNS; ++c) {
                 const uint32_t head = now.head[c][g];
-                const float step = step_of(head), zero = fmaf(-Meets<T>::kShift, step, zero_of(head)), scaled = step * (1.0f / Meets<T>::kUnit);
+                const float step = step_of(head), factor = plain_factor<T>(head);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) total[c][i] = fmaf(zero, plain[i], fmaf(scaled, sum[c][i], total[c][i]));
+                for (int i = 0; i < 4; ++i) total[c][i] = fmaf(factor, plain[i], fmaf(step, sum[c][i], total[c][i]));
             }
         }
         now = next;
@@ -279,15 +288,14 @@ __global__ __launch_bounds__(64 * WAVES) void linear4_few_kernel(FewArgs<T> a)
         float sum = joined[0][tile][place];
 #pragma unroll
         for (int w = 1; w < WAVES; ++w) sum += joined[w][tile][place];
-        sum += bias_of<T>(a.bias, a.wide_bias, n);
-        a.y[m * a.y_stride + n] = static_cast<T>(sum);
+        a.y[m * a.y_stride + n] = static_cast<T>(fmaf(sum, Meets<T>::kBack, bias_of<T>(a.bias, a.wide_bias, n)));
     }
 }
 
 // ----------------------------------------------------------------------------- many rows
 
 // What x looks like for the kernel below: 16-bit numbers, whole spans of k, zeros beyond the last input.  16-bit rows that are like that already are taken
-// as they lie; others are copied (binary32: split into the bfloat16 numbers that make it up).  Beside it the sums of every group of a row, as
+// as they lie; others are copied (binary32: split into the bfloat16 numbers that make it up).  Beside it the plain sums of every group of a row, as
 // three bfloat16 numbers each.
 template <typename T>
 struct PrepareArgs {
@@ -317,7 +325,7 @@ __global__ __launch_bounds__(256) void linear4_prepare_kernel(PrepareArgs<T> a)
     }
     float sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum += static_cast<float>(e.v[i]);
+    for (int i = 0; i < 8; ++i) sum = fmaf(static_cast<float>(e.v[i]), Meets<T>::kSum, sum);
 #pragma unroll
     for (int step = 1; step < GROUP / 8; step *= 2) sum += __shfl_xor(sum, step);
     if (!there) return;
@@ -367,7 +375,7 @@ __device__ __forceinline__ void arrived()
 // A workgroup's tile is ROWS rows x 256 outputs, made of blocks of 32 x 32: 128 rows, two by two blocks a wavefront, or 32, one.  A group's sums of products
 // and the total are both what ordinary instructions work with, so they share the 256 registers that these see, and 128 rows take two wavefronts a SIMD.  x, codes and headers
 // go from memory to the LDS without registers, two stages of 128 k ahead (binary32, three times the bytes: one of 64 with 128 rows; four stages ahead under 32 rows give nothing); a wavefront turns the codes of its outputs
-// into numbers in registers.  Under 32 rows, where memory is what counts, the groups' sums of x are one more product, with ones.
+// into numbers in registers.  Under 32 rows, where memory is what counts, the groups' plain sums of x are one more product.
 template <typename T, int GROUP, int ROWS>
 __global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
 {
@@ -432,7 +440,7 @@ __global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
     for (int i = 0; i < kRing - 1; ++i)
         if (begin + i * kDepth < end) load(begin + i * kDepth, i);
 
-    // zero times the groups' sums of x, and what the codes' shift leaves: products of the parts of both.  A lane takes four neighbouring groups at a time.
+    // the factors' two terms times the groups' plain sums: products of the parts of both.  A lane takes four neighbouring groups at a time.
     const int columns = kB == 2 ? wave % 4 * 64 : wave * 32, rows = kB == 2 ? wave / 4 * 64 : 0;   // the wavefront's place in the tile
     f32x16 total[kB][kB] = {};
     if constexpr (kB == 2) {
@@ -470,7 +478,7 @@ __global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
                     const uint32_t there = mine + q + j < groups ? ~0u : 0u;   // no NaN times zero
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
-                        const uint32_t head = h[r][q + j], zero = head & 0xffffu;
+                        const uint32_t head = h[r][q + j], zero = __builtin_bit_cast(uint32_t, Meets<T>::kZero * zero_of(head)) >> 16;
                         s[r][2 * j] = v[r][q + j][0] & there;
                         s[r][2 * j + 1] = v[r][q + j][1] & there;
                         z[r][2 * j] = zero | zero << 16;
@@ -496,7 +504,7 @@ __global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
         arrived<(kRing - 2) * kLoads>();
     else
         arrived<0>();
-    const V ones = __builtin_bit_cast(V, u32x4{Meets<T>::kOnes, Meets<T>::kOnes, Meets<T>::kOnes, Meets<T>::kOnes});
+    const V plainly = __builtin_bit_cast(V, u32x4{Meets<T>::kPlain, Meets<T>::kPlain, Meets<T>::kPlain, Meets<T>::kPlain});
     int buffer = 0;
     for (int k = begin; k < end; k += kDepth) {
         const int ahead = k + (kRing - 1) * kDepth;
@@ -538,7 +546,7 @@ __global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
                         const V v = __builtin_bit_cast(V, tile[p * kTilePlace + place(rows + 32 * r + at, chunk)]);
                         if constexpr (kB == 1) {
                             if (step == 0 && p == kP - 1) plain = f32x16{};
-                            plain = multiply(v, ones, plain);
+                            plain = multiply(v, plainly, plain);
                         }
 #pragma unroll
                         for (int c = 0; c < kB; ++c) {
@@ -549,13 +557,13 @@ __global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
             }
 #pragma unroll
             for (int c = 0; c < kB; ++c) {
-                const float step = step_of(head[c]), scaled = step * (1.0f / Meets<T>::kUnit), zero = fmaf(-Meets<T>::kShift, step, zero_of(head[c]));
+                const float step = step_of(head[c]), factor = plain_factor<T>(head[c]);
 #pragma unroll
                 for (int r = 0; r < kB; ++r)
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        total[r][c][i] = fmaf(scaled, sum[r][c][i], total[r][c][i]);
-                        if constexpr (kB == 1) total[r][c][i] = fmaf(zero, plain[i], total[r][c][i]);
+                        total[r][c][i] = fmaf(step, sum[r][c][i], total[r][c][i]);
+                        if constexpr (kB == 1) total[r][c][i] = fmaf(factor, plain[i], total[r][c][i]);
                     }
             }
         }
@@ -578,7 +586,7 @@ __global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int down = 32 * r + 8 * (i / 4) + i % 4;
-                    if (m + down < a.rows) to[down * static_cast<int64_t>(a.w.outputs)] = total[r][c][i];
+                    if (m + down < a.rows) to[down * static_cast<int64_t>(a.w.outputs)] = total[r][c][i] * Meets<T>::kBack;
                 }
             continue;
         }
@@ -589,7 +597,7 @@ __global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int down = 32 * r + 8 * (i / 4) + i % 4;
-                if (m + down < a.rows) to[down * a.y_stride] = static_cast<T>(total[r][c][i] + bias);
+                if (m + down < a.rows) to[down * a.y_stride] = static_cast<T>(fmaf(total[r][c][i], Meets<T>::kBack, bias));
             }
     }
 }

@@ -1,0 +1,47 @@
+"""Products with 4-bit weights at the ends of the range of their types: what is finite stays finite, in every kernel."""
+import pytest
+import torch
+
+import _layer as Y
+from paper_2104_14129_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+
+# rows, inputs, outputs, group: few rows, few rows of many outputs, tiles of 32 rows (several parts and one), tiles of 128 rows
+KERNELS = [(3, 300, 100, 32), (5, 300, 8200, 128), (40, 4100, 4000, 64), (64, 300, 5000, 128), (700, 2560, 5000, 64), (700, 2500, 5000, 128), (130, 4100, 8203, 32)]
+
+
+def _rows(rows, columns, dtype, seed):
+    return torch.randn((rows, columns), generator=torch.Generator().manual_seed(seed)).to(dtype).to(DEV)
+
+
+def _shape(case):
+    return pytest.param(*case, id="-".join(map(str, case)))
+
+
+@pytest.mark.parametrize("rows, inputs, outputs, group", map(_shape, KERNELS))
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("power", [124, -60])
+def test_a_power_of_two_in_x_is_one_in_the_result(rows, inputs, outputs, group, dtype, power):
+    """Every rounding commutes with it as long as nothing leaves the range.  x is below 2^3 times that power, weights below 2^-9, a result of 4100 of them (a sum of
+    either sign, 64 of its parts) below 2^120: finite in both types, while x times a code would not be."""
+    codes, header = (t.to(DEV) for t in Y.random_weights(outputs, inputs, group, 1))
+    header *= 2.0 ** -10
+    x = _rows(rows, inputs, dtype, 2)
+    y = B.linear4(x, codes, header)
+    scaled = B.linear4(x * 2.0 ** power, codes, header)
+    assert torch.isfinite(scaled).all() and (y != 0).any()
+    assert torch.equal(scaled, y * 2.0 ** power)
+
+
+@pytest.mark.parametrize("rows, inputs, outputs, group", map(_shape, KERNELS))
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_zeros_times_the_largest_weights(rows, inputs, outputs, group, dtype):
+    codes, header = (t.to(DEV) for t in Y.random_weights(outputs, inputs, group, 3))
+    header[..., 1] = header[..., 1].abs() * 2.0 ** 120
+    header[..., 0] = -header[..., 1]
+    assert torch.isfinite(header).all()
+    y = B.linear4(torch.zeros((rows, inputs), dtype=dtype, device=DEV), codes, header)
+    assert (y == 0).all()
