@@ -4,10 +4,10 @@
 //   W[n, k] = zero[n, g] + step[n, g] code[n, k],  g = k div group
 //
 // A word holds eight codes of neighbouring k, pair i of them in bits 4 i and 16 + 4 i, so that a shift and a mask leave a pair in the halves of a register.
-// Under the bits of 2^-8 that is a pair of bfloat16 numbers 2^-8 (1 + code / 128), under zeros one of subnormal binary16 numbers code 2^-24: the matrix
+// As the upper four bits of a fraction, under the exponent of 2^-8 (bfloat16) or 2^-14 (binary16), that is a pair of numbers 1 + code / 16 times that power: the matrix
 // instructions multiply both exactly.  So a group's sum of x code is a sum of exact products in binary32, to which step, and zero times the group's sum of
-// x (one more product, with a constant), come afterwards.  A binary32 x goes as the three bfloat16 numbers that make it up, and its codes as converted numbers
-// code / 2048: sums of 128 x beside those of x code would cost it 4 of its 24 bits.  All of these are so small that no group's sum is larger than its largest x, and none of
+// x (one more product, with a constant), come afterwards.  A binary32 x goes as the three bfloat16 numbers that make up x / 2048, and its codes as converted numbers:
+// sums of 16 x beside those of x code would cost it 2 of its 24 bits.  All of these are so small that no group's sum is larger than its largest x, and none of
 // finite x overflows; the total is kept in their unit until the end.
 //
 // Measured on one MI355X, whose copy of 1 GiB reaches 5.1 TB/s and whose library product of 8192^3 1.21 PFLOP/s in bfloat16: one row of 4096 x 4096 in groups of 128
@@ -27,27 +27,29 @@ __device__ __forceinline__ f32x4 multiply(f16x8 a, f16x8 b, f32x4 c) { return __
 __device__ __forceinline__ f32x16 multiply(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 multiply(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 
-// How a type of x meets the codes.  With sums of x times what stands for its code and of x times the plain number (kPlain as a pair of bits, kSum),
+// How a type of x meets the codes.  With sums of kScale x times what stands for its code, and of kScale x times a plain number (a pair of it: kPlain; kSum: both factors of x),
 // zero x + step x code = kBack (step sum + (kZero zero - kShift step) plain).
 template <typename T>
 struct Meets;
 template <>
 struct Meets<__bf16> {
     typedef bf16x8 vector;
-    static constexpr uint32_t kUnder = 0x3b803b80u, kPlain = 0x3b803b80u;   // 2^-8
-    static constexpr float kSum = 0x1p-8f, kZero = 0x1p-7f, kShift = 1.0f, kBack = 0x1p15f;
+    static constexpr uint32_t kPlain = 0x3b803b80u;   // 2^-8, and what lies under a code
+    static constexpr int kCodeBit = 3;
+    static constexpr float kScale = 1.0f, kSum = 0x1p-8f, kZero = 0x1p-4f, kShift = 1.0f, kBack = 0x1p12f;
 };
 template <>
 struct Meets<_Float16> {
     typedef f16x8 vector;
-    static constexpr uint32_t kUnder = 0u, kPlain = 0x04000400u;   // 2^-14, the smallest with all its bits: sums of products with smaller ones are less exact
-    static constexpr float kSum = 0x1p-14f, kZero = 0x1p-10f, kShift = 0.0f, kBack = 0x1p24f;
+    static constexpr uint32_t kPlain = 0x04000400u;   // 2^-14, the smallest with all its bits: sums of products with subnormal numbers are less exact
+    static constexpr int kCodeBit = 6;
+    static constexpr float kScale = 1.0f, kSum = 0x1p-14f, kZero = 0x1p-4f, kShift = 1.0f, kBack = 0x1p18f;
 };
 template <>
 struct Meets<float> {
     typedef bf16x8 vector;
-    static constexpr uint32_t kPlain = 0x3a003a00u;   // 2^-11, and so are the codes
-    static constexpr float kSum = 0x1p-11f, kZero = 1.0f, kShift = 0.0f, kBack = 0x1p11f;
+    static constexpr uint32_t kPlain = 0x3f803f80u;   // 1
+    static constexpr float kScale = 0x1p-11f, kSum = 0x1p-11f, kZero = 1.0f, kShift = 0.0f, kBack = 0x1p11f;
 };
 
 template <typename T>
@@ -59,22 +61,23 @@ __device__ __forceinline__ typename Meets<T>::vector codes_of(uint32_t w)
 {
     u32x4 v;
     if constexpr (sizeof(T) == 2) {
-        uint32_t under = Meets<T>::kUnder;
-        if (under) asm("" : "+v"(under));   // in a vector register: one instruction takes one constant from elsewhere, and so masks and sets at once
+        constexpr int kBit = Meets<T>::kCodeBit;
+        uint32_t under = Meets<T>::kPlain;
+        asm("" : "+v"(under));   // in a vector register: one instruction takes one constant from elsewhere, and so masks and sets at once
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = (w >> 4 * i & 0x000f000fu) | under;
+        for (int i = 0; i < 4; ++i) v[i] = ((4 * i < kBit ? w << (kBit - 4 * i) : w >> (4 * i - kBit)) & 0x000f000fu << kBit) | under;
     } else {
         const uint32_t half[2] = {w & 0x0f0f0f0fu, w >> 4 & 0x0f0f0f0fu};   // bytes of the codes 0, 4, 1, 5 and 2, 6, 3, 7
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float low = Meets<T>::kSum * static_cast<float>(half[i % 2] >> 8 * (i / 2) & 255u), high = Meets<T>::kSum * static_cast<float>(half[i % 2] >> 8 * (i / 2 + 2) & 255u);
+            const float low = static_cast<float>(half[i % 2] >> 8 * (i / 2) & 255u), high = static_cast<float>(half[i % 2] >> 8 * (i / 2 + 2) & 255u);
             v[i] = __builtin_bit_cast(uint32_t, low) >> 16 | __builtin_bit_cast(uint32_t, high);   // whole numbers up to 15 end in zeros
         }
     }
     return __builtin_bit_cast(typename Meets<T>::vector, v);
 }
 
-// Eight values of x as vectors for the matrix instructions.  Binary32: the upper 8 bits of a value's 24, of the rest, and what is left, each of them a
+// Eight values of kScale x as vectors for the matrix instructions.  Binary32: the upper 8 bits of a value's 24, of the rest, and what is left, each of them a
 // bfloat16 number.
 template <typename T>
 __device__ __forceinline__ void pieces_of(const Eight<T>& e, typename Meets<T>::vector (&v)[kPieces<T>])
@@ -88,7 +91,7 @@ __device__ __forceinline__ void pieces_of(const Eight<T>& e, typename Meets<T>::
             uint32_t bits[3][2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const float x = e.v[2 * i + j];
+                const float x = Meets<T>::kScale * e.v[2 * i + j];
                 bits[0][j] = __builtin_bit_cast(uint32_t, x) & 0xffff0000u;
                 const float rest = x - __builtin_bit_cast(float, bits[0][j]);
                 bits[1][j] = __builtin_bit_cast(uint32_t, rest) & 0xffff0000u;
