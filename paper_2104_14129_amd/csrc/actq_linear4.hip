@@ -27,7 +27,7 @@ __device__ __forceinline__ f32x4 multiply(f16x8 a, f16x8 b, f32x4 c) { return __
 __device__ __forceinline__ f32x16 multiply(f16x8 a, f16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x16 multiply(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 
-// How a type of x meets the codes.  With sums of kScale x times what stands for its code, and of kScale x times a plain number (a pair of it: kPlain; kSum: both factors of x),
+// How a type of x meets the codes.  With sums of x (binary32: kSum x) times what stands for its code, and times a plain number (a pair of it: kPlain), which are sums of kSum x,
 // zero x + step x code = kBack (step sum + (kZero zero - kShift step) plain).
 template <typename T>
 struct Meets;
@@ -36,20 +36,20 @@ struct Meets<__bf16> {
     typedef bf16x8 vector;
     static constexpr uint32_t kPlain = 0x3b803b80u;   // 2^-8, and what lies under a code
     static constexpr int kCodeBit = 3;
-    static constexpr float kScale = 1.0f, kSum = 0x1p-8f, kZero = 0x1p-4f, kShift = 1.0f, kBack = 0x1p12f;
+    static constexpr float kSum = 0x1p-8f, kZero = 0x1p-4f, kShift = 1.0f, kBack = 0x1p12f;
 };
 template <>
 struct Meets<_Float16> {
     typedef f16x8 vector;
     static constexpr uint32_t kPlain = 0x04000400u;   // 2^-14, the smallest with all its bits: sums of products with subnormal numbers are less exact
     static constexpr int kCodeBit = 6;
-    static constexpr float kScale = 1.0f, kSum = 0x1p-14f, kZero = 0x1p-4f, kShift = 1.0f, kBack = 0x1p18f;
+    static constexpr float kSum = 0x1p-14f, kZero = 0x1p-4f, kShift = 1.0f, kBack = 0x1p18f;
 };
 template <>
 struct Meets<float> {
     typedef bf16x8 vector;
     static constexpr uint32_t kPlain = 0x3f803f80u;   // 1
-    static constexpr float kScale = 0x1p-11f, kSum = 0x1p-11f, kZero = 1.0f, kShift = 0.0f, kBack = 0x1p11f;
+    static constexpr float kSum = 0x1p-11f, kZero = 1.0f, kShift = 0.0f, kBack = 0x1p11f;
 };
 
 template <typename T>
@@ -77,7 +77,7 @@ __device__ __forceinline__ typename Meets<T>::vector codes_of(uint32_t w)
     return __builtin_bit_cast(typename Meets<T>::vector, v);
 }
 
-// Eight values of kScale x as vectors for the matrix instructions.  Binary32: the upper 8 bits of a value's 24, of the rest, and what is left, each of them a
+// Eight values of x as vectors for the matrix instructions.  Binary32, times kSum: the upper 8 bits of a value's 24, of the rest, and what is left, each of them a
 // bfloat16 number.
 template <typename T>
 __device__ __forceinline__ void pieces_of(const Eight<T>& e, typename Meets<T>::vector (&v)[kPieces<T>])
@@ -91,7 +91,7 @@ __device__ __forceinline__ void pieces_of(const Eight<T>& e, typename Meets<T>::
             uint32_t bits[3][2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const float x = Meets<T>::kScale * e.v[2 * i + j];
+                const float x = Meets<T>::kSum * e.v[2 * i + j];
                 bits[0][j] = __builtin_bit_cast(uint32_t, x) & 0xffff0000u;
                 const float rest = x - __builtin_bit_cast(float, bits[0][j]);
                 bits[1][j] = __builtin_bit_cast(uint32_t, rest) & 0xffff0000u;
