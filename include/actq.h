@@ -650,11 +650,10 @@ int actq_linear4(const actq_weights4* w, const actq_rows* x, actq_dtype dt, int6
 
 /*
  * grad_x = grad_y W.  Sums are binary32 in a fixed order, a result is rounded once.  Where there are
- * many rows, a weight (zero + step * code) is multiplied as one number of 11 bits for ACTQ_BF16, as two of
- * them (22 bits) for ACTQ_F16 and ACTQ_F32, an element of grad_y as it is, or as 22 bits for
- * ACTQ_F32; else a weight as 16 bits or, for ACTQ_F32, as it is.  That is off by 2^-11, 2^-16 and
- * 2^-21 of a product at most, and where there are many rows by 2^-37 of its row's largest product
- * (a weight taken for its output's largest).
+ * many rows, a weight is multiplied as step * (code - 8), which is exact, and zero + 8 * step, as 22 bits, an
+ * element of grad_y as it is, or as 22 bits for ACTQ_F32; else a weight as 16 bits or, for ACTQ_F32, as it is.  That
+ * is off by 2^-22 (ACTQ_F32 2^-21) and 2^-16 (2^-24) of a product at most, and where there are many rows by 2^-37 of its row's
+ * largest product (a weight taken for its output's largest).
  *
  * grad_y [rows, outputs], grad_x [rows, inputs] of type dt, which may not overlap; workspace as above
  */

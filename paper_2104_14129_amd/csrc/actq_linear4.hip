@@ -837,12 +837,12 @@ __global__ __launch_bounds__(kGradThreads) void linear4_backward_kernel(GradArgs
 
 // Many rows: the weights are turned into numbers once, transposed, in memory, and the product is one of two matrices whose rows are contiguous along the outputs.
 // Both are binary16, scaled by powers of two so that it has the range: a weight by that of its output's largest one, which the elements of grad_y there make up for;
-// a row of grad_y by that of its largest element, for which the row of the result makes up.  bfloat16: a number for each, 11 bits, beside which the result's rounding to 8
-// counts; binary16: two for a weight (22 bits); binary32: two for both, without the product of the second ones.
+// a row of grad_y by that of its largest element, for which the row of the result makes up.  A weight is step (code - 8), which has the 11 bits of one number (8 of a step, 3 of
+// up to 8), and its group's zero + 8 step, of which there is one for `group` columns: two numbers (22 bits), and a product of their own.  An element of grad_y is one number, of
+// binary32 two, without the product of the second ones.
 template <typename T>
 constexpr int kGradNumbers = sizeof(T) == 4 ? 2 : 1;
-template <typename T>
-constexpr int kWeightNumbers = std::is_same<T, __bf16>::value ? 1 : 2;
+constexpr int kMiddleNumbers = 2;
 
 constexpr int kDeepest = 64;   // outputs are padded to a multiple
 
@@ -874,45 +874,51 @@ __global__ __launch_bounds__(256) void weights4_scale_kernel(Weights4 w, float* 
     if (threadIdx.x % 64 == 0) inverse[n] = 1.0f / scale_of(largest);
 }
 
-// 64 outputs x 128 inputs a workgroup; out [numbers][inputs][padded outputs].
-template <int GROUP, int NUMBERS>
-__global__ __launch_bounds__(256) void weights4_transpose_kernel(Weights4 w, const float* inverse, int32_t padded, uint16_t* out)
+// 64 outputs x 128 inputs a workgroup; out [inputs][padded outputs], middles [groups][numbers][padded outputs].
+template <int GROUP>
+__global__ __launch_bounds__(256) void weights4_transpose_kernel(Weights4 w, const float* inverse, int32_t padded, uint16_t* out, uint16_t* middles)
 {
+    typedef _Float16 four __attribute__((ext_vector_type(4)));
     __shared__ u32x2 turned[128 * 17];
-    const int row_words = w.groups * (GROUP / 8), column = threadIdx.x % 16, quad = threadIdx.x / 16;
-    const int word = min(static_cast<int>(blockIdx.x) * 16 + column, row_words - 1);
-    float v[4][8];
+    const int row_words = w.groups * (GROUP / 8), column = threadIdx.x % 16, quad = threadIdx.x / 16, wanted = blockIdx.x * 16 + column;
+    const int word = min(wanted, row_words - 1), group = word / (GROUP / 8);
+    float v[4][8], middle[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int n = blockIdx.y * 64 + 4 * quad + j;
         const bool there = n < w.outputs;
         const int64_t row = there ? n : 0;
-        const uint32_t codes = w.codes[row * row_words + word], h = there ? w.header[row * w.groups + word / (GROUP / 8)] : 0u;
-        const float scale = 1.0f / inverse[row];
+        const uint32_t codes = w.codes[row * row_words + word], h = there ? w.header[row * w.groups + group] : 0u;
+        const float scale = 1.0f / inverse[row], step = step_of(h) * scale;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[j][i] = fmaf(static_cast<float>(codes >> (4 * (i / 2) + 16 * (i % 2)) & 15u), step_of(h), zero_of(h)) * scale;
+        for (int i = 0; i < 8; ++i) v[j][i] = (static_cast<float>(codes >> (4 * (i / 2) + 16 * (i % 2)) & 15u) - 8.0f) * step;
+        middle[j] = fmaf(8.0f, step_of(h), zero_of(h)) * scale;
     }
+    if (wanted < row_words && column % (GROUP / 8) == 0) {
 #pragma unroll
-    for (int number = 0; number < NUMBERS; ++number) {
-        if (number > 0) __syncthreads();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            typedef _Float16 four __attribute__((ext_vector_type(4)));
+        for (int number = 0; number < kMiddleNumbers; ++number) {
             four f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                f[j] = static_cast<_Float16>(v[j][i]);
-                v[j][i] -= static_cast<float>(f[j]);
+                f[j] = static_cast<_Float16>(middle[j]);
+                middle[j] -= static_cast<float>(f[j]);
             }
-            turned[(8 * column + i) * 17 + quad] = __builtin_bit_cast(u32x2, f);
+            *reinterpret_cast<four*>(middles + (static_cast<int64_t>(group) * kMiddleNumbers + number) * padded + blockIdx.y * 64 + 4 * quad) = f;
         }
-        __syncthreads();
+    }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = i * 32 + threadIdx.x / 8, pair = threadIdx.x % 8 * 2, k = blockIdx.x * 128 + row;
-            const u32x2 a = turned[row * 17 + pair], b = turned[row * 17 + pair + 1];
-            if (k < w.inputs) *reinterpret_cast<u32x4*>(out + (static_cast<int64_t>(number) * w.inputs + k) * padded + blockIdx.y * 64 + 4 * pair) = u32x4{a[0], a[1], b[0], b[1]};
-        }
+    for (int i = 0; i < 8; ++i) {
+        four f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) f[j] = static_cast<_Float16>(v[j][i]);
+        turned[(8 * column + i) * 17 + quad] = __builtin_bit_cast(u32x2, f);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = i * 32 + threadIdx.x / 8, pair = threadIdx.x % 8 * 2, k = blockIdx.x * 128 + row;
+        const u32x2 a = turned[row * 17 + pair], b = turned[row * 17 + pair + 1];
+        if (k < w.inputs) *reinterpret_cast<u32x4*>(out + static_cast<int64_t>(k) * padded + blockIdx.y * 64 + 4 * pair) = u32x4{a[0], a[1], b[0], b[1]};
     }
 }
 
@@ -971,24 +977,26 @@ __global__ __launch_bounds__(256) void linear4_scale_rows_kernel(const T* grad, 
 template <typename T>
 struct TilesArgs {
     const uint16_t* grad;     // [numbers][rows][padded]
-    const uint16_t* weights;  // [numbers][inputs][padded]
+    const uint16_t* weights;  // [inputs][padded]; of the middles [groups][numbers][padded], all of which are inputs here
     const float* back;
-    int64_t rows;
+    const float* middles;     // [groups][padded_rows], what comes to a row's sums in a group
+    int32_t group_shift;
+    int64_t rows, padded_rows;   // whole tiles
     int32_t inputs, padded;
     int32_t row_tiles, column_tiles;
     T* out;
     int64_t out_stride;
     int32_t share;            // outputs of a part
-    float* parts;             // [parts][rows][inputs]; null: the only part writes out
+    float* parts;             // [parts][rows][inputs]; null: the only part writes out.  Of the middles [parts][groups][padded_rows], and nothing else
 };
 
-// A workgroup's tile is 256 rows x 128 inputs, a wavefront's 128 x 64, and both matrices go from memory to the LDS without registers, two stages ahead
-// (binary16, with half as many bytes again: one).  What bounds it: the matrix instructions, beside which the LDS is read three quarters of the time.
-template <typename T>
+// A workgroup's tile is 256 rows x 128 inputs, a wavefront's 128 x 64, and both matrices go from memory to the LDS without registers, two stages ahead.
+// What bounds it: the matrix instructions, beside which the LDS is read three quarters of the time.
+template <typename T, int GRADS, bool MIDDLES>
 __global__ __launch_bounds__(256, 1) void linear4_backward_tiles_kernel(TilesArgs<T> a)
 {
-    constexpr int kG = kGradNumbers<T>, kW = kWeightNumbers<T>, kDepth = kG == 1 ? 64 : 32, kRing = kG == kW ? 3 : 2, kRows = 256, kColumns = 128;
-    constexpr int kChunks = kDepth / 8, kGrads = kRows * kChunks, kWeights = kColumns * kChunks, kStage = kG * kGrads + kW * kWeights, kLoads = kStage / 256;
+    constexpr int kG = GRADS, kDepth = kG == 1 ? 64 : 32, kRing = 3, kRows = 256, kColumns = 128;
+    constexpr int kChunks = kDepth / 8, kGrads = kRows * kChunks, kWeights = kColumns * kChunks, kStage = kG * kGrads + kWeights, kLoads = kStage / 256;
     __shared__ u32x4 lds[kRing * kStage];   // one array, as above
     const int lane = threadIdx.x % 64, at = lane % 32, half = lane / 32;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), rows = wave / 2 * 128, columns = wave % 2 * 64;
@@ -1013,9 +1021,9 @@ __global__ __launch_bounds__(256, 1) void linear4_backward_tiles_kernel(TilesArg
     };
     const int begin = blockIdx.y * a.share, end = min(begin + a.share, a.padded);
     load(begin, 0);
-    if (kRing > 2 && begin + kDepth < end) load(begin + kDepth, 1);
+    if (begin + kDepth < end) load(begin + kDepth, 1);
     f32x16 sum[4][2] = {};
-    if (kRing > 2 && begin + kDepth < end)
+    if (begin + kDepth < end)
         arrived<kLoads>();
     else
         arrived<0>();
@@ -1026,7 +1034,7 @@ __global__ __launch_bounds__(256, 1) void linear4_backward_tiles_kernel(TilesArg
         const u32x4* const stage = lds + buffer * kStage;
 #pragma unroll
         for (int step = 0; step < kDepth / 16; ++step) {
-            f16x8 g[4][kG], w[2][kW];
+            f16x8 g[4][kG], w[2];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int row = rows + 32 * i + at;
@@ -1036,18 +1044,14 @@ __global__ __launch_bounds__(256, 1) void linear4_backward_tiles_kernel(TilesArg
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int row = columns + 32 * j + at;
-#pragma unroll
-                for (int p = 0; p < kW; ++p) w[j][p] = __builtin_bit_cast(f16x8, stage[kG * kGrads + p * kWeights + row * kChunks + ((2 * step + half) ^ swizzle(row))]);
+                w[j] = __builtin_bit_cast(f16x8, stage[kG * kGrads + row * kChunks + ((2 * step + half) ^ swizzle(row))]);
             }
 #pragma unroll
             for (int p = kG - 1; p >= 0; --p)
 #pragma unroll
-                for (int q = kW - 1; q >= 0; --q)
-                    if (p + q < 2)
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-#pragma unroll
-                            for (int j = 0; j < 2; ++j) sum[i][j] = multiply(g[i][p], w[j][q], sum[i][j]);
+                    for (int j = 0; j < 2; ++j) sum[i][j] = multiply(g[i][p], w[j], sum[i][j]);
         }
         if (ahead < end)
             arrived<(kRing - 2) * kLoads>();
@@ -1055,23 +1059,50 @@ __global__ __launch_bounds__(256, 1) void linear4_backward_tiles_kernel(TilesArg
             arrived<0>();
         buffer = buffer == kRing - 1 ? 0 : buffer + 1;
     }
+    // four neighbouring rows a lane and register quad; what goes with them is loaded for 32 rows at a time (one by one: 22 us more)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 4; ++i) {
+        const int64_t first = first_row + rows + 32 * i + 4 * half;
+        if constexpr (MIDDLES) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int64_t m = first_row + rows + 32 * i + 8 * (r / 4) + 4 * half + r % 4;
-            if (m >= a.rows) continue;
-            const float back = a.back[m];
+            for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int k = first_column + columns + 32 * j + at;
-                if (k >= a.inputs) continue;
-                if (a.parts)
-                    a.parts[(blockIdx.y * a.rows + m) * a.inputs + k] = sum[i][j][r] * back;
-                else
-                    a.out[m * a.out_stride + k] = static_cast<T>(sum[i][j][r] * back);
+                for (int j = 0; j < 2; ++j) {
+                    const int k = first_column + columns + 32 * j + at;
+                    f32x4 v;
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) v[r] = sum[i][j][4 * q + r] + dpp<kDppXor1>(sum[i][j][4 * q + r]);   // of both numbers
+                    if (k < a.inputs && k % kMiddleNumbers == 0)
+                        *reinterpret_cast<f32x4*>(a.parts + ((static_cast<int64_t>(blockIdx.y) * a.inputs + k) / kMiddleNumbers) * a.padded_rows + first + 8 * q) = v;
+                }
+        } else {
+            f32x4 back[4], middle[2][4] = {};
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                back[q] = *reinterpret_cast<const f32x4*>(a.back + first + 8 * q);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int64_t group = min(first_column + columns + 32 * j, a.inputs - 1) >> a.group_shift;
+                    if (blockIdx.y == 0) middle[j][q] = *reinterpret_cast<const f32x4*>(a.middles + group * a.padded_rows + first + 8 * q);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int64_t m = first + 8 * (r / 4) + r % 4;
+                if (m >= a.rows) continue;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int k = first_column + columns + 32 * j + at;
+                    if (k >= a.inputs) continue;
+                    const float v = (sum[i][j][r] + middle[j][r / 4][r % 4]) * back[r / 4][r % 4];
+                    if (a.parts)
+                        a.parts[(blockIdx.y * a.rows + m) * a.inputs + k] = v;
+                    else
+                        a.out[m * a.out_stride + k] = static_cast<T>(v);
+                }
             }
         }
+    }
 }
 
 // ----------------------------------------------------------------------------- the weights themselves
@@ -1193,8 +1224,17 @@ bool in_memory(const actq_weights4* w, int dtype, int64_t rows) { return rows * 
 struct GradPlan {
     bool tiles;               // of 256 rows, from numbers in memory
     int32_t row_tiles, column_tiles, padded, share, parts;
-    uint64_t inverse, back, grads, weights, sums;   // bytes of the workspace's pieces
+    int32_t middle_share, middle_parts;
+    uint64_t inverse, back, grads, weights, middles, middle_sums, sums;   // bytes of the workspace's pieces
 };
+
+// Outputs of a part (a multiple of kDeepest) and how many parts: as many as make `wanted` of the tiles, of `least` stages at least.
+void cut_outputs(int32_t padded, int64_t tiles, int64_t wanted, int64_t least, int32_t& share, int32_t& parts)
+{
+    const int64_t stages = padded / kDeepest, most = wanted / tiles < stages / least ? wanted / tiles : stages / least, each = most > 1 ? (stages + most - 1) / most : stages;
+    share = static_cast<int32_t>(each * kDeepest);
+    parts = static_cast<int32_t>((stages + each - 1) / each);
+}
 
 // Where the tiles are few, the outputs are cut into parts that make a workgroup for each compute unit (of the smaller tiles two), of four stages at least.
 GradPlan grad_plan(const actq_weights4* w, int dtype, int64_t rows)
@@ -1205,15 +1245,17 @@ GradPlan grad_plan(const actq_weights4* w, int dtype, int64_t rows)
     p.row_tiles = static_cast<int32_t>(p.tiles ? (rows + 255) / 256 : (rows + kGradRows - 1) / kGradRows);
     p.column_tiles = (w->inputs + kGradColumns - 1) / kGradColumns;
     p.padded = (w->outputs + kDeepest - 1) / kDeepest * kDeepest;
-    const int64_t stages = p.padded / kDeepest, wanted = (p.tiles ? 256 : 512) / (static_cast<int64_t>(p.row_tiles) * p.column_tiles);
-    const int64_t most = wanted < stages / 4 ? wanted : stages / 4, share = most > 1 ? (stages + most - 1) / most : stages;
-    p.share = static_cast<int32_t>(share * kDeepest);
-    p.parts = static_cast<int32_t>((stages + share - 1) / share);
+    cut_outputs(p.padded, static_cast<int64_t>(p.row_tiles) * p.column_tiles, p.tiles ? 256 : 512, 4, p.share, p.parts);
     if (p.tiles) {
+        const int32_t groups = (w->inputs + w->group - 1) / w->group;
+        cut_outputs(p.padded, static_cast<int64_t>(p.row_tiles) * ((kMiddleNumbers * groups + kGradColumns - 1) / kGradColumns), 256, 4, p.middle_share, p.middle_parts);
         p.inverse = (static_cast<uint64_t>(w->outputs) * sizeof(float) + 15) / 16 * 16;
-        p.back = (static_cast<uint64_t>(rows) * sizeof(float) + 15) / 16 * 16;
+        const uint64_t padded_rows = static_cast<uint64_t>(p.row_tiles) * 256;
+        p.back = padded_rows * sizeof(float);
         p.grads = static_cast<uint64_t>(rows) * p.padded * 2 * (dtype == ACTQ_F32 ? 2 : 1);
-        p.weights = static_cast<uint64_t>(w->inputs) * p.padded * 2 * (dtype == ACTQ_BF16 ? 1 : 2);
+        p.weights = static_cast<uint64_t>(w->inputs) * p.padded * 2;
+        p.middles = static_cast<uint64_t>(groups) * p.padded * 2 * kMiddleNumbers;
+        p.middle_sums = padded_rows * groups * sizeof(float) * (p.middle_parts > 1 ? p.middle_parts + 1 : 1);
     }
     p.sums = p.parts > 1 ? static_cast<uint64_t>(p.parts) * rows * w->inputs * sizeof(float) : 0;
     return p;
@@ -1222,7 +1264,7 @@ GradPlan grad_plan(const actq_weights4* w, int dtype, int64_t rows)
 uint64_t linear4_backward_workspace(const actq_weights4* w, int dtype, int64_t rows)
 {
     const GradPlan p = grad_plan(w, dtype, rows);
-    return p.inverse + p.back + p.grads + p.weights + p.sums;
+    return p.inverse + p.back + p.grads + p.weights + p.middles + p.middle_sums + p.sums;
 }
 
 template <typename T, int GROUP>
@@ -1233,27 +1275,45 @@ void launch_backward_tiles(const actq_weights4* w, const actq_rows* grad_y, int6
     float* const back = reinterpret_cast<float*>(at + p.inverse);
     uint16_t* const grads = reinterpret_cast<uint16_t*>(at + p.inverse + p.back);
     uint16_t* const weights = reinterpret_cast<uint16_t*>(at + p.inverse + p.back + p.grads);
+    uint16_t* const middles = reinterpret_cast<uint16_t*>(at + p.inverse + p.back + p.grads + p.weights);
+    float* const middle_sums = reinterpret_cast<float*>(at + p.inverse + p.back + p.grads + p.weights + p.middles);
     const Weights4 v = weights_of(w);
     launch(weights4_scale_kernel, static_cast<unsigned>((w->outputs + 3) / 4), 256, stream, v, inverse);
-    launch(weights4_transpose_kernel<GROUP, kWeightNumbers<T>>, dim3(static_cast<unsigned>((w->inputs + 127) / 128), static_cast<unsigned>(p.padded / 64)), 256, stream, v,
-           static_cast<const float*>(inverse), p.padded, weights);
+    launch(weights4_transpose_kernel<GROUP>, dim3(static_cast<unsigned>((w->inputs + 127) / 128), static_cast<unsigned>(p.padded / 64)), 256, stream, v,
+           static_cast<const float*>(inverse), p.padded, weights, middles);
     launch(linear4_scale_rows_kernel<T>, static_cast<unsigned>(rows), 256, stream, static_cast<const T*>(grad_y->data), grad_y->stride, rows, w->outputs, p.padded,
            static_cast<const float*>(inverse), grads, back);
+    const auto grid = [](int32_t row_tiles, int32_t column_tiles, int32_t count) {
+        return dim3(static_cast<unsigned>((static_cast<int64_t>(row_tiles) * column_tiles + 7) / 8 * 8), static_cast<unsigned>(count));
+    };
+    // what the groups' middles come to; parts of it lie behind it
+    const int64_t padded_rows = static_cast<int64_t>(p.row_tiles) * 256;
     TilesArgs<T> a = {};
     a.grad = grads;
-    a.weights = weights;
-    a.back = back;
+    a.weights = middles;
     a.rows = rows;
-    a.inputs = w->inputs;
+    a.padded_rows = padded_rows;
+    a.inputs = kMiddleNumbers * v.groups;
     a.padded = p.padded;
     a.row_tiles = p.row_tiles;
+    a.column_tiles = (a.inputs + kGradColumns - 1) / kGradColumns;
+    a.share = p.middle_share;
+    a.parts = p.middle_parts > 1 ? middle_sums + padded_rows * v.groups : middle_sums;
+    launch(linear4_backward_tiles_kernel<T, kGradNumbers<T>, true>, grid(a.row_tiles, a.column_tiles, p.middle_parts), 256, stream, a);
+    if (p.middle_parts > 1)
+        launch(linear4_join_kernel<float>, static_cast<unsigned>((padded_rows * v.groups + 255) / 256), 256, stream, static_cast<const float*>(a.parts), p.middle_parts, v.groups,
+               static_cast<int32_t>(padded_rows), static_cast<const void*>(nullptr), 0, middle_sums, padded_rows);
+    a.weights = weights;
+    a.back = back;
+    a.middles = middle_sums;
+    a.group_shift = __builtin_ctz(GROUP);
+    a.inputs = w->inputs;
     a.column_tiles = p.column_tiles;
     a.out = static_cast<T*>(grad_x->data);
     a.out_stride = grad_x->stride;
     a.share = p.share;
     a.parts = parts;
-    const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(p.row_tiles) * p.column_tiles + 7) / 8 * 8), static_cast<unsigned>(p.parts));
-    launch(linear4_backward_tiles_kernel<T>, grid, 256, stream, a);
+    launch(linear4_backward_tiles_kernel<T, kGradNumbers<T>, false>, grid(p.row_tiles, p.column_tiles, p.parts), 256, stream, a);
 }
 
 int launch_linear4(const actq_weights4* w, const actq_rows* x, int dtype, int64_t rows, const void* bias, int bias_dtype, const actq_rows* y, void* workspace, void* stream)
@@ -1295,7 +1355,7 @@ int launch_linear4_backward(const actq_weights4* w, const actq_rows* grad_y, int
             constexpr int kGroup = decltype(g)::value;
             const GradPlan p = grad_plan(w, dtype, rows);
             const hipStream_t at = static_cast<hipStream_t>(stream);
-            float* const parts = p.parts > 1 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + p.inverse + p.back + p.grads + p.weights) : nullptr;
+            float* const parts = p.parts > 1 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + p.inverse + p.back + p.grads + p.weights + p.middles + p.middle_sums) : nullptr;
             if (p.tiles) {
                 launch_backward_tiles<T, kGroup>(w, grad_y, rows, grad_x, p, workspace, parts, at);
             } else {

@@ -39,3 +39,22 @@ def test_sums_are_as_good_as_binary32_ones(rows, inputs, outputs, group, dtype):
     limit = float((2 * H.ROUNDOFF[dtype] * d * y.abs()).sum()) ** 0.5
     off = float((got - y.to(dtype).double()).norm())
     assert off <= limit, (off / limit, off / float(y.norm()))
+
+
+# rows, inputs, outputs, group: more than 2^33 products, from weights in memory, whole tiles and cut ones, one part of the outputs and several
+@pytest.mark.parametrize("rows, inputs, outputs, group", [(2048, 4096, 8192, 128), (1100, 4224, 2100, 32), (1500, 3001, 2100, 64), (9000, 2048, 1000, 128)])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_gradients_from_weights_in_memory_are_as_good_as_binary32_ones(rows, inputs, outputs, group, dtype):
+    """As above.  d: weights are exact but for the middles of their groups (22 bits, below the rest), sixteen products come in at a time, with two roundings at most; a
+    partial sum is at most as large as the root of the sum of squares of grad_y times what a weight is made of, step (code - 8) and zero + 8 step."""
+    codes, header = (t.to(DEV) for t in Y.random_weights(outputs, inputs, group, 1))
+    grad = torch.randn((rows, outputs), generator=torch.Generator().manual_seed(2)).to(dtype).to(DEV)
+    w, _ = _weights(codes, header, inputs)
+    middle = (header[..., :1].double() + 8 * header[..., 1:].double()).expand(-1, -1, group).flatten(1)[:, :inputs]
+    y = grad.double() @ w
+    partial = ((grad.double() ** 2) @ ((w - middle) ** 2 + middle ** 2)) ** 0.5
+    got = B.linear4_backward(grad, codes, header, inputs).double()
+    d = Y.UNIT * (outputs / 8 / 3) ** 0.5 * partial
+    limit = float((2 * H.ROUNDOFF[dtype] * d * y.abs()).sum()) ** 0.5
+    off = float((got - y.to(dtype).double()).norm())
+    assert off <= limit, (off / limit, off / float(y.norm()))
