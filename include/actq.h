@@ -653,7 +653,8 @@ int actq_linear4(const actq_weights4* w, const actq_rows* x, actq_dtype dt, int6
  * many rows, a weight is multiplied as step * (code - 8), which is exact, and zero + 8 * step, as 22 bits, an
  * element of grad_y as it is, or as 22 bits for ACTQ_F32; else a weight as 16 bits or, for ACTQ_F32, as it is.  That
  * is off by 2^-22 (ACTQ_F32 2^-21) and 2^-16 (2^-24) of a product at most, and where there are many rows by 2^-37 of its row's
- * largest product (a weight taken for its output's largest).
+ * largest product (a weight taken for its output's largest), as long as that is 2^-110 or more.  A row of grad_y
+ * with an infinity or NaN gives no finite number.
  *
  * grad_y [rows, outputs], grad_x [rows, inputs] of type dt, which may not overlap; workspace as above
  */

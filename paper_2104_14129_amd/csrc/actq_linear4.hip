@@ -846,17 +846,14 @@ constexpr int kMiddleNumbers = 2;
 
 constexpr int kDeepest = 64;   // outputs are padded to a multiple
 
-// The power of two that takes a number of this magnitude into [2^13, 2^14).  Zero counts as
+// The exponent of the power of two that takes a number of this magnitude into [2^13, 2^14): from -114 to 140.  Zero counts as
 // the smallest: an output without weights, whose element of grad_y adds nothing, must not
 // be its row's largest.
-__device__ __forceinline__ float scale_of(uint32_t largest)
-{
-    const int exponent = static_cast<int>(largest >> 23) - 127;
-    const int power = largest >= 0x7f800000u ? 0 : max(min(13 - exponent, 100), -100);
-    return __builtin_bit_cast(float, static_cast<uint32_t>(power + 127) << 23);
-}
+__device__ __forceinline__ int power_of(uint32_t largest) { return largest >= 0x7f800000u ? 0 : 140 - static_cast<int>(largest >> 23); }
 
-// 1 / the scale of every output, a wavefront each.
+__device__ __forceinline__ float two_to(int power) { return __builtin_bit_cast(float, static_cast<uint32_t>(power + 127) << 23); }   // from -126 to 127
+
+// 1 / the scale of every output, a wavefront each: both are normal numbers, which leaves weights below 2^-113 in [0, 2^13).
 __global__ __launch_bounds__(256) void weights4_scale_kernel(Weights4 w, float* inverse)
 {
     const int n = blockIdx.x * 4 + threadIdx.x / 64;
@@ -871,7 +868,7 @@ __global__ __launch_bounds__(256) void weights4_scale_kernel(Weights4 w, float* 
     }
 #pragma unroll
     for (int step = 1; step < 64; step *= 2) largest = max(largest, static_cast<uint32_t>(__shfl_xor(static_cast<int>(largest), step)));
-    if (threadIdx.x % 64 == 0) inverse[n] = 1.0f / scale_of(largest);
+    if (threadIdx.x % 64 == 0) inverse[n] = two_to(-min(power_of(largest), 126));
 }
 
 // 64 outputs x 128 inputs a workgroup; out [inputs][padded outputs], middles [groups][numbers][padded outputs].
@@ -955,8 +952,10 @@ __global__ __launch_bounds__(256) void linear4_scale_rows_kernel(const T* grad, 
     if (threadIdx.x % 64 == 0) shares[threadIdx.x / 64] = largest;
     __syncthreads();
     largest = max(max(shares[0], shares[1]), max(shares[2], shares[3]));
-    const float scale = scale_of(largest);
-    if (threadIdx.x == 0) back[m] = 1.0f / scale;
+    // in two steps, as one of them has no room for the smallest numbers
+    const int power = power_of(largest), half = power / 2;
+    const float first = two_to(half), second = two_to(power - half);
+    if (threadIdx.x == 0) back[m] = two_to(-half) * two_to(half - power);
     for (int n = 8 * threadIdx.x; n < padded; n += 8 * 256) {
         float f[8];
         at(n, f);
@@ -965,7 +964,7 @@ __global__ __launch_bounds__(256) void linear4_scale_rows_kernel(const T* grad, 
             f16x8 v;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (number == 0) f[i] *= scale;
+                if (number == 0) f[i] = f[i] * first * second;
                 v[i] = static_cast<_Float16>(f[i]);
                 f[i] -= static_cast<float>(v[i]);
             }

@@ -45,3 +45,18 @@ def test_zeros_times_the_largest_weights(rows, inputs, outputs, group, dtype):
     assert torch.isfinite(header).all()
     y = B.linear4(torch.zeros((rows, inputs), dtype=dtype, device=DEV), codes, header)
     assert (y == 0).all()
+
+
+# rows, inputs, outputs: few rows, and from weights in memory
+@pytest.mark.parametrize("rows, inputs, outputs", [(20, 640, 400), (1100, 4224, 2100)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("of_grad, of_weights", [(-90, 0), (100, 0), (60, -100), (-60, 117)])
+def test_powers_of_two_in_a_gradient(rows, inputs, outputs, dtype, of_grad, of_weights):
+    """Every rounding commutes with them as long as nothing leaves the range: weights are between 2^-8 and 2 (but for what is rounded off in any case), elements of
+    grad_y below 2^3, so that 24 bits of both and of their products fit it with these powers."""
+    codes, header = (t.to(DEV) for t in Y.random_weights(outputs, inputs, 64, 1))
+    grad = _rows(rows, outputs, dtype, 2)
+    want = B.linear4_backward(grad, codes, header, inputs)
+    got = B.linear4_backward(grad * 2.0 ** of_grad, codes, header * 2.0 ** of_weights, inputs)
+    assert torch.isfinite(got).all() and (want != 0).any()
+    assert torch.equal(got, want * 2.0 ** (of_grad + of_weights))
