@@ -638,7 +638,7 @@ int actq_weights4_dequantize(const actq_weights4* w, const actq_rows* out, actq_
  * y = x W^T + bias.  Products are exact (of a binary32 x: of the three bfloat16 numbers that make it
  * up), their sums binary32, a result is rounded once.  Sums are kept in a unit below the result's, so that no finite
  * x and weights overflow where their products do not; of a bfloat16 or binary32 x below 2^-98 bits may be lost for that.
- * A row of x with an infinity or NaN gives NaN.
+ * A row of x with an infinity or NaN gives no finite number (which of the two goes by the kernel).
  *
  * x [rows, inputs], y [rows, outputs] of type dt; rows at least 0, below 2^20; y may not overlap x
  * bias       device [outputs] of type dt or ACTQ_F32, or NULL

@@ -60,3 +60,16 @@ def test_powers_of_two_in_a_gradient(rows, inputs, outputs, dtype, of_grad, of_w
     got = B.linear4_backward(grad * 2.0 ** of_grad, codes, header * 2.0 ** of_weights, inputs)
     assert torch.isfinite(got).all() and (want != 0).any()
     assert torch.equal(got, want * 2.0 ** (of_grad + of_weights))
+
+
+@pytest.mark.parametrize("rows, inputs, outputs, group", map(_shape, KERNELS))
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_an_infinity_in_a_row_leaves_nothing_finite_there(rows, inputs, outputs, group, dtype):
+    """Nor does it where every weight is above zero, and nothing takes from it."""
+    codes, header = (t.to(DEV) for t in Y.random_weights(outputs, inputs, group, 1))
+    header[..., 1] = header[..., 1].abs()
+    header[: outputs // 2, :, 0] = 300 * header[: outputs // 2, :, 1]
+    x = _rows(rows, inputs, dtype, 2)
+    x[0, 5], x[rows - 1, inputs - 1] = float("inf"), -float("inf")
+    finite = torch.isfinite(B.linear4(x, codes, header))
+    assert not finite[0].any() and not finite[rows - 1].any() and finite[1:rows - 1].all()
