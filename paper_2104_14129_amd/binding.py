@@ -473,7 +473,8 @@ def cache_attention(q, key_codes, key_header, value_codes, value_header, table, 
 
 def cache_append(q, k, v, q_weight, k_weight, positions, cos, sin, slots, key_codes, key_header, value_codes, value_header, eps=1e-6, interleaved: bool = False,
                  q_out=None):
-    """Device: head_norm_rotate of q and k and cache_write of the keys and v, in one launch; returns q_out (q_out = q works in place).
+    """Device: head_norm_rotate of q and k and cache_write of the keys and v, in one launch; returns q_out (q_out = q works in place; other memory
+    that is read is refused).
     With eps None queries and keys are rotated only; q None appends keys and values alone.  Keys are quantised from binary32 values that are
     rounded once, not from values of the tensors' type."""
     return (_host or host()).cache_append(q, k, v, q_weight, k_weight, positions, cos, sin, slots, key_codes, key_header, value_codes, value_header,
@@ -488,7 +489,7 @@ def block_norm(x, h, gate, weight, post_weight=None, scale: float = 1.0, eps: fl
     """Device: the norms behind and before a block with the residual sum between, in one launch, x and h [tokens, width]:
     r = x + scale * gate * norm(h) * post_weight and y = norm(r) * weight, norm(v) = v (mean(v^2) + eps)^(-1/2).  post_weight None: h goes
     without a norm; gate None, [width] or [tokens, width]; h None: r is x.  Weights and a gate [width] have the rows' type or float32.  Returns
-    (r, y); r = x, y = h and the like work in place."""
+    (r, y); r = x, y = h and the like work in place, outputs that share memory with inputs otherwise are refused."""
     return (_host or host()).block_norm(x, h, gate, weight, post_weight, float(scale), float(eps), r, y)
 
 

@@ -63,7 +63,7 @@ def host_source_hash() -> str:
     """The same for the binding's native half, which depends on the interpreter's binary interface and on torch's as well."""
     import sysconfig
     import torch
-    return _digest([os.path.join(CSRC, HOST_SOURCE), os.path.join(ROOT, "include", "actq.h")], " ".join(HOST_FLAGS),
+    return _digest([os.path.join(CSRC, HOST_SOURCE), os.path.join(CSRC, "actq_overlap.h"), os.path.join(ROOT, "include", "actq.h")], " ".join(HOST_FLAGS),
                    f"{sysconfig.get_config_var('SOABI')} torch {torch.__version__} {_abi_flag()}")
 
 

@@ -21,7 +21,6 @@
 
 #include <torch/extension.h>
 
-#include <ATen/MemoryOverlap.h>
 #include <ATen/TensorSubclassLikeUtils.h>
 #include <ATen/autocast_mode.h>
 #include <c10/core/GradMode.h>
@@ -34,6 +33,7 @@
 #include <torch/csrc/jit/frontend/tracer.h>
 
 #include "actq.h"
+#include "actq_overlap.h"
 
 namespace {
 
@@ -684,6 +684,41 @@ void same_heads(const Tensor& t, const Tensor& like, const char* name)
     TORCH_CHECK_TYPE(t.scalar_type() == like.scalar_type(), name, " must be ", dtype_name(like.scalar_type()), ", got ", dtype_name(t.scalar_type()));
 }
 
+// The memory of a tensor [rows, columns], [tokens, heads, dim], or of any shape and contiguous.
+actq::Strips strips_of(const Tensor& t)
+{
+    const int64_t size = static_cast<int64_t>(t.element_size()), at = reinterpret_cast<int64_t>(t.data_ptr());
+    if (t.numel() == 0) return {};
+    if (t.is_contiguous()) return {{at, 0, 1, t.numel() * size}};
+    const bool heads = t.dim() == 3;
+    return actq::strips_of(at, t.size(0), t.stride(0) * size, heads ? t.size(1) : 1, heads ? t.stride(1) * size : 0, t.size(t.dim() - 1) * size);
+}
+
+bool same_place(const Tensor& a, const Tensor& b)
+{
+    if (a.data_ptr() != b.data_ptr() || a.sizes() != b.sizes()) return false;
+    for (int64_t i = 0; i < a.dim(); ++i)
+        if (a.size(i) > 1 && a.stride(i) != b.stride(i)) return false;
+    return true;
+}
+
+// An output may not share memory with an input, but for one that it replaces element by element.  (What ATen offers for this passes
+// tensors that lie inside wider ones.)
+struct Written {
+    const Tensor& t;
+    const char* name;
+    actq::Strips strips;
+    Written(const Tensor& tensor, const char* called) : t(tensor), name(called), strips(strips_of(tensor)) {}
+    void beside(const Tensor& input, const char* its_name, bool in_place = false) const
+    {
+        TORCH_CHECK((in_place && same_place(t, input)) || !actq::overlap(strips, strips_of(input)), name, " must not share memory with ", its_name);
+    }
+    void beside(const std::optional<Tensor>& input, const char* its_name, bool in_place = false) const
+    {
+        if (input) beside(*input, its_name, in_place);
+    }
+};
+
 struct Norm {
     Tensor q, positions, cos, sin;
     std::optional<Tensor> k, q_weight, k_weight;
@@ -947,6 +982,14 @@ PyObject* cache_append_impl(PyObject* const* a)
         q_out = heads_output(a[15], n.q, "q_out");
         ho = heads_to(q_out, "q_out");
     }
+    if (a[15] != Py_None) {
+        const Written w(q_out, "q_out");
+        TORCH_CHECK(actq::apart(w.strips), "q_out must not have elements that share memory");
+        w.beside(n.q, "q", true);
+        const std::pair<const char*, int> others[] = {{"k", 1}, {"v", 2}, {"q_weight", 3}, {"k_weight", 4}, {"positions", 5}, {"cos", 6}, {"sin", 7},
+                                                      {"slots", 8}, {"key_codes", 9}, {"key_header", 10}, {"value_codes", 11}, {"value_header", 12}};
+        for (const auto& [name, at] : others) w.beside(optional_tensor(a[at], name), name);
+    }
     call(api.cache_append, &c, queries ? &n.hq : nullptr, &hk, &hv, n.dt, n.tokens, queries ? n.wq.p : nullptr, queries ? n.wk.p : n.wq.p, n.weight_dt, &n.rotation,
          static_cast<int32_t>(normed), normed ? n.eps : 0.0f, sp, queries ? &ho : nullptr, current_stream());
     return queries ? give(a[15], q_out) : wrap_or_none(q_out);
@@ -1048,14 +1091,17 @@ PyObject* block_norm_impl(PyObject* const* a)
     }
     const Tensor y = rows_output(a[8], k.x, "y");
     const actq_rows hy = rows_to(y, "y");
-    // over an input element by element or beside it
-    for (const Tensor* out : std::initializer_list<const Tensor*>{&r, &y})
-        if (out->defined()) {
-            at::assert_no_partial_overlap(*out, k.x);
-            if (k.h) at::assert_no_partial_overlap(*out, *k.h);
-            if (k.gates) at::assert_no_partial_overlap(*out, *k.gates);
-        }
-    if (r.defined()) at::assert_no_overlap(r, y);
+    const auto beside_inputs = [&](const Tensor& out, const char* name) {
+        const Written w(out, name);
+        w.beside(k.x, "x", true);
+        w.beside(k.h, "h", true);
+        w.beside(optional_tensor(a[2], "gate"), "gate", k.gates.has_value());
+        w.beside(tensor_of(a[3], "weight"), "weight");
+        w.beside(optional_tensor(a[4], "post_weight"), "post_weight");
+    };
+    if (a[7] != Py_None) beside_inputs(r, "r");
+    if (a[8] != Py_None) beside_inputs(y, "y");
+    if (a[7] != Py_None && a[8] != Py_None) Written(r, "r").beside(y, "y");
     call(api.block_norm, &k.b, &k.hx, k.h_rows, k.h ? &hr : nullptr, &hy, current_stream());
     return tuple_of({k.h ? give(a[7], r) : give(a[0], k.x), give(a[8], y)});
 }
@@ -1189,7 +1235,13 @@ PyObject* linear4_impl(PyObject* const* a)
     TORCH_CHECK_VALUE(out.dim() == 2 || out.is_contiguous(), "out must be contiguous or have two dimensions");
     const Tensor y = as_rows(out, "out");
     const actq_rows hy = rows_to(y, "out");
-    at::assert_no_overlap(y, x);
+    if (a[4] != Py_None) {
+        const Written w(y, "out");
+        w.beside(x, "x");
+        w.beside(bias, "bias");
+        w.beside(tensor_of(a[1], "codes"), "codes");
+        w.beside(tensor_of(a[2], "header"), "header");
+    }
     uint64_t bytes = 0;
     call(api.linear4_workspace, &w, dt, x.size(0), &bytes);
     Tensor workspace;
