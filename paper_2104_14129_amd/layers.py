@@ -568,6 +568,10 @@ class QBlockNorm(nn.Module):
     def forward(self, x, h=None, gate=None):
         if gate is not None and (self.gate is not None or h is None):
             raise ValueError("a gate of every token goes with h and without a learned gate")
+        if x.dim() == 0 or x.shape[-1] != self.width:
+            raise ValueError(f"x must be [..., width], width {self.width}")
+        if any(t is not None and t.shape != x.shape for t in (h, gate)):
+            raise ValueError("h and a gate of every token must have x's shape")
         weight, post, gate = self.weight, None if h is None else self.post_weight, gate if h is None or self.gate is None else self.gate
         shape = x.shape
         rows = [None if t is None else t if t is self.gate else t.reshape(-1, self.width) for t in (x, h, gate)]
