@@ -609,6 +609,8 @@ class Linear4(nn.Module):
         return B.dequantize_weights(self.codes, self.header.view(torch.bfloat16), self.inputs, dtype)
 
     def forward(self, x):
+        if x.dim() == 0 or x.shape[-1] != self.inputs:
+            raise ValueError(f"x must be [..., inputs] with {self.inputs} inputs")
         header, bias = self.header.view(torch.bfloat16), self.bias
         if torch.is_grad_enabled() and (x.requires_grad or bias is not None and bias.requires_grad):
             return _Linear4Fn.apply(x, self.codes, header, bias)

@@ -17,3 +17,14 @@ def test_block_norm_takes_inputs_of_one_shape():
             layer(x)
         with pytest.raises(ValueError, match="width"):
             layer(x, x)
+
+
+@pytest.mark.parametrize("columns", [193, 199, 201, 256])
+def test_linear4_takes_as_many_inputs_as_it_has(columns):
+    """Of whole groups a few more or less would meet codes that stand for nothing, or leave weights out."""
+    layer = L.Linear4(torch.zeros((5, 32), dtype=torch.int32), torch.zeros((5, 4, 2), dtype=torch.bfloat16), 200)
+    for x in (torch.zeros((3, columns)), torch.zeros((2, 3, columns)), torch.zeros(columns), torch.zeros((3, columns), requires_grad=True)):
+        with pytest.raises(ValueError, match="200 inputs"):
+            layer(x)
+    with pytest.raises(ValueError, match="200 inputs"):
+        layer(torch.zeros(()))
