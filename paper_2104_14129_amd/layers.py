@@ -574,7 +574,7 @@ class QBlockNorm(nn.Module):
             raise ValueError("h and a gate of every token must have x's shape")
         weight, post, gate = self.weight, None if h is None else self.post_weight, gate if h is None or self.gate is None else self.gate
         shape = x.shape
-        rows = [None if t is None else t if t is self.gate else t.reshape(-1, self.width) for t in (x, h, gate)]
+        rows = [None if t is None else t if t is self.gate else _in_rows(t, self.width) for t in (x, h, gate)]
         inputs = [t for t in (*rows, weight, post) if t is not None]
         if torch.is_grad_enabled() and any(t.requires_grad for t in inputs):
             out = _QBlockNormFn.apply(*rows, weight, post, float(self.scale), float(self.eps))
@@ -611,6 +611,7 @@ class Linear4(nn.Module):
     def forward(self, x):
         if x.dim() == 0 or x.shape[-1] != self.inputs:
             raise ValueError(f"x must be [..., inputs] with {self.inputs} inputs")
+        x = x if x.stride(-1) == 1 else x.contiguous()
         header, bias = self.header.view(torch.bfloat16), self.bias
         if torch.is_grad_enabled() and (x.requires_grad or bias is not None and bias.requires_grad):
             return _Linear4Fn.apply(x, self.codes, header, bias)
