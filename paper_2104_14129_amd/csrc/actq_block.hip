@@ -108,7 +108,7 @@ struct BlockArgs {
     const void* post_weight;
     const void* gate;
     int32_t wide;
-    int64_t tokens;
+    int64_t tokens, first;   // first: workgroups of earlier launches
     int32_t width;
     float mean;   // 1 / width
     float scale, eps;
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(kBlockThreads<WAVES>) void block_norm_kernel(BlockA
     __shared__ Team<WAVES, 1> team;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int lane = WAVES == 1 ? threadIdx.x % 64 : threadIdx.x;
-    const int64_t token = WAVES == 1 ? static_cast<int64_t>(blockIdx.x) * kSmallTeams + wave : blockIdx.x;
+    const int64_t block = a.first + blockIdx.x, token = WAVES == 1 ? block * kSmallTeams + wave : block;
     if (WAVES == 1 && token >= a.tokens) return;
     int turn = 0;
     float r[PARTS][8];
@@ -505,7 +505,10 @@ int launch_block_norm(const actq_block* b, const actq_rows* x, const actq_rows* 
             a.scale = b->scale;
             a.eps = b->eps;
             const int64_t blocks = kWaves == 1 ? (b->tokens + kSmallTeams - 1) / kSmallTeams : b->tokens;
-            launch(block_norm_kernel<T, kWaves, kParts>, static_cast<unsigned>(blocks), kBlockThreads<kWaves>, static_cast<hipStream_t>(stream), a);
+            launches(blocks, kBlockThreads<kWaves>, [&](int64_t first, unsigned count) {
+                a.first = first;
+                launch(block_norm_kernel<T, kWaves, kParts>, count, kBlockThreads<kWaves>, static_cast<hipStream_t>(stream), a);
+            });
             return launched("actq_block_norm");
         });
     });

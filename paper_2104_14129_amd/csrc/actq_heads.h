@@ -267,6 +267,14 @@ __device__ __forceinline__ void quantise(const float (&x)[8], int bits, uint8_t*
     }
 }
 
+// A launch has fewer than 2^32 threads: what needs more goes in several, f(first, blocks) each.
+template <typename F>
+inline void launches(int64_t blocks, int threads, F f)
+{
+    const int64_t most = ((int64_t(1) << 32) - 1) / threads;
+    for (int64_t first = 0; first < blocks; first += most) f(first, static_cast<unsigned>(blocks - first < most ? blocks - first : most));
+}
+
 inline int launched(const char* who)
 {
     const hipError_t e = hipGetLastError();

@@ -305,7 +305,7 @@ struct PrepareArgs {
     const T* x;
     int64_t stride;
     int32_t inputs, padded;   // whole spans
-    int64_t rows;
+    int64_t rows, first;      // first: workgroups of earlier launches
     u32x4* copy;              // [pieces][rows][padded / 8]; null: none
     u32x2* sums;              // [padded / group][rows]
 };
@@ -314,7 +314,7 @@ template <typename T, int GROUP>
 __global__ __launch_bounds__(256) void linear4_prepare_kernel(PrepareArgs<T> a)
 {
     const int chunks = a.padded / 8;
-    const int64_t unit = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t unit = (a.first + blockIdx.x) * 256 + threadIdx.x;
     const bool there = unit < a.rows * chunks;
     const int64_t m = there ? unit / chunks : 0;
     const int chunk = there ? static_cast<int>(unit - m * chunks) : 0, k = 8 * chunk;
@@ -675,7 +675,11 @@ int launch_tiles(const actq_weights4* w, const actq_rows* x, int64_t rows, bool 
     p.rows = rows;
     p.copy = copy;
     p.sums = sums;
-    if (!low || copied) launch(linear4_prepare_kernel<T, GROUP>, static_cast<unsigned>((rows * (padded / 8) + 255) / 256), 256, stream, p);
+    if (!low || copied)
+        launches((rows * (padded / 8) + 255) / 256, 256, [&](int64_t first, unsigned count) {
+            p.first = first;
+            launch(linear4_prepare_kernel<T, GROUP>, count, 256, stream, p);
+        });
     ManyArgs<T> a = {};
     a.w = weights_of(w);
     a.x = copied ? reinterpret_cast<const uint16_t*>(copy) : static_cast<const uint16_t*>(x->data);
@@ -1109,9 +1113,9 @@ __global__ __launch_bounds__(256, 1) void linear4_backward_tiles_kernel(TilesArg
 // A thread is a word.  zero = min and step = (max - min) / 15 are rounded to bfloat16 before the codes are worked out with them; a group with an infinity or
 // NaN, or whose zero or step overflows, reads as NaN.
 template <typename T>
-__global__ __launch_bounds__(256) void weights4_quantize_kernel(const T* w, int64_t stride, int32_t inputs, int32_t group, int32_t row_words, int64_t words, uint32_t* codes, uint32_t* header)
+__global__ __launch_bounds__(256) void weights4_quantize_kernel(const T* w, int64_t stride, int32_t inputs, int32_t group, int32_t row_words, int64_t words, int64_t first, uint32_t* codes, uint32_t* header)
 {
-    const int64_t unit = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t unit = (first + blockIdx.x) * 256 + threadIdx.x;
     const bool there = unit < words;
     const int64_t n = there ? unit / row_words : 0;
     const int word = there ? static_cast<int>(unit - n * row_words) : 0;
@@ -1156,9 +1160,9 @@ __global__ __launch_bounds__(256) void weights4_quantize_kernel(const T* w, int6
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void weights4_dequantize_kernel(Weights4 w, int32_t group, int64_t words, T* out, int64_t stride)
+__global__ __launch_bounds__(256) void weights4_dequantize_kernel(Weights4 w, int32_t group, int64_t words, int64_t first, T* out, int64_t stride)
 {
-    const int64_t unit = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t unit = (first + blockIdx.x) * 256 + threadIdx.x;
     if (unit >= words) return;
     const int row_words = w.groups * (group / 8);
     const int64_t n = unit / row_words;
@@ -1192,8 +1196,10 @@ int launch_weights4_quantize(const actq_rows* w, int dtype, const actq_weights4*
         const Weights4 v = weights_of(to);
         const int32_t row_words = v.groups * (to->group / 8);
         const int64_t words = static_cast<int64_t>(v.outputs) * row_words;
-        launch(weights4_quantize_kernel<T>, static_cast<unsigned>((words + 255) / 256), 256, static_cast<hipStream_t>(stream), static_cast<const T*>(w->data), w->stride, to->inputs,
-               to->group, row_words, words, const_cast<uint32_t*>(v.codes), const_cast<uint32_t*>(v.header));
+        launches((words + 255) / 256, 256, [&](int64_t first, unsigned count) {
+            launch(weights4_quantize_kernel<T>, count, 256, static_cast<hipStream_t>(stream), static_cast<const T*>(w->data), w->stride, to->inputs, to->group, row_words, words, first,
+                   const_cast<uint32_t*>(v.codes), const_cast<uint32_t*>(v.header));
+        });
         return launched("actq_weights4_quantize");
     });
 }
@@ -1204,7 +1210,9 @@ int launch_weights4_dequantize(const actq_weights4* w, const actq_rows* out, int
         typedef decltype(type) T;
         const Weights4 v = weights_of(w);
         const int64_t words = static_cast<int64_t>(v.outputs) * v.groups * (w->group / 8);
-        launch(weights4_dequantize_kernel<T>, static_cast<unsigned>((words + 255) / 256), 256, static_cast<hipStream_t>(stream), v, w->group, words, static_cast<T*>(out->data), out->stride);
+        launches((words + 255) / 256, 256, [&](int64_t first, unsigned count) {
+            launch(weights4_dequantize_kernel<T>, count, 256, static_cast<hipStream_t>(stream), v, w->group, words, first, static_cast<T*>(out->data), out->stride);
+        });
         return launched("actq_weights4_dequantize");
     });
 }
