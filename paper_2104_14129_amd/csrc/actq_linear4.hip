@@ -1224,9 +1224,16 @@ uint64_t linear4_workspace(const actq_weights4* w, int dtype, int64_t rows)
     return kernel == kFew || kernel == kFewWide ? 0 : sums_bytes(w, rows) + copy_bytes(w, dtype, rows) + parts_bytes(w, rows, kernel == kLowTiles);
 }
 
-// Whether the weights are turned into numbers in memory: from so many products on (bfloat16: 2^33 in 256 rows 74 us, the other kernel 72; 512 rows 92 and 126;
-// 2047 233 and 463; 1000 rows of 1024 x 1024 45 and 29.  binary32: 2^32 in 128 rows 106 and 95, 256 rows 115 and 169).
-bool in_memory(const actq_weights4* w, int dtype, int64_t rows) { return rows * w->inputs * w->outputs > int64_t(1) << (dtype == ACTQ_F32 ? 32 : 33); }
+// Whether the weights are turned into numbers in memory, two bytes for each: from so many products on, and so many rows, which make up for writing them.  The other kernel
+// takes a tile of 128 rows in little more time than one.  us, from memory and by the other kernel, groups of 128:
+//   bfloat16  256 rows, 4096 inputs, 8192 outputs 83, 71; 384 99, 104; 8192 rows of 1024 x 1024 67, 64; 1500 of 2048 x 2048 66, 71; 128 rows of 8192 x 65536 784, 536; 129 789, 998
+//   binary16  192 rows, 4096 inputs, 8192 outputs 80, 83; 1024 of 2048 x 2048 58, 53; 1500 67, 86; 128 of 8192 x 65536 787, 648; 129 789, 1237
+//   binary32  512 rows of 2048 x 2048 59, 61; 1024 70, 99; 128 rows, 4096 inputs, 8192 outputs 95, 95; 64 of 8192 x 16384 271, 291; 64 of 8192 x 65536 990, 1257, for which it takes
+//             no GiB; 100 1014, 1406
+bool in_memory(const actq_weights4* w, int dtype, int64_t rows)
+{
+    return rows > (dtype == ACTQ_F32 ? 64 : 128) && rows * w->inputs * w->outputs > int64_t(1) << (dtype == ACTQ_F32 ? 31 : dtype == ACTQ_F16 ? 32 : 33);
+}
 
 struct GradPlan {
     bool tiles;               // of 256 rows, from numbers in memory
