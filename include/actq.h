@@ -662,6 +662,17 @@ int actq_linear4_backward_workspace(const actq_weights4* w, actq_dtype dt, int64
 int actq_linear4_backward(const actq_weights4* w, const actq_rows* grad_y, actq_dtype dt, int64_t rows,
                           const actq_rows* grad_x, void* workspace, uint64_t workspace_bytes, void* stream);
 
+/*
+ * The gradient of the bias: grad_bias = sum of grad_y [rows, outputs] over its rows, four at a time in binary32, these in
+ * binary64 and up to 512 parts of that rounded to binary32, in a fixed order.
+ *
+ * grad_bias  device, out: [outputs] of type dt or ACTQ_F32; zeros without rows
+ * workspace  device, actq_linear4_backward_bias_workspace bytes (may be 0: then NULL), 16-byte aligned
+ */
+int actq_linear4_backward_bias_workspace(int64_t rows, int32_t outputs, uint64_t* bytes_host);
+int actq_linear4_backward_bias(const actq_rows* grad_y, actq_dtype dt, int64_t rows, int32_t outputs, void* grad_bias,
+                               actq_dtype bias_dt, void* workspace, uint64_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

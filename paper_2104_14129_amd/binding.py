@@ -33,7 +33,7 @@ EXPORTS = ("actq_version", "actq_source_hash", "actq_last_error", "actq_packed_b
            "actq_head_norm_rotate", "actq_head_norm_workspace", "actq_head_norm_rotate_backward", "actq_cache_write", "actq_cache_read",
            "actq_cache_attention_workspace", "actq_cache_attention", "actq_cache_append", "actq_block_norm", "actq_block_norm_workspace",
            "actq_block_norm_backward", "actq_weights4_quantize", "actq_weights4_dequantize", "actq_linear4_workspace", "actq_linear4",
-           "actq_linear4_backward_workspace", "actq_linear4_backward")
+           "actq_linear4_backward_workspace", "actq_linear4_backward", "actq_linear4_backward_bias_workspace", "actq_linear4_backward_bias")
 
 
 class ActqError(RuntimeError):
@@ -206,6 +206,10 @@ def lib() -> ctypes.CDLL:
     L.actq_linear4.argtypes = [weights4, rows, c.c_int, i64, vp, c.c_int, rows, vp, u64, vp]
     L.actq_linear4_backward.restype = c.c_int
     L.actq_linear4_backward.argtypes = [weights4, rows, c.c_int, i64, rows, vp, u64, vp]
+    L.actq_linear4_backward_bias_workspace.restype = c.c_int
+    L.actq_linear4_backward_bias_workspace.argtypes = [i64, i32, vp]
+    L.actq_linear4_backward_bias.restype = c.c_int
+    L.actq_linear4_backward_bias.argtypes = [rows, c.c_int, i64, i32, vp, c.c_int, vp, u64, vp]
     L.actq_allocate_bits_device.restype = c.c_int
     L.actq_allocate_bits_device.argtypes = [vp, vp, i64, i64, i32, i64, c.c_uint32, vp, vp, vp, vp]
     _lib = L
@@ -219,7 +223,8 @@ _ATTACHED = ("actq_last_error", "actq_group_stats", "actq_sample_sensitivity", "
              "actq_maxpool2d_forward", "actq_maxpool2d_backward", "actq_linear_backward", "actq_head_norm_rotate", "actq_head_norm_workspace",
              "actq_head_norm_rotate_backward", "actq_cache_write", "actq_cache_read", "actq_cache_attention_workspace", "actq_cache_attention",
              "actq_cache_append", "actq_block_norm", "actq_block_norm_workspace", "actq_block_norm_backward", "actq_weights4_quantize",
-             "actq_weights4_dequantize", "actq_linear4_workspace", "actq_linear4", "actq_linear4_backward_workspace", "actq_linear4_backward")
+             "actq_weights4_dequantize", "actq_linear4_workspace", "actq_linear4", "actq_linear4_backward_workspace", "actq_linear4_backward",
+             "actq_linear4_backward_bias_workspace", "actq_linear4_backward_bias")
 
 
 def host():
@@ -531,6 +536,11 @@ def linear4(x, codes, header, bias=None, out=None):
 def linear4_backward(grad_y, codes, header, inputs: int):
     """Device: the gradient of linear4's x, grad_y [..., outputs] times the weights."""
     return (_host or host()).linear4_backward(grad_y, codes, header, int(inputs))
+
+
+def linear4_backward_bias(grad_y, dtype):
+    """Device: the gradient of linear4's bias, the sum of grad_y [..., outputs] over its rows, of type dtype (grad_y's or float32)."""
+    return (_host or host()).linear4_backward_bias(grad_y, dtype)
 
 
 # ----------------------------------------------------------------------------- several tensors per launch

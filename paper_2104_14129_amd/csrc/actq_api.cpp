@@ -830,4 +830,35 @@ int actq_linear4_backward(const actq_weights4* w, const actq_rows* grad_y, actq_
     return launch_linear4_backward(w, grad_y, dt, rows, grad_x, need > 0 ? workspace : nullptr, stream);
 }
 
+static int check_bias(const char* who, int64_t rows, int32_t outputs)
+{
+    if (rows < 0 || rows >= (int64_t(1) << 20)) return fail(ACTQ_EINVAL, "%s: rows must be in [0, 2^20)", who);
+    if (outputs < 1 || outputs > (1 << 20)) return fail(ACTQ_EINVAL, "%s: outputs must be in [1, 2^20]", who);
+    return ACTQ_OK;
+}
+
+int actq_linear4_backward_bias_workspace(int64_t rows, int32_t outputs, uint64_t* bytes_host)
+{
+    const char* who = "actq_linear4_backward_bias_workspace";
+    if (int rc = check_bias(who, rows, outputs)) return rc;
+    if (!bytes_host) return fail(ACTQ_EINVAL, "%s: null output", who);
+    *bytes_host = linear4_backward_bias_workspace(rows, outputs);
+    return ACTQ_OK;
+}
+
+int actq_linear4_backward_bias(const actq_rows* grad_y, actq_dtype dt, int64_t rows, int32_t outputs, void* grad_bias, actq_dtype bias_dt, void* workspace,
+                               uint64_t workspace_bytes, void* stream)
+{
+    const char* who = "actq_linear4_backward_bias";
+    if (int rc = check_bias(who, rows, outputs)) return rc;
+    if (int rc = check_heads_dtype(who, dt)) return rc;
+    if (int rc = check_rows(who, "grad_y", grad_y, dt, rows)) return rc;
+    if (bias_dt != dt && bias_dt != ACTQ_F32) return fail(ACTQ_EINVAL, "%s: the bias must have the rows' type or ACTQ_F32", who);
+    if (!grad_bias || !aligned(grad_bias, size_of(bias_dt))) return fail(ACTQ_EINVAL, "%s: grad_bias is null or not aligned to its element size", who);
+    const uint64_t need = linear4_backward_bias_workspace(rows, outputs);
+    if (need > 0 && (!workspace || !aligned(workspace, 16) || workspace_bytes < need))
+        return fail(ACTQ_EINVAL, "%s: the workspace is null, misaligned or smaller than actq_linear4_backward_bias_workspace says", who);
+    return launch_linear4_backward_bias(grad_y, dt, rows, outputs, grad_bias, bias_dt, need > 0 ? workspace : nullptr, stream);
+}
+
 }  // extern "C"

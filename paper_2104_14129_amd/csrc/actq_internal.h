@@ -131,6 +131,8 @@ uint64_t linear4_workspace(const actq_weights4* w, int dtype, int64_t rows);
 int launch_linear4(const actq_weights4* w, const actq_rows* x, int dtype, int64_t rows, const void* bias, int bias_dtype, const actq_rows* y, void* workspace, void* stream);
 uint64_t linear4_backward_workspace(const actq_weights4* w, int dtype, int64_t rows);
 int launch_linear4_backward(const actq_weights4* w, const actq_rows* grad_y, int dtype, int64_t rows, const actq_rows* grad_x, void* workspace, void* stream);
+uint64_t linear4_backward_bias_workspace(int64_t rows, int32_t outputs);
+int launch_linear4_backward_bias(const actq_rows* grad_y, int dtype, int64_t rows, int32_t outputs, void* grad_bias, int bias_dtype, void* workspace, void* stream);
 
 }  // namespace actq
 

@@ -1108,6 +1108,85 @@ __global__ __launch_bounds__(256, 1) void linear4_backward_tiles_kernel(TilesArg
     }
 }
 
+// ----------------------------------------------------------------------------- the bias
+
+// Sums of columns.  A wavefront takes every fourth row of its workgroup's, 512 columns of it, four rows in flight, whose sums are binary32 and above them binary64; the workgroups' sums are
+// added up by a second kernel.  What bounds it: memory (a library's sum of many rows clears its counters with an operation of its own, which graphs
+// do not replay rightly here).
+constexpr int kBiasColumns = 512, kBiasAhead = 4;
+
+template <typename T>
+__global__ __launch_bounds__(256) void linear4_bias_kernel(const T* grad, int64_t stride, int64_t rows, int64_t share, int32_t outputs, float* parts, void* out, int wide)
+{
+    __shared__ double sums[4][kBiasColumns];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), column = blockIdx.x * kBiasColumns + kLaneValues * lane;
+    const int64_t begin = blockIdx.y * share, end = begin + share < rows ? begin + share : rows;
+    double sum[8] = {};
+    for (int64_t m = begin + wave; m < end; m += 4 * kBiasAhead) {
+        Eight<T> e[kBiasAhead];
+#pragma unroll
+        for (int u = 0; u < kBiasAhead; ++u) {
+            const T* const row = grad + (m + 4 * u) * stride;
+            e[u].v = {};
+            if (m + 4 * u < end && column + kLaneValues <= outputs) {
+                e[u].load(row + column);
+            } else if (m + 4 * u < end) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (column + i < outputs) e[u].v[i] = row[column + i];
+            }
+        }
+        float four[8] = {};
+#pragma unroll
+        for (int u = 0; u < kBiasAhead; ++u) {
+            float f[8];
+            e[u].widen(f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) four[i] += f[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += static_cast<double>(four[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[wave][kLaneValues * lane + i] = sum[i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < kBiasColumns; i += 256) {
+        const int n = blockIdx.x * kBiasColumns + i;
+        if (n >= outputs) continue;
+        const float all = static_cast<float>((sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]));
+        if (parts)
+            parts[static_cast<int64_t>(blockIdx.y) * outputs + n] = all;
+        else if (wide)
+            static_cast<float*>(out)[n] = all;
+        else
+            static_cast<T*>(out)[n] = static_cast<T>(all);
+    }
+}
+
+// 16 columns a workgroup, 16 threads for each.
+template <typename W>
+__global__ __launch_bounds__(256) void linear4_bias_join_kernel(const float* parts, int32_t count, int32_t outputs, W* out)
+{
+    __shared__ double sums[16][16];
+    const int at = threadIdx.x % 16, row = threadIdx.x / 16, n = blockIdx.x * 16 + at;
+    double sum = 0.0;
+#pragma unroll 4
+    for (int i = row; i < count; i += 16) sum += n < outputs ? static_cast<double>(parts[static_cast<int64_t>(i) * outputs + n]) : 0.0;
+    sums[row][at] = sum;
+    __syncthreads();
+    if (row > 0 || n >= outputs) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) sum += sums[i][at];
+    out[n] = static_cast<W>(static_cast<float>(sum));
+}
+
+// Parts of the rows: two workgroups a compute unit, of 16 rows at least.
+int32_t bias_parts(int64_t rows, int32_t outputs)
+{
+    const int64_t tiles = (outputs + kBiasColumns - 1) / kBiasColumns, most = (rows + 15) / 16, wanted = 512 / tiles < most ? 512 / tiles : most;
+    return static_cast<int32_t>(wanted > 1 ? wanted : 1);
+}
+
 // ----------------------------------------------------------------------------- the weights themselves
 
 // A thread is a word.  zero = min and step = (max - min) / 15 are rounded to bfloat16 before the codes are worked out with them; a group with an infinity or
@@ -1391,6 +1470,32 @@ int launch_linear4_backward(const actq_weights4* w, const actq_rows* grad_y, int
             return launched("actq_linear4_backward");
         });
     });
+}
+
+uint64_t linear4_backward_bias_workspace(int64_t rows, int32_t outputs)
+{
+    const int32_t parts = bias_parts(rows, outputs);
+    return parts > 1 ? static_cast<uint64_t>(parts) * outputs * sizeof(float) : 0;
+}
+
+int launch_linear4_backward_bias(const actq_rows* grad_y, int dtype, int64_t rows, int32_t outputs, void* grad_bias, int bias_dtype, void* workspace, void* stream)
+{
+    const hipStream_t at = static_cast<hipStream_t>(stream);
+    const int32_t parts = bias_parts(rows, outputs);
+    float* const sums = parts > 1 ? static_cast<float*>(workspace) : nullptr;
+    by_dtype(dtype, [&](auto type) {
+        typedef decltype(type) T;
+        launch(linear4_bias_kernel<T>, dim3(static_cast<unsigned>((outputs + kBiasColumns - 1) / kBiasColumns), static_cast<unsigned>(parts)), 256, at, static_cast<const T*>(grad_y->data),
+               grad_y->stride, rows, (rows + parts - 1) / parts, outputs, sums, grad_bias, static_cast<int>(bias_dtype == ACTQ_F32));
+        return ACTQ_OK;
+    });
+    if (sums)
+        by_dtype(bias_dtype, [&](auto type) {
+            typedef decltype(type) W;
+            launch(linear4_bias_join_kernel<W>, static_cast<unsigned>((outputs + 15) / 16), 256, at, static_cast<const float*>(sums), parts, outputs, static_cast<W*>(grad_bias));
+            return ACTQ_OK;
+        });
+    return launched("actq_linear4_backward_bias");
 }
 
 }  // namespace actq

@@ -70,6 +70,8 @@ struct Api {
     decltype(&actq_linear4) linear4;
     decltype(&actq_linear4_backward_workspace) linear4_backward_workspace;
     decltype(&actq_linear4_backward) linear4_backward;
+    decltype(&actq_linear4_backward_bias_workspace) linear4_backward_bias_workspace;
+    decltype(&actq_linear4_backward_bias) linear4_backward_bias;
 };
 Api api = {};
 PyObject* actq_error = nullptr;   // the binding's exception class, called with (code, message)
@@ -1275,6 +1277,30 @@ PyObject* linear4_backward_impl(PyObject* const* a)
 }
 ACTQ_ENTRY(linear4_backward, 4)
 
+// (grad_y [..., outputs], the bias's dtype) -> its gradient [outputs]
+PyObject* linear4_backward_bias_impl(PyObject* const* a)
+{
+    const Tensor& given = tensor_of(a[0], "grad_y");
+    on_current_device(given, "grad_y");
+    const actq_dtype dt = heads_dtype(given, "grad_y");
+    TORCH_CHECK_TYPE(THPDtype_Check(a[1]), "dtype must be a torch dtype");
+    const at::ScalarType type = reinterpret_cast<THPDtype*>(a[1])->scalar_type;
+    TORCH_CHECK_TYPE(type == given.scalar_type() || type == at::kFloat, "bias must have the rows' dtype or torch.float32");
+    const Tensor g = as_rows(given, "grad_y");
+    const actq_rows hg = rows_of(g, "grad_y");
+    TORCH_CHECK_VALUE(g.size(1) <= INT32_MAX, "too many outputs");
+    const int32_t outputs = static_cast<int32_t>(g.size(1));
+    uint64_t bytes = 0;
+    call(api.linear4_backward_bias_workspace, g.size(0), outputs, &bytes);
+    const Tensor out = empty_on(given, {g.size(1)}, type);
+    Tensor workspace;
+    if (bytes > 0) workspace = empty_on(given, {static_cast<int64_t>(bytes)}, at::kByte);
+    void* const wp = bytes > 0 ? workspace.data_ptr() : nullptr;
+    call(api.linear4_backward_bias, &hg, dt, g.size(0), outputs, out.data_ptr(), type == at::kFloat ? ACTQ_F32 : dt, wp, bytes, current_stream());
+    return THPVariable_Wrap(out);
+}
+ACTQ_ENTRY(linear4_backward_bias, 2)
+
 // ----------------------------------------------------------------------------- autograd
 
 using torch::autograd::AutogradContext;
@@ -1548,7 +1574,7 @@ PyMethodDef methods[] = {
     ACTQ_METHOD(maxpool2d_forward), ACTQ_METHOD(maxpool2d_backward), ACTQ_METHOD(linear_one_launch), ACTQ_METHOD(linear_gradients), ACTQ_METHOD(linear), ACTQ_METHOD(relu), ACTQ_METHOD(maxpool2d),
     ACTQ_METHOD(head_norm_rotate), ACTQ_METHOD(head_norm_rotate_backward), ACTQ_METHOD(cache_write), ACTQ_METHOD(cache_read), ACTQ_METHOD(cache_attention),
     ACTQ_METHOD(cache_append), ACTQ_METHOD(block_norm), ACTQ_METHOD(block_norm_backward), ACTQ_METHOD(weights4_quantize), ACTQ_METHOD(weights4_dequantize),
-    ACTQ_METHOD(linear4), ACTQ_METHOD(linear4_backward),
+    ACTQ_METHOD(linear4), ACTQ_METHOD(linear4_backward), ACTQ_METHOD(linear4_backward_bias),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "actq_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -469,7 +469,7 @@ class _Linear4Fn(torch.autograd.Function):
             _no_tangents(grad_y, who="Linear4")
         rows = _in_rows(grad_y, grad_y.shape[-1])
         grad_x = B.linear4_backward(rows, codes, header, ctx.inputs).view(*grad_y.shape[:-1], ctx.inputs) if ctx.needs_input_grad[0] else None
-        grad_b = rows.sum(0, dtype=torch.float32).to(bias.dtype) if bias is not None and ctx.needs_input_grad[3] else None
+        grad_b = B.linear4_backward_bias(rows, bias.dtype) if bias is not None and ctx.needs_input_grad[3] else None
         grad_x, grad_b = _last(_LastOfLinear4, [grad_x, grad_b], grad_y)
         return grad_x, None, None, grad_b
 
