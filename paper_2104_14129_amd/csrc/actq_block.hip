@@ -12,7 +12,8 @@
 // y comes from the sum r before r is rounded, so that each result is rounded once.
 //
 // Measured on one MI355X, whose copy of 1 GiB reaches 5.1 TB/s: 8192 tokens of 4096 in binary16 43 us (6.2 TB/s, some of it from the caches), eight tokens 3.8 us; gradients
-// of 16384 tokens in bfloat16 157 + 6 us (5.1 TB/s), of 1023 tokens of 2047 in binary32 20 + 7 us (2.5 TB/s: rows that start at any element).
+// of 16384 tokens in bfloat16 157 + 6 us (5.1 TB/s), of 1023 tokens of 2047 in binary32 20 + 7 us (2.5 TB/s: rows that start at any element; of 2048, from the host, 19.9 instead of 26.2 us
+// for both kernels).  binary32: 8192 tokens of 4096 99 us (5.4 TB/s), gradients of as many 165 us (4.9 TB/s).
 #include "actq_heads.h"
 
 namespace actq {

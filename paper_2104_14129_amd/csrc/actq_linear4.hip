@@ -10,9 +10,10 @@
 // sums of 16 x beside those of x code would cost it 2 of its 24 bits.  All of these are so small that no group's sum is larger than its largest x, and none of
 // finite x overflows; the total is kept in their unit until the end.
 //
-// Measured on one MI355X, whose copy of 1 GiB reaches 5.1 TB/s and whose library product of 8192^3 1.21 PFLOP/s in bfloat16: one row of 4096 x 4096 in groups of 128
-// 4.9 us, 23 rows of 8192 x 16384 in binary16 and groups of 64 26 us (3.0 TB/s), 4096 rows of 8192 x 8192 in bfloat16 541 us (1.02 PFLOP/s), the gradient of 2047 rows of
-// 4096 inputs and 8192 outputs 204 us (675 TFLOP/s).
+// Measured on one MI355X, whose copy of 1 GiB reaches 5.1 TB/s and whose library product of 8192^3 1.21 PFLOP/s in bfloat16, from the host, calls one behind the other (a
+// profiler's trace, which lets no kernel begin before the last has ended, shows up to 0.9 us more for each): one row of 4096 x 4096 in groups of 128
+// 4.9 us, 23 rows of 8192 x 16384 in binary16 and groups of 64 26 us (3.0 TB/s), 4096 rows of 8192 x 8192 in bfloat16 555 us (990 TFLOP/s), the gradient of 2047 rows of
+// 4096 inputs and 8192 outputs 214 us (640 TFLOP/s).
 #include "actq_heads.h"
 
 namespace actq {
@@ -168,7 +169,7 @@ __global__ __launch_bounds__(256) void linear4_join_kernel(const float* parts, i
 
 // 16 rows and COLUMNS x 16 outputs a workgroup, whose wavefronts take spans of 128 k in turn: for one token of a small matrix every compute unit has 16 wavefronts
 // with all that they need on its way at once.  A lane's codes of a group are neighbours (a quarter of the group), and so are its x.  What bounds it: the chain of trips to
-// memory, and the loads of x, which are as many for a row as for 16.
+// memory, and the loads of x, of which it makes as many for a row as for 16.
 template <typename T>
 struct FewArgs {
     Weights4 w;
@@ -606,12 +607,14 @@ __global__ __launch_bounds__(512, 2) void linear4_many_kernel(ManyArgs<T> a)
 }
 
 // Which kernel serves.  What counts is the units of 16 rows, 16 outputs and a span; measured on one MI355X, us, bfloat16 with groups of 128 where nothing is said:
-//   kFew         small matrices: up to 8192 units, 4096 of groups of 32 (one row of 4096 x 4096 5.5, tiles of 32 rows 8.2; 16 rows 7.8 and 9.8; at 16384 units 13.8
-//                and 12.1; groups of 32, 64 rows of 2048 x 2048 10.7 and 8.5), unless a wavefront had more than two spans (16 rows of 8192 x 2048 12.8 and 8.7)
-//   kFewWide     a few rows of many outputs: x is read once for 64 outputs (one row of 8192 x 16384 19.7, tiles 23.0; binary32 29.5 and 48.4; groups of
-//                32 44 and 30)
-//   kLowTiles    up to 64 rows, or 131072 units (binary32, where products are three times as many, 32768): 128 rows of 4096 x 4096 18.1, tiles of 128 rows 26.6;
-//                192 23.7 and 26.4; 301 33.3 and 31.1; 128 of 8192 x 8192 39.7 and 35.6; binary32, 301 rows of 1000 x 1501 18.8 and 26.1, 300 of 2048 x 2048 29.7 and 27.8
+//   kFew         small matrices: up to 8192 units, 4096 of groups of 32 (one row of 4096 x 4096 5.2, tiles of 32 rows 8.2; 16 rows 7.6 and 10.1; groups of 32, 64 rows of
+//                2048 x 2048 10.7 and 8.5, 16 of 2048 x 8000 11.1 and 10.7, one 8.3 and 8.5), unless a wavefront had more than two spans (16 rows of 8192 x 2048 12.9 and 9.3).
+//                Beyond both borders it is the other way from eight rows on (4096 x 6144 11.2 and 10.1, 5120 x 5120 13.1 and 10.6, 14336 x 4096 16.7 and 13.9; 8192 x 4096
+//                10.7 and 11.2); one row alone would still gain (8.7 and 9.7, 9.9 and 10.2, 12.3 and 13.5, 8.3 and 10.5)
+//   kFewWide     a few rows of many outputs: x is read once for 64 outputs (one row of 8192 x 16384 19.4, tiles 23.0; of 2048 x 16384 7.2 and 10.1, 16 8.7 and 11.7; binary32 10.4
+//                and 18.2, 12.4 and 20.3; groups of 32 44 and 30)
+//   kLowTiles    up to 64 rows, or 131072 units (binary32, where products are three times as many, 32768): 128 rows of 4096 x 4096 16.9, tiles of 128 rows 26.6;
+//                192 23.1 and 26.4; 301 33.3 and 31.1; 128 of 8192 x 8192 39.7 and 35.6; binary32, 301 rows of 1000 x 1501 18.8 and 26.1, 300 of 2048 x 2048 29.7 and 27.8
 //   kHighTiles   else
 enum Kernel { kFew, kFewWide, kLowTiles, kHighTiles };
 
@@ -708,8 +711,9 @@ int launch_tiles(const actq_weights4* w, const actq_rows* x, int64_t rows, bool 
 
 // Few rows.  A workgroup's tile is 128 x 128 of grad_x, gathered over 64 outputs at a time from the LDS.  A weight goes there as two bfloat16 numbers (16 bits of
 // it; three for binary32), an element of grad_y as those that make it up (binary16: two, binary32: three): products below 2^-16 (2^-24) of the largest are left out.
-// What bounds it: turning the weights into numbers, 6 instructions a code, which every tile does for itself.  One row of 4096 inputs and 8192 outputs 34 us (one
-// part of the outputs: 315).
+// What bounds it: the trips to memory of its stages, one behind the other: a stage's words, headers and rows are asked for when the last one has been multiplied.  Of 31 us for one row
+// of 4096 inputs and 8192 outputs (one part of the outputs: 315) turning the weights into numbers, 6 instructions a code, is some 5, the products of a tile, as many for a row
+// as for 128, some 7; 64 rows 38, 128 45 (binary16 39, 46, 52; binary32 75, 84, 95).
 template <typename T>
 struct GradArgs {
     Weights4 w;
