@@ -584,8 +584,8 @@ typedef struct actq_block {
     float eps;               /* finite, above zero */
 } actq_block;
 
-/* x, h (or NULL), r (NULL without h), y: [tokens, width].  r or y may be x or h; nothing else that
- * is written may overlap what is read. */
+/* x, h (or NULL), r (NULL without h), y: [tokens, width].  r or y may be x, h or the gates, r and y not
+ * each other; nothing else that is written may overlap what is read. */
 int actq_block_norm(const actq_block* block, const actq_rows* x, const actq_rows* h, const actq_rows* r,
                     const actq_rows* y, void* stream);
 
